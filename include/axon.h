@@ -355,6 +355,143 @@ int axon_decode_step_noalloc(axon_model* m, const int32_t* d_tokens, int32_t B, 
  * before the call are dropped. */
 int axon_moe_routing_record(axon_model* m, int32_t* d_experts, int32_t rows);
 
+/* ---------------------------------------------------------------------
+ * Operators on a paged key/value cache, without a model pass: attention that
+ * reads the cache, and the management of its blocks (vLLM's PagedAttention
+ * manager, Sec. Related Work; causal masks with a window, appendix GPT-2
+ * listing). All of them only enqueue work on `stream`, allocate nothing and
+ * keep nothing: every buffer is the caller's and every pointer except the
+ * three descriptor structs is a device pointer.
+ *
+ * Errors. What the host can see is refused at once (AXON_ERR_INVALID_ARG,
+ * AXON_ERR_UNSUPPORTED). What only the device can see -- a block number, a
+ * length or a row out of range -- sets a bit of the caller's error word
+ * *d_err (one int32, zeroed by the caller; NULL: not reported) and the access
+ * is skipped; axon_check_error reads and clears the word.
+ *
+ * Workspaces are device memory, 16-byte aligned, of at least the size that
+ * the matching query returns. The attention's must be zero before its first
+ * use and every call leaves it fit for the next one; the block operators' may
+ * hold anything. Calls that may overlap (different streams) need their own. */
+
+/* The pools of all layers: [num_layers][num_blocks][num_kv_heads][16][head_dim],
+ * keys after RoPE, 16-byte aligned. Block numbers are common to all layers. */
+typedef struct axon_kv_cache {
+  void* k_pool;
+  void* v_pool;
+  int32_t num_layers;
+  int32_t num_blocks;
+  int32_t num_kv_heads;
+  int32_t block_size; /* 16 */
+  int32_t head_dim;   /* 64 or 128 */
+  int32_t precision;  /* element type: AXON_BF16, AXON_FP16, or AXON_FP32_DEBUG (block operators only) */
+} axon_kv_cache;
+
+/* The cache of a model, either layout (the pools stay the model's). */
+int axon_kv_cache_get(const axon_model* m, axon_kv_cache* out);
+
+/* Who holds which block. A block is free when its count is 0; the counts
+ * are the number of table entries that name it. */
+typedef struct axon_kv_seqs {
+  int32_t* block_table;   /* [max_seqs][blocks_per_seq] block numbers, -1: none */
+  int32_t* context_lens;  /* [max_seqs] tokens in the cache, as axon_decode_step advances them */
+  int32_t* refs;          /* [num_blocks] */
+  int32_t max_seqs;       /* at most 8192 */
+  int32_t blocks_per_seq;
+} axon_kv_seqs;
+
+/* Attention of one new token per row, split over the cache's length and
+ * joined. Row b's query stands at position p = context_lens[b], whose key and
+ * value are in the cache already, as everything before them; key t is visible
+ * when t <= p and (window = 0 or t > p - window or t < sinks):
+ *   o = sum_t softmax_t(scale q.k_t) v_t,   lse = log sum_t exp(scale q.k_t).
+ *   d_q, d_out      [B][num_heads][head_dim] of the cache's type, last
+ *                   dimension dense, the others with strides in elements
+ *                   (multiples of 8, at least head_dim; 16-byte aligned
+ *                   base; a row's heads may not overlap in d_out).
+ *   B               1 .. 2048
+ *   num_heads       a multiple of num_kv_heads, at most 16 times as many;
+ *                   head h reads kv head h / (num_heads / num_kv_heads)
+ *   d_context_lens  [B]; negative: an idle row, o = 0 and lse = -infinity
+ *   d_block_table   [B][blocks_per_seq], or NULL: row b holds blocks
+ *                   b * blocks_per_seq onward
+ *   window, sinks   0: none; sinks only count under a window. Blocks that
+ *                   the mask hides are not looked at (-1 will do).
+ *   scale           0: 1 / sqrt(head_dim)
+ *   d_lse           [B][num_heads] fp32, or NULL
+ * P enters the product with V in two 16-bit terms; sums, maxima and lse are
+ * fp32. The result does not depend on timing. Cache slots that the mask hides
+ * from a row never reach its output, whatever they hold; a visible value that is
+ * infinite or not a number leaves its dim of the output not finite. */
+int axon_attn_decode(const axon_kv_cache* cache, int32_t layer, const void* d_q, int64_t q_row_stride,
+                     int64_t q_head_stride, int32_t B, int32_t num_heads, const int32_t* d_context_lens,
+                     const int32_t* d_block_table, int32_t blocks_per_seq, int32_t window, int32_t sinks, float scale,
+                     void* d_out, int64_t out_row_stride, int64_t out_head_stride, float* d_lse, void* d_workspace,
+                     int64_t workspace_bytes, int32_t* d_err, void* stream);
+int axon_attn_decode_workspace(const axon_kv_cache* cache, int32_t num_heads, int32_t B, int64_t* bytes);
+
+/* The same for chunks of tokens, packed row after row as in
+ * axon_prefill_varlen: chunk b is rows cu_seqlens[b] .. cu_seqlens[b+1]-1 of
+ * d_q and d_out (T rows in all; a chunk may be empty), its row i stands at
+ * position context_lens[b] + i, and the chunk's keys and values are in the
+ * cache already. max_chunk bounds the longest chunk. context_lens is not
+ * advanced. Slots past a row's last token never reach an output, whatever they
+ * hold; a later token of the same chunk that is not finite may reach earlier rows. */
+int axon_attn_prefill(const axon_kv_cache* cache, int32_t layer, const void* d_q, int64_t q_row_stride,
+                      int64_t q_head_stride, int32_t B, int32_t T, int32_t num_heads, const int32_t* d_cu_seqlens,
+                      const int32_t* d_context_lens, int32_t max_chunk, const int32_t* d_block_table,
+                      int32_t blocks_per_seq, int32_t window, int32_t sinks, float scale, void* d_out,
+                      int64_t out_row_stride, int64_t out_head_stride, int32_t* d_err, void* stream);
+
+/* Block dst[i] becomes a copy of block src[i], in all layers, for i < n. No
+ * block may be a destination twice, or a source and a destination. */
+int axon_kv_copy_blocks(const axon_kv_cache* cache, const int32_t* d_src, const int32_t* d_dst, int32_t n,
+                        int32_t* d_err, void* stream);
+
+/* Rows dst[i] take over what rows src[i] hold, for i < n (n <= max_seqs): parallel
+ * samples of one prompt, or the beams that survive a step. Every row is taken as it
+ * was before the call; a row may be a source any number of times, a
+ * destination once. A destination first gives back what it holds. Whole blocks are
+ * shared; a last block that is only part-filled is copied into a free one, so
+ * that each row can be appended to. src[i] = dst[i] changes nothing. Copies take
+ * the lowest free numbers in the order of i; blocks that the call gives back are free to
+ * them. Blocks reserved beyond the length are not shared. A row whose
+ * copy finds no free block keeps the whole blocks only (its length rounded down to
+ * them) and the call reports it. */
+int axon_kv_fork(const axon_kv_cache* cache, const axon_kv_seqs* seqs, const int32_t* d_src, const int32_t* d_dst,
+                 int32_t n, void* d_workspace, int64_t workspace_bytes, int32_t* d_err, void* stream);
+
+/* Rows give blocks back (d_rows [n], or NULL: rows 0 .. n-1; n <= max_seqs).
+ * window = 0: everything, and the row's length becomes 0. window > 0: the blocks that no
+ * query from position context_lens[r] on can see under that window and these
+ * sinks; their table entries become -1, the length stays. */
+int axon_kv_release(const axon_kv_cache* cache, const axon_kv_seqs* seqs, const int32_t* d_rows, int32_t n,
+                    int32_t window, int32_t sinks, int32_t* d_err, void* stream);
+
+/* Rows (each at most once) take blocks for d_new_tokens[i] more tokens after their
+ * context_lens, the lowest free numbers in the order of the rows; blocks that a row
+ * has beyond its length already are kept and counted, from the front. When the pool
+ * runs out, the rows served first keep theirs, the entries left over stay
+ * -1, and the call reports it. Lengths are not advanced. */
+int axon_kv_reserve(const axon_kv_cache* cache, const axon_kv_seqs* seqs, const int32_t* d_rows,
+                    const int32_t* d_new_tokens, int32_t n, void* d_workspace, int64_t workspace_bytes,
+                    int32_t* d_err, void* stream);
+
+/* Blocks in use move to the front: the k-th one whose number is at least their count
+ * goes to the k-th free number below it, in all layers, and the table and the
+ * counts follow. d_moved [num_blocks] (or NULL) gets each block's
+ * number afterwards, -1 for free ones, and d_live [1] (or NULL) their count. */
+int axon_kv_compact(const axon_kv_cache* cache, const axon_kv_seqs* seqs, int32_t* d_moved, int32_t* d_live,
+                    void* d_workspace, int64_t workspace_bytes, int32_t* d_err, void* stream);
+
+/* Workspace of axon_kv_fork, axon_kv_reserve and axon_kv_compact. */
+int axon_kv_workspace(const axon_kv_cache* cache, const axon_kv_seqs* seqs, int64_t* bytes);
+
+/* Synchronise `stream` and read and clear an operator's error word: AXON_OK,
+ * AXON_ERR_DEVICE_CHECK or AXON_ERR_TIMEOUT; *bits (optional) receives it. Bits:
+ * 2 block number, 4 position, 8 wait expired, 16 row or row offsets, 32 no free block. */
+int axon_check_error(int32_t* d_err, void* stream, int32_t* bits);
+
 /* Release everything the model owns. NULL is a no-op. */
 void axon_free(axon_model* m);
 

@@ -32,7 +32,10 @@ AXON_ACT_SILU, AXON_ACT_GELU_TANH = 0, 1
 
 EXPORTED = ["axon_model_create", "axon_prefill", "axon_prefill_varlen", "axon_decode_step", "axon_reset",
             "axon_check_device", "axon_kv_view_get", "axon_profile_decode_step", "axon_profile_prefill",
-            "axon_decode_step_noalloc", "axon_moe_routing_record", "axon_free", "axon_status_string"]
+            "axon_decode_step_noalloc", "axon_moe_routing_record", "axon_kv_cache_get", "axon_attn_decode",
+            "axon_attn_decode_workspace", "axon_attn_prefill", "axon_kv_copy_blocks", "axon_kv_fork", "axon_kv_release",
+            "axon_kv_reserve", "axon_kv_compact", "axon_kv_workspace", "axon_check_error", "axon_free",
+            "axon_status_string"]
 
 
 class axon_config(ctypes.Structure):
@@ -61,6 +64,16 @@ class axon_kv_view(ctypes.Structure):
 class axon_kernel_time(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char * 32), ("launches", ctypes.c_int32), ("total_ms", ctypes.c_float),
                 ("bytes", ctypes.c_double), ("flops", ctypes.c_double)]
+
+
+class axon_kv_cache(ctypes.Structure):
+    _fields_ = [("k_pool", ctypes.c_void_p), ("v_pool", ctypes.c_void_p)] + [
+        (n, ctypes.c_int32) for n in ("num_layers", "num_blocks", "num_kv_heads", "block_size", "head_dim", "precision")]
+
+
+class axon_kv_seqs(ctypes.Structure):
+    _fields_ = [("block_table", ctypes.c_void_p), ("context_lens", ctypes.c_void_p), ("refs", ctypes.c_void_p),
+                ("max_seqs", ctypes.c_int32), ("blocks_per_seq", ctypes.c_int32)]
 
 
 class AxonError(RuntimeError):
@@ -93,13 +106,29 @@ def lib() -> ctypes.CDLL:
         L.axon_profile_decode_step.argtypes = [vp, vp, i32, vp, vp, vp, vp, ctypes.POINTER(axon_kernel_time), i32,
                                                p_i32]
         L.axon_profile_prefill.argtypes = [vp, vp, i32, i32, vp, vp, vp, ctypes.POINTER(axon_kernel_time), i32, p_i32]
+        i64, f32, p_i64 = ctypes.c_int64, ctypes.c_float, ctypes.POINTER(ctypes.c_int64)
+        L.axon_kv_cache_get.argtypes = [vp, ctypes.POINTER(axon_kv_cache)]
+        L.axon_attn_decode.argtypes = [vp, i32, vp, i64, i64, i32, i32, vp, vp, i32, i32, i32, f32, vp, i64, i64, vp, vp,
+                                       i64, vp, vp]
+        L.axon_attn_decode_workspace.argtypes = [vp, i32, i32, p_i64]
+        L.axon_attn_prefill.argtypes = [vp, i32, vp, i64, i64, i32, i32, i32, vp, vp, i32, vp, i32, i32, i32, f32, vp,
+                                        i64, i64, vp, vp]
+        L.axon_kv_copy_blocks.argtypes = [vp, vp, vp, i32, vp, vp]
+        L.axon_kv_fork.argtypes = [vp, vp, vp, vp, i32, vp, i64, vp, vp]
+        L.axon_kv_release.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp]
+        L.axon_kv_reserve.argtypes = [vp, vp, vp, vp, i32, vp, i64, vp, vp]
+        L.axon_kv_compact.argtypes = [vp, vp, vp, vp, vp, i64, vp, vp]
+        L.axon_kv_workspace.argtypes = [vp, vp, p_i64]
+        L.axon_check_error.argtypes = [vp, vp, p_i32]
         L.axon_free.argtypes = [vp]
         L.axon_free.restype = None
         L.axon_status_string.argtypes = [ctypes.c_int]
         L.axon_status_string.restype = ctypes.c_char_p
         for n in ("axon_model_create", "axon_prefill", "axon_prefill_varlen", "axon_decode_step", "axon_reset",
                   "axon_check_device", "axon_kv_view_get", "axon_profile_decode_step", "axon_profile_prefill",
-                  "axon_decode_step_noalloc", "axon_moe_routing_record"):
+                  "axon_decode_step_noalloc", "axon_moe_routing_record", "axon_kv_cache_get", "axon_attn_decode",
+                  "axon_attn_decode_workspace", "axon_attn_prefill", "axon_kv_copy_blocks", "axon_kv_fork",
+                  "axon_kv_release", "axon_kv_reserve", "axon_kv_compact", "axon_kv_workspace", "axon_check_error"):
             getattr(L, n).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -251,3 +280,173 @@ def axon_profile_prefill(m, ids, block_table=None, next_tokens=None, stream=None
 
 def axon_free(m):
     lib().axon_free(m)
+
+
+# ------------------------------------------------- operators on a paged cache
+
+
+def _is(t, dtype, what, *shape):
+    """Refuse a tensor the C call could not tell from a right one: device, type, shape, dense layout."""
+    if not t.is_cuda or t.dtype != dtype or not t.is_contiguous() or (shape and t.shape != shape):
+        raise TypeError(f"{what}: a dense {dtype} device tensor{' of shape ' + str(shape) if shape else ''} is wanted, "
+                        f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _ints(t, what, *shape):
+    import torch
+    return None if t is None else _is(t, torch.int32, what, *shape)
+
+
+def make_kv_cache(k, v) -> axon_kv_cache:
+    """Descriptor of the pools k, v: dense device tensors [layers, blocks, kv heads, 16, head_dim] (bf16, fp16; the
+    block operators also take fp32). It holds their addresses: keep the tensors."""
+    import torch
+    prec = {torch.bfloat16: AXON_BF16, torch.float16: AXON_FP16, torch.float32: AXON_FP32_DEBUG}.get(k.dtype)
+    if prec is None or k.dim() != 5:
+        raise TypeError(f"k: a bf16, fp16 or fp32 tensor of 5 dimensions is wanted, got {k.dtype} {tuple(k.shape)}")
+    L, N, G, bs, d = k.shape
+    c = axon_kv_cache(_is(k, k.dtype, "k"), _is(v, k.dtype, "v", *k.shape), L, N, G, bs, d, prec)
+    c.dtype = k.dtype
+    c.ref = ctypes.byref(c)
+    return c
+
+
+def axon_kv_cache_get(m) -> axon_kv_cache:
+    """Descriptor of a model's own cache."""
+    import torch
+    c = axon_kv_cache()
+    _check("axon_kv_cache_get", lib().axon_kv_cache_get(m, ctypes.byref(c)))
+    c.dtype = {AXON_BF16: torch.bfloat16, AXON_FP16: torch.float16, AXON_FP32_DEBUG: torch.float32}[c.precision]
+    c.ref = ctypes.byref(c)
+    return c
+
+
+def make_kv_seqs(block_table, context_lens, refs) -> axon_kv_seqs:
+    """Descriptor of a block table [rows, blocks per row], lengths [rows] and counts [blocks] (int32, device). It holds
+    their addresses: keep the tensors."""
+    R, P = block_table.shape
+    s = axon_kv_seqs(_ints(block_table, "block_table"), _ints(context_lens, "context_lens", R), _ints(refs, "refs"), R, P)
+    s.num_blocks = refs.numel()
+    s.ref = ctypes.byref(s)
+    return s
+
+
+def make_attn_workspace(cache, rows, heads):
+    """Zeroed workspace of axon_attn_decode for up to `rows` rows of `heads` heads."""
+    import torch
+    n = ctypes.c_int64(0)
+    _check("axon_attn_decode_workspace", lib().axon_attn_decode_workspace(cache.ref, heads, rows, ctypes.byref(n)))
+    return torch.zeros(n.value, dtype=torch.uint8, device="cuda")
+
+
+def make_kv_workspace(cache, seqs):
+    """Workspace of axon_kv_fork, axon_kv_reserve and axon_kv_compact."""
+    import torch
+    n = ctypes.c_int64(0)
+    _check("axon_kv_workspace", lib().axon_kv_workspace(cache.ref, seqs.ref, ctypes.byref(n)))
+    return torch.empty(n.value, dtype=torch.uint8, device="cuda")
+
+
+def _rows_of(t, cache, what):
+    """(address, row stride, head stride) of a [rows, heads, head_dim] tensor of the cache's type."""
+    row, head, one = t.stride()
+    if t.dtype != cache.dtype or not t.is_cuda or one != 1 or t.shape[2] != cache.head_dim:
+        raise TypeError(f"{what}: a {cache.dtype} device tensor [rows, heads, {cache.head_dim}] with a dense last "
+                        f"dimension is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr(), row, head
+
+
+def _table_of(block_table, blocks_per_seq, rows):
+    if block_table is None:
+        return None, int(blocks_per_seq)
+    return _ints(block_table, "block_table", rows, block_table.shape[1]), block_table.shape[1]
+
+
+def axon_attn_decode(cache, layer, q, context_lens, out, workspace, block_table=None, blocks_per_seq=0, window=0, sinks=0,
+                     scale=0.0, lse=None, err=None, stream=None):
+    """Attention of one new token per row (see include/axon.h). q, out: [B, heads, head_dim], any row and head strides;
+    context_lens: int32 [B]; block_table: int32 [B, blocks], or None with blocks_per_seq for contiguous rows;
+    workspace: make_attn_workspace; lse: fp32 [B, heads] or None; err: int32 [1] error word or None."""
+    import torch
+    B, H, _ = q.shape
+    if out.shape != q.shape:
+        raise TypeError(f"out: the shape of q {tuple(q.shape)} is wanted, got {tuple(out.shape)}")
+    qp, qr, qh = _rows_of(q, cache, "q")
+    op, orow, ohead = _rows_of(out, cache, "out")
+    table, per = _table_of(block_table, blocks_per_seq, B)
+    _check("axon_attn_decode", lib().axon_attn_decode(
+        cache.ref, layer, qp, qr, qh, B, H, _ints(context_lens, "context_lens", B), table, per, window, sinks, scale, op,
+        orow, ohead, None if lse is None else _is(lse, torch.float32, "lse", B, H), workspace.data_ptr(),
+        workspace.numel(), _ints(err, "err", 1), _stream(stream)))
+
+
+def axon_attn_prefill(cache, layer, q, cu_seqlens, context_lens, max_chunk, out, block_table=None, blocks_per_seq=0,
+                      window=0, sinks=0, scale=0.0, err=None, stream=None):
+    """Attention of packed chunks (see include/axon.h). q, out: [T, heads, head_dim]; cu_seqlens: int32 [B+1];
+    context_lens: int32 [B] tokens before each chunk (not advanced); the rest as in axon_attn_decode."""
+    T, H, _ = q.shape
+    B = context_lens.shape[0]
+    if out.shape != q.shape:
+        raise TypeError(f"out: the shape of q {tuple(q.shape)} is wanted, got {tuple(out.shape)}")
+    qp, qr, qh = _rows_of(q, cache, "q")
+    op, orow, ohead = _rows_of(out, cache, "out")
+    table, per = _table_of(block_table, blocks_per_seq, B)
+    _check("axon_attn_prefill", lib().axon_attn_prefill(
+        cache.ref, layer, qp, qr, qh, B, T, H, _ints(cu_seqlens, "cu_seqlens", B + 1),
+        _ints(context_lens, "context_lens", B), int(max_chunk), table, per, window, sinks, scale, op, orow, ohead,
+        _ints(err, "err", 1), _stream(stream)))
+
+
+def _same_pool(cache, seqs):
+    if cache.num_blocks != seqs.num_blocks:
+        raise TypeError(f"refs: {cache.num_blocks} counts are wanted, one per block, got {seqs.num_blocks}")
+
+
+def axon_kv_copy_blocks(cache, src, dst, err=None, stream=None):
+    """Copy blocks src[i] to dst[i] (int32 [n]) in all layers."""
+    n = src.shape[0]
+    _check("axon_kv_copy_blocks", lib().axon_kv_copy_blocks(
+        cache.ref, _ints(src, "src", n), _ints(dst, "dst", n), n, _ints(err, "err", 1), _stream(stream)))
+
+
+def axon_kv_fork(cache, seqs, src, dst, workspace, err=None, stream=None):
+    """Rows dst[i] take over what rows src[i] hold (int32 [n]); workspace: make_kv_workspace."""
+    _same_pool(cache, seqs)
+    n = src.shape[0]
+    _check("axon_kv_fork", lib().axon_kv_fork(
+        cache.ref, seqs.ref, _ints(src, "src", n), _ints(dst, "dst", n), n, workspace.data_ptr(), workspace.numel(),
+        _ints(err, "err", 1), _stream(stream)))
+
+
+def axon_kv_release(cache, seqs, rows, window=0, sinks=0, err=None, stream=None):
+    """Rows (int32 [n]) give back everything, or with a window what no later query sees."""
+    _same_pool(cache, seqs)
+    n = rows.shape[0]
+    _check("axon_kv_release", lib().axon_kv_release(cache.ref, seqs.ref, _ints(rows, "rows", n), n, window, sinks,
+                                                    _ints(err, "err", 1), _stream(stream)))
+
+
+def axon_kv_reserve(cache, seqs, rows, new_tokens, workspace, err=None, stream=None):
+    """Rows (int32 [n]) take blocks for new_tokens (int32 [n]) more tokens; workspace: make_kv_workspace."""
+    _same_pool(cache, seqs)
+    n = rows.shape[0]
+    _check("axon_kv_reserve", lib().axon_kv_reserve(
+        cache.ref, seqs.ref, _ints(rows, "rows", n), _ints(new_tokens, "new_tokens", n), n, workspace.data_ptr(),
+        workspace.numel(), _ints(err, "err", 1), _stream(stream)))
+
+
+def axon_kv_compact(cache, seqs, workspace, moved=None, live=None, err=None, stream=None):
+    """Move the blocks in use to the front of the pool. moved: int32 [blocks] each block's number afterwards (-1: free);
+    live: int32 [1] their count; workspace: make_kv_workspace."""
+    _same_pool(cache, seqs)
+    _check("axon_kv_compact", lib().axon_kv_compact(
+        cache.ref, seqs.ref, _ints(moved, "moved", cache.num_blocks), _ints(live, "live", 1), workspace.data_ptr(),
+        workspace.numel(), _ints(err, "err", 1), _stream(stream)))
+
+
+def axon_check_error(err, stream=None) -> tuple[int, int]:
+    """(status, bits) of an operator's error word (int32 [1]) after synchronising the stream; the word is cleared."""
+    bits = ctypes.c_int32(0)
+    rc = lib().axon_check_error(_ints(err, "err", 1), _stream(stream), ctypes.byref(bits))
+    return rc, bits.value

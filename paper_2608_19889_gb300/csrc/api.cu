@@ -1835,6 +1835,19 @@ int axon_check_device(axon_model* m, void* stream, int32_t* bits) {
   return AXON_OK;
 }
 
+int axon_kv_cache_get(const axon_model* m, axon_kv_cache* out) {
+  if (!m || !out) return AXON_ERR_INVALID_ARG;
+  out->k_pool = m->kpool;
+  out->v_pool = m->vpool;
+  out->num_layers = m->L;
+  out->num_blocks = static_cast<int32_t>(m->num_blocks);
+  out->num_kv_heads = m->G;
+  out->block_size = 16;
+  out->head_dim = m->d;
+  out->precision = m->cfg.precision;
+  return AXON_OK;
+}
+
 int axon_kv_view_get(const axon_model* m, axon_kv_view* out) {
   if (!m || !out) return AXON_ERR_INVALID_ARG;
   out->k_pool = m->kpool;

@@ -1,0 +1,517 @@
+// Attention of one new token per sequence over the paged cache: causal, grouped
+// queries, optional sliding window whose first tokens (sinks) stay visible.
+//
+//   o = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale q.k_t - m),  m = max_t scale q.k_t
+//   t visible  <=>  t <= pos and (window = 0 or t > pos - window or t < sinks)
+//
+// Every visible key and value is read once: the bound is HBM (2 * d * 2 bytes per
+// key and kv head against 4 * d * H/G operations).
+//
+// Work is cut evenly whatever the lengths: the visible 16-token pages of all
+// (sequence, kv head) items form one line of units, which the workers (groups of
+// 1, 2 or 4 warps, the warps of a group taking pages in turn) split into equal
+// ranges. An item inside one range is finished there; the partial states (m, sum,
+// O) of an item cut between workers go to the workspace, and the last of them to
+// take a ticket joins them in order, so that results do not depend on timing.
+//
+// A page's products run on mma.sync with the keys as the 16-row operand and the
+// H/G heads (padded to 8 or 16) as the 8-wide one, S^T = K Q^T and O^T = V^T P^T:
+// 8 heads fill the tile, where heads as rows would leave half of it empty. Keys
+// and values go from global memory straight into the operand registers: the sum
+// over dims and the order of output dims are free, so lane (r, c) takes 16-byte
+// pieces of key rows r and r + 8, and of value rows 2c, 2c+1, 2c+8, 2c+9, whose
+// 16-bit halves are then paired by byte permutes. P turns from accumulator to operand layout
+// by movmatrix. P has two 16-bit terms (the products are far from bounding), so
+// that the output's only rounding that counts is its own.
+#include <math.h>
+
+#include "kernels.h"
+
+namespace {
+
+constexpr int DW = 4;  // warps per CTA
+
+template <int HD, int NT>
+struct DCfg {
+  static constexpr int HEADS = 8 * NT;
+  static constexpr int PITCH = HD + 4;                       // floats per head row of a warp's state
+  static constexpr int STATE = HEADS * PITCH + 2 * HEADS;    // O, m, sum
+  static constexpr int PART = HEADS * (HD + 2);              // floats of a partial state in the workspace
+};
+
+AXON_DEV float ex2f(float v) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+AXON_DEV uint32_t movm(uint32_t v) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+AXON_DEV void group_sync(int group, int warps) {
+  if (warps == 1)
+    __syncwarp();
+  else
+    asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(warps * 32) : "memory");
+}
+// Two probabilities in [0, 1] as one 16-bit pair, and what the rounding lost.
+template <typename T> AXON_DEV uint32_t pack_prob(float a, float b, float& ra, float& rb);
+template <> AXON_DEV uint32_t pack_prob<bf16>(float a, float b, float& ra, float& rb) {
+  const uint32_t p = pack_bf2(a, b);
+  ra = a - bf_lo(p);
+  rb = b - bf_hi(p);
+  return p;
+}
+template <> AXON_DEV uint32_t pack_prob<f16>(float a, float b, float& ra, float& rb) {
+  __half2 h = __floats2half2_rn(a, b);
+  const float2 f = __half22float2(h);
+  ra = a - f.x;
+  rb = b - f.y;
+  return *reinterpret_cast<uint32_t*>(&h);
+}
+
+// Pages of a row: `sink` pages from the front, then those from page `first` on.
+struct RowPages {
+  int pos, lo, sink, first, n;
+};
+AXON_DEV RowPages row_pages(const PagedAttnArgs& p, int b) {
+  RowPages r;
+  r.pos = p.ctx[b] + p.pos_add;
+  const bool ok = r.pos < p.blocks_per_seq * 16;
+  if (!ok) set_err(p.err, DEVERR_POS);
+  if (!ok || r.pos < 0) {
+    r.lo = r.sink = r.first = r.n = 0;
+    r.pos = -1;
+    return r;
+  }
+  r.lo = (p.window > 0 && r.pos >= p.window) ? r.pos - p.window + 1 : 0;
+  r.first = r.lo >> 4;
+  r.sink = min((min(p.sinks, r.pos + 1) + 15) >> 4, r.first);
+  r.n = r.sink + (r.pos >> 4) + 1 - r.first;
+  return r;
+}
+
+// LO: q and o carry second 16-bit terms (q_lo read, o_lo written).
+template <int HD, typename T16, int NT, bool LO>
+__global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_kernel(const PagedAttnArgs p) {
+  using C = DCfg<HD, NT>;
+  constexpr int KI = HD / 32;  // 16-byte pieces per key row and lane
+  constexpr int VI = HD / 64;  // 16-byte pieces per value row and lane
+  constexpr int MT = HD / 16;  // 16-dim tiles of O^T
+  extern __shared__ __align__(16) float sm[];
+  float* const state = sm;                                        // [DW][STATE]
+  long long* const before = reinterpret_cast<long long*>(sm + DW * C::STATE);  // [B + 1] pages of the rows before
+  __shared__ int s_scan[DW], s_last[DW];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, c = lane & 3;
+  const int HPG = p.H / p.G;
+  grid_dep_launch();
+  grid_dep_wait();
+
+  // ---- pages before each row
+  {
+    long long base = 0;
+    for (int b0 = 0; b0 < p.B; b0 += DW * 32) {
+      const int b = b0 + tid;
+      int n = b < p.B ? row_pages(p, b).n : 0;
+      int inc = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int t = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += t;
+      }
+      if (lane == 31) s_scan[warp] = inc;
+      __syncthreads();
+      int add = 0, all = 0;
+#pragma unroll
+      for (int w = 0; w < DW; ++w) {
+        add += w < warp ? s_scan[w] : 0;
+        all += s_scan[w];
+      }
+      if (b < p.B) before[b] = base + add + inc - n;
+      base += all;
+      __syncthreads();
+    }
+    if (tid == 0) before[p.B] = base;
+    __syncthreads();
+  }
+  const long long total = before[p.B] * p.G;
+
+  // ---- rows that see nothing
+  for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
+    if (before[b + 1] != before[b]) continue;
+    for (int i = tid; i < p.H * (HD / 8); i += DW * 32) {
+      const int h = i / (HD / 8), x = i % (HD / 8);
+      const long long at = b * p.o_row + h * p.o_head + x * 8;
+      *reinterpret_cast<uint4*>(static_cast<T16*>(p.o) + at) = make_uint4(0, 0, 0, 0);
+      if (LO) *reinterpret_cast<uint4*>(static_cast<T16*>(p.o_lo) + at) = make_uint4(0, 0, 0, 0);
+      if (p.lse && x == 0) p.lse[static_cast<long long>(b) * p.H + h] = -INFINITY;
+    }
+  }
+  if (total == 0) return;
+
+  // ---- workers: more warps share an item the longer the items are
+  const long long avg = total / (static_cast<long long>(p.B) * p.G);
+  const int gs = avg >= 16 ? 4 : avg >= 4 ? 2 : 1;
+  const int group = warp / gs, wg = warp - group * gs;
+  const long long all_groups = static_cast<long long>(gridDim.x) * (DW / gs);
+  const long long nw = min(all_groups, max(1ll, total / gs));  // a page per warp at least
+  const long long wid = blockIdx.x + static_cast<long long>(gridDim.x) * group;
+  if (wid >= nw) return;
+  const long long u0 = total * wid / nw, u1 = total * (wid + 1) / nw;
+
+  int b = 0;
+  {
+    int hi = p.B;  // last row with before * G <= u0
+    while (hi - b > 1) {
+      const int mid = (b + hi) >> 1;
+      if (before[mid] * p.G <= u0) b = mid; else hi = mid;
+    }
+  }
+  const long long page_elems = 16ll * HD, block_elems = p.G * page_elems;
+  const T16* const kpool = static_cast<const T16*>(p.k);
+  const T16* const vpool = static_cast<const T16*>(p.v);
+  float* const mine = state + warp * C::STATE;
+  const float sl2 = p.scale_log2;
+
+  for (long long u = u0; u < u1;) {
+    while (before[b + 1] * p.G <= u) ++b;
+    const RowPages rp = row_pages(p, b);
+    const long long row0 = before[b] * p.G;
+    const int g = static_cast<int>((u - row0) / rp.n);
+    const long long item0 = row0 + static_cast<long long>(g) * rp.n;
+    const int off = static_cast<int>(u - item0);
+    const int cnt = static_cast<int>(min(static_cast<long long>(rp.n - off), u1 - u));
+
+    // ---- queries of the item's heads as the 8-wide operand
+    uint32_t q[NT][KI][4];
+    uint32_t ql[NT][KI][4];  // LO
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < KI; ++i) {
+        uint4 v = make_uint4(0, 0, 0, 0), w = v;
+        if (n * 8 + r < HPG) {
+          const long long at = b * p.q_row + (g * HPG + n * 8 + r) * p.q_head + (4 * i + c) * 8;
+          v = ld16(static_cast<const T16*>(p.q) + at);
+          if (LO) w = ld16(static_cast<const T16*>(p.q_lo) + at);
+        }
+        q[n][i][0] = v.x; q[n][i][1] = v.y; q[n][i][2] = v.z; q[n][i][3] = v.w;
+        ql[n][i][0] = w.x; ql[n][i][1] = w.y; ql[n][i][2] = w.z; ql[n][i][3] = w.w;
+      }
+
+    float m[NT][2], l[NT][2], o[NT][MT][4];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      m[n][0] = m[n][1] = -INFINITY;
+      l[n][0] = l[n][1] = 0.f;
+#pragma unroll
+      for (int j = 0; j < MT; ++j) o[n][j][0] = o[n][j][1] = o[n][j][2] = o[n][j][3] = 0.f;
+    }
+
+    // ---- this warp's pages: off + wg, off + wg + gs, ...
+    const int pages = cnt > wg ? (cnt - wg + gs - 1) / gs : 0;
+    auto logical = [&](int k) {  // page of the row that is this warp's k-th
+      const int i = off + wg + k * gs;
+      return i < rp.sink ? i : i - rp.sink + rp.first;
+    };
+    auto entries = [&](int k0) {  // pool blocks of this warp's pages k0 .. k0 + 31, one per lane
+      const int k = k0 + lane;
+      if (k >= pages) return -1;
+      const int j = logical(k);
+      const int blk = p.block_table ? p.block_table[static_cast<long long>(b) * p.blocks_per_seq + j]
+                                    : b * p.blocks_per_seq + j;
+      if (blk >= 0 && blk < p.num_blocks) return blk;
+      set_err(p.err, DEVERR_BLOCK);
+      return -1;
+    };
+    uint4 kv[2][KI], vv[4][VI];
+    auto seen = [&](int t) { return t <= rp.pos && (t >= rp.lo || t < p.sinks); };
+    auto load_k = [&](int blk, int t0) {
+      const T16* at = kpool + blk * block_elems + g * page_elems;
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int i = 0; i < KI; ++i)
+          kv[x][i] = (blk >= 0 && seen(t0 + r + 8 * x)) ? ld_stream16(at + (r + 8 * x) * HD + (4 * i + c) * 8)
+                                                        : make_uint4(0, 0, 0, 0);
+    };
+    // rows of tokens that are not visible are left out, not multiplied by zero:
+    // what a page holds there may be anything
+    auto load_v = [&](int blk, int t0) {
+      const T16* at = vpool + blk * block_elems + g * page_elems;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int t = 2 * c + (x & 1) + 8 * (x >> 1);
+#pragma unroll
+        for (int i = 0; i < VI; ++i)
+          vv[x][i] = (blk >= 0 && seen(t0 + t)) ? ld_stream16(at + t * HD + (r + 8 * i) * 8) : make_uint4(0, 0, 0, 0);
+      }
+    };
+    if (pages > 0) {
+      int ent = entries(0);
+      int blk = __shfl_sync(0xffffffffu, ent, 0), t0 = logical(0) * 16;
+      load_k(blk, t0);
+      load_v(blk, t0);
+      for (int k = 0; k < pages; ++k) {
+        float s[NT][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          float e[4] = {0.f, 0.f, 0.f, 0.f}, f[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < KI; ++i) {
+            const uint32_t a0[4] = {kv[0][i].x, kv[1][i].x, kv[0][i].y, kv[1][i].y};
+            const uint32_t a1[4] = {kv[0][i].z, kv[1][i].z, kv[0][i].w, kv[1][i].w};
+            mma16816<T16>(e, a0, &q[n][i][0]);
+            mma16816<T16>(f, a1, &q[n][i][2]);
+            if (LO) {
+              mma16816<T16>(e, a0, &ql[n][i][0]);
+              mma16816<T16>(f, a1, &ql[n][i][2]);
+            }
+          }
+#pragma unroll
+          for (int x = 0; x < 4; ++x) s[n][x] = e[x] + f[x];
+        }
+        const bool ok0 = blk >= 0 && seen(t0 + r), ok1 = blk >= 0 && seen(t0 + r + 8);
+        if (((k + 1) & 31) == 0) ent = entries(k + 1);
+        const int nblk = __shfl_sync(0xffffffffu, ent, (k + 1) & 31), nt0 = logical(k + 1) * 16;
+        const bool more = k + 1 < pages;
+        if (more) load_k(nblk, nt0);
+
+        uint32_t ph[NT][2], pl[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          float mx[2];
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            s[n][x] = ok0 ? s[n][x] * sl2 : -INFINITY;
+            s[n][2 + x] = ok1 ? s[n][2 + x] * sl2 : -INFINITY;
+            mx[x] = fmaxf(s[n][x], s[n][2 + x]);
+#pragma unroll
+            for (int w = 4; w < 32; w <<= 1) mx[x] = fmaxf(mx[x], __shfl_xor_sync(0xffffffffu, mx[x], w));
+            mx[x] = fmaxf(mx[x], m[n][x]);
+          }
+          if (__any_sync(0xffffffffu, mx[0] > m[n][0] || mx[1] > m[n][1])) {
+            const float f0 = mx[0] > m[n][0] ? ex2f(m[n][0] - mx[0]) : 1.f;
+            const float f1 = mx[1] > m[n][1] ? ex2f(m[n][1] - mx[1]) : 1.f;
+            m[n][0] = mx[0];
+            m[n][1] = mx[1];
+            l[n][0] *= f0;
+            l[n][1] *= f1;
+#pragma unroll
+            for (int j = 0; j < MT; ++j) {
+              o[n][j][0] *= f0;
+              o[n][j][1] *= f1;
+              o[n][j][2] *= f0;
+              o[n][j][3] *= f1;
+            }
+          }
+          const float b0 = m[n][0] == -INFINITY ? 0.f : m[n][0], b1 = m[n][1] == -INFINITY ? 0.f : m[n][1];
+          const float p0 = ex2f(s[n][0] - b0), p1 = ex2f(s[n][1] - b1);
+          const float p2 = ex2f(s[n][2] - b0), p3 = ex2f(s[n][3] - b1);
+          l[n][0] += p0 + p2;
+          l[n][1] += p1 + p3;
+          float r0, r1, r2, r3, z;
+          ph[n][0] = movm(pack_prob<T16>(p0, p1, r0, r1));
+          ph[n][1] = movm(pack_prob<T16>(p2, p3, r2, r3));
+          pl[n][0] = movm(pack_prob<T16>(r0, r1, z, z));
+          pl[n][1] = movm(pack_prob<T16>(r2, r3, z, z));
+        }
+#pragma unroll
+        for (int i = 0; i < VI; ++i) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            auto word = [&](const uint4& v) { return x == 0 ? v.x : x == 1 ? v.y : x == 2 ? v.z : v.w; };
+            const uint32_t w0 = word(vv[0][i]), w1 = word(vv[1][i]), w2 = word(vv[2][i]), w3 = word(vv[3][i]);
+            const uint32_t a[4] = {__byte_perm(w0, w1, 0x5410), __byte_perm(w0, w1, 0x7632),
+                                   __byte_perm(w2, w3, 0x5410), __byte_perm(w2, w3, 0x7632)};
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              mma16816<T16>(o[n][4 * i + x], a, ph[n]);
+              mma16816<T16>(o[n][4 * i + x], a, pl[n]);
+            }
+          }
+        }
+        if (more) load_v(nblk, nt0);
+        blk = nblk;
+        t0 = nt0;
+      }
+    }
+
+    // ---- the group's states, joined
+    float* const sO = mine;
+    float* const sM = mine + C::HEADS * C::PITCH;
+    float* const sL = sM + C::HEADS;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+#pragma unroll
+        for (int w = 4; w < 32; w <<= 1) l[n][x] += __shfl_xor_sync(0xffffffffu, l[n][x], w);
+        if (r == 0) {
+          sM[n * 8 + 2 * c + x] = m[n][x];
+          sL[n * 8 + 2 * c + x] = l[n][x];
+        }
+#pragma unroll
+        for (int i = 0; i < VI; ++i)
+#pragma unroll
+          for (int w = 0; w < 2; ++w)
+            *reinterpret_cast<float4*>(sO + (n * 8 + 2 * c + x) * C::PITCH + (r + 8 * i) * 8 + w * 4) =
+                make_float4(o[n][4 * i + 2 * w][x], o[n][4 * i + 2 * w][2 + x], o[n][4 * i + 2 * w + 1][x],
+                            o[n][4 * i + 2 * w + 1][2 + x]);
+      }
+    }
+    group_sync(group, gs);
+    const long long item = static_cast<long long>(b) * p.G + g;
+    const bool whole = off == 0 && cnt == rp.n;
+    float* const part = p.part + (2 * wid + (off > 0 ? 0 : 1)) * C::PART;
+    const float* const gstate = state + group * gs * C::STATE;
+    const int gl = wg * 32 + lane;
+    auto finish = [&](int h, int x, const float (&v)[8], float M, float L) {
+      const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
+      const long long at = b * p.o_row + (g * HPG + h) * p.o_head + x * 8;
+      uint32_t w[4], wl[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float a = v[2 * i] * inv, e = v[2 * i + 1] * inv;
+        w[i] = pack2<T16>(a, e);
+        if (LO) {
+          const T16* hv = reinterpret_cast<const T16*>(&w[i]);
+          wl[i] = pack2<T16>(a - to_f(hv[0]), e - to_f(hv[1]));
+        }
+      }
+      *reinterpret_cast<uint4*>(static_cast<T16*>(p.o) + at) = make_uint4(w[0], w[1], w[2], w[3]);
+      if (LO) *reinterpret_cast<uint4*>(static_cast<T16*>(p.o_lo) + at) = make_uint4(wl[0], wl[1], wl[2], wl[3]);
+      if (p.lse && x == 0)
+        p.lse[static_cast<long long>(b) * p.H + g * HPG + h] = (M + log2f(L)) * 0.69314718055994531f;
+    };
+    for (int i = gl; i < HPG * (HD / 8); i += gs * 32) {
+      const int h = i / (HD / 8), x = i % (HD / 8);
+      float M = -INFINITY, L = 0.f, v[8] = {};
+      for (int w = 0; w < gs; ++w) M = fmaxf(M, gstate[w * C::STATE + C::HEADS * C::PITCH + h]);
+      const float base = M == -INFINITY ? 0.f : M;
+      for (int w = 0; w < gs; ++w) {
+        const float* st = gstate + w * C::STATE;
+        const float f = ex2f(st[C::HEADS * C::PITCH + h] - base);
+        L += f * st[C::HEADS * C::PITCH + C::HEADS + h];
+#pragma unroll
+        for (int y = 0; y < 8; ++y) v[y] += f * st[h * C::PITCH + x * 8 + y];
+      }
+      if (whole) {
+        finish(h, x, v, M, L);
+      } else {
+        float* at = part + h * HD + x * 8;
+        *reinterpret_cast<float4*>(at) = make_float4(v[0], v[1], v[2], v[3]);
+        *reinterpret_cast<float4*>(at + 4) = make_float4(v[4], v[5], v[6], v[7]);
+        if (x == 0) {
+          part[C::HEADS * HD + h] = M;
+          part[C::HEADS * HD + C::HEADS + h] = L;
+        }
+      }
+    }
+    group_sync(group, gs);
+    if (!whole) {
+      // the workers of units item0 .. item0 + n - 1 hold a part each
+      const long long first = ((item0 + 1) * nw - 1) / total, last = ((item0 + rp.n) * nw - 1) / total;
+      if (gl == 0) {
+        const int parts = static_cast<int>(last - first + 1);
+        const bool is_last = atom_add_acq_rel_gpu(p.ticket + item, 1) == parts - 1;
+        if (is_last) p.ticket[item] = 0;
+        s_last[group] = is_last;
+      }
+      group_sync(group, gs);
+      if (s_last[group]) {
+        for (int i = gl; i < HPG * (HD / 8); i += gs * 32) {
+          const int h = i / (HD / 8), x = i % (HD / 8);
+          float M = -INFINITY, L = 0.f, v[8] = {};
+          for (long long w0 = first; w0 <= last; w0 += 4) {
+            float pm[4], ps[4];
+            float4 pa[4], pb[4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              const long long w = w0 + y;
+              if (w <= last) {
+                const float* at = p.part + (2 * w + (w > first ? 0 : 1)) * C::PART;
+                pm[y] = __ldcg(at + C::HEADS * HD + h);
+                ps[y] = __ldcg(at + C::HEADS * HD + C::HEADS + h);
+                pa[y] = __ldcg(reinterpret_cast<const float4*>(at + h * HD + x * 8));
+                pb[y] = __ldcg(reinterpret_cast<const float4*>(at + h * HD + x * 8 + 4));
+              } else {
+                pm[y] = -INFINITY;
+                ps[y] = 0.f;
+                pa[y] = pb[y] = make_float4(0.f, 0.f, 0.f, 0.f);
+              }
+            }
+            const float nm = fmaxf(fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])), M);
+            const float base = nm == -INFINITY ? 0.f : nm;
+            const float f = ex2f(M - base);
+            M = nm;
+            L *= f;
+#pragma unroll
+            for (int y = 0; y < 8; ++y) v[y] *= f;
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              const float e = ex2f(pm[y] - base);
+              L += e * ps[y];
+              v[0] += e * pa[y].x; v[1] += e * pa[y].y; v[2] += e * pa[y].z; v[3] += e * pa[y].w;
+              v[4] += e * pb[y].x; v[5] += e * pb[y].y; v[6] += e * pb[y].z; v[7] += e * pb[y].w;
+            }
+          }
+          finish(h, x, v, M, L);
+        }
+      }
+      group_sync(group, gs);
+    }
+    u += cnt;
+  }
+}
+
+template <int HD, int NT>
+constexpr size_t smem_bytes(int B) {
+  return static_cast<size_t>(DW) * DCfg<HD, NT>::STATE * 4 + (static_cast<size_t>(B) + 1) * 8;
+}
+
+template <int HD, typename T16, int NT, bool LO>
+cudaError_t launch_nt(const LaunchCtx& lc, const PagedAttnArgs& a) {
+  const size_t smem = smem_bytes<HD, NT>(a.B);
+  cudaError_t e = cudaFuncSetAttribute(attn_paged_decode_kernel<HD, T16, NT, LO>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       static_cast<int>(smem_bytes<HD, NT>(PAGED_ATTN_MAX_B)));
+  if (e != cudaSuccess) return e;
+  // no more CTAs than pages that can be visible, at a page per warp
+  long long row = a.blocks_per_seq;
+  if (a.window > 0) row = min(row, static_cast<long long>(a.window - 1) / 16 + 2 + (a.sinks + 15ll) / 16);
+  const long long pages = row * a.B * a.G, most = static_cast<long long>(lc.num_sms) * (NT == 1 ? 3 : 2);
+  const long long grid = min(most, (pages + DW - 1) / DW);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(grid));
+  cfg.blockDim = dim3(DW * 32);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = lc.stream;
+  cudaLaunchAttribute attr[2];
+  cfg.numAttrs = chain_attrs(lc, attr);
+  cfg.attrs = attr;
+  return cudaLaunchKernelEx(&cfg, attn_paged_decode_kernel<HD, T16, NT, LO>, a);
+}
+
+template <int HD, typename T16>
+cudaError_t launch_hd(const LaunchCtx& lc, const PagedAttnArgs& a) {
+  if (a.q_lo) return a.H / a.G <= 8 ? launch_nt<HD, T16, 1, true>(lc, a) : launch_nt<HD, T16, 2, true>(lc, a);
+  return a.H / a.G <= 8 ? launch_nt<HD, T16, 1, false>(lc, a) : launch_nt<HD, T16, 2, false>(lc, a);
+}
+
+}  // namespace
+
+// Partial states first, then the tickets (zero between calls).
+size_t paged_attn_part_bytes(int H, int G, int d, int num_sms) {
+  const bool two = H / G > 8;
+  const size_t workers = static_cast<size_t>(num_sms) * (two ? 2 : 3) * DW;
+  return 2 * workers * (two ? 16 : 8) * (d + 2) * 4;
+}
+
+cudaError_t launch_attn_paged_decode(const LaunchCtx& lc, const PagedAttnArgs& a) {
+  if (a.H / a.G > 16 || a.B < 1 || a.B > PAGED_ATTN_MAX_B || !a.q_lo != !a.o_lo)
+    return cudaErrorInvalidValue;
+  if (a.d == 64) return lc.f16 ? launch_hd<64, f16>(lc, a) : launch_hd<64, bf16>(lc, a);
+  if (a.d == 128) return lc.f16 ? launch_hd<128, f16>(lc, a) : launch_hd<128, bf16>(lc, a);
+  return cudaErrorInvalidValue;
+}

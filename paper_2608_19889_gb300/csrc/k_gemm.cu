@@ -426,11 +426,14 @@ bool make_tma_2d_16(CUtensorMap* map, const void* base, uint64_t rows, uint64_t 
 }
 
 bool make_tma_3d_16(CUtensorMap* map, const void* base, uint64_t d0, uint64_t d1, uint64_t d2, uint32_t box1,
-                    uint32_t box2, bool f16) {
+                    uint32_t box2, bool f16, uint64_t stride1, uint64_t stride2) {
   PFN_cuTensorMapEncodeTiled_v12000 fn = encode_fn();
-  if (!fn || (reinterpret_cast<uintptr_t>(base) & 15) || ((d0 * 2) & 15)) return false;
+  if (!stride1) stride1 = d0;
+  if (!stride2) stride2 = d0 * d1;
+  if (!fn || (reinterpret_cast<uintptr_t>(base) & 15) || ((d0 * 2) & 15) || ((stride1 * 2) & 15) || ((stride2 * 2) & 15))
+    return false;
   cuuint64_t dims[3] = {d0, d1, d2};
-  cuuint64_t strides[2] = {d0 * 2, d0 * d1 * 2};
+  cuuint64_t strides[2] = {stride1 * 2, stride2 * 2};
   cuuint32_t box[3] = {static_cast<cuuint32_t>(BK), box1, box2};
   cuuint32_t estr[3] = {1, 1, 1};
   return fn(map, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base),

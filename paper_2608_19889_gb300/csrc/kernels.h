@@ -184,6 +184,65 @@ bool make_attn_maps(AttnMaps* maps, const void* q, long long rows, const void* k
 cudaError_t launch_attn_prefill_tc(const LaunchCtx& lc, const AttnArgs& a, const AttnMaps& maps, int layer, int B,
                                    const AttnVarlen* vl = nullptr);
 cudaError_t prepare_attn_tc_kernels();
+// What the tcgen05 prefill attention takes beyond a model's own buffers (k_attn_tc.cu,
+// EXT instantiations): sinks (with a window, the first tokens that stay visible),
+// output strides in elements; row offsets and lengths are checked, as nothing else does.
+struct AttnExt {
+  int sinks;
+  long long o_row, o_head;
+};
+// q [rows][H][d] with these strides in elements; the pools hold one layer.
+bool make_attn_maps_strided(AttnMaps* maps, const void* q, long long rows, long long q_row, long long q_head,
+                            const void* kpool, const void* vpool, long long pool_rows, int H, int G, int d, bool f16);
+cudaError_t launch_attn_prefill_ext(const LaunchCtx& lc, const AttnArgs& a, const AttnMaps& maps, int layer, int B,
+                                    const AttnVarlen* vl, const AttnExt& ext);
+
+// ---- attention of one new token per row over the paged cache (k_attn_paged.cu)
+constexpr int PAGED_ATTN_MAX_B = 2048;
+struct PagedAttnArgs {
+  const void* q;  // [B][H][d], strides in elements
+  long long q_row, q_head;
+  const void* q_lo;  // optional second term of q, same strides (then o_lo too)
+  const void* k;     // layer pool [num_blocks][G][16][d]
+  const void* v;
+  const int* ctx;  // row b's query is at position ctx[b] + pos_add; negative: the row is idle
+  int pos_add;
+  const int* block_table;  // [B][blocks_per_seq], or null: blocks b * blocks_per_seq + j
+  int blocks_per_seq, num_blocks;
+  int B, H, G, d;
+  int window, sinks;
+  float scale_log2;
+  void* o;
+  long long o_row, o_head;
+  void* o_lo;
+  float* lse;   // optional [B][H], natural logarithm
+  float* part;  // paged_attn_part_bytes
+  int* ticket;  // [B * G], zero between calls
+  int* err;
+};
+size_t paged_attn_part_bytes(int H, int G, int d, int num_sms);
+cudaError_t launch_attn_paged_decode(const LaunchCtx& lc, const PagedAttnArgs& a);
+
+// ---- blocks of the paged cache (k_pages.cu)
+struct PagesArgs {
+  void* k;  // [L][N][block_bytes / 16]
+  void* v;
+  int L, N;
+  long long block_bytes;  // of one layer's keys (or values) in a block, a multiple of 2048
+  int* table;             // [R][P]
+  int* ctx;               // [R]
+  int* refs;              // [N]
+  int R, P;
+  int* work;  // pages_work_ints
+  int* err;
+};
+size_t pages_work_ints(int N, int R, int P);
+cudaError_t launch_pages_copy(const LaunchCtx& lc, const PagesArgs& a, const int* src, const int* dst, int n);
+cudaError_t launch_pages_release(const LaunchCtx& lc, const PagesArgs& a, const int* rows, int n, int window, int sinks);
+cudaError_t launch_pages_reserve(const LaunchCtx& lc, const PagesArgs& a, const int* rows, const int* more, int n);
+cudaError_t launch_pages_fork(const LaunchCtx& lc, const PagesArgs& a, const int* src, const int* dst, int n);
+cudaError_t launch_pages_compact(const LaunchCtx& lc, const PagesArgs& a, int* moved, int* live);
+
 // Key splits of the decode attention (1 .. min(max_blocks, 64)): the count
 // with the smallest estimated makespan over num_sms SMs, or, with
 // target_ctas > 0, as many as keep B x G x splits within that many CTAs.
@@ -214,9 +273,10 @@ struct GemmMaps {
   const GemmMaps* n128 = nullptr;  // the same operands with 128-row weight boxes (128-wide tiles), or null
 };
 bool make_tma_2d_16(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows, bool f16);
-// [d2][d1][d0] 16-bit tensor, box box2 x box1 x 64 elements, 128-byte swizzle.
+// [d2][d1][d0] 16-bit tensor, box box2 x box1 x 64 elements, 128-byte swizzle;
+// strides in elements (0: dense).
 bool make_tma_3d_16(CUtensorMap* map, const void* base, uint64_t d0, uint64_t d1, uint64_t d2, uint32_t box1,
-                    uint32_t box2, bool f16);
+                    uint32_t box2, bool f16, uint64_t stride1 = 0, uint64_t stride2 = 0);
 // Row-major [rows][cols] 16-bit matrix, box box_cols x box_rows, no swizzle
 // (dense rows in shared memory); out-of-range elements read as zero.
 bool make_tma_2d_plain(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint32_t box_cols,

@@ -83,11 +83,13 @@ class AxonError(RuntimeError):
 
 
 _lib = None
+_torch = None  # imported with the library
+_raw_stream = None  # (device index) -> the current stream's handle
 
 
 def lib() -> ctypes.CDLL:
     """Load the CUDA library (raises if it has not been built)."""
-    global _lib
+    global _lib, _torch, _raw_stream
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} is missing: build it with paper_2608_19889_gb300.build.build()")
@@ -130,6 +132,10 @@ def lib() -> ctypes.CDLL:
                   "axon_attn_decode_workspace", "axon_attn_prefill", "axon_kv_copy_blocks", "axon_kv_fork",
                   "axon_kv_release", "axon_kv_reserve", "axon_kv_compact", "axon_kv_workspace", "axon_check_error"):
             getattr(L, n).restype = ctypes.c_int
+        import torch
+        _torch = torch
+        # a handle without the Stream object around it (0.1 us against 3 us), where this torch has the call
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         _lib = L
     return _lib
 
@@ -140,8 +146,10 @@ def _ptr(t):
 
 def _stream(stream):
     if stream is None:
-        import torch
-        stream = torch.cuda.current_stream()
+        lib()
+        if _raw_stream is not None:
+            return ctypes.c_void_p(_raw_stream(_torch.cuda.current_device()))
+        stream = _torch.cuda.current_stream()
     return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
 
@@ -287,21 +295,21 @@ def axon_free(m):
 
 def _is(t, dtype, what, *shape):
     """Refuse a tensor the C call could not tell from a right one: device, type, shape, dense layout."""
-    if not t.is_cuda or t.dtype != dtype or not t.is_contiguous() or (shape and t.shape != shape):
+    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous() or (shape and t.shape != shape):
         raise TypeError(f"{what}: a dense {dtype} device tensor{' of shape ' + str(shape) if shape else ''} is wanted, "
                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
 def _ints(t, what, *shape):
-    import torch
-    return None if t is None else _is(t, torch.int32, what, *shape)
+    return None if t is None else _is(t, _torch.int32, what, *shape)
 
 
 def make_kv_cache(k, v) -> axon_kv_cache:
     """Descriptor of the pools k, v: dense device tensors [layers, blocks, kv heads, 16, head_dim] (bf16, fp16; the
     block operators also take fp32). It holds their addresses: keep the tensors."""
-    import torch
+    lib()
+    torch = _torch
     prec = {torch.bfloat16: AXON_BF16, torch.float16: AXON_FP16, torch.float32: AXON_FP32_DEBUG}.get(k.dtype)
     if prec is None or k.dim() != 5:
         raise TypeError(f"k: a bf16, fp16 or fp32 tensor of 5 dimensions is wanted, got {k.dtype} {tuple(k.shape)}")
@@ -314,10 +322,9 @@ def make_kv_cache(k, v) -> axon_kv_cache:
 
 def axon_kv_cache_get(m) -> axon_kv_cache:
     """Descriptor of a model's own cache."""
-    import torch
     c = axon_kv_cache()
     _check("axon_kv_cache_get", lib().axon_kv_cache_get(m, ctypes.byref(c)))
-    c.dtype = {AXON_BF16: torch.bfloat16, AXON_FP16: torch.float16, AXON_FP32_DEBUG: torch.float32}[c.precision]
+    c.dtype = {AXON_BF16: _torch.bfloat16, AXON_FP16: _torch.float16, AXON_FP32_DEBUG: _torch.float32}[c.precision]
     c.ref = ctypes.byref(c)
     return c
 
@@ -325,6 +332,7 @@ def axon_kv_cache_get(m) -> axon_kv_cache:
 def make_kv_seqs(block_table, context_lens, refs) -> axon_kv_seqs:
     """Descriptor of a block table [rows, blocks per row], lengths [rows] and counts [blocks] (int32, device). It holds
     their addresses: keep the tensors."""
+    lib()
     R, P = block_table.shape
     s = axon_kv_seqs(_ints(block_table, "block_table"), _ints(context_lens, "context_lens", R), _ints(refs, "refs"), R, P)
     s.num_blocks = refs.numel()
@@ -334,24 +342,22 @@ def make_kv_seqs(block_table, context_lens, refs) -> axon_kv_seqs:
 
 def make_attn_workspace(cache, rows, heads):
     """Zeroed workspace of axon_attn_decode for up to `rows` rows of `heads` heads."""
-    import torch
     n = ctypes.c_int64(0)
     _check("axon_attn_decode_workspace", lib().axon_attn_decode_workspace(cache.ref, heads, rows, ctypes.byref(n)))
-    return torch.zeros(n.value, dtype=torch.uint8, device="cuda")
+    return _torch.zeros(n.value, dtype=_torch.uint8, device="cuda")
 
 
 def make_kv_workspace(cache, seqs):
     """Workspace of axon_kv_fork, axon_kv_reserve and axon_kv_compact."""
-    import torch
     n = ctypes.c_int64(0)
     _check("axon_kv_workspace", lib().axon_kv_workspace(cache.ref, seqs.ref, ctypes.byref(n)))
-    return torch.empty(n.value, dtype=torch.uint8, device="cuda")
+    return _torch.empty(n.value, dtype=_torch.uint8, device="cuda")
 
 
 def _rows_of(t, cache, what):
     """(address, row stride, head stride) of a [rows, heads, head_dim] tensor of the cache's type."""
     row, head, one = t.stride()
-    if t.dtype != cache.dtype or not t.is_cuda or one != 1 or t.shape[2] != cache.head_dim:
+    if t.dtype is not cache.dtype or not t.is_cuda or one != 1 or t.shape[2] != cache.head_dim:
         raise TypeError(f"{what}: a {cache.dtype} device tensor [rows, heads, {cache.head_dim}] with a dense last "
                         f"dimension is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr(), row, head
@@ -368,7 +374,6 @@ def axon_attn_decode(cache, layer, q, context_lens, out, workspace, block_table=
     """Attention of one new token per row (see include/axon.h). q, out: [B, heads, head_dim], any row and head strides;
     context_lens: int32 [B]; block_table: int32 [B, blocks], or None with blocks_per_seq for contiguous rows;
     workspace: make_attn_workspace; lse: fp32 [B, heads] or None; err: int32 [1] error word or None."""
-    import torch
     B, H, _ = q.shape
     if out.shape != q.shape:
         raise TypeError(f"out: the shape of q {tuple(q.shape)} is wanted, got {tuple(out.shape)}")
@@ -377,7 +382,7 @@ def axon_attn_decode(cache, layer, q, context_lens, out, workspace, block_table=
     table, per = _table_of(block_table, blocks_per_seq, B)
     _check("axon_attn_decode", lib().axon_attn_decode(
         cache.ref, layer, qp, qr, qh, B, H, _ints(context_lens, "context_lens", B), table, per, window, sinks, scale, op,
-        orow, ohead, None if lse is None else _is(lse, torch.float32, "lse", B, H), workspace.data_ptr(),
+        orow, ohead, None if lse is None else _is(lse, _torch.float32, "lse", B, H), workspace.data_ptr(),
         workspace.numel(), _ints(err, "err", 1), _stream(stream)))
 
 

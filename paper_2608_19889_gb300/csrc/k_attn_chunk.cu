@@ -1,0 +1,626 @@
+// Attention of chunks of new tokens over the paged cache (axon_attn_prefill): causal,
+// grouped queries, optional sliding window with sinks, on the 5th-generation tensor
+// cores.
+//
+//   o = sum_t p_t v_t / sum_t p_t,  p_t = 2^(s_t - m),  s_t = scale log2(e) q.k_t
+//
+// A tile is 128 rows = PW consecutive positions x the H/G query heads of one kv head
+// (PW = 128 / (H/G)). An item is two such tiles of consecutive positions, which share the
+// keys: 128 per step (eight 16-token blocks), those of the sinks first. One CTA per SM takes items in
+// turn; the copies and the first scores of the next item run under the end of the
+// one before. Warps:
+//   0..3, 4..7  softmax of tile 0 and 1, one thread per row (no shuffles), with 208
+//               registers each (setmaxnreg), so that 128 scores stay in registers;
+//   8           TMA producer: Q of an item, K and V through a ring of 32 KB (16 KB)
+//               stages, lane i fetching the table entry of block i;
+//   9           MMA issuer: S = Q K^T into TMEM, O += P V with P read back from TMEM;
+//   10          finds the items, two ahead, and publishes them.
+// The 512 TMEM columns hold S0, S1 (128 each, later P in the first 64) and O0, O1.
+//
+// The running maximum m lags: it is raised, and O rescaled, only when a row's
+// scores exceed it by more than 8 (p <= 2^8): rounding to 16 bits is relative, so the
+// error of a probability is the same, and most steps touch O not at all. The row sum
+// is fp32 of the unrounded probabilities.
+//
+// Bound: a 128 x 128 tile at head_dim 128 takes 1024 tensor cycles (2 x 2 x 128^3
+// operations at 8192 per cycle), and per scheduler 512 cycles of the exponential
+// unit and about 430 issue slots, so two tiles in turn can keep the tensor pipe
+// busy while the softmax of one takes no longer than the products of the other.
+#include <math.h>
+
+#include "kernels.h"
+
+namespace {
+
+constexpr int THREADS = 384;
+constexpr int KT = 128;  // keys per step
+constexpr float LAG = 8.f;
+
+template <int HD>
+struct KCfg {
+  static constexpr int CH = HD / 64;                // 64-dim chunks (128-byte swizzled rows)
+  static constexpr int CHUNK = 128 * 128;           // bytes of one 128-row chunk
+  static constexpr int TILE = CH * CHUNK;           // Q, K or V tile
+  static constexpr int STAGES = HD == 128 ? 5 : 8;  // K and V tiles in flight
+  static constexpr int BARS = 2 * STAGES + 12 + 4;
+  static constexpr int SMEM = 2 * TILE + STAGES * TILE + 8 * BARS + 2 * 32 + 16 + 1024;
+};
+
+AXON_DEV void tma_load_3d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+          dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
+      : "memory");
+}
+// D[tmem] (+)= A[tmem] * B[smem desc] (A: 128 lanes, two 16-bit values per column).
+AXON_DEV void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(
+          d_tmem),
+      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+AXON_DEV void ld32(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,"
+      "%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+}
+AXON_DEV void st32(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,"
+      "%30,%31,%32};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+      "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+      "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+AXON_DEV void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+AXON_DEV float ex2(float v) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+// Two fp32 values in one 64-bit register: one issue slot for both.
+AXON_DEV uint64_t pk2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+AXON_DEV void upk2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+AXON_DEV uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+AXON_DEV uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+AXON_DEV uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// Probabilities lie in [0, 2^8]: no saturation needed.
+template <typename T> AXON_DEV uint32_t pack_p(float lo, float hi);
+template <> AXON_DEV uint32_t pack_p<bf16>(float lo, float hi) { return pack_bf2(lo, hi); }
+template <> AXON_DEV uint32_t pack_p<f16>(float lo, float hi) {
+  __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<uint32_t*>(&h);
+}
+// The V tile as the B operand of P V: N = dims (contiguous in memory), K = tokens at
+// 128-byte pitch; 8-token groups 1024 bytes apart, the second 64 dims one chunk further.
+template <int HD>
+AXON_DEV uint64_t v_desc(uint32_t addr) {
+  uint64_t d = smem_desc_sw128(addr);
+  d &= ~(static_cast<uint64_t>(0x3FFFu) << 16);
+  d |= static_cast<uint64_t>(KCfg<HD>::CHUNK >> 4) << 16;
+  return d;
+}
+
+// Bits c of 0 .. 15 with lo <= base + c < hi.
+AXON_DEV uint32_t bits16(int base, int lo, int hi) {
+  const int a = min(max(lo - base, 0), 16), b = min(max(hi - base, 0), 16);
+  return b > a ? (1u << b) - (1u << a) : 0u;
+}
+
+// A work item: tiles of PC = 2 PW positions of one sequence's chunk and one kv head.
+struct Item {
+  int b, g, p0, row0, S, past;  // b < 0: none
+};
+
+// Item `item` of the launch: sequences in order, a sequence's position pairs from the
+// end (those with the most keys first), the kv heads of a pair together. Offsets and lengths that do not
+// fit are reported and give no items.
+AXON_DEV Item find_item(const ChunkArgs& p, int PC, long long item) {
+  Item r;
+  r.b = -1;
+  r.g = static_cast<int>(item % p.G);
+  const long long pair = item / p.G;
+  const int lane = threadIdx.x & 31;
+  long long before = 0;
+  for (int b0 = 0; b0 < p.B; b0 += 32) {
+    int r0 = 0, len = 0, ps = 0;
+    if (b0 + lane < p.B) {
+      r0 = p.cu[b0 + lane];
+      const int r1 = p.cu[b0 + lane + 1];
+      ps = p.past[b0 + lane];
+      len = r1 - r0;
+      const bool off = r0 < 0 || r1 < r0 || r1 > p.T || len > p.max_chunk;
+      const bool far = ps < 0 || ps > p.blocks_per_seq * 16 - len;
+      if (off || far) {
+        if (off || len) set_err(p.err, off ? DEVERR_SEQ : DEVERR_POS);
+        len = 0;
+      }
+      if ((b0 + lane == 0 && r0 != 0) || (b0 + lane == p.B - 1 && r1 != p.T)) set_err(p.err, DEVERR_SEQ);
+    }
+    const int mine = (len + PC - 1) / PC;
+    int end = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int t = __shfl_up_sync(0xffffffffu, end, o);
+      if (lane >= o) end += t;
+    }
+    const unsigned hit = __ballot_sync(0xffffffffu, pair < before + end);
+    if (hit) {
+      const int src = __ffs(hit) - 1;
+      r.b = b0 + src;
+      r.row0 = __shfl_sync(0xffffffffu, r0, src);
+      r.S = __shfl_sync(0xffffffffu, len, src);
+      r.past = __shfl_sync(0xffffffffu, ps, src);
+      r.p0 = static_cast<int>(before + __shfl_sync(0xffffffffu, end, src) - 1 - pair) * PC;
+      return r;
+    }
+    before += __shfl_sync(0xffffffffu, end, 31);
+  }
+  return r;
+}
+
+// Which blocks an item's tiles see: `ns` blocks of sinks, then those from `jlo` on; nb[w]
+// of them reach tile w.
+struct Span {
+  int nw, jlo, ns, pend;
+  int nb[2];
+  AXON_DEV int steps(int w) const { return (nb[w] + 7) >> 3; }
+};
+AXON_DEV Span span_of(const ChunkArgs& p, const Item& it, int PW) {
+  Span s;
+  s.nw = it.p0 + PW < it.S ? 2 : 1;
+  const int first = it.past + it.p0;
+  s.jlo = p.window > 0 && first >= p.window ? (first - p.window + 1) >> 4 : 0;
+  s.ns = min((p.sinks + 15) >> 4, s.jlo);
+  s.pend = it.past + min(it.p0 + s.nw * PW, it.S);
+  const int pend0 = it.past + min(it.p0 + PW, it.S);
+  s.nb[0] = s.ns + ((pend0 + 15) >> 4) - s.jlo;
+  s.nb[1] = s.ns + ((s.pend + 15) >> 4) - s.jlo;
+  return s;
+}
+
+template <int HD, typename T16>
+__global__ void __launch_bounds__(THREADS, 1)
+    attn_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                      const __grid_constant__ CUtensorMap tmV, const ChunkArgs p, int PW, int pool_row0, int pool_rows) {
+  using C = KCfg<HD>;
+  constexpr int NS = C::STAGES;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  const uint32_t sQ = base, sKV = base + 2 * C::TILE, bars = sKV + NS * C::TILE;
+  auto kv_full = [&](int s) { return bars + 8 * s; };
+  auto kv_empty = [&](int s) { return bars + 8 * (NS + s); };
+  const uint32_t more = bars + 8 * (2 * NS);
+  auto q_full = [&](int w) { return more + 8 * w; };
+  auto q_empty = [&](int w) { return more + 8 * (2 + w); };
+  auto s_full = [&](int w) { return more + 8 * (4 + w); };
+  auto p_full = [&](int w) { return more + 8 * (6 + w); };
+  auto o_full = [&](int w) { return more + 8 * (8 + w); };
+  auto o_empty = [&](int w) { return more + 8 * (10 + w); };
+  auto item_full = [&](int k) { return more + 8 * (12 + k); };
+  auto item_empty = [&](int k) { return more + 8 * (14 + k); };
+  const uint32_t items = bars + 8 * C::BARS;  // two Items of 32 bytes
+  const uint32_t tmem_slot = items + 64;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int HPG = p.H / p.G;
+
+  grid_dep_launch();
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < NS; ++s) {
+      mbar_init(kv_full(s), 1);
+      mbar_init(kv_empty(s), 1);
+    }
+    for (int w = 0; w < 2; ++w) {
+      mbar_init(q_full(w), 1);
+      mbar_init(q_empty(w), 1);
+      mbar_init(s_full(w), 1);
+      mbar_init(p_full(w), 128);
+      mbar_init(o_full(w), 1);
+      mbar_init(o_empty(w), 128);
+      mbar_init(item_full(w), 1);
+      mbar_init(item_empty(w), 10);  // the producer, the issuer and the softmax warps
+    }
+    fence_mbar_init();
+    fence_proxy_async();
+    tma_prefetch_desc(&tmQ);
+    tma_prefetch_desc(&tmK);
+    tma_prefetch_desc(&tmV);
+  }
+  if (warp == 9) {
+    tmem_alloc(tmem_slot, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *reinterpret_cast<const uint32_t*>(smem_raw + (tmem_slot - raw));
+  grid_dep_wait();
+
+  // The k-th item of this CTA, as warp 10 published it; called by whole warps, or by lane 0
+  // alone (solo). b < 0: no more (or a wait ran out).
+  auto take_item = [&](int k, bool solo) {
+    Item it;
+    bool ok = mbar_wait(item_full(k & 1), (k >> 1) & 1, p.err);
+    if (!solo) ok = __all_sync(0xffffffffu, ok);
+    it.b = -1;
+    if (!ok) return it;
+    const int* d = reinterpret_cast<const int*>(smem_raw + (items - raw) + 32 * (k & 1));
+    it.b = d[0];
+    it.g = d[1];
+    it.p0 = d[2];
+    it.row0 = d[3];
+    it.S = d[4];
+    it.past = d[5];
+    if (!solo) __syncwarp();
+    if (solo || lane == 0) mbar_arrive(item_empty(k & 1));
+    return it;
+  };
+
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if (warp == 10) {
+      // -------------------------------------------------------------- items
+      for (int k = 0;; ++k) {
+        const Item it = find_item(p, 2 * PW, blockIdx.x + static_cast<long long>(k) * gridDim.x);
+        if (!__all_sync(0xffffffffu, mbar_wait(item_empty(k & 1), ((k >> 1) & 1) ^ 1, p.err))) break;
+        if (lane == 0) {
+          int* d = reinterpret_cast<int*>(smem_raw + (items - raw) + 32 * (k & 1));
+          d[0] = it.b;
+          d[1] = it.g;
+          d[2] = it.p0;
+          d[3] = it.row0;
+          d[4] = it.S;
+          d[5] = it.past;
+          mbar_arrive(item_full(k & 1));
+        }
+        __syncwarp();
+        if (it.b < 0) break;
+      }
+    } else if (warp == 8) {
+      // ----------------------------------------------------------- producer
+      int iq[2] = {0, 0}, it = 0;
+      bool ok = true;
+      for (int k = 0; ok; ++k) {
+        const Item item = take_item(k, false);
+        if (item.b < 0) break;
+        const Span sp = span_of(p, item, PW);
+        for (int w = 0; w < sp.nw; ++w) {
+          ok = __all_sync(0xffffffffu, mbar_wait(q_empty(w), (iq[w] & 1) ^ 1, p.err));
+          if (!ok) break;
+          if (lane == 0) {
+            mbar_arrive_expect_tx(q_full(w), HPG * PW * HD * 2);
+            for (int c = 0; c < C::CH; ++c)
+              tma_load_3d(sQ + w * C::TILE + c * C::CHUNK, &tmQ, q_full(w), c * 64, item.g * HPG,
+                          item.row0 + item.p0 + w * PW);
+          }
+          ++iq[w];
+        }
+        const int nb = sp.nb[sp.nw - 1], nt = (nb + 7) >> 3;
+        // pool row of this lane's block of step t; past the last block and for table entries
+        // out of range (reported) the row lies outside the pool, where a box reads zeros
+        auto pool_row = [&](int t) {
+          const int i = t * 8 + lane;
+          if (lane >= 8 || t >= nt || i >= nb) return pool_rows;
+          const int j = i < sp.ns ? i : i - sp.ns + sp.jlo;
+          const int blk = p.block_table ? p.block_table[static_cast<long long>(item.b) * p.blocks_per_seq + j]
+                                        : item.b * p.blocks_per_seq + j;
+          if (blk < 0 || blk >= p.num_blocks) {
+            set_err(p.err, DEVERR_BLOCK);
+            return pool_rows;
+          }
+          return pool_row0 + (blk * p.G + item.g) * 16;
+        };
+        int next = pool_row(0);
+        for (int t = 0; t < nt && ok; ++t) {
+          const int y = next;
+          next = pool_row(t + 1);
+          for (int kv = 0; kv < 2; ++kv, ++it) {
+            const int s = it % NS;
+            ok = __all_sync(0xffffffffu, mbar_wait(kv_empty(s), ((it / NS) & 1) ^ 1, p.err));
+            if (!ok) break;
+            if (lane == 0) mbar_arrive_expect_tx(kv_full(s), C::TILE);
+            __syncwarp();
+            if (lane < 8)
+              for (int c = 0; c < C::CH; ++c)
+                tma_load_2d(sKV + s * C::TILE + c * C::CHUNK + lane * 2048, kv ? &tmV : &tmK, kv_full(s), c * 64, y);
+          }
+        }
+      }
+      // every copy lands before the CTA's shared memory goes away
+      for (int w = 0; w < 2; ++w)
+        if (iq[w] > 0) mbar_wait(q_full(w), (iq[w] - 1) & 1, p.err);
+      for (int i = it > NS ? it - NS : 0; i < it; ++i) mbar_wait(kv_full(i % NS), (i / NS) & 1, p.err);
+    } else if (warp == 9 && lane == 0) {
+      // --------------------------------------------------------- MMA issuer
+      constexpr uint32_t id_s = idesc_f32acc(128, KT, MmaFmt<T16>::v);
+      constexpr uint32_t id_o = idesc_f32acc(128, HD, MmaFmt<T16>::v) | (1u << 16);  // B stored N-contiguous
+      int iq[2] = {0, 0}, np[2] = {0, 0}, it = 0;  // items and steps of each tile, stages used
+      auto issue_s = [&](int w, int slot, bool last) {
+#pragma unroll
+        for (int k = 0; k < HD / 16; ++k) {
+          const uint32_t off = (k >> 2) * C::CHUNK + (k & 3) * 32;
+          tc_mma_f16(tmem + w * KT, smem_desc_sw128(sQ + w * C::TILE + off), smem_desc_sw128(sKV + slot * C::TILE + off),
+                     id_s, k != 0);
+        }
+        tc_commit(s_full(w));
+        if (last) tc_commit(q_empty(w));
+      };
+      bool ok = true;
+      Item item = take_item(0, true);
+      for (int k = 0; item.b >= 0 && ok; ++k) {
+        const Span sp = span_of(p, item, PW);
+        const int nt[2] = {sp.steps(0), sp.nw == 2 ? sp.steps(1) : 0};
+        const int nt_all = nt[sp.nw - 1];
+        // the scores of step 0
+        ok = mbar_wait(kv_full(it % NS), (it / NS) & 1, p.err);
+        for (int w = 0; w < sp.nw && ok; ++w) {
+          ok = mbar_wait(q_full(w), iq[w] & 1, p.err);
+          if (!ok) break;
+          tc_fence_after();
+          issue_s(w, it % NS, nt[w] == 1);
+        }
+        if (!ok) break;
+        tc_commit(kv_empty(it % NS));
+        for (int t = 0; t < nt_all && ok; ++t) {
+          const int iv = it + 2 * t + 1, ik = iv + 1;
+          const int sv = iv % NS, sk = ik % NS;
+          const bool more_keys = t + 1 < nt_all;
+          ok = mbar_wait(kv_full(sv), (iv / NS) & 1, p.err) && (!more_keys || mbar_wait(kv_full(sk), (ik / NS) & 1, p.err));
+          for (int w = 0; w < sp.nw && ok; ++w) {
+            if (t >= nt[w]) continue;
+            ok = mbar_wait(p_full(w), np[w] & 1, p.err);
+            if (ok && t == 0) ok = mbar_wait(o_empty(w), (iq[w] & 1) ^ 1, p.err);
+            if (!ok) break;
+            ++np[w];
+            tc_fence_after();
+            const int ks = min(KT / 16, sp.nb[w] - 8 * t);
+            for (int x = 0; x < ks; ++x)
+              mma_ts(tmem + 2 * KT + w * HD, tmem + w * KT + x * 8, v_desc<HD>(sKV + sv * C::TILE + x * 2048), id_o,
+                     (t != 0 || x != 0) ? 1u : 0u);
+            // MMAs run in issue order: the next scores may overwrite the probabilities
+            // just issued, and s_full implies that O is up to date
+            if (t + 1 < nt[w])
+              issue_s(w, sk, t + 2 == nt[w]);
+            else
+              tc_commit(o_full(w));
+          }
+          if (ok) {
+            tc_commit(kv_empty(sv));
+            if (more_keys) tc_commit(kv_empty(sk));
+          }
+        }
+        if (!ok) break;
+        for (int w = 0; w < sp.nw; ++w) ++iq[w];
+        it += 2 * nt_all;
+        item = take_item(k + 1, true);
+      }
+    }
+    __syncwarp();
+  } else {
+    // --------------------------------------------------------------- softmax
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    const int w = warp >> 2;
+    const int i = threadIdx.x & 127;  // row of the tile
+    const int pl = i / HPG, h = i - pl * HPG;
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t tS = tmem + lanes + w * KT, tO = tmem + lanes + 2 * KT + w * HD;
+    const float sl2 = p.scale_log2;
+    const uint64_t sl2p = pk2(sl2, sl2);
+    int ns_ = 0, no = 0, it = 0;  // scores and outputs taken; stages used by the items before
+    bool ok = true;
+    for (int k = 0; ok; ++k) {
+      const Item item = take_item(k, false);
+      if (item.b < 0) break;
+      const Span sp = span_of(p, item, PW);
+      const int nt_all = sp.steps(sp.nw - 1);
+      if (w >= sp.nw) {
+        it += 2 * nt_all;
+        continue;
+      }
+      const int ip = item.p0 + w * PW + pl;
+      const bool valid = i < HPG * PW && ip < item.S;
+      const int pos = valid ? item.past + ip : -1;
+      const int lo = (p.window > 0 && pos >= p.window) ? pos - p.window + 1 : 0;
+      const int nt = sp.steps(w);
+      // the tile whose product is the first to read the block with the last token clears what follows it
+      const bool clears = (sp.pend & 15) && sp.nb[w] == sp.nb[sp.nw - 1] && (w == 0 || sp.nb[0] < sp.nb[1]);
+      float m = -INFINITY;
+      uint64_t l2 = pk2(0.f, 0.f);
+      for (int t = 0; t < nt; ++t) {
+        ok = __all_sync(0xffffffffu, mbar_wait(s_full(w), ns_ & 1, p.err));
+        if (!ok) break;
+        ++ns_;
+        tc_fence_after();
+        const int blocks = sp.nb[w] - 8 * t;
+        // a short last step: its columns past 64 are neither exponentiated nor multiplied
+        const bool half = blocks <= 4;
+        float s[KT];
+        ld32(tS, reinterpret_cast<uint32_t*>(s));
+        ld32(tS + 32, reinterpret_cast<uint32_t*>(s) + 32);
+        if (!half) {
+          ld32(tS + 64, reinterpret_cast<uint32_t*>(s) + 64);
+          ld32(tS + 96, reinterpret_cast<uint32_t*>(s) + 96);
+        }
+        tmem_wait_ld();
+        if (half) {
+#pragma unroll
+          for (int c = 64; c < KT; ++c) s[c] = -INFINITY;
+        }
+        const int tok0 = (sp.jlo - sp.ns + t * 8) * 16;  // token of column 0, of steps past the sinks
+        // padding rows reach no output: they alone never ask for the mask
+        if (!__all_sync(0xffffffffu, !valid || (t * 8 >= sp.ns && tok0 + KT - 1 <= pos && tok0 >= lo))) {
+#pragma unroll
+          for (int x = 0; x < KT / 16; ++x) {
+            const int at = t * 8 + x < sp.ns ? (t * 8 + x) * 16 : tok0 + x * 16;
+            const uint32_t see = bits16(at, lo, pos + 1) | bits16(at, 0, min(p.sinks, pos + 1));
+#pragma unroll
+            for (int c = 0; c < 16; ++c) s[x * 16 + c] = (see >> c) & 1 ? s[x * 16 + c] : -INFINITY;
+          }
+        }
+        float mx[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+        for (int c = 4; c < KT; c += 8) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+            mx[u] = c + 4 + u < KT ? fmaxf(mx[u], fmaxf(s[c + u], s[c + 4 + u])) : fmaxf(mx[u], s[c + u]);
+        }
+        const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sl2;
+        if (t == 0) {
+          m = mt;
+        } else if (__any_sync(0xffffffffu, mt > m + LAG)) {
+          const bool up = mt > m + LAG;
+          const float f = up ? (m == -INFINITY ? 0.f : ex2(m - mt)) : 1.f;
+          m = up ? mt : m;
+          const uint64_t f2 = pk2(f, f);
+          l2 = mul2(l2, f2);
+#pragma unroll 1
+          for (int c = 0; c < HD; c += 32) {
+            float o[32];
+            ld32(tO + c, reinterpret_cast<uint32_t*>(o));
+            tmem_wait_ld();
+#pragma unroll
+            for (int u = 0; u < 32; u += 2) upk2(mul2(pk2(o[u], o[u + 1]), f2), o[u], o[u + 1]);
+            st32(tO + c, reinterpret_cast<uint32_t*>(o));
+          }
+        }
+        const float nb = m == -INFINITY ? 0.f : -m;
+        const uint64_t nbp = pk2(nb, nb);
+        uint64_t sum[4] = {0, 0, 0, 0};  // pairs of 0.f
+#pragma unroll
+        for (int c0 = 0; c0 < KT; c0 += 64) {
+          if (c0 == 64 && half) break;
+          uint32_t pr[32];
+#pragma unroll
+          for (int c = 0; c < 32; ++c) {
+            float a, e;
+            upk2(fma2(pk2(s[c0 + 2 * c], s[c0 + 2 * c + 1]), sl2p, nbp), a, e);
+            a = ex2(a);
+            e = ex2(e);
+            pr[c] = pack_p<T16>(a, e);
+            sum[c & 3] = add2(sum[c & 3], pk2(a, e));
+          }
+          st32(tS + c0 / 2, pr);
+        }
+        wait_st();
+        if (clears && t == nt - 1) {
+          const int iv = it + 2 * t + 1, sv = iv % NS;
+          ok = __all_sync(0xffffffffu, mbar_wait(kv_full(sv), (iv / NS) & 1, p.err));
+          if (!ok) break;
+          const int end = blocks * 16, first = end - 16 + (sp.pend & 15);
+          for (int x = i; x < (end - first) * C::CH * 8; x += 128) {
+            const int row = first + x / (C::CH * 8), piece = x % (C::CH * 8);
+            *reinterpret_cast<uint4*>(smem_raw + (sKV - raw) + sv * C::TILE + (piece >> 3) * C::CHUNK + row * 128 +
+                                      (piece & 7) * 16) = make_uint4(0, 0, 0, 0);
+          }
+          fence_proxy_async();
+        }
+        tc_fence_before();
+        mbar_arrive(p_full(w));
+        l2 = add2(l2, add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])));
+      }
+      it += 2 * nt_all;
+      if (!ok) break;
+      ok = __all_sync(0xffffffffu, mbar_wait(o_full(w), no & 1, p.err));
+      if (!ok) break;
+      ++no;
+      tc_fence_after();
+      float la, lb;
+      upk2(l2, la, lb);
+      const float l = la + lb;
+      const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+      uint4* dst = reinterpret_cast<uint4*>(static_cast<T16*>(p.o) + (static_cast<long long>(item.row0) + ip) * p.o_row +
+                                            (item.g * HPG + h) * p.o_head);
+#pragma unroll
+      for (int c = 0; c < HD; c += 64) {
+        uint32_t o[64];
+        ld32(tO + c, o);
+        ld32(tO + c + 32, o + 32);
+        tmem_wait_ld();
+        if (c + 64 == HD) {
+          tc_fence_before();
+          mbar_arrive(o_empty(w));
+        }
+        if (valid) {
+#pragma unroll
+          for (int u = 0; u < 64; u += 8) {
+            float v[8];
+#pragma unroll
+            for (int x = 0; x < 8; ++x) v[x] = __uint_as_float(o[u + x]) * inv;
+            dst[(c + u) >> 3] = make_uint4(pack2<T16>(v[0], v[1]), pack2<T16>(v[2], v[3]), pack2<T16>(v[4], v[5]),
+                                           pack2<T16>(v[6], v[7]));
+          }
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+template <int HD, typename T16>
+cudaError_t launch_hd(const LaunchCtx& lc, const ChunkArgs& a, const AttnMaps& maps) {
+  const int PW = attn_tile_positions(a.H, a.G), PC = 2 * PW;
+  cudaError_t e = cudaFuncSetAttribute(attn_chunk_kernel<HD, T16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       KCfg<HD>::SMEM);
+  if (e != cudaSuccess) return e;
+  const long long items = (static_cast<long long>(a.T) / PC + a.B) * a.G;  // at most
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(items < lc.num_sms ? items : lc.num_sms));
+  cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = KCfg<HD>::SMEM;
+  cfg.stream = lc.stream;
+  cudaLaunchAttribute attr[2];
+  cfg.numAttrs = chain_attrs(lc, attr);
+  cfg.attrs = attr;
+  return cudaLaunchKernelEx(&cfg, attn_chunk_kernel<HD, T16>, maps.q, maps.k, maps.v, a, PW, 0, maps.pool_rows);
+}
+
+}  // namespace
+
+bool make_attn_maps_strided(AttnMaps* maps, const void* q, long long rows, long long q_row, long long q_head,
+                            const void* kpool, const void* vpool, long long pool_rows, int H, int G, int d, bool f16) {
+  if (pool_rows > 0x7fffff00ll) return false;  // box rows are 32-bit coordinates
+  maps->pool_rows = static_cast<int>(pool_rows);
+  return make_tma_3d_16(&maps->q, q, d, H, rows, H / G, attn_tile_positions(H, G), f16, q_head, q_row) &&
+         make_tma_2d_16(&maps->k, kpool, pool_rows, d, 16, f16) && make_tma_2d_16(&maps->v, vpool, pool_rows, d, 16, f16);
+}
+
+cudaError_t launch_attn_chunk(const LaunchCtx& lc, const ChunkArgs& a, const AttnMaps& maps) {
+  if (a.H / a.G > 16 || a.B < 1 || a.T < 1) return cudaErrorInvalidValue;
+  if (a.d == 64) return lc.f16 ? launch_hd<64, f16>(lc, a, maps) : launch_hd<64, bf16>(lc, a, maps);
+  if (a.d == 128) return lc.f16 ? launch_hd<128, f16>(lc, a, maps) : launch_hd<128, bf16>(lc, a, maps);
+  return cudaErrorInvalidValue;
+}

@@ -174,7 +174,6 @@ AXON_DEV uint64_t v_desc(uint32_t addr) {
 // with the short items. Variable-length: a linear index over the sequences'
 // pairs (at most rows / (2 PW) + B of them), found by scanning the offsets
 // 32 sequences at a time. Returns false when the CTA has no item.
-template <bool CHECK>
 AXON_DEV bool find_item(const AttnArgs& p, const AttnVarlen& vl, int B, int PC, int item, int& b, int& pb, int& row0,
                         int& S, int& past) {
   if (!vl.cu) {
@@ -195,12 +194,8 @@ AXON_DEV bool find_item(const AttnArgs& p, const AttnVarlen& vl, int B, int PC, 
       const int r1 = vl.cu[b0 + lane + 1];
       ps = vl.past[b0 + lane];
       len = r1 - r0;
-      // inconsistent offsets (reported by the row-map kernel, or here): no work
-      if (r0 < 0 || r1 > vl.rows || len < 0 || len > p.S || ps < 0 || ps > p.blocks_per_seq * 16 - len) {
-        if (CHECK && len != 0) set_err(p.err, r0 < 0 || r1 > vl.rows || len < 0 || len > p.S ? DEVERR_SEQ : DEVERR_POS);
-        len = 0;
-      }
-      if (CHECK && ((b0 + lane == 0 && r0 != 0) || (b0 + lane == B - 1 && r1 != vl.rows))) set_err(p.err, DEVERR_SEQ);
+      // inconsistent offsets (reported by the row-map kernel): no work
+      if (r0 < 0 || r1 > vl.rows || len < 0 || len > p.S || ps < 0 || ps + len > p.blocks_per_seq * 16) len = 0;
     }
     const int mine = (len + PC - 1) / PC;
     int end = mine;
@@ -224,14 +219,11 @@ AXON_DEV bool find_item(const AttnArgs& p, const AttnVarlen& vl, int B, int PC, 
   return false;
 }
 
-// EXT: sinks, output strides, offsets that are checked here, and cache rows past
-// the last token that may hold anything (their values are cleared in shared memory
-// before the product: zero times an infinity or a NaN would reach the output).
-template <int HD, typename T16, bool EXT>
+template <int HD, typename T16>
 __global__ void __launch_bounds__(TC_THREADS, 1)
     attn_prefill_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                            const __grid_constant__ CUtensorMap tmV, AttnArgs p, int B, int PW, int pool_row0,
-                           int pool_rows, AttnVarlen vl, AttnExt ext) {
+                           int pool_rows, AttnVarlen vl) {
   using C = ACfg<HD>;
   constexpr int NS = C::STAGES;
   extern __shared__ uint8_t smem_raw[];
@@ -279,7 +271,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
 
   const int g = blockIdx.x % p.G;
   int b = 0, pb = 0, row0 = 0, S = 0, past = 0;
-  const bool item = find_item<EXT>(p, vl, B, 2 * PW, blockIdx.x / p.G, b, pb, row0, S, past);
+  const bool item = find_item(p, vl, B, 2 * PW, blockIdx.x / p.G, b, pb, row0, S, past);
   const int p0 = pb * 2 * PW;  // first position of the chunk in tile 0
   const int nw = !item ? 0 : (p0 + PW < S ? 2 : 1);  // tiles with rows
   // Keys klo .. pend-1 are visible to some row (klo > 0 only under a sliding
@@ -288,11 +280,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
   const int pend = past + min(p0 + nw * PW, S);
   const int klo = (W > 0 && past + p0 >= W) ? past + p0 - W + 1 : 0;
   const int jlo = klo >> 4, jend = (pend + 15) >> 4;
-  // blocks of sinks before the window's first one
-  const int ns = EXT ? min((ext.sinks + 15) >> 4, jlo) : 0;
-  const int nb = ns + jend - jlo;
-  const int nt = (nb + 7) >> 3;
-  const int tail = nb * 16 - (nt - 1) * KT;  // keys of the last tile, a multiple of 16
+  const int nt = (jend - jlo + 7) >> 3;
+  const int tail = (jend - jlo) * 16 - (nt - 1) * KT;  // keys of the last tile, a multiple of 16
 
   if (!item) {
     // a spare CTA of a variable-length batch: only TMEM to give back
@@ -308,9 +297,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     // table entries out of range (reported) the row lies outside the pool,
     // where a box reads zeros
     auto pool_row = [&](int t) {
-      const int i = t * 8 + lane;
-      if (lane >= 8 || t >= nt || i >= nb) return pool_rows;
-      const int j = EXT && i < ns ? i : i - ns + jlo;
+      const int j = jlo + t * 8 + lane;
+      if (lane >= 8 || t >= nt || j >= jend) return pool_rows;
       const int blk =
           p.block_table ? p.block_table[static_cast<long long>(b) * p.bt_stride + j] : b * p.blocks_per_seq + j;
       if (blk < 0 || blk >= p.num_blocks) {
@@ -422,26 +410,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
 #pragma unroll
           for (int c = 64; c < KT; ++c) s[c] = -INFINITY;
         }
-        const int tok0 = (jlo - ns + t * 8) * 16;
+        const int tok0 = (jlo + t * 8) * 16;
         // padding rows reach no output: they alone never ask for the mask
-        if (EXT && t * 8 < ns) {
-          // blocks of sinks, and in the last of these tiles of the window too
-#pragma unroll
-          for (int x = 0; x < KT / 16; ++x) {
-            const int base = t * 8 + x < ns ? (t * 8 + x) * 16 : tok0 + x * 16;
-#pragma unroll
-            for (int y = 0; y < 16; ++y) {
-              const int c = base + y;
-              s[x * 16 + y] = c <= pos && (c >= lo || c < ext.sinks) ? s[x * 16 + y] : -INFINITY;
-            }
-          }
-        } else if (EXT && ext.sinks > 0) {
-          if (!__all_sync(0xffffffffu, !valid || (tok0 + KT - 1 <= pos && tok0 >= lo))) {
-#pragma unroll
-            for (int c = 0; c < KT; ++c)
-              s[c] = (tok0 + c <= pos && (tok0 + c >= lo || tok0 + c < ext.sinks)) ? s[c] : -INFINITY;
-          }
-        } else if (!__all_sync(0xffffffffu, !valid || (tok0 + KT - 1 <= pos && tok0 >= lo))) {
+        if (!__all_sync(0xffffffffu, !valid || (tok0 + KT - 1 <= pos && tok0 >= lo))) {
 #pragma unroll
           for (int c = 0; c < KT; ++c) s[c] = (tok0 + c <= pos && tok0 + c >= lo) ? s[c] : -INFINITY;
         }
@@ -497,20 +468,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
           tmem_st32(tS + c0 / 2, pr);
         }
         tmem_wait_st();
-        if (EXT && w == 0 && t == nt - 1 && (pend & 15)) {
-          // the cache rows past the last token, of the value tile that the MMAs of
-          // both row tiles are about to read
-          const int iv = 2 * t + 1, sv = iv % NS;
-          ok = __all_sync(0xffffffffu, mbar_wait(kv_full(sv), (iv / NS) & 1, p.err));
-          if (!ok) break;
-          const int first = tail - 16 + (pend & 15);
-          for (int x = threadIdx.x; x < (tail - first) * C::CH * 8; x += 128) {
-            const int row = first + x / (C::CH * 8), piece = x % (C::CH * 8);
-            *reinterpret_cast<uint4*>(smem_raw + (sKV - raw) + sv * C::TILE + (piece >> 3) * C::CHUNK + row * 128 +
-                                      (piece & 7) * 16) = make_uint4(0, 0, 0, 0);
-          }
-          fence_proxy_async();
-        }
         tc_fence_before();
         mbar_arrive(p_full(w));
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
@@ -519,9 +476,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       if (ok) {
         tc_fence_after();
         const float inv = l > 0.f ? 1.f / l : 0.f;
-        const long long o_row = EXT ? ext.o_row : static_cast<long long>(p.H) * HD, o_head = EXT ? ext.o_head : HD;
-        uint4* dst = reinterpret_cast<uint4*>(static_cast<T16*>(p.o) + (static_cast<long long>(row0) + ip) * o_row +
-                                              (g * HPG + h) * o_head);
+        uint4* dst = reinterpret_cast<uint4*>(static_cast<T16*>(p.o) +
+                                              (static_cast<long long>(row0) + ip) * p.H * HD + (g * HPG + h) * HD);
 #pragma unroll 1
         for (int c = 0; c < HD; c += 32) {
           uint32_t o[32];
@@ -549,9 +505,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
   }
 }
 
-template <int HD, typename T16, bool EXT>
+template <int HD, typename T16>
 cudaError_t launch_hd(const LaunchCtx& lc, const AttnArgs& a, const AttnMaps& maps, int layer, int B,
-                      const AttnVarlen& vl, const AttnExt& ext) {
+                      const AttnVarlen& vl) {
   const int PW = attn_tile_positions(a.H, a.G), PC = 2 * PW;
   const long long pairs = vl.cu ? vl.rows / PC + B : static_cast<long long>((a.S + PC - 1) / PC) * B;
   const int layer_rows = a.num_blocks * a.G * 16;
@@ -565,31 +521,14 @@ cudaError_t launch_hd(const LaunchCtx& lc, const AttnArgs& a, const AttnMaps& ma
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = lc.pdl ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, attn_prefill_tc_kernel<HD, T16, EXT>, maps.q, maps.k, maps.v, a, B, PW,
-                            layer * layer_rows, maps.pool_rows, vl, ext);
+  return cudaLaunchKernelEx(&cfg, attn_prefill_tc_kernel<HD, T16>, maps.q, maps.k, maps.v, a, B, PW,
+                            layer * layer_rows, maps.pool_rows, vl);
 }
 
 template <int HD, typename T16>
 cudaError_t prepare_hd() {
-  cudaError_t e = cudaFuncSetAttribute(attn_prefill_tc_kernel<HD, T16, false>,
-                                       cudaFuncAttributeMaxDynamicSharedMemorySize, ACfg<HD>::SMEM);
-  if (e != cudaSuccess) return e;
-  return cudaFuncSetAttribute(attn_prefill_tc_kernel<HD, T16, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+  return cudaFuncSetAttribute(attn_prefill_tc_kernel<HD, T16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                               ACfg<HD>::SMEM);
-}
-
-template <bool EXT>
-cudaError_t launch_any(const LaunchCtx& lc, const AttnArgs& a, const AttnMaps& maps, int layer, int B,
-                       const AttnVarlen* vl, const AttnExt& x) {
-  const AttnVarlen v = vl ? *vl : AttnVarlen{};
-  if (a.H / a.G > 16 || B < 1 || a.S < 1) return cudaErrorInvalidValue;
-  if (a.d == 64)
-    return lc.f16 ? launch_hd<64, f16, EXT>(lc, a, maps, layer, B, v, x)
-                  : launch_hd<64, bf16, EXT>(lc, a, maps, layer, B, v, x);
-  if (a.d == 128)
-    return lc.f16 ? launch_hd<128, f16, EXT>(lc, a, maps, layer, B, v, x)
-                  : launch_hd<128, bf16, EXT>(lc, a, maps, layer, B, v, x);
-  return cudaErrorInvalidValue;
 }
 
 }  // namespace
@@ -610,20 +549,13 @@ bool make_attn_maps(AttnMaps* maps, const void* q, long long rows, const void* k
          make_tma_2d_16(&maps->k, kpool, pool_rows, d, 16, f16) && make_tma_2d_16(&maps->v, vpool, pool_rows, d, 16, f16);
 }
 
-bool make_attn_maps_strided(AttnMaps* maps, const void* q, long long rows, long long q_row, long long q_head,
-                            const void* kpool, const void* vpool, long long pool_rows, int H, int G, int d, bool f16) {
-  if (pool_rows > 0x7fffff00ll) return false;
-  maps->pool_rows = static_cast<int>(pool_rows);
-  return make_tma_3d_16(&maps->q, q, d, H, rows, H / G, attn_tile_positions(H, G), f16, q_head, q_row) &&
-         make_tma_2d_16(&maps->k, kpool, pool_rows, d, 16, f16) && make_tma_2d_16(&maps->v, vpool, pool_rows, d, 16, f16);
-}
-
 cudaError_t launch_attn_prefill_tc(const LaunchCtx& lc, const AttnArgs& a, const AttnMaps& maps, int layer, int B,
                                    const AttnVarlen* vl) {
-  return launch_any<false>(lc, a, maps, layer, B, vl, AttnExt{});
-}
-
-cudaError_t launch_attn_prefill_ext(const LaunchCtx& lc, const AttnArgs& a, const AttnMaps& maps, int layer, int B,
-                                    const AttnVarlen* vl, const AttnExt& ext) {
-  return launch_any<true>(lc, a, maps, layer, B, vl, ext);
+  const AttnVarlen v = vl ? *vl : AttnVarlen{};
+  if (a.H / a.G > 16 || B < 1 || a.S < 1) return cudaErrorInvalidValue;
+  if (a.d == 64)
+    return lc.f16 ? launch_hd<64, f16>(lc, a, maps, layer, B, v) : launch_hd<64, bf16>(lc, a, maps, layer, B, v);
+  if (a.d == 128)
+    return lc.f16 ? launch_hd<128, f16>(lc, a, maps, layer, B, v) : launch_hd<128, bf16>(lc, a, maps, layer, B, v);
+  return cudaErrorInvalidValue;
 }

@@ -184,18 +184,24 @@ bool make_attn_maps(AttnMaps* maps, const void* q, long long rows, const void* k
 cudaError_t launch_attn_prefill_tc(const LaunchCtx& lc, const AttnArgs& a, const AttnMaps& maps, int layer, int B,
                                    const AttnVarlen* vl = nullptr);
 cudaError_t prepare_attn_tc_kernels();
-// What the tcgen05 prefill attention takes beyond a model's own buffers (k_attn_tc.cu,
-// EXT instantiations): sinks (with a window, the first tokens that stay visible),
-// output strides in elements; row offsets and lengths are checked, as nothing else does.
-struct AttnExt {
-  int sinks;
+// ---- attention of chunks over the paged cache (k_attn_chunk.cu)
+struct ChunkArgs {
+  const int* cu;    // [B + 1] row offsets
+  const int* past;  // [B] tokens before each chunk
+  const int* block_table;  // [B][blocks_per_seq], or null: blocks b * blocks_per_seq + j
+  int blocks_per_seq, num_blocks;
+  int B, T, max_chunk;
+  int H, G, d;
+  int window, sinks;
+  float scale_log2;
+  void* o;  // [T][H][d], strides in elements
   long long o_row, o_head;
+  int* err;
 };
 // q [rows][H][d] with these strides in elements; the pools hold one layer.
 bool make_attn_maps_strided(AttnMaps* maps, const void* q, long long rows, long long q_row, long long q_head,
                             const void* kpool, const void* vpool, long long pool_rows, int H, int G, int d, bool f16);
-cudaError_t launch_attn_prefill_ext(const LaunchCtx& lc, const AttnArgs& a, const AttnMaps& maps, int layer, int B,
-                                    const AttnVarlen* vl, const AttnExt& ext);
+cudaError_t launch_attn_chunk(const LaunchCtx& lc, const ChunkArgs& a, const AttnMaps& maps);
 
 // ---- attention of one new token per row over the paged cache (k_attn_paged.cu)
 constexpr int PAGED_ATTN_MAX_B = 2048;

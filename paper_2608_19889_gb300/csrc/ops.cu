@@ -183,7 +183,6 @@ int axon_attn_prefill(const axon_kv_cache* cache, int32_t layer, const void* d_q
   if (static_cast<long long>(B) + T > INT_MAX / cache->num_kv_heads) return AXON_ERR_UNSUPPORTED;
   LaunchCtx lc;
   if ((rc = launch_ctx(cache, stream, &lc))) return rc;
-  if ((rc = status(prepare_attn_tc_kernels()))) return rc;
   const int G = cache->num_kv_heads, d = cache->head_dim;
   const void* k = layer_pool(cache, cache->k_pool, layer);
   const void* v = layer_pool(cache, cache->v_pool, layer);
@@ -191,26 +190,27 @@ int axon_attn_prefill(const axon_kv_cache* cache, int32_t layer, const void* d_q
   if (!make_attn_maps_strided(&maps, d_q, T, q_row_stride, q_head_stride, k, v,
                               static_cast<long long>(cache->num_blocks) * G * 16, num_heads, G, d, lc.f16))
     return AXON_ERR_UNSUPPORTED;
-  AttnArgs a;
+  ChunkArgs a;
   memset(&a, 0, sizeof(a));
-  a.q = d_q;
-  a.k = k;
-  a.v = v;
-  a.o = d_out;
+  a.cu = d_cu_seqlens;
+  a.past = d_context_lens;
   a.block_table = d_block_table;
-  a.bt_stride = blocks_per_seq;
   a.blocks_per_seq = blocks_per_seq;
   a.num_blocks = cache->num_blocks;
+  a.B = B;
+  a.T = T;
+  a.max_chunk = max_chunk;
   a.H = num_heads;
   a.G = G;
   a.d = d;
-  a.S = max_chunk;
   a.window = window;
+  a.sinks = window > 0 ? sinks : 0;
   a.scale_log2 = scale_log2(scale, d);
+  a.o = d_out;
+  a.o_row = out_row_stride;
+  a.o_head = out_head_stride;
   a.err = d_err;
-  const AttnVarlen vl{d_cu_seqlens, d_context_lens, T, nullptr};
-  const AttnExt ext{window > 0 ? sinks : 0, out_row_stride, out_head_stride};
-  return status(launch_attn_prefill_ext(lc, a, maps, 0, B, &vl, ext));
+  return status(launch_attn_chunk(lc, a, maps));
 }
 
 int axon_kv_workspace(const axon_kv_cache* cache, const axon_kv_seqs* seqs, int64_t* bytes) {

@@ -13,14 +13,18 @@
 //               registers each (setmaxnreg), so that 128 scores stay in registers;
 //   8           TMA producer: Q of an item, K and V through a ring of 32 KB (16 KB)
 //               stages, lane i fetching the table entry of block i;
-//   9           MMA issuer: S = Q K^T into TMEM, O += P V with P read back from TMEM;
+//   9, 11       MMA issuers of tile 0 and 1: S = Q K^T into TMEM, O += P V with P read back
+//               from TMEM;
 //   10          finds the items, two ahead, and publishes them.
 // The 512 TMEM columns hold S0, S1 (128 each, later P in the first 64) and O0, O1.
 //
-// The running maximum m lags: it is raised, and O rescaled, only when a row's
-// scores exceed it by more than 8 (p <= 2^8): rounding to 16 bits is relative, so the
-// error of a probability is the same, and most steps touch O not at all. The row sum
-// is fp32 of the unrounded probabilities.
+// m is not the running maximum but a bound that lags: the maximum of a row's first visible step,
+// raised (and O rescaled) only when it has become too small. Rounding to 16 bits is
+// relative, so the error of a probability does not depend on m; what must hold is that
+// none overflows, and the row sum of a step, which is needed anyway, tells: above 2^14 the
+// step is taken again with m raised. So the usual step reads its scores once and
+// computes no maximum. Steps under a mask, and a row's first, pass over the scores
+// before that. The row sum is fp32 of the unrounded probabilities.
 //
 // Bound: a 128 x 128 tile at head_dim 128 takes 1024 tensor cycles (2 x 2 x 128^3
 // operations at 8192 per cycle), and per scheduler 512 cycles of the exponential
@@ -34,7 +38,8 @@ namespace {
 
 constexpr int THREADS = 384;
 constexpr int KT = 128;  // keys per step
-constexpr float LAG = 8.f;
+constexpr float LAG = 4.f;          // how far a maximum that is looked at may exceed m (log2)
+constexpr float SUM_MAX = 16384.f;  // largest sum of a row's 128 probabilities
 
 template <int HD>
 struct KCfg {
@@ -42,10 +47,24 @@ struct KCfg {
   static constexpr int CHUNK = 128 * 128;           // bytes of one 128-row chunk
   static constexpr int TILE = CH * CHUNK;           // Q, K or V tile
   static constexpr int STAGES = HD == 128 ? 5 : 8;  // K and V tiles in flight
-  static constexpr int BARS = 2 * STAGES + 12 + 4;
+  static constexpr int BARS = 2 * STAGES + 14 + 4;
   static constexpr int SMEM = 2 * TILE + STAGES * TILE + 8 * BARS + 2 * 32 + 16 + 1024;
 };
 
+// mbar_wait with a loop of few instructions: the kernel waits in some twenty places, and its
+// instruction fetches are on the critical path (122 KB of code as it was, 20 KB so).
+AXON_DEV bool wait_bar(uint32_t bar, uint32_t parity, int* err) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const uint64_t t0 = global_ns();
+#pragma unroll 1
+  while (!mbar_try_wait(bar, parity)) {
+    if (global_ns() - t0 > 2000000000ull) {
+      set_err(err, DEVERR_TIMEOUT);
+      return false;
+    }
+  }
+  return true;
+}
 AXON_DEV void tma_load_3d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
@@ -84,6 +103,16 @@ AXON_DEV void st32(uint32_t taddr, const uint32_t* r) {
       "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
       : "memory");
 }
+AXON_DEV void st_global32(void* at, const uint32_t* v) {
+  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
+               "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
+AXON_DEV bool elect_one() {
+  uint32_t r;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(r));
+  return r != 0;
+}
 AXON_DEV void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 AXON_DEV float ex2(float v) {
   float r;
@@ -110,6 +139,11 @@ AXON_DEV uint64_t mul2(uint64_t a, uint64_t b) {
 AXON_DEV uint64_t add2(uint64_t a, uint64_t b) {
   uint64_t r;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+AXON_DEV float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
 // Probabilities lie in [0, 2^8]: no saturation needed.
@@ -228,16 +262,17 @@ __global__ void __launch_bounds__(THREADS, 1)
   auto o_empty = [&](int w) { return more + 8 * (10 + w); };
   auto item_full = [&](int k) { return more + 8 * (12 + k); };
   auto item_empty = [&](int k) { return more + 8 * (14 + k); };
+  auto turn = [&](int w) { return more + 8 * (16 + w); };
   const uint32_t items = bars + 8 * C::BARS;  // two Items of 32 bytes
   const uint32_t tmem_slot = items + 64;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int HPG = p.H / p.G;
 
   grid_dep_launch();
   if (threadIdx.x == 0) {
     for (int s = 0; s < NS; ++s) {
       mbar_init(kv_full(s), 1);
-      mbar_init(kv_empty(s), 1);
+      mbar_init(kv_empty(s), 2);  // both issuers
     }
     for (int w = 0; w < 2; ++w) {
       mbar_init(q_full(w), 1);
@@ -246,8 +281,9 @@ __global__ void __launch_bounds__(THREADS, 1)
       mbar_init(p_full(w), 128);
       mbar_init(o_full(w), 1);
       mbar_init(o_empty(w), 128);
+      mbar_init(turn(w), 1);
       mbar_init(item_full(w), 1);
-      mbar_init(item_empty(w), 10);  // the producer, the issuer and the softmax warps
+      mbar_init(item_empty(w), 11);  // the producer, the issuers and the softmax warps
     }
     fence_mbar_init();
     fence_proxy_async();
@@ -265,12 +301,11 @@ __global__ void __launch_bounds__(THREADS, 1)
   const uint32_t tmem = *reinterpret_cast<const uint32_t*>(smem_raw + (tmem_slot - raw));
   grid_dep_wait();
 
-  // The k-th item of this CTA, as warp 10 published it; called by whole warps, or by lane 0
-  // alone (solo). b < 0: no more (or a wait ran out).
-  auto take_item = [&](int k, bool solo) {
+  // The k-th item of this CTA, as warp 10 published it; called by whole warps. b < 0: no more
+  // (or a wait ran out).
+  auto take_item = [&](int k) {
     Item it;
-    bool ok = mbar_wait(item_full(k & 1), (k >> 1) & 1, p.err);
-    if (!solo) ok = __all_sync(0xffffffffu, ok);
+    const bool ok = __all_sync(0xffffffffu, wait_bar(item_full(k & 1), (k >> 1) & 1, p.err));
     it.b = -1;
     if (!ok) return it;
     const int* d = reinterpret_cast<const int*>(smem_raw + (items - raw) + 32 * (k & 1));
@@ -280,8 +315,8 @@ __global__ void __launch_bounds__(THREADS, 1)
     it.row0 = d[3];
     it.S = d[4];
     it.past = d[5];
-    if (!solo) __syncwarp();
-    if (solo || lane == 0) mbar_arrive(item_empty(k & 1));
+    __syncwarp();
+    if (lane == 0) mbar_arrive(item_empty(k & 1));
     return it;
   };
 
@@ -290,8 +325,10 @@ __global__ void __launch_bounds__(THREADS, 1)
     if (warp == 10) {
       // -------------------------------------------------------------- items
       for (int k = 0;; ++k) {
-        const Item it = find_item(p, 2 * PW, blockIdx.x + static_cast<long long>(k) * gridDim.x);
-        if (!__all_sync(0xffffffffu, mbar_wait(item_empty(k & 1), ((k >> 1) & 1) ^ 1, p.err))) break;
+        // there and back over the CTAs, since items get shorter along a sequence
+        const unsigned at = k & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
+        const Item it = find_item(p, 2 * PW, at + static_cast<long long>(k) * gridDim.x);
+        if (!__all_sync(0xffffffffu, wait_bar(item_empty(k & 1), ((k >> 1) & 1) ^ 1, p.err))) break;
         if (lane == 0) {
           int* d = reinterpret_cast<int*>(smem_raw + (items - raw) + 32 * (k & 1));
           d[0] = it.b;
@@ -310,11 +347,11 @@ __global__ void __launch_bounds__(THREADS, 1)
       int iq[2] = {0, 0}, it = 0;
       bool ok = true;
       for (int k = 0; ok; ++k) {
-        const Item item = take_item(k, false);
+        const Item item = take_item(k);
         if (item.b < 0) break;
         const Span sp = span_of(p, item, PW);
         for (int w = 0; w < sp.nw; ++w) {
-          ok = __all_sync(0xffffffffu, mbar_wait(q_empty(w), (iq[w] & 1) ^ 1, p.err));
+          ok = __all_sync(0xffffffffu, wait_bar(q_empty(w), (iq[w] & 1) ^ 1, p.err));
           if (!ok) break;
           if (lane == 0) {
             mbar_arrive_expect_tx(q_full(w), HPG * PW * HD * 2);
@@ -345,7 +382,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           next = pool_row(t + 1);
           for (int kv = 0; kv < 2; ++kv, ++it) {
             const int s = it % NS;
-            ok = __all_sync(0xffffffffu, mbar_wait(kv_empty(s), ((it / NS) & 1) ^ 1, p.err));
+            ok = __all_sync(0xffffffffu, wait_bar(kv_empty(s), ((it / NS) & 1) ^ 1, p.err));
             if (!ok) break;
             if (lane == 0) mbar_arrive_expect_tx(kv_full(s), C::TILE);
             __syncwarp();
@@ -357,71 +394,107 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
       // every copy lands before the CTA's shared memory goes away
       for (int w = 0; w < 2; ++w)
-        if (iq[w] > 0) mbar_wait(q_full(w), (iq[w] - 1) & 1, p.err);
-      for (int i = it > NS ? it - NS : 0; i < it; ++i) mbar_wait(kv_full(i % NS), (i / NS) & 1, p.err);
-    } else if (warp == 9 && lane == 0) {
-      // --------------------------------------------------------- MMA issuer
+        if (iq[w] > 0) wait_bar(q_full(w), (iq[w] - 1) & 1, p.err);
+      for (int i = it > NS ? it - NS : 0; i < it; ++i) wait_bar(kv_full(i % NS), (i / NS) & 1, p.err);
+    } else if (warp != 10) {
+      // -------------------------------------------------------- MMA issuers
+      // A warp per tile. What an issuer itself executes is on the critical path (a product takes 64
+      // cycles), so its values are the same in all lanes by construction, which lets the
+      // descriptors live in uniform registers; one elected lane issues.
+      const int w = warp == 9 ? 0 : 1;
+      const bool lead = elect_one();
       constexpr uint32_t id_s = idesc_f32acc(128, KT, MmaFmt<T16>::v);
       constexpr uint32_t id_o = idesc_f32acc(128, HD, MmaFmt<T16>::v) | (1u << 16);  // B stored N-contiguous
-      int iq[2] = {0, 0}, np[2] = {0, 0}, it = 0;  // items and steps of each tile, stages used
-      auto issue_s = [&](int w, int slot, bool last) {
-#pragma unroll
-        for (int k = 0; k < HD / 16; ++k) {
-          const uint32_t off = (k >> 2) * C::CHUNK + (k & 3) * 32;
-          tc_mma_f16(tmem + w * KT, smem_desc_sw128(sQ + w * C::TILE + off), smem_desc_sw128(sKV + slot * C::TILE + off),
-                     id_s, k != 0);
-        }
-        tc_commit(s_full(w));
-        if (last) tc_commit(q_empty(w));
+      const uint64_t dQ = smem_desc_sw128(sQ + w * C::TILE), dK = smem_desc_sw128(sKV), dV = v_desc<HD>(sKV);
+      const uint32_t tS = tmem + w * KT, tO = tmem + 2 * KT + w * HD;
+      uint32_t st = 0, ph = 0;  // ring: next stage and its phase
+      auto next_stage = [&]() {
+        st = st + 1 == NS ? 0 : st + 1;
+        ph ^= st == 0;
       };
-      bool ok = true;
-      Item item = take_item(0, true);
-      for (int k = 0; item.b >= 0 && ok; ++k) {
+      auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_bar(bar, parity, p.err)) != 0; };
+      uint32_t ph_q = 0, ph_p = 0;  // phases of this tile's items and steps
+      uint32_t turns = 0;
+      // The issuers alternate: one tile's products run under the other's softmax. (Left to
+      // themselves they fall into step, both waiting for their softmax at the same time.)
+      auto my_turn = [&]() { return wait_all(turn(w), (turns & 1) ^ (w ^ 1)); };
+      // scores from the keys in stage st; the turn passes two products before the end, which is
+      // what the other needs to start
+      auto scores = [&](bool last) {
+        const uint64_t kd = dK + st * (C::TILE >> 4);
+        if (lead) {
+#pragma unroll
+          for (int k = 0; k < HD / 16; ++k) {
+            const int off = ((k >> 2) * C::CHUNK + (k & 3) * 32) >> 4;
+            if (k == HD / 16 - 2) mbar_arrive(turn(w ^ 1));
+            tc_mma_f16(tS, dQ + off, kd + off, id_s, k != 0);
+          }
+          tc_commit(s_full(w));
+          if (last) tc_commit(q_empty(w));
+        }
+        ++turns;
+      };
+      auto pass_turn = [&]() {
+        if (lead) mbar_arrive(turn(w ^ 1));
+        ++turns;
+      };
+      auto same = [&](int v) { return __shfl_sync(0xffffffffu, v, 0); };
+      Item item = take_item(0);
+      for (int k = 0; same(item.b) >= 0; ++k) {
         const Span sp = span_of(p, item, PW);
-        const int nt[2] = {sp.steps(0), sp.nw == 2 ? sp.steps(1) : 0};
-        const int nt_all = nt[sp.nw - 1];
-        // the scores of step 0
-        ok = mbar_wait(kv_full(it % NS), (it / NS) & 1, p.err);
-        for (int w = 0; w < sp.nw && ok; ++w) {
-          ok = mbar_wait(q_full(w), iq[w] & 1, p.err);
+        const int nb = same(w < sp.nw ? sp.nb[w] : 0), nt = (nb + 7) >> 3;  // of this tile
+        const int nt_all = same(sp.steps(sp.nw - 1));
+        bool ok = wait_all(kv_full(st), ph) && (!nt || wait_all(q_full(w), ph_q)) && my_turn();
+        if (!ok) break;
+        tc_fence_after();
+        if (nt)
+          scores(nt == 1);
+        else
+          pass_turn();
+        if (lead) tc_commit(kv_empty(st));
+        next_stage();
+        for (int t = 0; t < nt_all; ++t) {
+          const bool mine = t < nt, keys = t + 1 < nt_all;
+          const uint32_t sv = st, phv = ph;
+          next_stage();
+          ok = wait_all(kv_full(sv), phv) && (!keys || wait_all(kv_full(st), ph)) &&
+               (!mine || t != 0 || wait_all(o_empty(w), ph_q ^ 1)) && my_turn() && (!mine || wait_all(p_full(w), ph_p));
           if (!ok) break;
           tc_fence_after();
-          issue_s(w, it % NS, nt[w] == 1);
+          if (mine) {
+            const uint64_t vd = dV + sv * (C::TILE >> 4);
+            ph_p ^= 1;
+            const int blocks = nb - 8 * t;
+            if (t != 0 && blocks >= 8) {
+              if (lead) {
+#pragma unroll
+                for (int x = 0; x < 8; ++x) mma_ts(tO, tS + x * 8, vd + x * 128, id_o, 1u);
+              }
+            } else if (lead) {
+              // the first step starts the sums; blocks past the last hold no values
+#pragma unroll 1
+              for (int x = 0; x < min(8, blocks); ++x) mma_ts(tO, tS + x * 8, vd + x * 128, id_o, (t | x) != 0 ? 1u : 0u);
+            }
+            // MMAs run in issue order: the next scores may overwrite the probabilities just
+            // issued, and s_full implies that O is up to date
+            if (t + 1 < nt) {
+              scores(t + 2 == nt);
+            } else {
+              pass_turn();
+              if (lead) tc_commit(o_full(w));
+            }
+          } else {
+            pass_turn();
+          }
+          if (lead) tc_commit(kv_empty(sv));
+          if (keys) {
+            if (lead) tc_commit(kv_empty(st));
+            next_stage();
+          }
         }
         if (!ok) break;
-        tc_commit(kv_empty(it % NS));
-        for (int t = 0; t < nt_all && ok; ++t) {
-          const int iv = it + 2 * t + 1, ik = iv + 1;
-          const int sv = iv % NS, sk = ik % NS;
-          const bool more_keys = t + 1 < nt_all;
-          ok = mbar_wait(kv_full(sv), (iv / NS) & 1, p.err) && (!more_keys || mbar_wait(kv_full(sk), (ik / NS) & 1, p.err));
-          for (int w = 0; w < sp.nw && ok; ++w) {
-            if (t >= nt[w]) continue;
-            ok = mbar_wait(p_full(w), np[w] & 1, p.err);
-            if (ok && t == 0) ok = mbar_wait(o_empty(w), (iq[w] & 1) ^ 1, p.err);
-            if (!ok) break;
-            ++np[w];
-            tc_fence_after();
-            const int ks = min(KT / 16, sp.nb[w] - 8 * t);
-            for (int x = 0; x < ks; ++x)
-              mma_ts(tmem + 2 * KT + w * HD, tmem + w * KT + x * 8, v_desc<HD>(sKV + sv * C::TILE + x * 2048), id_o,
-                     (t != 0 || x != 0) ? 1u : 0u);
-            // MMAs run in issue order: the next scores may overwrite the probabilities
-            // just issued, and s_full implies that O is up to date
-            if (t + 1 < nt[w])
-              issue_s(w, sk, t + 2 == nt[w]);
-            else
-              tc_commit(o_full(w));
-          }
-          if (ok) {
-            tc_commit(kv_empty(sv));
-            if (more_keys) tc_commit(kv_empty(sk));
-          }
-        }
-        if (!ok) break;
-        for (int w = 0; w < sp.nw; ++w) ++iq[w];
-        it += 2 * nt_all;
-        item = take_item(k + 1, true);
+        if (nt) ph_q ^= 1;
+        item = take_item(k + 1);
       }
     }
     __syncwarp();
@@ -435,10 +508,12 @@ __global__ void __launch_bounds__(THREADS, 1)
     const uint32_t tS = tmem + lanes + w * KT, tO = tmem + lanes + 2 * KT + w * HD;
     const float sl2 = p.scale_log2;
     const uint64_t sl2p = pk2(sl2, sl2);
+    const bool wide = ((reinterpret_cast<uintptr_t>(p.o) | static_cast<uintptr_t>(p.o_row * 2) |
+                        static_cast<uintptr_t>(p.o_head * 2)) & 31) == 0;  // 32-byte stores: whole sectors
     int ns_ = 0, no = 0, it = 0;  // scores and outputs taken; stages used by the items before
     bool ok = true;
     for (int k = 0; ok; ++k) {
-      const Item item = take_item(k, false);
+      const Item item = take_item(k);
       if (item.b < 0) break;
       const Span sp = span_of(p, item, PW);
       const int nt_all = sp.steps(sp.nw - 1);
@@ -451,91 +526,106 @@ __global__ void __launch_bounds__(THREADS, 1)
       const int pos = valid ? item.past + ip : -1;
       const int lo = (p.window > 0 && pos >= p.window) ? pos - p.window + 1 : 0;
       const int nt = sp.steps(w);
-      // the tile whose product is the first to read the block with the last token clears what follows it
-      const bool clears = (sp.pend & 15) && sp.nb[w] == sp.nb[sp.nw - 1] && (w == 0 || sp.nb[0] < sp.nb[1]);
-      float m = -INFINITY;
+      // a tile that reads the block with the last token clears what follows it before its product
+      const bool clears = (sp.pend & 15) && sp.nb[w] == sp.nb[sp.nw - 1];
+      float m = valid ? -INFINITY : 0.f;
       uint64_t l2 = pk2(0.f, 0.f);
       for (int t = 0; t < nt; ++t) {
-        ok = __all_sync(0xffffffffu, mbar_wait(s_full(w), ns_ & 1, p.err));
+        const int tok0 = (sp.jlo - sp.ns + t * 8) * 16;  // token of column 0, of steps past the sinks
+        // padding rows reach no output: they alone never ask for it
+        bool look = __any_sync(0xffffffffu, valid && (t * 8 < sp.ns || tok0 + KT - 1 > pos || tok0 < lo || m == -INFINITY));
+        ok = __all_sync(0xffffffffu, wait_bar(s_full(w), ns_ & 1, p.err));
         if (!ok) break;
         ++ns_;
         tc_fence_after();
-        const int blocks = sp.nb[w] - 8 * t;
-        // a short last step: its columns past 64 are neither exponentiated nor multiplied
-        const bool half = blocks <= 4;
-        float s[KT];
-        ld32(tS, reinterpret_cast<uint32_t*>(s));
-        ld32(tS + 32, reinterpret_cast<uint32_t*>(s) + 32);
-        if (!half) {
+        uint32_t pr[KT / 2];
+        uint64_t sum[4];
+#pragma unroll 1
+        for (int round = 0; round < 2; ++round) {
+          if (look) {
+            // hidden scores to -inf (written back), the step's maximum, and m raised to it where it is far
+            // below: a rolled loop, for the few steps that need it
+            float mx = -INFINITY;
+#pragma unroll 1
+            for (int c = 0; c < KT; c += 64) {
+              float s[64];
+              ld32(tS + c, reinterpret_cast<uint32_t*>(s));
+              ld32(tS + c + 32, reinterpret_cast<uint32_t*>(s) + 32);
+              tmem_wait_ld();
+              if (!round) {
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                  const int blk = t * 8 + c / 16 + x, at = blk < sp.ns ? blk * 16 : tok0 + c + x * 16;
+                  const uint32_t see = bits16(at, lo, pos + 1) | bits16(at, 0, min(p.sinks, pos + 1));
+#pragma unroll
+                  for (int u = 0; u < 16; ++u) s[x * 16 + u] = (see >> u) & 1 ? s[x * 16 + u] : -INFINITY;
+                }
+                st32(tS + c, reinterpret_cast<uint32_t*>(s));
+                st32(tS + c + 32, reinterpret_cast<uint32_t*>(s) + 32);
+              }
+              float m4[4] = {mx, s[0], s[1], s[2]};
+#pragma unroll
+              for (int u = 3; u < 59; u += 8) {
+#pragma unroll
+                for (int y = 0; y < 4; ++y) m4[y] = max3(m4[y], s[u + y], s[u + 4 + y]);
+              }
+              mx = max3(max3(m4[0], s[59], s[60]), max3(m4[1], s[61], s[62]), max3(m4[2], m4[3], s[63]));
+            }
+            wait_st();
+            const float mt = mx * sl2;
+            const bool up = valid && mt > (m == -INFINITY ? m : m + LAG);
+            if (__any_sync(0xffffffffu, up)) {
+              const float f = up ? (m == -INFINITY ? 0.f : ex2(m - mt)) : 1.f;
+              m = up ? mt : m;
+              const uint64_t f2 = pk2(f, f);
+              l2 = mul2(l2, f2);
+              if (t > 0) {
+#pragma unroll 1
+                for (int c = 0; c < HD; c += 32) {
+                  float o[32];
+                  ld32(tO + c, reinterpret_cast<uint32_t*>(o));
+                  tmem_wait_ld();
+#pragma unroll
+                  for (int u = 0; u < 32; u += 2) upk2(mul2(pk2(o[u], o[u + 1]), f2), o[u], o[u + 1]);
+                  st32(tO + c, reinterpret_cast<uint32_t*>(o));
+                }
+                wait_st();
+              }
+            }
+          }
+          const float nb = m == -INFINITY ? 0.f : -m;
+          const uint64_t nbp = pk2(nb, nb);
+          float s[KT];
+          ld32(tS, reinterpret_cast<uint32_t*>(s));
+          ld32(tS + 32, reinterpret_cast<uint32_t*>(s) + 32);
+          tmem_wait_ld();
           ld32(tS + 64, reinterpret_cast<uint32_t*>(s) + 64);
           ld32(tS + 96, reinterpret_cast<uint32_t*>(s) + 96);
-        }
-        tmem_wait_ld();
-        if (half) {
 #pragma unroll
-          for (int c = 64; c < KT; ++c) s[c] = -INFINITY;
-        }
-        const int tok0 = (sp.jlo - sp.ns + t * 8) * 16;  // token of column 0, of steps past the sinks
-        // padding rows reach no output: they alone never ask for the mask
-        if (!__all_sync(0xffffffffu, !valid || (t * 8 >= sp.ns && tok0 + KT - 1 <= pos && tok0 >= lo))) {
+          for (int x = 0; x < 4; ++x) sum[x] = 0;  // pairs of 0.f
 #pragma unroll
-          for (int x = 0; x < KT / 16; ++x) {
-            const int at = t * 8 + x < sp.ns ? (t * 8 + x) * 16 : tok0 + x * 16;
-            const uint32_t see = bits16(at, lo, pos + 1) | bits16(at, 0, min(p.sinks, pos + 1));
-#pragma unroll
-            for (int c = 0; c < 16; ++c) s[x * 16 + c] = (see >> c) & 1 ? s[x * 16 + c] : -INFINITY;
-          }
-        }
-        float mx[4] = {s[0], s[1], s[2], s[3]};
-#pragma unroll
-        for (int c = 4; c < KT; c += 8) {
-#pragma unroll
-          for (int u = 0; u < 4; ++u)
-            mx[u] = c + 4 + u < KT ? fmaxf(mx[u], fmaxf(s[c + u], s[c + 4 + u])) : fmaxf(mx[u], s[c + u]);
-        }
-        const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sl2;
-        if (t == 0) {
-          m = mt;
-        } else if (__any_sync(0xffffffffu, mt > m + LAG)) {
-          const bool up = mt > m + LAG;
-          const float f = up ? (m == -INFINITY ? 0.f : ex2(m - mt)) : 1.f;
-          m = up ? mt : m;
-          const uint64_t f2 = pk2(f, f);
-          l2 = mul2(l2, f2);
-#pragma unroll 1
-          for (int c = 0; c < HD; c += 32) {
-            float o[32];
-            ld32(tO + c, reinterpret_cast<uint32_t*>(o));
-            tmem_wait_ld();
-#pragma unroll
-            for (int u = 0; u < 32; u += 2) upk2(mul2(pk2(o[u], o[u + 1]), f2), o[u], o[u + 1]);
-            st32(tO + c, reinterpret_cast<uint32_t*>(o));
-          }
-        }
-        const float nb = m == -INFINITY ? 0.f : -m;
-        const uint64_t nbp = pk2(nb, nb);
-        uint64_t sum[4] = {0, 0, 0, 0};  // pairs of 0.f
-#pragma unroll
-        for (int c0 = 0; c0 < KT; c0 += 64) {
-          if (c0 == 64 && half) break;
-          uint32_t pr[32];
-#pragma unroll
-          for (int c = 0; c < 32; ++c) {
+          for (int c = 0; c < KT / 2; ++c) {
+            if (c == KT / 4) tmem_wait_ld();
             float a, e;
-            upk2(fma2(pk2(s[c0 + 2 * c], s[c0 + 2 * c + 1]), sl2p, nbp), a, e);
+            upk2(fma2(pk2(s[2 * c], s[2 * c + 1]), sl2p, nbp), a, e);
             a = ex2(a);
             e = ex2(e);
             pr[c] = pack_p<T16>(a, e);
             sum[c & 3] = add2(sum[c & 3], pk2(a, e));
           }
-          st32(tS + c0 / 2, pr);
+          sum[0] = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
+          float sa, sb;
+          upk2(sum[0], sa, sb);
+          if (look || !__any_sync(0xffffffffu, valid && !(sa + sb <= SUM_MAX))) break;
+          look = true;  // a score far above m: raise it and take the step again
         }
-        wait_st();
+        st32(tS, pr);
+        st32(tS + 32, pr + 32);
         if (clears && t == nt - 1) {
           const int iv = it + 2 * t + 1, sv = iv % NS;
-          ok = __all_sync(0xffffffffu, mbar_wait(kv_full(sv), (iv / NS) & 1, p.err));
+          ok = __all_sync(0xffffffffu, wait_bar(kv_full(sv), (iv / NS) & 1, p.err));
           if (!ok) break;
-          const int end = blocks * 16, first = end - 16 + (sp.pend & 15);
+          const int end = min(8, sp.nb[w] - 8 * t) * 16, first = end - 16 + (sp.pend & 15);
           for (int x = i; x < (end - first) * C::CH * 8; x += 128) {
             const int row = first + x / (C::CH * 8), piece = x % (C::CH * 8);
             *reinterpret_cast<uint4*>(smem_raw + (sKV - raw) + sv * C::TILE + (piece >> 3) * C::CHUNK + row * 128 +
@@ -543,13 +633,14 @@ __global__ void __launch_bounds__(THREADS, 1)
           }
           fence_proxy_async();
         }
+        wait_st();
         tc_fence_before();
         mbar_arrive(p_full(w));
-        l2 = add2(l2, add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])));
+        l2 = add2(l2, sum[0]);
       }
       it += 2 * nt_all;
       if (!ok) break;
-      ok = __all_sync(0xffffffffu, mbar_wait(o_full(w), no & 1, p.err));
+      ok = __all_sync(0xffffffffu, wait_bar(o_full(w), no & 1, p.err));
       if (!ok) break;
       ++no;
       tc_fence_after();
@@ -571,12 +662,17 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         if (valid) {
 #pragma unroll
-          for (int u = 0; u < 64; u += 8) {
-            float v[8];
+          for (int u = 0; u < 64; u += 16) {
+            uint32_t v[8];
 #pragma unroll
-            for (int x = 0; x < 8; ++x) v[x] = __uint_as_float(o[u + x]) * inv;
-            dst[(c + u) >> 3] = make_uint4(pack2<T16>(v[0], v[1]), pack2<T16>(v[2], v[3]), pack2<T16>(v[4], v[5]),
-                                           pack2<T16>(v[6], v[7]));
+            for (int x = 0; x < 8; ++x)
+              v[x] = pack2<T16>(__uint_as_float(o[u + 2 * x]) * inv, __uint_as_float(o[u + 2 * x + 1]) * inv);
+            if (wide) {
+              st_global32(dst + ((c + u) >> 3), v);
+            } else {
+              dst[(c + u) >> 3] = make_uint4(v[0], v[1], v[2], v[3]);
+              dst[((c + u) >> 3) + 1] = make_uint4(v[4], v[5], v[6], v[7]);
+            }
           }
         }
       }

@@ -12,7 +12,9 @@
 // 1, 2 or 4 warps, the warps of a group taking pages in turn) split into equal
 // ranges. An item inside one range is finished there; the partial states (m, sum,
 // O) of an item cut between workers go to the workspace, and the last of them to
-// take a ticket joins them in order, so that results do not depend on timing.
+// take a ticket joins them in order, so that results do not depend on timing. More than
+// 16 parts are joined in two levels, by many workers: one CTA reading a few hundred parts, eight
+// in flight, took longer than the pass over the keys (MEASURE).
 //
 // A page's products run on mma.sync with the keys as the 16-row operand and the
 // H/G heads (padded to 8 or 16) as the 8-wide one, S^T = K Q^T and O^T = V^T P^T:
@@ -227,32 +229,51 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
     };
     uint4 kv[2][KI], vv[4][VI];
     auto seen = [&](int t) { return t <= rp.pos && (t >= rp.lo || t < p.sinks); };
-    auto load_k = [&](int blk, int t0) {
-      const T16* at = kpool + blk * block_elems + g * page_elems;
+    // every token of the page is visible: the usual page, loaded without predicates
+    auto whole_page = [&](int blk, int t0) {
+      return blk >= 0 && t0 + 15 <= rp.pos && (t0 >= rp.lo || t0 + 15 < p.sinks);
+    };
+    const long long kofs = g * page_elems + r * HD + c * 8, vofs = g * page_elems + 2 * c * HD + r * 8;
+    auto load_k = [&](int blk, int t0, bool all) {
+      const T16* at = kpool + blk * block_elems + kofs;
+      if (all) {
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int i = 0; i < KI; ++i)
-          kv[x][i] = (blk >= 0 && seen(t0 + r + 8 * x)) ? ld_stream16(at + (r + 8 * x) * HD + (4 * i + c) * 8)
-                                                        : make_uint4(0, 0, 0, 0);
+          for (int i = 0; i < KI; ++i) kv[x][i] = ld_stream16(at + x * 8 * HD + i * 32);
+      } else {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int i = 0; i < KI; ++i)
+            kv[x][i] = (blk >= 0 && seen(t0 + r + 8 * x)) ? ld_stream16(at + x * 8 * HD + i * 32) : make_uint4(0, 0, 0, 0);
+      }
     };
     // rows of tokens that are not visible are left out, not multiplied by zero:
     // what a page holds there may be anything
-    auto load_v = [&](int blk, int t0) {
-      const T16* at = vpool + blk * block_elems + g * page_elems;
+    auto load_v = [&](int blk, int t0, bool all) {
+      const T16* at = vpool + blk * block_elems + vofs;
+      if (all) {
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const int t = 2 * c + (x & 1) + 8 * (x >> 1);
+        for (int x = 0; x < 4; ++x)
 #pragma unroll
-        for (int i = 0; i < VI; ++i)
-          vv[x][i] = (blk >= 0 && seen(t0 + t)) ? ld_stream16(at + t * HD + (r + 8 * i) * 8) : make_uint4(0, 0, 0, 0);
+          for (int i = 0; i < VI; ++i) vv[x][i] = ld_stream16(at + ((x & 1) + 8 * (x >> 1)) * HD + i * 64);
+      } else {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const int t = (x & 1) + 8 * (x >> 1);
+#pragma unroll
+          for (int i = 0; i < VI; ++i)
+            vv[x][i] = (blk >= 0 && seen(t0 + 2 * c + t)) ? ld_stream16(at + t * HD + i * 64) : make_uint4(0, 0, 0, 0);
+        }
       }
     };
     if (pages > 0) {
       int ent = entries(0);
       int blk = __shfl_sync(0xffffffffu, ent, 0), t0 = logical(0) * 16;
-      load_k(blk, t0);
-      load_v(blk, t0);
+      bool all = whole_page(blk, t0);
+      load_k(blk, t0, all);
+      load_v(blk, t0, all);
       for (int k = 0; k < pages; ++k) {
         float s[NT][4];
 #pragma unroll
@@ -272,11 +293,12 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
 #pragma unroll
           for (int x = 0; x < 4; ++x) s[n][x] = e[x] + f[x];
         }
-        const bool ok0 = blk >= 0 && seen(t0 + r), ok1 = blk >= 0 && seen(t0 + r + 8);
+        const bool ok0 = all || (blk >= 0 && seen(t0 + r)), ok1 = all || (blk >= 0 && seen(t0 + r + 8));
         if (((k + 1) & 31) == 0) ent = entries(k + 1);
         const int nblk = __shfl_sync(0xffffffffu, ent, (k + 1) & 31), nt0 = logical(k + 1) * 16;
         const bool more = k + 1 < pages;
-        if (more) load_k(nblk, nt0);
+        const bool nall = whole_page(nblk, nt0);
+        if (more) load_k(nblk, nt0, nall);
 
         uint32_t ph[NT][2], pl[NT][2];
 #pragma unroll
@@ -332,7 +354,8 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
             }
           }
         }
-        if (more) load_v(nblk, nt0);
+        if (more) load_v(nblk, nt0, nall);
+        all = nall;
         blk = nblk;
         t0 = nt0;
       }
@@ -364,102 +387,124 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
     group_sync(group, gs);
     const long long item = static_cast<long long>(b) * p.G + g;
     const bool whole = off == 0 && cnt == rp.n;
-    float* const part = p.part + (2 * wid + (off > 0 ? 0 : 1)) * C::PART;
     const float* const gstate = state + group * gs * C::STATE;
     const int gl = wg * 32 + lane;
-    auto finish = [&](int h, int x, const float (&v)[8], float M, float L) {
+    constexpr int PX = HD / 4;  // 4-dim pieces of a head
+    auto finish = [&](int h, int x, float4 v, float M, float L) {
       const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
-      const long long at = b * p.o_row + (g * HPG + h) * p.o_head + x * 8;
-      uint32_t w[4], wl[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float a = v[2 * i] * inv, e = v[2 * i + 1] * inv;
-        w[i] = pack2<T16>(a, e);
-        if (LO) {
-          const T16* hv = reinterpret_cast<const T16*>(&w[i]);
-          wl[i] = pack2<T16>(a - to_f(hv[0]), e - to_f(hv[1]));
-        }
+      const long long at = b * p.o_row + (g * HPG + h) * p.o_head + x * 4;
+      v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+      const uint2 w = make_uint2(pack2<T16>(v.x, v.y), pack2<T16>(v.z, v.w));
+      *reinterpret_cast<uint2*>(static_cast<T16*>(p.o) + at) = w;
+      if (LO) {
+        const T16* hv = reinterpret_cast<const T16*>(&w);
+        *reinterpret_cast<uint2*>(static_cast<T16*>(p.o_lo) + at) =
+            make_uint2(pack2<T16>(v.x - to_f(hv[0]), v.y - to_f(hv[1])), pack2<T16>(v.z - to_f(hv[2]), v.w - to_f(hv[3])));
       }
-      *reinterpret_cast<uint4*>(static_cast<T16*>(p.o) + at) = make_uint4(w[0], w[1], w[2], w[3]);
-      if (LO) *reinterpret_cast<uint4*>(static_cast<T16*>(p.o_lo) + at) = make_uint4(wl[0], wl[1], wl[2], wl[3]);
       if (p.lse && x == 0)
         p.lse[static_cast<long long>(b) * p.H + g * HPG + h] = (M + log2f(L)) * 0.69314718055994531f;
     };
-    for (int i = gl; i < HPG * (HD / 8); i += gs * 32) {
-      const int h = i / (HD / 8), x = i % (HD / 8);
-      float M = -INFINITY, L = 0.f, v[8] = {};
+    // parts of the item: workers first .. last hold one each, in this slot of the workspace
+    const long long first = ((item0 + 1) * nw - 1) / total, last = ((item0 + rp.n) * nw - 1) / total;
+    auto slot = [&](long long w) { return 2 * w + (w > first ? 0 : 1); };
+    auto put = [&](float* at, int h, int x, float4 v, float M, float L) {
+      *reinterpret_cast<float4*>(at + h * HD + x * 4) = v;
+      if (x == 0) {
+        at[C::HEADS * HD + h] = M;
+        at[C::HEADS * HD + C::HEADS + h] = L;
+      }
+    };
+    for (int i = gl; i < HPG * PX; i += gs * 32) {
+      const int h = i / PX, x = i % PX;
+      float M = -INFINITY, L = 0.f;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
       for (int w = 0; w < gs; ++w) M = fmaxf(M, gstate[w * C::STATE + C::HEADS * C::PITCH + h]);
       const float base = M == -INFINITY ? 0.f : M;
       for (int w = 0; w < gs; ++w) {
         const float* st = gstate + w * C::STATE;
         const float f = ex2f(st[C::HEADS * C::PITCH + h] - base);
         L += f * st[C::HEADS * C::PITCH + C::HEADS + h];
-#pragma unroll
-        for (int y = 0; y < 8; ++y) v[y] += f * st[h * C::PITCH + x * 8 + y];
+        const float4 e = *reinterpret_cast<const float4*>(st + h * C::PITCH + x * 4);
+        v = make_float4(v.x + f * e.x, v.y + f * e.y, v.z + f * e.z, v.w + f * e.w);
       }
-      if (whole) {
+      if (whole)
         finish(h, x, v, M, L);
-      } else {
-        float* at = part + h * HD + x * 8;
-        *reinterpret_cast<float4*>(at) = make_float4(v[0], v[1], v[2], v[3]);
-        *reinterpret_cast<float4*>(at + 4) = make_float4(v[4], v[5], v[6], v[7]);
-        if (x == 0) {
-          part[C::HEADS * HD + h] = M;
-          part[C::HEADS * HD + C::HEADS + h] = L;
-        }
-      }
+      else
+        put(p.part + slot(wid) * C::PART, h, x, v, M, L);
     }
     group_sync(group, gs);
     if (!whole) {
-      // the workers of units item0 .. item0 + n - 1 hold a part each
-      const long long first = ((item0 + 1) * nw - 1) / total, last = ((item0 + rp.n) * nw - 1) / total;
-      if (gl == 0) {
-        const int parts = static_cast<int>(last - first + 1);
-        const bool is_last = atom_add_acq_rel_gpu(p.ticket + item, 1) == parts - 1;
-        if (is_last) p.ticket[item] = 0;
-        s_last[group] = is_last;
-      }
-      group_sync(group, gs);
-      if (s_last[group]) {
-        for (int i = gl; i < HPG * (HD / 8); i += gs * 32) {
-          const int h = i / (HD / 8), x = i % (HD / 8);
-          float M = -INFINITY, L = 0.f, v[8] = {};
-          for (long long w0 = first; w0 <= last; w0 += 4) {
-            float pm[4], ps[4];
-            float4 pa[4], pb[4];
+      // `count` parts from worker w0 on, `step` apart, joined in order: into a slot of the second
+      // level, or into the output
+      const long long joined = 2ll * gridDim.x * DW;  // second level's slots
+      auto join = [&](long long w0, int count, int step, bool out) {
+        const long long from = step > 1 ? joined : 0;
+        for (int i = gl; i < HPG * PX; i += gs * 32) {
+          const int h = i / PX, x = i % PX;
+          float M = -INFINITY, L = 0.f;
+          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int j0 = 0; j0 < count; j0 += 8) {
+            float pm[8], ps[8];
+            float4 pv[8];
 #pragma unroll
-            for (int y = 0; y < 4; ++y) {
-              const long long w = w0 + y;
-              if (w <= last) {
-                const float* at = p.part + (2 * w + (w > first ? 0 : 1)) * C::PART;
+            for (int y = 0; y < 8; ++y) {
+              pm[y] = -INFINITY;
+              ps[y] = 0.f;
+              pv[y] = make_float4(0.f, 0.f, 0.f, 0.f);
+              if (j0 + y < count) {
+                const float* at = p.part + (from + slot(w0 + static_cast<long long>(j0 + y) * step)) * C::PART;
                 pm[y] = __ldcg(at + C::HEADS * HD + h);
                 ps[y] = __ldcg(at + C::HEADS * HD + C::HEADS + h);
-                pa[y] = __ldcg(reinterpret_cast<const float4*>(at + h * HD + x * 8));
-                pb[y] = __ldcg(reinterpret_cast<const float4*>(at + h * HD + x * 8 + 4));
-              } else {
-                pm[y] = -INFINITY;
-                ps[y] = 0.f;
-                pa[y] = pb[y] = make_float4(0.f, 0.f, 0.f, 0.f);
+                pv[y] = __ldcg(reinterpret_cast<const float4*>(at + h * HD + x * 4));
               }
             }
-            const float nm = fmaxf(fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])), M);
+            float nm = M;
+#pragma unroll
+            for (int y = 0; y < 8; ++y) nm = fmaxf(nm, pm[y]);
             const float base = nm == -INFINITY ? 0.f : nm;
             const float f = ex2f(M - base);
             M = nm;
             L *= f;
+            v = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
 #pragma unroll
-            for (int y = 0; y < 8; ++y) v[y] *= f;
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
+            for (int y = 0; y < 8; ++y) {
               const float e = ex2f(pm[y] - base);
               L += e * ps[y];
-              v[0] += e * pa[y].x; v[1] += e * pa[y].y; v[2] += e * pa[y].z; v[3] += e * pa[y].w;
-              v[4] += e * pb[y].x; v[5] += e * pb[y].y; v[6] += e * pb[y].z; v[7] += e * pb[y].w;
+              v = make_float4(v.x + e * pv[y].x, v.y + e * pv[y].y, v.z + e * pv[y].z, v.w + e * pv[y].w);
             }
           }
-          finish(h, x, v, M, L);
+          if (out) {
+            finish(h, x, v, M, L);
+          } else {
+            put(p.part + (joined + slot(w0)) * C::PART, h, x, v, M, L);
+          }
         }
+      };
+      // whether this is the last of `count` arrivals at a ticket (which is zero again then)
+      auto last_of = [&](int* ticket, int count) {
+        group_sync(group, gs);
+        if (gl == 0) {
+          const bool is_last = atom_add_acq_rel_gpu(ticket, 1) == count - 1;
+          if (is_last) *ticket = 0;
+          s_last[group] = is_last;
+        }
+        group_sync(group, gs);
+        return s_last[group] != 0;
+      };
+      const int parts = static_cast<int>(last - first + 1);
+      int radix = 16;
+      while (radix * radix < parts) radix += 16;
+      bool joiner = true;
+      int step = 1, count = parts;
+      if (parts > radix) {
+        // two levels: the last of each `radix` neighbours joins them, the last of these joins the results
+        const int j = static_cast<int>(wid - first) / radix * radix, n = min(radix, parts - j);
+        joiner = last_of(p.ticket + p.B * p.G + slot(first + j), n);
+        if (joiner) join(first + j, n, 1, false);
+        step = radix;
+        count = (parts + radix - 1) / radix;
       }
+      if (joiner && last_of(p.ticket + item, count)) join(first, count, step, true);
       group_sync(group, gs);
     }
     u += cnt;
@@ -505,7 +550,11 @@ cudaError_t launch_hd(const LaunchCtx& lc, const PagedAttnArgs& a) {
 size_t paged_attn_part_bytes(int H, int G, int d, int num_sms) {
   const bool two = H / G > 8;
   const size_t workers = static_cast<size_t>(num_sms) * (two ? 2 : 3) * DW;
-  return 2 * workers * (two ? 16 : 8) * (d + 2) * 4;
+  return 2 * 2 * workers * (two ? 16 : 8) * (d + 2) * 4;
+}
+// A ticket per item and per worker's slot.
+size_t paged_attn_tickets(int B, int H, int G, int num_sms) {
+  return static_cast<size_t>(B) * G + 2 * static_cast<size_t>(num_sms) * (H / G > 8 ? 2 : 3) * DW;
 }
 
 cudaError_t launch_attn_paged_decode(const LaunchCtx& lc, const PagedAttnArgs& a) {

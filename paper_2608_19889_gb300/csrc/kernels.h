@@ -223,10 +223,11 @@ struct PagedAttnArgs {
   void* o_lo;
   float* lse;   // optional [B][H], natural logarithm
   float* part;  // paged_attn_part_bytes
-  int* ticket;  // [B * G], zero between calls
+  int* ticket;  // paged_attn_tickets, zero between calls
   int* err;
 };
 size_t paged_attn_part_bytes(int H, int G, int d, int num_sms);
+size_t paged_attn_tickets(int B, int H, int G, int num_sms);
 cudaError_t launch_attn_paged_decode(const LaunchCtx& lc, const PagedAttnArgs& a);
 
 // ---- blocks of the paged cache (k_pages.cu)

@@ -118,7 +118,7 @@ int axon_attn_decode_workspace(const axon_kv_cache* cache, int32_t num_heads, in
   LaunchCtx lc;
   if ((rc = launch_ctx(cache, nullptr, &lc))) return rc;
   *bytes = static_cast<int64_t>(paged_attn_part_bytes(num_heads, cache->num_kv_heads, cache->head_dim, lc.num_sms)) +
-           4ll * B * cache->num_kv_heads;
+           4 * static_cast<int64_t>(paged_attn_tickets(B, num_heads, cache->num_kv_heads, lc.num_sms));
   return AXON_OK;
 }
 
@@ -139,7 +139,9 @@ int axon_attn_decode(const axon_kv_cache* cache, int32_t layer, const void* d_q,
   if ((rc = launch_ctx(cache, stream, &lc))) return rc;
   const int64_t part =
       static_cast<int64_t>(paged_attn_part_bytes(num_heads, cache->num_kv_heads, cache->head_dim, lc.num_sms));
-  if (workspace_bytes < part + 4ll * B * cache->num_kv_heads) return AXON_ERR_INVALID_ARG;
+  if (workspace_bytes <
+      part + 4 * static_cast<int64_t>(paged_attn_tickets(B, num_heads, cache->num_kv_heads, lc.num_sms)))
+    return AXON_ERR_INVALID_ARG;
   PagedAttnArgs a;
   memset(&a, 0, sizeof(a));
   a.q = d_q;

@@ -137,6 +137,10 @@ typedef struct axon_config {
   int32_t n_shared_experts;
   int32_t first_k_dense_replace;
   int32_t norm_topk_prob;
+  int32_t sink_tokens;         /* with a sliding window: the first sink_tokens positions stay visible to
+                                  every query (0: none; without a window it must be 0). 16-bit modes
+                                  only; decode takes the launch chain. Cache blocks that neither the
+                                  window nor the sinks reach are not read (axon_kv_release). */
 } axon_config;
 
 /* One named checkpoint tensor, HF Llama naming and [out, in] matrices, as a

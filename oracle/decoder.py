@@ -101,6 +101,7 @@ class DecoderConfig:
     theta: float  # rope_theta
     eps: float  # rms_norm_eps
     window: int = 0  # sliding_window (0: none)
+    sinks: int = 0  # with a window: first positions that stay visible
     # rope_scaling of Llama-3.1-family configs (rope_factor 0: none)
     rope_factor: float = 0.0
     rope_low: float = 1.0  # low_freq_factor
@@ -121,7 +122,8 @@ class DecoderConfig:
         return DecoderConfig(L=int(c["L"]), D=int(c["D"]), H=int(c["H"]), G=int(c["G"]),
                              d=int(c["d"]), F=int(c["F"]), V=int(c["V"]), tie=bool(c["tie"]),
                              bias=bool(c["bias"]), theta=float(c["theta"]), eps=float(c["eps"]),
-                             window=int(c.get("window", 0)), rope_factor=float(c.get("rope_factor", 0.0)),
+                             window=int(c.get("window", 0)), sinks=int(c.get("sinks", 0)),
+                             rope_factor=float(c.get("rope_factor", 0.0)),
                              rope_low=float(c.get("rope_low", 1.0)), rope_high=float(c.get("rope_high", 4.0)),
                              rope_orig=int(c.get("rope_orig", 8192)), act=str(c.get("act", "silu")),
                              qk_norm=bool(c.get("qk_norm", False)), n_experts=int(c.get("n_experts", 0)),
@@ -272,13 +274,13 @@ def attention_one_query(q, K, V, H, G):
     return o
 
 
-def causal_attention(q, K, V, q_pos, H, G, window=0):
+def causal_attention(q, K, V, q_pos, H, G, window=0, sinks=0):
     """Masking.causal_mask + Attention.attention for S queries of one sequence
     (Sec. Built-In Libraries, attention and masking; the `window=` argument
     of causal_mask_for_input, appendix GPT-2 listing).
     q: [S, H, d] at positions q_pos [S]; K, V: [T, G, d] at positions 0..T-1.
     Key t is visible to query i iff t <= q_pos[i] and, with a window W > 0,
-    t > q_pos[i] - W. Returns o: [S, H, d]."""
+    t > q_pos[i] - W or t < sinks. Returns o: [S, H, d]."""
     q = np.asarray(q, dtype=np.float64)
     S, _, d = q.shape
     T = K.shape[0]
@@ -286,7 +288,7 @@ def causal_attention(q, K, V, q_pos, H, G, window=0):
     p = np.asarray(q_pos)[:, None]
     keep = t <= p  # [S, T]
     if window > 0:
-        keep = keep & (t > p - window)
+        keep = keep & ((t > p - window) | (t < sinks))
     o = np.empty_like(q)
     per = H // G
     for h in range(H):
@@ -441,7 +443,7 @@ class Oracle:
             for b in range(B):
                 cache.write(l, b, pos[b], k[b], v[b])
                 Kb, Vb = cache.read(l, b, int(pos[b, -1]) + 1)
-                o[b] = causal_attention(q[b], Kb, Vb, pos[b], c.H, c.G, c.window)
+                o[b] = causal_attention(q[b], Kb, Vb, pos[b], c.H, c.G, c.window, c.sinks)
             x = x + linear(o.reshape(B, S, c.H * c.d), self._w(p + "self_attn.o_proj.weight"))
             h2 = rmsnorm(x, self._w(p + "post_attention_layernorm.weight"), c.eps)
             if c.is_moe_layer(l):

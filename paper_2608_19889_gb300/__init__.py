@@ -48,7 +48,7 @@ class axon_config(ctypes.Structure):
         (n, ctypes.c_float) for n in ("rope_scaling_factor", "rope_low_freq_factor", "rope_high_freq_factor")] + [
         ("rope_original_max_position", ctypes.c_int32), ("hidden_act", ctypes.c_int32), ("qk_norm", ctypes.c_int32)] + [
         (n, ctypes.c_int32) for n in ("n_routed_experts", "num_experts_per_tok", "moe_intermediate_size",
-                                      "n_shared_experts", "first_k_dense_replace", "norm_topk_prob")]
+                                      "n_shared_experts", "first_k_dense_replace", "norm_topk_prob", "sink_tokens")]
 
 
 class axon_tensor(ctypes.Structure):
@@ -165,7 +165,7 @@ def axon_status_string(status: int) -> str:
 def make_config(m: dict, max_batch: int, max_context: int, kv_layout=AXON_KV_CONTIGUOUS, kv_num_blocks=0,
                 precision=AXON_BF16, max_prefill_tokens=0) -> axon_config:
     """axon_config from a shape dict with keys L, D, H, G, d, F, V, tie, bias, theta, eps (and optionally
-    window, the sliding window, rope_factor / rope_low / rope_high / rope_orig, the RoPE frequency
+    window, the sliding window, sinks, the first tokens that stay visible under it, rope_factor / rope_low / rope_high / rope_orig, the RoPE frequency
     scaling, 0 or absent = none; act, "silu" (default) or "gelu_tanh"; qk_norm, per-head RMSNorm of q and k;
     n_experts, top_k, moe_F, n_shared, first_dense, norm_topk: the mixture-of-experts MLP)."""
     return axon_config(m["L"], m["D"], m["H"], m["G"], m["d"], m["F"], m["V"], int(m["tie"]), int(m["bias"]),
@@ -175,7 +175,7 @@ def make_config(m: dict, max_batch: int, max_context: int, kv_layout=AXON_KV_CON
                        AXON_ACT_GELU_TANH if m.get("act", "silu") == "gelu_tanh" else AXON_ACT_SILU,
                        int(bool(m.get("qk_norm", False))), int(m.get("n_experts", 0)), int(m.get("top_k", 0)),
                        int(m.get("moe_F", 0)), int(m.get("n_shared", 0)), int(m.get("first_dense", 0)),
-                       int(bool(m.get("norm_topk", False))))
+                       int(bool(m.get("norm_topk", False))), int(m.get("sinks", 0)))
 
 
 def axon_model_create(cfg: axon_config, weights: dict, stream=None) -> ctypes.c_void_p:

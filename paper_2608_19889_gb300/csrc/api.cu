@@ -110,6 +110,7 @@ struct axon_model {
   float* attn_part = nullptr;
   int* attn_cnt = nullptr;
   int max_splits = 1;
+  void* sink_work = nullptr;  // sliding window with sinks: workspace of the paged decode attention
   int* err = nullptr;
   AttnMaps attn_maps{};  // prefill attention
   // activation operands of the few-token projections: a, o, u by MLP width, gathered last rows
@@ -322,6 +323,8 @@ int validate_config(const axon_config* c) {
     return AXON_ERR_INVALID_ARG;
   if (c->kv_block_size != 16) return AXON_ERR_UNSUPPORTED;
   if (c->sliding_window < 0) return AXON_ERR_INVALID_ARG;
+  if (c->sink_tokens < 0 || (c->sink_tokens > 0 && c->sliding_window == 0)) return AXON_ERR_INVALID_ARG;
+  if (c->sink_tokens > 0 && c->precision == AXON_FP32_DEBUG) return AXON_ERR_UNSUPPORTED;
   if (c->rope_scaling_factor < 0.f) return AXON_ERR_INVALID_ARG;
   if (c->hidden_act != AXON_ACT_SILU && c->hidden_act != AXON_ACT_GELU_TANH) return AXON_ERR_INVALID_ARG;
   if (c->qk_norm != 0 && c->qk_norm != 1) return AXON_ERR_INVALID_ARG;
@@ -398,6 +401,61 @@ AttnArgs base_attn(const axon_model* m, int layer, const int* block_table) {
   a.d = m->d;
   a.scale_log2 = static_cast<float>(1.0 / std::sqrt(static_cast<double>(m->d)) * 1.4426950408889634);
   a.window = m->cfg.sliding_window;
+  a.err = m->err;
+  return a;
+}
+
+// The same for the kernels that know sinks.
+PagedAttnArgs sink_decode(const axon_model* m, const AttnArgs& at, int B) {
+  PagedAttnArgs a;
+  memset(&a, 0, sizeof(a));
+  a.q = at.q;
+  a.q_lo = at.q_lo;
+  a.o = at.o;
+  a.o_lo = at.o_lo;
+  a.q_row = a.o_row = static_cast<long long>(m->H) * m->d;
+  a.q_head = a.o_head = m->d;
+  a.k = at.k;
+  a.v = at.v;
+  a.ctx = at.ctx;
+  a.block_table = at.block_table;
+  a.blocks_per_seq = at.blocks_per_seq;
+  a.num_blocks = at.num_blocks;
+  a.B = B;
+  a.H = m->H;
+  a.G = m->G;
+  a.d = m->d;
+  a.window = at.window;
+  a.sinks = m->cfg.sink_tokens;
+  a.scale_log2 = at.scale_log2;
+  a.part = static_cast<float*>(m->sink_work);
+  a.ticket = reinterpret_cast<int*>(static_cast<char*>(m->sink_work) + paged_attn_part_bytes(m->H, m->G, m->d, m->num_sms));
+  a.err = m->err;
+  return a;
+}
+ChunkArgs sink_chunk(const axon_model* m, const AttnArgs& at, const AttnVarlen* vl, int B, int T, int layer) {
+  ChunkArgs a;
+  memset(&a, 0, sizeof(a));
+  if (vl) {
+    a.cu = vl->cu;
+    a.past = vl->past;
+  }
+  a.block_table = at.block_table;
+  a.blocks_per_seq = at.blocks_per_seq;
+  a.num_blocks = at.num_blocks;
+  a.B = B;
+  a.T = T;
+  a.max_chunk = at.S;
+  a.H = m->H;
+  a.G = m->G;
+  a.d = m->d;
+  a.window = at.window;
+  a.sinks = m->cfg.sink_tokens;
+  a.scale_log2 = at.scale_log2;
+  a.o = at.o;
+  a.o_row = static_cast<long long>(m->H) * m->d;
+  a.o_head = m->d;
+  a.pool_row0 = layer * static_cast<int>(m->num_blocks) * m->G * 16;
   a.err = m->err;
   return a;
 }
@@ -789,7 +847,9 @@ int enqueue_prefill(axon_model* m, const int32_t* ids, int B, int S, const int32
     at.S = vl ? vl->max_chunk : S;
     const AttnVarlen avl{vl ? vl->cu : nullptr, vl ? vl->ctx : nullptr, M, rowmap};
     pbeg(pf, "prefill_attention");
-    if (attn_tc)
+    if (m->cfg.sink_tokens)
+      CK(launch_attn_chunk(lc, sink_chunk(m, at, vl ? &avl : nullptr, B, M, l), m->attn_maps));
+    else if (attn_tc)
       CK(launch_attn_prefill_tc(lc, at, m->attn_maps, l, B, vl ? &avl : nullptr));
     else
       CK(launch_attn_prefill(lc, m->fp32, at, B, vl ? &avl : nullptr));
@@ -891,9 +951,10 @@ int enqueue_prefill(axon_model* m, const int32_t* ids, int B, int S, const int32
 // The persistent step's attention always pairs q's two terms in one MMA
 // tile, which needs at most 8 query heads per kv head; qk-norm needs a
 // kernel of its own between QKV and attention and mixture-of-experts layers
-// their routing kernels, so those models decode on the launch chain.
+// their routing kernels, and its attention knows no sinks, so those models decode on the
+// launch chain.
 bool persist_eligible(const axon_model* m, int B) {
-  return m->persist_ctas > 0 && !m->fp32 && !m->cfg.qk_norm && !m->moe && m->H / m->G <= 8 &&
+  return m->persist_ctas > 0 && !m->fp32 && !m->cfg.qk_norm && !m->moe && !m->cfg.sink_tokens && m->H / m->G <= 8 &&
          persist_fits(m->d, m->f16, B, m->D, std::max(std::max(m->D, m->H * m->d), m->F));
 }
 
@@ -1047,7 +1108,10 @@ launch_chain:
     at.o_lo = m->o_lo;
     at.q_lo = m->q_lo;
     pbeg(pf, "decode_attention");
-    CK(launch_attn_decode(lc, m->fp32, at, B));
+    if (m->cfg.sink_tokens)
+      CK(launch_attn_paged_decode(lc, sink_decode(m, at, B)));
+    else
+      CK(launch_attn_decode(lc, m->fp32, at, B));
     pend(pf, kv_tokens * 2.0 * m->G * m->d * es + 2.0 * B * Hd * es, 4.0 * kv_tokens * m->H * m->d);
 
     EpiArgs r = base_epi(m);
@@ -1184,7 +1248,8 @@ int axon_model_create(const axon_config* cfg, const axon_tensor* weights, int32_
   int major = 0;
   cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, m->device);
   if (major < 10) return fail(AXON_ERR_UNSUPPORTED);
-  if (prepare_attn_kernels() != cudaSuccess || prepare_attn_tc_kernels() != cudaSuccess ||
+  if (prepare_attn_paged_kernels() != cudaSuccess || prepare_attn_chunk_kernels() != cudaSuccess ||
+      prepare_attn_kernels() != cudaSuccess || prepare_attn_tc_kernels() != cudaSuccess ||
       prepare_skinny_kernels() != cudaSuccess || prepare_gemm_kernels() != cudaSuccess ||
       prepare_gemv_kernels() != cudaSuccess)
     return fail(AXON_ERR_CUDA);
@@ -1484,6 +1549,12 @@ int axon_model_create(const axon_config* cfg, const axon_tensor* weights, int32_
   m->attn_part = static_cast<float*>(p);
   if ((rc = dev_alloc(m, &p, static_cast<size_t>(dec_b) * m->G * 4))) return fail(rc);
   m->attn_cnt = static_cast<int*>(p);
+  if (cfg->sink_tokens > 0) {
+    const size_t bytes = paged_attn_part_bytes(m->H, m->G, m->d, m->num_sms) +
+                         4 * paged_attn_tickets(dec_b, m->H, m->G, m->num_sms);
+    if ((rc = dev_alloc(m, &m->sink_work, bytes))) return fail(rc);
+    if (cudaMemsetAsync(m->sink_work, 0, bytes, st) != cudaSuccess) return fail(AXON_ERR_CUDA);
+  }
   if ((rc = dev_alloc(m, &p, 16))) return fail(rc);
   m->err = static_cast<int*>(p);
   if (cudaMemsetAsync(m->keys, 0, static_cast<size_t>(Mcap) * 8, st) != cudaSuccess ||

@@ -187,9 +187,9 @@ AXON_DEV Item find_item(const ChunkArgs& p, int PC, long long item) {
   for (int b0 = 0; b0 < p.B; b0 += 32) {
     int r0 = 0, len = 0, ps = 0;
     if (b0 + lane < p.B) {
-      r0 = p.cu[b0 + lane];
-      const int r1 = p.cu[b0 + lane + 1];
-      ps = p.past[b0 + lane];
+      r0 = p.cu ? p.cu[b0 + lane] : (b0 + lane) * p.max_chunk;
+      const int r1 = p.cu ? p.cu[b0 + lane + 1] : r0 + p.max_chunk;
+      ps = p.cu ? p.past[b0 + lane] : 0;
       len = r1 - r0;
       const bool off = r0 < 0 || r1 < r0 || r1 > p.T || len > p.max_chunk;
       const bool far = ps < 0 || ps > p.blocks_per_seq * 16 - len;
@@ -244,7 +244,7 @@ AXON_DEV Span span_of(const ChunkArgs& p, const Item& it, int PW) {
 template <int HD, typename T16>
 __global__ void __launch_bounds__(THREADS, 1)
     attn_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
-                      const __grid_constant__ CUtensorMap tmV, const ChunkArgs p, int PW, int pool_row0, int pool_rows) {
+                      const __grid_constant__ CUtensorMap tmV, const ChunkArgs p, int PW, int pool_rows) {
   using C = KCfg<HD>;
   constexpr int NS = C::STAGES;
   extern __shared__ uint8_t smem_raw[];
@@ -374,7 +374,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             set_err(p.err, DEVERR_BLOCK);
             return pool_rows;
           }
-          return pool_row0 + (blk * p.G + item.g) * 16;
+          return p.pool_row0 + (blk * p.G + item.g) * 16;
         };
         int next = pool_row(0);
         for (int t = 0; t < nt && ok; ++t) {
@@ -687,11 +687,13 @@ __global__ void __launch_bounds__(THREADS, 1)
 }
 
 template <int HD, typename T16>
+cudaError_t prepare_hd() {
+  return cudaFuncSetAttribute(attn_chunk_kernel<HD, T16>, cudaFuncAttributeMaxDynamicSharedMemorySize, KCfg<HD>::SMEM);
+}
+
+template <int HD, typename T16>
 cudaError_t launch_hd(const LaunchCtx& lc, const ChunkArgs& a, const AttnMaps& maps) {
   const int PW = attn_tile_positions(a.H, a.G), PC = 2 * PW;
-  cudaError_t e = cudaFuncSetAttribute(attn_chunk_kernel<HD, T16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       KCfg<HD>::SMEM);
-  if (e != cudaSuccess) return e;
   const long long items = (static_cast<long long>(a.T) / PC + a.B) * a.G;  // at most
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(items < lc.num_sms ? items : lc.num_sms));
@@ -701,10 +703,18 @@ cudaError_t launch_hd(const LaunchCtx& lc, const ChunkArgs& a, const AttnMaps& m
   cudaLaunchAttribute attr[2];
   cfg.numAttrs = chain_attrs(lc, attr);
   cfg.attrs = attr;
-  return cudaLaunchKernelEx(&cfg, attn_chunk_kernel<HD, T16>, maps.q, maps.k, maps.v, a, PW, 0, maps.pool_rows);
+  return cudaLaunchKernelEx(&cfg, attn_chunk_kernel<HD, T16>, maps.q, maps.k, maps.v, a, PW, maps.pool_rows);
 }
 
 }  // namespace
+
+cudaError_t prepare_attn_chunk_kernels() {
+  cudaError_t e = prepare_hd<64, bf16>();
+  if (e == cudaSuccess) e = prepare_hd<64, f16>();
+  if (e == cudaSuccess) e = prepare_hd<128, bf16>();
+  if (e == cudaSuccess) e = prepare_hd<128, f16>();
+  return e;
+}
 
 bool make_attn_maps_strided(AttnMaps* maps, const void* q, long long rows, long long q_row, long long q_head,
                             const void* kpool, const void* vpool, long long pool_rows, int H, int G, int d, bool f16) {

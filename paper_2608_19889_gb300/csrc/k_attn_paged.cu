@@ -94,7 +94,7 @@ AXON_DEV RowPages row_pages(const PagedAttnArgs& p, int b) {
   return r;
 }
 
-// LO: q and o carry second 16-bit terms (q_lo read, o_lo written).
+// LO: q has a second 16-bit term, and o one too where o_lo is given.
 template <int HD, typename T16, int NT, bool LO>
 __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_kernel(const PagedAttnArgs p) {
   using C = DCfg<HD, NT>;
@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
       const int h = i / (HD / 8), x = i % (HD / 8);
       const long long at = b * p.o_row + h * p.o_head + x * 8;
       *reinterpret_cast<uint4*>(static_cast<T16*>(p.o) + at) = make_uint4(0, 0, 0, 0);
-      if (LO) *reinterpret_cast<uint4*>(static_cast<T16*>(p.o_lo) + at) = make_uint4(0, 0, 0, 0);
+      if (LO && p.o_lo) *reinterpret_cast<uint4*>(static_cast<T16*>(p.o_lo) + at) = make_uint4(0, 0, 0, 0);
       if (p.lse && x == 0) p.lse[static_cast<long long>(b) * p.H + h] = -INFINITY;
     }
   }
@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
   const int gs = avg >= 16 ? 4 : avg >= 4 ? 2 : 1;
   const int group = warp / gs, wg = warp - group * gs;
   const long long all_groups = static_cast<long long>(gridDim.x) * (DW / gs);
-  const long long nw = min(all_groups, max(1ll, total / gs));  // a page per warp at least
+  const long long nw = min(all_groups, max(1ll, total / (2 * gs)));  // two pages per warp at least
   const long long wid = blockIdx.x + static_cast<long long>(gridDim.x) * group;
   if (wid >= nw) return;
   const long long u0 = total * wid / nw, u1 = total * (wid + 1) / nw;
@@ -396,7 +396,7 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
       v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
       const uint2 w = make_uint2(pack2<T16>(v.x, v.y), pack2<T16>(v.z, v.w));
       *reinterpret_cast<uint2*>(static_cast<T16*>(p.o) + at) = w;
-      if (LO) {
+      if (LO && p.o_lo) {
         const T16* hv = reinterpret_cast<const T16*>(&w);
         *reinterpret_cast<uint2*>(static_cast<T16*>(p.o_lo) + at) =
             make_uint2(pack2<T16>(v.x - to_f(hv[0]), v.y - to_f(hv[1])), pack2<T16>(v.z - to_f(hv[2]), v.w - to_f(hv[3])));
@@ -516,12 +516,20 @@ constexpr size_t smem_bytes(int B) {
   return static_cast<size_t>(DW) * DCfg<HD, NT>::STATE * 4 + (static_cast<size_t>(B) + 1) * 8;
 }
 
+template <int HD, typename T16>
+cudaError_t prepare_hd() {
+  const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  const int one = static_cast<int>(smem_bytes<HD, 1>(PAGED_ATTN_MAX_B)), two = static_cast<int>(smem_bytes<HD, 2>(PAGED_ATTN_MAX_B));
+  cudaError_t e = cudaFuncSetAttribute(attn_paged_decode_kernel<HD, T16, 1, false>, attr, one);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_paged_decode_kernel<HD, T16, 1, true>, attr, one);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_paged_decode_kernel<HD, T16, 2, false>, attr, two);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_paged_decode_kernel<HD, T16, 2, true>, attr, two);
+  return e;
+}
+
 template <int HD, typename T16, int NT, bool LO>
 cudaError_t launch_nt(const LaunchCtx& lc, const PagedAttnArgs& a) {
   const size_t smem = smem_bytes<HD, NT>(a.B);
-  cudaError_t e = cudaFuncSetAttribute(attn_paged_decode_kernel<HD, T16, NT, LO>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       static_cast<int>(smem_bytes<HD, NT>(PAGED_ATTN_MAX_B)));
-  if (e != cudaSuccess) return e;
   // no more CTAs than pages that can be visible, at a page per warp
   long long row = a.blocks_per_seq;
   if (a.window > 0) row = min(row, static_cast<long long>(a.window - 1) / 16 + 2 + (a.sinks + 15ll) / 16);
@@ -557,8 +565,16 @@ size_t paged_attn_tickets(int B, int H, int G, int num_sms) {
   return static_cast<size_t>(B) * G + 2 * static_cast<size_t>(num_sms) * (H / G > 8 ? 2 : 3) * DW;
 }
 
+cudaError_t prepare_attn_paged_kernels() {
+  cudaError_t e = prepare_hd<64, bf16>();
+  if (e == cudaSuccess) e = prepare_hd<64, f16>();
+  if (e == cudaSuccess) e = prepare_hd<128, bf16>();
+  if (e == cudaSuccess) e = prepare_hd<128, f16>();
+  return e;
+}
+
 cudaError_t launch_attn_paged_decode(const LaunchCtx& lc, const PagedAttnArgs& a) {
-  if (a.H / a.G > 16 || a.B < 1 || a.B > PAGED_ATTN_MAX_B || !a.q_lo != !a.o_lo)
+  if (a.H / a.G > 16 || a.B < 1 || a.B > PAGED_ATTN_MAX_B || (a.o_lo && !a.q_lo))
     return cudaErrorInvalidValue;
   if (a.d == 64) return lc.f16 ? launch_hd<64, f16>(lc, a) : launch_hd<64, bf16>(lc, a);
   if (a.d == 128) return lc.f16 ? launch_hd<128, f16>(lc, a) : launch_hd<128, bf16>(lc, a);

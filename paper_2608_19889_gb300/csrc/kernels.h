@@ -186,7 +186,7 @@ cudaError_t launch_attn_prefill_tc(const LaunchCtx& lc, const AttnArgs& a, const
 cudaError_t prepare_attn_tc_kernels();
 // ---- attention of chunks over the paged cache (k_attn_chunk.cu)
 struct ChunkArgs {
-  const int* cu;    // [B + 1] row offsets
+  const int* cu;    // [B + 1] row offsets, or null: chunks of max_chunk rows from position 0
   const int* past;  // [B] tokens before each chunk
   const int* block_table;  // [B][blocks_per_seq], or null: blocks b * blocks_per_seq + j
   int blocks_per_seq, num_blocks;
@@ -196,11 +196,13 @@ struct ChunkArgs {
   float scale_log2;
   void* o;  // [T][H][d], strides in elements
   long long o_row, o_head;
+  int pool_row0;  // row of the maps' pools at which the layer begins
   int* err;
 };
 // q [rows][H][d] with these strides in elements; the pools hold one layer.
 bool make_attn_maps_strided(AttnMaps* maps, const void* q, long long rows, long long q_row, long long q_head,
                             const void* kpool, const void* vpool, long long pool_rows, int H, int G, int d, bool f16);
+cudaError_t prepare_attn_chunk_kernels();
 cudaError_t launch_attn_chunk(const LaunchCtx& lc, const ChunkArgs& a, const AttnMaps& maps);
 
 // ---- attention of one new token per row over the paged cache (k_attn_paged.cu)
@@ -208,7 +210,7 @@ constexpr int PAGED_ATTN_MAX_B = 2048;
 struct PagedAttnArgs {
   const void* q;  // [B][H][d], strides in elements
   long long q_row, q_head;
-  const void* q_lo;  // optional second term of q, same strides (then o_lo too)
+  const void* q_lo;  // optional second term of q, same strides
   const void* k;     // layer pool [num_blocks][G][16][d]
   const void* v;
   const int* ctx;  // row b's query is at position ctx[b] + pos_add; negative: the row is idle
@@ -220,7 +222,7 @@ struct PagedAttnArgs {
   float scale_log2;
   void* o;
   long long o_row, o_head;
-  void* o_lo;
+  void* o_lo;   // optional second term of o, same strides (with q_lo only)
   float* lse;   // optional [B][H], natural logarithm
   float* part;  // paged_attn_part_bytes
   int* ticket;  // paged_attn_tickets, zero between calls
@@ -228,6 +230,7 @@ struct PagedAttnArgs {
 };
 size_t paged_attn_part_bytes(int H, int G, int d, int num_sms);
 size_t paged_attn_tickets(int B, int H, int G, int num_sms);
+cudaError_t prepare_attn_paged_kernels();
 cudaError_t launch_attn_paged_decode(const LaunchCtx& lc, const PagedAttnArgs& a);
 
 // ---- blocks of the paged cache (k_pages.cu)

@@ -6,6 +6,8 @@
 #include <stdint.h>
 #include <string.h>
 
+#include <atomic>
+
 #include "../../include/axon.h"
 #include "kernels.h"
 
@@ -32,6 +34,32 @@ long long block_bytes(const axon_kv_cache* c) {
 // One layer's keys or values of a cache.
 void* layer_pool(const axon_kv_cache* c, void* pool, int layer) {
   return static_cast<char*>(pool) + static_cast<long long>(layer) * c->num_blocks * block_bytes(c);
+}
+
+// The kernels' shared-memory limits belong to the device's context; they are set with the first
+// attention call on a device, and again after its context was torn down (the launch of a kernel
+// without them fails, and is then repeated once by with_limits).
+template <typename Launch>
+cudaError_t with_limits(Launch launch) {
+  static std::atomic<uint64_t> ready{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  for (int round = 0; round < 2; ++round) {
+    const bool known = (ready.load(std::memory_order_acquire) & bit) != 0;
+    if (!known) {
+      e = prepare_attn_chunk_kernels();
+      if (e == cudaSuccess) e = prepare_attn_paged_kernels();
+      if (e != cudaSuccess) return e;
+      ready.fetch_or(bit, std::memory_order_release);
+    }
+    e = launch();
+    if (e != cudaErrorInvalidValue || !known) return e;
+    cudaGetLastError();
+    ready.fetch_and(~bit, std::memory_order_release);
+  }
+  return e;
 }
 
 int launch_ctx(const axon_kv_cache* c, void* stream, LaunchCtx* lc) {
@@ -167,7 +195,7 @@ int axon_attn_decode(const axon_kv_cache* cache, int32_t layer, const void* d_q,
   a.part = static_cast<float*>(d_workspace);
   a.ticket = reinterpret_cast<int*>(static_cast<char*>(d_workspace) + part);
   a.err = d_err;
-  return status(launch_attn_paged_decode(lc, a));
+  return status(with_limits([&] { return launch_attn_paged_decode(lc, a); }));
 }
 
 int axon_attn_prefill(const axon_kv_cache* cache, int32_t layer, const void* d_q, int64_t q_row_stride,
@@ -212,7 +240,7 @@ int axon_attn_prefill(const axon_kv_cache* cache, int32_t layer, const void* d_q
   a.o_row = out_row_stride;
   a.o_head = out_head_stride;
   a.err = d_err;
-  return status(launch_attn_chunk(lc, a, maps));
+  return status(with_limits([&] { return launch_attn_chunk(lc, a, maps); }));
 }
 
 int axon_kv_workspace(const axon_kv_cache* cache, const axon_kv_seqs* seqs, int64_t* bytes) {

@@ -148,7 +148,7 @@ def _stream(stream):
     if stream is None:
         lib()
         if _raw_stream is not None:
-            return ctypes.c_void_p(_raw_stream(_torch.cuda.current_device()))
+            return _raw_stream(_torch.cuda.current_device())
         stream = _torch.cuda.current_stream()
     return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
@@ -291,32 +291,52 @@ def axon_free(m):
 
 
 # ------------------------------------------------- operators on a paged cache
+# Small calls are bound by the host: what a wrapper reads of a tensor costs 0.05 to 0.15 us apiece.
 
 
-def _is(t, dtype, what, *shape):
-    """Refuse a tensor the C call could not tell from a right one: device, type, shape, dense layout."""
-    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous() or (shape and t.shape != shape):
-        raise TypeError(f"{what}: a dense {dtype} device tensor{' of shape ' + str(shape) if shape else ''} is wanted, "
-                        f"got {t.dtype} {tuple(t.shape)} on {t.device}")
-    return t.data_ptr()
+def _want(t, dtype, what, n):
+    """Address of a dense device tensor of n elements; refuse what the C call could not tell from one."""
+    if t.dtype is dtype and t.is_cuda and t.is_contiguous() and t.numel() == n:
+        return t.data_ptr()
+    raise TypeError(f"{what}: a dense {dtype} device tensor of {n} elements is wanted, got {t.dtype} {tuple(t.shape)} "
+                    f"with strides {t.stride()} on {t.device}")
 
 
-def _ints(t, what, *shape):
-    return None if t is None else _is(t, _torch.int32, what, *shape)
+def _list(t, what):
+    """Address and length of a dense int32 device vector."""
+    if t.dim() != 1:
+        raise TypeError(f"{what}: a vector is wanted, got {tuple(t.shape)}")
+    n = t.numel()
+    return _want(t, _torch.int32, what, n), n
+
+
+def _word(err):
+    return None if err is None else _want(err, _torch.int32, "err", 1)
+
+
+def _handle(stream, t):
+    """The stream's handle; None: the current one of the tensor's device."""
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(t.get_device())
+    return _stream(stream)
 
 
 def make_kv_cache(k, v) -> axon_kv_cache:
     """Descriptor of the pools k, v: dense device tensors [layers, blocks, kv heads, 16, head_dim] (bf16, fp16; the
     block operators also take fp32). It holds their addresses: keep the tensors."""
     lib()
-    torch = _torch
-    prec = {torch.bfloat16: AXON_BF16, torch.float16: AXON_FP16, torch.float32: AXON_FP32_DEBUG}.get(k.dtype)
-    if prec is None or k.dim() != 5:
-        raise TypeError(f"k: a bf16, fp16 or fp32 tensor of 5 dimensions is wanted, got {k.dtype} {tuple(k.shape)}")
+    prec = {_torch.bfloat16: AXON_BF16, _torch.float16: AXON_FP16, _torch.float32: AXON_FP32_DEBUG}.get(k.dtype)
+    if prec is None or k.dim() != 5 or v.shape != k.shape:
+        raise TypeError(f"k, v: bf16, fp16 or fp32 tensors of the same 5 dimensions are wanted, got {k.dtype} "
+                        f"{tuple(k.shape)} and {v.dtype} {tuple(v.shape)}")
     L, N, G, bs, d = k.shape
-    c = axon_kv_cache(_is(k, k.dtype, "k"), _is(v, k.dtype, "v", *k.shape), L, N, G, bs, d, prec)
-    c.dtype = k.dtype
-    c.ref = ctypes.byref(c)
+    return _described(axon_kv_cache(_want(k, k.dtype, "k", k.numel()), _want(v, k.dtype, "v", k.numel()), L, N, G, bs, d, prec))
+
+
+def _described(c):
+    """What the wrappers read of a descriptor at every call, as plain attributes."""
+    c.dtype = {AXON_BF16: _torch.bfloat16, AXON_FP16: _torch.float16, AXON_FP32_DEBUG: _torch.float32}[c.precision]
+    c.blocks, c.dim, c.ref = c.num_blocks, c.head_dim, ctypes.byref(c)
     return c
 
 
@@ -324,9 +344,7 @@ def axon_kv_cache_get(m) -> axon_kv_cache:
     """Descriptor of a model's own cache."""
     c = axon_kv_cache()
     _check("axon_kv_cache_get", lib().axon_kv_cache_get(m, ctypes.byref(c)))
-    c.dtype = {AXON_BF16: _torch.bfloat16, AXON_FP16: _torch.float16, AXON_FP32_DEBUG: _torch.float32}[c.precision]
-    c.ref = ctypes.byref(c)
-    return c
+    return _described(c)
 
 
 def make_kv_seqs(block_table, context_lens, refs) -> axon_kv_seqs:
@@ -334,9 +352,9 @@ def make_kv_seqs(block_table, context_lens, refs) -> axon_kv_seqs:
     their addresses: keep the tensors."""
     lib()
     R, P = block_table.shape
-    s = axon_kv_seqs(_ints(block_table, "block_table"), _ints(context_lens, "context_lens", R), _ints(refs, "refs"), R, P)
-    s.num_blocks = refs.numel()
-    s.ref = ctypes.byref(s)
+    s = axon_kv_seqs(_want(block_table, _torch.int32, "block_table", R * P), _want(context_lens, _torch.int32, "context_lens", R),
+                     _list(refs, "refs")[0], R, P)
+    s.blocks, s.ref = refs.numel(), ctypes.byref(s)
     return s
 
 
@@ -354,19 +372,21 @@ def make_kv_workspace(cache, seqs):
     return _torch.empty(n.value, dtype=_torch.uint8, device="cuda")
 
 
-def _rows_of(t, cache, what):
-    """(address, row stride, head stride) of a [rows, heads, head_dim] tensor of the cache's type."""
-    row, head, one = t.stride()
-    if t.dtype is not cache.dtype or not t.is_cuda or one != 1 or t.shape[2] != cache.head_dim:
-        raise TypeError(f"{what}: a {cache.dtype} device tensor [rows, heads, {cache.head_dim}] with a dense last "
-                        f"dimension is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
-    return t.data_ptr(), row, head
+def _rows(q, out, cache):
+    """(rows, heads, row stride, head stride of q, of out) of [rows, heads, head_dim] tensors of the cache's type."""
+    shape, qs, os_ = q.shape, q.stride(), out.stride()
+    if (len(shape) != 3 or out.shape != shape or shape[2] != cache.dim or q.dtype is not cache.dtype or
+            out.dtype is not cache.dtype or qs[2] != 1 or os_[2] != 1 or not q.is_cuda or not out.is_cuda):
+        raise TypeError(f"q, out: {cache.dtype} device tensors [rows, heads, {cache.dim}] with a dense last dimension are "
+                        f"wanted, got {q.dtype} {tuple(shape)} on {q.device}, {out.dtype} {tuple(out.shape)} on {out.device}")
+    return shape[0], shape[1], qs[0], qs[1], os_[0], os_[1]
 
 
-def _table_of(block_table, blocks_per_seq, rows):
+def _table(block_table, blocks_per_seq, rows):
     if block_table is None:
-        return None, int(blocks_per_seq)
-    return _ints(block_table, "block_table", rows, block_table.shape[1]), block_table.shape[1]
+        return None, blocks_per_seq
+    per = block_table.shape[-1]
+    return _want(block_table, _torch.int32, "block_table", rows * per), per
 
 
 def axon_attn_decode(cache, layer, q, context_lens, out, workspace, block_table=None, blocks_per_seq=0, window=0, sinks=0,
@@ -374,84 +394,78 @@ def axon_attn_decode(cache, layer, q, context_lens, out, workspace, block_table=
     """Attention of one new token per row (see include/axon.h). q, out: [B, heads, head_dim], any row and head strides;
     context_lens: int32 [B]; block_table: int32 [B, blocks], or None with blocks_per_seq for contiguous rows;
     workspace: make_attn_workspace; lse: fp32 [B, heads] or None; err: int32 [1] error word or None."""
-    B, H, _ = q.shape
-    if out.shape != q.shape:
-        raise TypeError(f"out: the shape of q {tuple(q.shape)} is wanted, got {tuple(out.shape)}")
-    qp, qr, qh = _rows_of(q, cache, "q")
-    op, orow, ohead = _rows_of(out, cache, "out")
-    table, per = _table_of(block_table, blocks_per_seq, B)
-    _check("axon_attn_decode", lib().axon_attn_decode(
-        cache.ref, layer, qp, qr, qh, B, H, _ints(context_lens, "context_lens", B), table, per, window, sinks, scale, op,
-        orow, ohead, None if lse is None else _is(lse, _torch.float32, "lse", B, H), workspace.data_ptr(),
-        workspace.numel(), _ints(err, "err", 1), _stream(stream)))
+    B, H, qr, qh, orow, ohead = _rows(q, out, cache)
+    table, per = _table(block_table, blocks_per_seq, B)
+    rc = _lib.axon_attn_decode(
+        cache.ref, layer, q.data_ptr(), qr, qh, B, H, _want(context_lens, _torch.int32, "context_lens", B), table, per, window,
+        sinks, scale, out.data_ptr(), orow, ohead, None if lse is None else _want(lse, _torch.float32, "lse", B * H),
+        workspace.data_ptr(), workspace.nbytes, None if err is None else _word(err), _handle(stream, q))
+    if rc:
+        raise AxonError("axon_attn_decode", rc)
 
 
 def axon_attn_prefill(cache, layer, q, cu_seqlens, context_lens, max_chunk, out, block_table=None, blocks_per_seq=0,
                       window=0, sinks=0, scale=0.0, err=None, stream=None):
     """Attention of packed chunks (see include/axon.h). q, out: [T, heads, head_dim]; cu_seqlens: int32 [B+1];
     context_lens: int32 [B] tokens before each chunk (not advanced); the rest as in axon_attn_decode."""
-    T, H, _ = q.shape
-    B = context_lens.shape[0]
-    if out.shape != q.shape:
-        raise TypeError(f"out: the shape of q {tuple(q.shape)} is wanted, got {tuple(out.shape)}")
-    qp, qr, qh = _rows_of(q, cache, "q")
-    op, orow, ohead = _rows_of(out, cache, "out")
-    table, per = _table_of(block_table, blocks_per_seq, B)
-    _check("axon_attn_prefill", lib().axon_attn_prefill(
-        cache.ref, layer, qp, qr, qh, B, T, H, _ints(cu_seqlens, "cu_seqlens", B + 1),
-        _ints(context_lens, "context_lens", B), int(max_chunk), table, per, window, sinks, scale, op, orow, ohead,
-        _ints(err, "err", 1), _stream(stream)))
+    T, H, qr, qh, orow, ohead = _rows(q, out, cache)
+    past, B = _list(context_lens, "context_lens")
+    table, per = _table(block_table, blocks_per_seq, B)
+    rc = _lib.axon_attn_prefill(
+        cache.ref, layer, q.data_ptr(), qr, qh, B, T, H, _want(cu_seqlens, _torch.int32, "cu_seqlens", B + 1), past, max_chunk,
+        table, per, window, sinks, scale, out.data_ptr(), orow, ohead, None if err is None else _word(err),
+        _handle(stream, q))
+    if rc:
+        raise AxonError("axon_attn_prefill", rc)
 
 
 def _same_pool(cache, seqs):
-    if cache.num_blocks != seqs.num_blocks:
-        raise TypeError(f"refs: {cache.num_blocks} counts are wanted, one per block, got {seqs.num_blocks}")
+    if cache.blocks != seqs.blocks:
+        raise TypeError(f"refs: {cache.blocks} counts are wanted, one per block, got {seqs.blocks}")
 
 
 def axon_kv_copy_blocks(cache, src, dst, err=None, stream=None):
     """Copy blocks src[i] to dst[i] (int32 [n]) in all layers."""
-    n = src.shape[0]
-    _check("axon_kv_copy_blocks", lib().axon_kv_copy_blocks(
-        cache.ref, _ints(src, "src", n), _ints(dst, "dst", n), n, _ints(err, "err", 1), _stream(stream)))
+    s, n = _list(src, "src")
+    _check("axon_kv_copy_blocks", _lib.axon_kv_copy_blocks(cache.ref, s, _want(dst, _torch.int32, "dst", n), n, _word(err),
+                                                           _handle(stream, src)))
 
 
 def axon_kv_fork(cache, seqs, src, dst, workspace, err=None, stream=None):
     """Rows dst[i] take over what rows src[i] hold (int32 [n]); workspace: make_kv_workspace."""
     _same_pool(cache, seqs)
-    n = src.shape[0]
-    _check("axon_kv_fork", lib().axon_kv_fork(
-        cache.ref, seqs.ref, _ints(src, "src", n), _ints(dst, "dst", n), n, workspace.data_ptr(), workspace.numel(),
-        _ints(err, "err", 1), _stream(stream)))
+    s, n = _list(src, "src")
+    _check("axon_kv_fork", _lib.axon_kv_fork(cache.ref, seqs.ref, s, _want(dst, _torch.int32, "dst", n), n,
+                                             workspace.data_ptr(), workspace.nbytes, _word(err), _handle(stream, src)))
 
 
 def axon_kv_release(cache, seqs, rows, window=0, sinks=0, err=None, stream=None):
     """Rows (int32 [n]) give back everything, or with a window what no later query sees."""
     _same_pool(cache, seqs)
-    n = rows.shape[0]
-    _check("axon_kv_release", lib().axon_kv_release(cache.ref, seqs.ref, _ints(rows, "rows", n), n, window, sinks,
-                                                    _ints(err, "err", 1), _stream(stream)))
+    r, n = _list(rows, "rows")
+    _check("axon_kv_release", _lib.axon_kv_release(cache.ref, seqs.ref, r, n, window, sinks, _word(err), _handle(stream, rows)))
 
 
 def axon_kv_reserve(cache, seqs, rows, new_tokens, workspace, err=None, stream=None):
     """Rows (int32 [n]) take blocks for new_tokens (int32 [n]) more tokens; workspace: make_kv_workspace."""
     _same_pool(cache, seqs)
-    n = rows.shape[0]
-    _check("axon_kv_reserve", lib().axon_kv_reserve(
-        cache.ref, seqs.ref, _ints(rows, "rows", n), _ints(new_tokens, "new_tokens", n), n, workspace.data_ptr(),
-        workspace.numel(), _ints(err, "err", 1), _stream(stream)))
+    r, n = _list(rows, "rows")
+    _check("axon_kv_reserve", _lib.axon_kv_reserve(cache.ref, seqs.ref, r, _want(new_tokens, _torch.int32, "new_tokens", n), n,
+                                                   workspace.data_ptr(), workspace.nbytes, _word(err), _handle(stream, rows)))
 
 
 def axon_kv_compact(cache, seqs, workspace, moved=None, live=None, err=None, stream=None):
     """Move the blocks in use to the front of the pool. moved: int32 [blocks] each block's number afterwards (-1: free);
     live: int32 [1] their count; workspace: make_kv_workspace."""
     _same_pool(cache, seqs)
-    _check("axon_kv_compact", lib().axon_kv_compact(
-        cache.ref, seqs.ref, _ints(moved, "moved", cache.num_blocks), _ints(live, "live", 1), workspace.data_ptr(),
-        workspace.numel(), _ints(err, "err", 1), _stream(stream)))
+    _check("axon_kv_compact", _lib.axon_kv_compact(
+        cache.ref, seqs.ref, None if moved is None else _want(moved, _torch.int32, "moved", cache.blocks),
+        None if live is None else _want(live, _torch.int32, "live", 1), workspace.data_ptr(), workspace.nbytes, _word(err),
+        _handle(stream, workspace)))
 
 
 def axon_check_error(err, stream=None) -> tuple[int, int]:
     """(status, bits) of an operator's error word (int32 [1]) after synchronising the stream; the word is cleared."""
     bits = ctypes.c_int32(0)
-    rc = lib().axon_check_error(_ints(err, "err", 1), _stream(stream), ctypes.byref(bits))
+    rc = lib().axon_check_error(_want(err, _torch.int32, "err", 1), _stream(stream), ctypes.byref(bits))
     return rc, bits.value

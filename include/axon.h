@@ -413,7 +413,8 @@ typedef struct axon_kv_seqs {
  *                   dimension dense, the others with strides in elements
  *                   (multiples of 8, at least head_dim; 16-byte aligned
  *                   base; a row's heads may not overlap in d_out).
- *   B               1 .. 2048
+ *   B               1 .. 2048 (and B * num_kv_heads * the blocks that a row can see
+ *                   below 2^31)
  *   num_heads       a multiple of num_kv_heads, at most 16 times as many;
  *                   head h reads kv head h / (num_heads / num_kv_heads)
  *   d_context_lens  [B]; negative: an idle row, o = 0 and lse = -infinity

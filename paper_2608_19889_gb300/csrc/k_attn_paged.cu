@@ -77,21 +77,25 @@ template <> AXON_DEV uint32_t pack_prob<f16>(float a, float b, float& ra, float&
 struct RowPages {
   int pos, lo, sink, first, n;
 };
-AXON_DEV RowPages row_pages(const PagedAttnArgs& p, int b) {
+AXON_DEV RowPages row_pages(const PagedAttnArgs& p, int pos) {
   RowPages r;
-  r.pos = p.ctx[b] + p.pos_add;
-  const bool ok = r.pos < p.blocks_per_seq * 16;
-  if (!ok) set_err(p.err, DEVERR_POS);
-  if (!ok || r.pos < 0) {
+  r.pos = pos;
+  if (pos < 0) {
     r.lo = r.sink = r.first = r.n = 0;
-    r.pos = -1;
     return r;
   }
-  r.lo = (p.window > 0 && r.pos >= p.window) ? r.pos - p.window + 1 : 0;
+  r.lo = (p.window > 0 && pos >= p.window) ? pos - p.window + 1 : 0;
   r.first = r.lo >> 4;
-  r.sink = min((min(p.sinks, r.pos + 1) + 15) >> 4, r.first);
-  r.n = r.sink + (r.pos >> 4) + 1 - r.first;
+  r.sink = min((min(p.sinks, pos + 1) + 15) >> 4, r.first);
+  r.n = r.sink + (pos >> 4) + 1 - r.first;
   return r;
+}
+// Position of row b's query; -1: the row sees nothing.
+AXON_DEV int row_pos(const PagedAttnArgs& p, int b) {
+  const long long pos = static_cast<long long>(p.ctx[b]) + p.pos_add;
+  if (pos < p.blocks_per_seq * 16ll) return pos < 0 ? -1 : static_cast<int>(pos);
+  set_err(p.err, DEVERR_POS);
+  return -1;
 }
 
 // LO: q has a second 16-bit term, and o one too where o_lo is given.
@@ -103,7 +107,8 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
   constexpr int MT = HD / 16;  // 16-dim tiles of O^T
   extern __shared__ __align__(16) float sm[];
   float* const state = sm;                                        // [DW][STATE]
-  long long* const before = reinterpret_cast<long long*>(sm + DW * C::STATE);  // [B + 1] pages of the rows before
+  unsigned* const before = reinterpret_cast<unsigned*>(sm + DW * C::STATE);  // [B + 1] pages of the rows before
+  int* const rpos = reinterpret_cast<int*>(before + p.B + 1);                // [B] the rows' positions
   __shared__ int s_scan[DW], s_last[DW];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, c = lane & 3;
   const int HPG = p.H / p.G;
@@ -111,11 +116,28 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
   grid_dep_wait();
 
   // ---- pages before each row
-  {
-    long long base = 0;
+  if (p.B <= 32) {
+    if (warp == 0) {
+      const int pos = lane < p.B ? row_pos(p, lane) : -1;
+      const int n = row_pages(p, pos).n;
+      int inc = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int t = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += t;
+      }
+      if (lane < p.B) {
+        before[lane] = inc - n;
+        rpos[lane] = pos;
+      }
+      if (lane == 31) before[p.B] = inc;
+    }
+  } else {
+    int base = 0;
     for (int b0 = 0; b0 < p.B; b0 += DW * 32) {
       const int b = b0 + tid;
-      int n = b < p.B ? row_pages(p, b).n : 0;
+      const int pos = b < p.B ? row_pos(p, b) : -1;
+      const int n = row_pages(p, pos).n;
       int inc = n;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -130,14 +152,17 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
         add += w < warp ? s_scan[w] : 0;
         all += s_scan[w];
       }
-      if (b < p.B) before[b] = base + add + inc - n;
+      if (b < p.B) {
+        before[b] = base + add + inc - n;
+        rpos[b] = pos;
+      }
       base += all;
       __syncthreads();
     }
     if (tid == 0) before[p.B] = base;
-    __syncthreads();
   }
-  const long long total = before[p.B] * p.G;
+  __syncthreads();
+  const unsigned total = before[p.B] * p.G;  // below 2^31: the launcher saw to it
 
   // ---- rows that see nothing
   for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
@@ -153,14 +178,20 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
   if (total == 0) return;
 
   // ---- workers: more warps share an item the longer the items are
-  const long long avg = total / (static_cast<long long>(p.B) * p.G);
+  const unsigned avg = total / (p.B * p.G);
   const int gs = avg >= 16 ? 4 : avg >= 4 ? 2 : 1;
   const int group = warp / gs, wg = warp - group * gs;
-  const long long all_groups = static_cast<long long>(gridDim.x) * (DW / gs);
-  const long long nw = min(all_groups, max(1ll, total / (2 * gs)));  // two pages per warp at least
-  const long long wid = blockIdx.x + static_cast<long long>(gridDim.x) * group;
+  const unsigned all_groups = gridDim.x * (DW / gs);
+  const unsigned nw = min(all_groups, max(1u, total / (2 * gs)));  // two pages per warp at least
+  const unsigned wid = blockIdx.x + gridDim.x * group;
   if (wid >= nw) return;
-  const long long u0 = total * wid / nw, u1 = total * (wid + 1) / nw;
+  // the first `extra` workers take a page more than the others
+  const unsigned share = total / nw, extra = total - share * nw;
+  const unsigned u0 = wid * share + min(wid, extra), u1 = u0 + share + (wid < extra ? 1 : 0);
+  auto worker_of = [&](unsigned u) {
+    const unsigned cut = extra * (share + 1);
+    return u < cut ? u / (share + 1) : extra + (u - cut) / share;
+  };
 
   int b = 0;
   {
@@ -176,14 +207,32 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
   float* const mine = state + warp * C::STATE;
   const float sl2 = p.scale_log2;
 
-  for (long long u = u0; u < u1;) {
+  for (unsigned u = u0; u < u1;) {
     while (before[b + 1] * p.G <= u) ++b;
-    const RowPages rp = row_pages(p, b);
-    const long long row0 = before[b] * p.G;
+    const RowPages rp = row_pages(p, rpos[b]);
+    const unsigned row0 = before[b] * p.G;
     const int g = static_cast<int>((u - row0) / rp.n);
-    const long long item0 = row0 + static_cast<long long>(g) * rp.n;
+    const unsigned item0 = row0 + static_cast<unsigned>(g) * rp.n;
     const int off = static_cast<int>(u - item0);
-    const int cnt = static_cast<int>(min(static_cast<long long>(rp.n - off), u1 - u));
+    const int cnt = static_cast<int>(min(static_cast<unsigned>(rp.n - off), u1 - u));
+
+    // ---- this warp's pages: off + wg, off + wg + gs, ...
+    const int pages = cnt > wg ? (cnt - wg + gs - 1) / gs : 0;
+    auto logical = [&](int k) {  // page of the row that is this warp's k-th
+      const int i = off + wg + k * gs;
+      return i < rp.sink ? i : i - rp.sink + rp.first;
+    };
+    auto entries = [&](int k0) {  // pool blocks of this warp's pages k0 .. k0 + 31, one per lane
+      const int k = k0 + lane;
+      if (k >= pages) return -1;
+      const int j = logical(k);
+      const int blk = p.block_table ? p.block_table[static_cast<long long>(b) * p.blocks_per_seq + j]
+                                    : b * p.blocks_per_seq + j;
+      if (blk >= 0 && blk < p.num_blocks) return blk;
+      set_err(p.err, DEVERR_BLOCK);
+      return -1;
+    };
+    int ent = entries(0);
 
     // ---- queries of the item's heads as the 8-wide operand
     uint32_t q[NT][KI][4];
@@ -211,22 +260,6 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
       for (int j = 0; j < MT; ++j) o[n][j][0] = o[n][j][1] = o[n][j][2] = o[n][j][3] = 0.f;
     }
 
-    // ---- this warp's pages: off + wg, off + wg + gs, ...
-    const int pages = cnt > wg ? (cnt - wg + gs - 1) / gs : 0;
-    auto logical = [&](int k) {  // page of the row that is this warp's k-th
-      const int i = off + wg + k * gs;
-      return i < rp.sink ? i : i - rp.sink + rp.first;
-    };
-    auto entries = [&](int k0) {  // pool blocks of this warp's pages k0 .. k0 + 31, one per lane
-      const int k = k0 + lane;
-      if (k >= pages) return -1;
-      const int j = logical(k);
-      const int blk = p.block_table ? p.block_table[static_cast<long long>(b) * p.blocks_per_seq + j]
-                                    : b * p.blocks_per_seq + j;
-      if (blk >= 0 && blk < p.num_blocks) return blk;
-      set_err(p.err, DEVERR_BLOCK);
-      return -1;
-    };
     uint4 kv[2][KI], vv[4][VI];
     auto seen = [&](int t) { return t <= rp.pos && (t >= rp.lo || t < p.sinks); };
     // every token of the page is visible: the usual page, loaded without predicates
@@ -269,7 +302,6 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
       }
     };
     if (pages > 0) {
-      int ent = entries(0);
       int blk = __shfl_sync(0xffffffffu, ent, 0), t0 = logical(0) * 16;
       bool all = whole_page(blk, t0);
       load_k(blk, t0, all);
@@ -405,8 +437,8 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
         p.lse[static_cast<long long>(b) * p.H + g * HPG + h] = (M + log2f(L)) * 0.69314718055994531f;
     };
     // parts of the item: workers first .. last hold one each, in this slot of the workspace
-    const long long first = ((item0 + 1) * nw - 1) / total, last = ((item0 + rp.n) * nw - 1) / total;
-    auto slot = [&](long long w) { return 2 * w + (w > first ? 0 : 1); };
+    const unsigned first = worker_of(item0), last = worker_of(item0 + rp.n - 1);
+    auto slot = [&](unsigned w) { return 2ll * w + (w > first ? 0 : 1); };
     auto put = [&](float* at, int h, int x, float4 v, float M, float L) {
       *reinterpret_cast<float4*>(at + h * HD + x * 4) = v;
       if (x == 0) {
@@ -437,7 +469,7 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
       // `count` parts from worker w0 on, `step` apart, joined in order: into a slot of the second
       // level, or into the output
       const long long joined = 2ll * gridDim.x * DW;  // second level's slots
-      auto join = [&](long long w0, int count, int step, bool out) {
+      auto join = [&](unsigned w0, int count, int step, bool out) {
         const long long from = step > 1 ? joined : 0;
         for (int i = gl; i < HPG * PX; i += gs * 32) {
           const int h = i / PX, x = i % PX;
@@ -452,7 +484,7 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
               ps[y] = 0.f;
               pv[y] = make_float4(0.f, 0.f, 0.f, 0.f);
               if (j0 + y < count) {
-                const float* at = p.part + (from + slot(w0 + static_cast<long long>(j0 + y) * step)) * C::PART;
+                const float* at = p.part + (from + slot(w0 + (j0 + y) * step)) * C::PART;
                 pm[y] = __ldcg(at + C::HEADS * HD + h);
                 ps[y] = __ldcg(at + C::HEADS * HD + C::HEADS + h);
                 pv[y] = __ldcg(reinterpret_cast<const float4*>(at + h * HD + x * 4));
@@ -513,7 +545,7 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
 
 template <int HD, int NT>
 constexpr size_t smem_bytes(int B) {
-  return static_cast<size_t>(DW) * DCfg<HD, NT>::STATE * 4 + (static_cast<size_t>(B) + 1) * 8;
+  return static_cast<size_t>(DW) * DCfg<HD, NT>::STATE * 4 + (2 * static_cast<size_t>(B) + 1) * 4;
 }
 
 template <int HD, typename T16>
@@ -531,9 +563,9 @@ template <int HD, typename T16, int NT, bool LO>
 cudaError_t launch_nt(const LaunchCtx& lc, const PagedAttnArgs& a) {
   const size_t smem = smem_bytes<HD, NT>(a.B);
   // no more CTAs than pages that can be visible, at a page per warp
-  long long row = a.blocks_per_seq;
-  if (a.window > 0) row = min(row, static_cast<long long>(a.window - 1) / 16 + 2 + (a.sinks + 15ll) / 16);
-  const long long pages = row * a.B * a.G, most = static_cast<long long>(lc.num_sms) * (NT == 1 ? 3 : 2);
+  const long long pages = paged_attn_most_pages(a.B, a.G, a.blocks_per_seq, a.window, a.sinks);
+  const long long most = static_cast<long long>(lc.num_sms) * (NT == 1 ? 3 : 2);
+  if (pages > 0x7fffffff) return cudaErrorInvalidValue;
   const long long grid = min(most, (pages + DW - 1) / DW);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(grid));

@@ -230,6 +230,15 @@ struct PagedAttnArgs {
 };
 size_t paged_attn_part_bytes(int H, int G, int d, int num_sms);
 size_t paged_attn_tickets(int B, int H, int G, int num_sms);
+// Pages that can be visible to B rows, times the kv heads; at most 2^31 - 1 are supported.
+inline long long paged_attn_most_pages(int B, int G, int blocks_per_seq, int window, int sinks) {
+  long long row = blocks_per_seq;
+  if (window > 0) {
+    const long long seen = (window - 1ll) / 16 + 2 + (sinks + 15ll) / 16;
+    row = seen < row ? seen : row;
+  }
+  return row * B * G;
+}
 cudaError_t prepare_attn_paged_kernels();
 cudaError_t launch_attn_paged_decode(const LaunchCtx& lc, const PagedAttnArgs& a);
 

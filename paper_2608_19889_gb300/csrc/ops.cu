@@ -158,7 +158,8 @@ int axon_attn_decode(const axon_kv_cache* cache, int32_t layer, const void* d_q,
   int rc = check_attn(cache, layer, d_q, d_out, num_heads, blocks_per_seq, window, sinks, scale);
   if (rc) return rc;
   if (!d_context_lens || !d_workspace || unaligned(d_workspace) || B < 1) return AXON_ERR_INVALID_ARG;
-  if (B > PAGED_ATTN_MAX_B) return AXON_ERR_UNSUPPORTED;
+  if (B > PAGED_ATTN_MAX_B || paged_attn_most_pages(B, cache->num_kv_heads, blocks_per_seq, window, sinks) > INT_MAX)
+    return AXON_ERR_UNSUPPORTED;
   if ((rc = check_strides(B, num_heads, cache->head_dim, q_row_stride, q_head_stride)) ||
       (rc = check_strides(B, num_heads, cache->head_dim, out_row_stride, out_head_stride)))
     return rc;

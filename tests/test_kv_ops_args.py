@@ -68,6 +68,7 @@ def test_caches_that_the_attention_refuses(ax, change, want):
 
 def test_limits(ax):
     assert decode(ax, B=2049) == ax.AXON_ERR_UNSUPPORTED
+    assert decode(ax, B=2048, per=1 << 20) == ax.AXON_ERR_UNSUPPORTED  # 2^32 pages
     assert decode(ax, H=34, qr=34 * 64, orow=34 * 64) == ax.AXON_ERR_UNSUPPORTED  # 17 query heads per kv head
     assert prefill(ax, H=34, qr=34 * 64, orow=34 * 64) == ax.AXON_ERR_UNSUPPORTED
     assert ax.lib().axon_attn_decode(None, 0, FAKE, 64, 64, 1, 1, FAKE, FAKE, 1, 0, 0, 0.0, FAKE, 64, 64, None, FAKE, 1 << 40,

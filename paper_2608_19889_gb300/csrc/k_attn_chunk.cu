@@ -32,12 +32,15 @@
 // busy while the softmax of one takes no longer than the products of the other.
 #include <math.h>
 
+#include <algorithm>
+
 #include "kernels.h"
 
 namespace {
 
 constexpr int THREADS = 384;
 constexpr int KT = 128;  // keys per step
+constexpr int MIN_STEPS = 2;         // steps of a CTA at least, where an item is split
 constexpr float LAG = 4.f;          // how far a maximum that is looked at may exceed m (log2)
 constexpr float SUM_MAX = 16384.f;  // largest sum of a row's 128 probabilities
 
@@ -107,6 +110,26 @@ AXON_DEV void st_global32(void* at, const uint32_t* v) {
   asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
                "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
                : "memory");
+}
+AXON_DEV void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// Shared memory of CTA `rank` of the cluster, at the address that it has here.
+AXON_DEV float ld_cluster(uint32_t at, int rank) {
+  float v;
+  asm volatile("{\n .reg .b32 a;\n mapa.shared::cluster.u32 a, %1, %2;\n ld.shared::cluster.f32 %0, [a];\n}"
+               : "=f"(v)
+               : "r"(at), "r"(rank)
+               : "memory");
+  return v;
+}
+AXON_DEV float4 ld_cluster4(uint32_t at, int rank) {
+  float4 v;
+  asm volatile("{\n .reg .b32 a;\n mapa.shared::cluster.u32 a, %4, %5;\n ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [a];\n}"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "r"(at), "r"(rank)
+               : "memory");
+  return v;
 }
 AXON_DEV bool elect_one() {
   uint32_t r;
@@ -221,14 +244,18 @@ AXON_DEV Item find_item(const ChunkArgs& p, int PC, long long item) {
   return r;
 }
 
-// Which blocks an item's tiles see: `ns` blocks of sinks, then those from `jlo` on; nb[w]
-// of them reach tile w.
+// Which blocks an item's tiles see: `ns` blocks of sinks, then those from `jlo` on. This CTA
+// takes them from number `base` on, nb(w) of them for tile w; clears(w): among them is the block with
+// the last token, and slots after it.
 struct Span {
-  int nw, jlo, ns, pend;
-  int nb[2];
-  AXON_DEV int steps(int w) const { return (nb[w] + 7) >> 3; }
+  int nw, jlo, ns, pend, base;
+  int nb0, nb1;
+  bool clears0, clears1;
+  AXON_DEV int nb(int w) const { return w ? nb1 : nb0; }
+  AXON_DEV bool clears(int w) const { return w ? clears1 : clears0; }
+  AXON_DEV int steps(int w) const { return (nb(w) + 7) >> 3; }
 };
-AXON_DEV Span span_of(const ChunkArgs& p, const Item& it, int PW) {
+AXON_DEV Span span_of(const ChunkArgs& p, const Item& it, int PW, int part, int parts) {
   Span s;
   s.nw = it.p0 + PW < it.S ? 2 : 1;
   const int first = it.past + it.p0;
@@ -236,15 +263,24 @@ AXON_DEV Span span_of(const ChunkArgs& p, const Item& it, int PW) {
   s.ns = min((p.sinks + 15) >> 4, s.jlo);
   s.pend = it.past + min(it.p0 + s.nw * PW, it.S);
   const int pend0 = it.past + min(it.p0 + PW, it.S);
-  s.nb[0] = s.ns + ((pend0 + 15) >> 4) - s.jlo;
-  s.nb[1] = s.ns + ((s.pend + 15) >> 4) - s.jlo;
+  const int n0 = s.ns + ((pend0 + 15) >> 4) - s.jlo, n1 = s.ns + ((s.pend + 15) >> 4) - s.jlo;
+  const int all = s.nw == 2 ? n1 : n0, steps = (all + 7) >> 3;
+  s.base = 8 * (steps * part / parts);
+  const int end = min(all, 8 * (steps * (part + 1) / parts));
+  const bool last = (s.pend & 15) && end == all && end > s.base;
+  s.clears0 = last && n0 == all;
+  s.clears1 = last && n1 == all;
+  s.nb0 = max(0, min(n0, end) - s.base);
+  s.nb1 = max(0, min(n1, end) - s.base);
   return s;
 }
 
-template <int HD, typename T16>
+// SPLIT: a cluster of CTAs shares one item, each with a part of its keys, and joins their
+// states through distributed shared memory.
+template <int HD, typename T16, bool SPLIT>
 __global__ void __launch_bounds__(THREADS, 1)
     attn_chunk_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
-                      const __grid_constant__ CUtensorMap tmV, const ChunkArgs p, int PW, int pool_rows) {
+                      const __grid_constant__ CUtensorMap tmV, const ChunkArgs p, int PW, int pool_rows, int parts) {
   using C = KCfg<HD>;
   constexpr int NS = C::STAGES;
   extern __shared__ uint8_t smem_raw[];
@@ -267,6 +303,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   const uint32_t tmem_slot = items + 64;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int HPG = p.H / p.G;
+  const int part = SPLIT ? static_cast<int>(blockIdx.x) % parts : 0;
 
   grid_dep_launch();
   if (threadIdx.x == 0) {
@@ -327,7 +364,8 @@ __global__ void __launch_bounds__(THREADS, 1)
       for (int k = 0;; ++k) {
         // there and back over the CTAs, since items get shorter along a sequence
         const unsigned at = k & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
-        const Item it = find_item(p, 2 * PW, at + static_cast<long long>(k) * gridDim.x);
+        Item it = find_item(p, 2 * PW, SPLIT ? blockIdx.x / parts : at + static_cast<long long>(k) * gridDim.x);
+        if (SPLIT && k > 0) it.b = -1;
         if (!__all_sync(0xffffffffu, wait_bar(item_empty(k & 1), ((k >> 1) & 1) ^ 1, p.err))) break;
         if (lane == 0) {
           int* d = reinterpret_cast<int*>(smem_raw + (items - raw) + 32 * (k & 1));
@@ -349,8 +387,9 @@ __global__ void __launch_bounds__(THREADS, 1)
       for (int k = 0; ok; ++k) {
         const Item item = take_item(k);
         if (item.b < 0) break;
-        const Span sp = span_of(p, item, PW);
+        const Span sp = span_of(p, item, PW, part, SPLIT ? parts : 1);
         for (int w = 0; w < sp.nw; ++w) {
+          if (SPLIT && !sp.nb(w)) continue;
           ok = __all_sync(0xffffffffu, wait_bar(q_empty(w), (iq[w] & 1) ^ 1, p.err));
           if (!ok) break;
           if (lane == 0) {
@@ -361,13 +400,14 @@ __global__ void __launch_bounds__(THREADS, 1)
           }
           ++iq[w];
         }
-        const int nb = sp.nb[sp.nw - 1], nt = (nb + 7) >> 3;
+        const int nb = sp.nb(sp.nw - 1), nt = (nb + 7) >> 3;
         // pool row of this lane's block of step t; past the last block and for table entries
         // out of range (reported) the row lies outside the pool, where a box reads zeros
         auto pool_row = [&](int t) {
           const int i = t * 8 + lane;
           if (lane >= 8 || t >= nt || i >= nb) return pool_rows;
-          const int j = i < sp.ns ? i : i - sp.ns + sp.jlo;
+          const int x = i + sp.base;
+          const int j = x < sp.ns ? x : x - sp.ns + sp.jlo;
           const int blk = p.block_table ? p.block_table[static_cast<long long>(item.b) * p.blocks_per_seq + j]
                                         : item.b * p.blocks_per_seq + j;
           if (blk < 0 || blk >= p.num_blocks) {
@@ -441,9 +481,10 @@ __global__ void __launch_bounds__(THREADS, 1)
       auto same = [&](int v) { return __shfl_sync(0xffffffffu, v, 0); };
       Item item = take_item(0);
       for (int k = 0; same(item.b) >= 0; ++k) {
-        const Span sp = span_of(p, item, PW);
-        const int nb = same(w < sp.nw ? sp.nb[w] : 0), nt = (nb + 7) >> 3;  // of this tile
+        const Span sp = span_of(p, item, PW, part, SPLIT ? parts : 1);
+        const int nb = same(w < sp.nw ? sp.nb(w) : 0), nt = (nb + 7) >> 3;  // of this tile
         const int nt_all = same(sp.steps(sp.nw - 1));
+        if (SPLIT && !nt_all) break;  // no keys for this CTA
         bool ok = wait_all(kv_full(st), ph) && (!nt || wait_all(q_full(w), ph_q)) && my_turn();
         if (!ok) break;
         tc_fence_after();
@@ -515,9 +556,9 @@ __global__ void __launch_bounds__(THREADS, 1)
     for (int k = 0; ok; ++k) {
       const Item item = take_item(k);
       if (item.b < 0) break;
-      const Span sp = span_of(p, item, PW);
+      const Span sp = span_of(p, item, PW, part, SPLIT ? parts : 1);
       const int nt_all = sp.steps(sp.nw - 1);
-      if (w >= sp.nw) {
+      if (!SPLIT && w >= sp.nw) {
         it += 2 * nt_all;
         continue;
       }
@@ -525,15 +566,13 @@ __global__ void __launch_bounds__(THREADS, 1)
       const bool valid = i < HPG * PW && ip < item.S;
       const int pos = valid ? item.past + ip : -1;
       const int lo = (p.window > 0 && pos >= p.window) ? pos - p.window + 1 : 0;
-      const int nt = sp.steps(w);
-      // a tile that reads the block with the last token clears what follows it before its product
-      const bool clears = (sp.pend & 15) && sp.nb[w] == sp.nb[sp.nw - 1];
+      const int nt = w < sp.nw ? sp.steps(w) : 0;
       float m = valid ? -INFINITY : 0.f;
       uint64_t l2 = pk2(0.f, 0.f);
       for (int t = 0; t < nt; ++t) {
-        const int tok0 = (sp.jlo - sp.ns + t * 8) * 16;  // token of column 0, of steps past the sinks
+        const int tok0 = (sp.jlo - sp.ns + sp.base + t * 8) * 16;  // token of column 0, of steps past the sinks
         // padding rows reach no output: they alone never ask for it
-        bool look = __any_sync(0xffffffffu, valid && (t * 8 < sp.ns || tok0 + KT - 1 > pos || tok0 < lo || m == -INFINITY));
+        bool look = __any_sync(0xffffffffu, valid && (sp.base + t * 8 < sp.ns || tok0 + KT - 1 > pos || tok0 < lo || m == -INFINITY));
         ok = __all_sync(0xffffffffu, wait_bar(s_full(w), ns_ & 1, p.err));
         if (!ok) break;
         ++ns_;
@@ -555,7 +594,7 @@ __global__ void __launch_bounds__(THREADS, 1)
               if (!round) {
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                  const int blk = t * 8 + c / 16 + x, at = blk < sp.ns ? blk * 16 : tok0 + c + x * 16;
+                  const int blk = sp.base + t * 8 + c / 16 + x, at = blk < sp.ns ? blk * 16 : tok0 + c + x * 16;
                   const uint32_t see = bits16(at, lo, pos + 1) | bits16(at, 0, min(p.sinks, pos + 1));
 #pragma unroll
                   for (int u = 0; u < 16; ++u) s[x * 16 + u] = (see >> u) & 1 ? s[x * 16 + u] : -INFINITY;
@@ -621,11 +660,12 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         st32(tS, pr);
         st32(tS + 32, pr + 32);
-        if (clears && t == nt - 1) {
+        // the slots past the last token, before the product reads them
+        if (sp.clears(w) && t == nt - 1) {
           const int iv = it + 2 * t + 1, sv = iv % NS;
           ok = __all_sync(0xffffffffu, wait_bar(kv_full(sv), (iv / NS) & 1, p.err));
           if (!ok) break;
-          const int end = min(8, sp.nb[w] - 8 * t) * 16, first = end - 16 + (sp.pend & 15);
+          const int end = min(8, sp.nb(w) - 8 * t) * 16, first = end - 16 + (sp.pend & 15);
           for (int x = i; x < (end - first) * C::CH * 8; x += 128) {
             const int row = first + x / (C::CH * 8), piece = x % (C::CH * 8);
             *reinterpret_cast<uint4*>(smem_raw + (sKV - raw) + sv * C::TILE + (piece >> 3) * C::CHUNK + row * 128 +
@@ -639,6 +679,34 @@ __global__ void __launch_bounds__(THREADS, 1)
         l2 = add2(l2, sum[0]);
       }
       it += 2 * nt_all;
+      if (SPLIT) {
+        // the row's state into the stages that the keys and values no longer need
+        if (nt && ok) ok = __all_sync(0xffffffffu, wait_bar(o_full(w), 0, p.err));
+        tc_fence_after();
+        asm volatile("barrier.cta.sync 1, 256;" ::: "memory");  // both tiles' products are done
+        float la, lb;
+        upk2(l2, la, lb);
+        float* const stats = reinterpret_cast<float*>(smem_raw + (sKV - raw)) + (w * 128 + i) * 2;
+        stats[0] = nt && ok ? m : -INFINITY;
+        stats[1] = nt && ok ? la + lb : 0.f;
+        // 16-byte pieces exchanged within the row, so that a warp's 32 rows fall on all banks
+        uint4* const mine = reinterpret_cast<uint4*>(smem_raw + (sKV - raw) + 2048) + (w * 128 + i) * (HD / 4);
+#pragma unroll 1
+        for (int c = 0; c < HD; c += 32) {
+          uint32_t o[32];
+          if (nt && ok) {
+            ld32(tO + c, o);
+            tmem_wait_ld();
+          } else {
+#pragma unroll
+            for (int u = 0; u < 32; ++u) o[u] = 0;
+          }
+#pragma unroll
+          for (int u = 0; u < 8; ++u)
+            mine[(c / 4 + u) ^ (i & (HD / 4 - 1))] = make_uint4(o[4 * u], o[4 * u + 1], o[4 * u + 2], o[4 * u + 3]);
+        }
+        break;
+      }
       if (!ok) break;
       ok = __all_sync(0xffffffffu, wait_bar(o_full(w), no & 1, p.err));
       if (!ok) break;
@@ -678,6 +746,48 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
     }
   }
+  if (SPLIT) {
+    // each CTA of the cluster joins a share of the 256 rows (those without an item have nothing in
+    // the stages and write nothing)
+    __syncwarp();
+    cluster_sync();
+    const int* d = reinterpret_cast<const int*>(smem_raw + (items - raw));
+    if (warp < 8 && d[0] >= 0) {
+      const int rows = 256 / parts;        // 32 .. 128: a row per 256 / rows threads
+      const int per = 256 / rows, R = part * rows + threadIdx.x / per;
+      const int w = R >> 7, i = R & 127, pl = i / HPG, h = i - pl * HPG, ip = d[2] + w * PW + pl;
+      if (i < HPG * PW && ip < d[4]) {
+        float M = -INFINITY, L = 0.f, f[8];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          f[x] = -INFINITY;
+          if (x < parts) f[x] = ld_cluster(sKV + (w * 128 + i) * 8, x);
+          M = fmaxf(M, f[x]);
+        }
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          f[x] = M == -INFINITY ? 0.f : ex2(f[x] - M);
+          if (x < parts) L += f[x] * ld_cluster(sKV + (w * 128 + i) * 8 + 4, x);
+        }
+        const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
+        T16* const dst = static_cast<T16*>(p.o) + (static_cast<long long>(d[3]) + ip) * p.o_row + (d[1] * HPG + h) * p.o_head;
+        for (int c = threadIdx.x % per; c < HD / 4; c += per) {
+          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+          const uint32_t at = sKV + 2048 + ((w * 128 + i) * (HD / 4) + (c ^ (i & (HD / 4 - 1)))) * 16;
+#pragma unroll
+          for (int x = 0; x < 8; ++x) {
+            if (x < parts) {
+              const float4 e = ld_cluster4(at, x);
+              v = make_float4(v.x + f[x] * e.x, v.y + f[x] * e.y, v.z + f[x] * e.z, v.w + f[x] * e.w);
+            }
+          }
+          *reinterpret_cast<uint2*>(dst + c * 4) = make_uint2(pack2<T16>(v.x * inv, v.y * inv), pack2<T16>(v.z * inv, v.w * inv));
+        }
+      }
+    }
+    __syncwarp();
+    cluster_sync();  // nobody's shared memory goes away while another reads it
+  }
   tc_fence_before();
   __syncthreads();
   if (warp == 9) {
@@ -688,22 +798,44 @@ __global__ void __launch_bounds__(THREADS, 1)
 
 template <int HD, typename T16>
 cudaError_t prepare_hd() {
-  return cudaFuncSetAttribute(attn_chunk_kernel<HD, T16>, cudaFuncAttributeMaxDynamicSharedMemorySize, KCfg<HD>::SMEM);
+  const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  const cudaError_t e = cudaFuncSetAttribute(attn_chunk_kernel<HD, T16, false>, attr, KCfg<HD>::SMEM);
+  return e == cudaSuccess ? cudaFuncSetAttribute(attn_chunk_kernel<HD, T16, true>, attr, KCfg<HD>::SMEM) : e;
+}
+
+// CTAs that share an item: as many as leave none without an SM, where each has two steps
+// of keys at least for the longest row that the table allows.
+int parts_for(const ChunkArgs& a, int PC, int num_sms) {
+  const long long items = (static_cast<long long>(a.T) / PC + a.B) * a.G;  // at most
+  long long keys = a.blocks_per_seq * 16ll;
+  if (a.window > 0) keys = std::min(keys, a.window + PC + a.sinks + 0ll);
+  int parts = 1;
+  while (parts < 8 && items * parts * 2 <= num_sms && keys >= parts * 2 * MIN_STEPS * KT) parts *= 2;
+  return parts;
 }
 
 template <int HD, typename T16>
 cudaError_t launch_hd(const LaunchCtx& lc, const ChunkArgs& a, const AttnMaps& maps) {
   const int PW = attn_tile_positions(a.H, a.G), PC = 2 * PW;
   const long long items = (static_cast<long long>(a.T) / PC + a.B) * a.G;  // at most
+  const int parts = parts_for(a, PC, lc.num_sms);
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(items < lc.num_sms ? items : lc.num_sms));
   cfg.blockDim = dim3(THREADS);
   cfg.dynamicSmemBytes = KCfg<HD>::SMEM;
   cfg.stream = lc.stream;
-  cudaLaunchAttribute attr[2];
-  cfg.numAttrs = chain_attrs(lc, attr);
+  cudaLaunchAttribute chain[2], attr[3];
+  cfg.numAttrs = chain_attrs(lc, chain);
+  for (unsigned i = 0; i < cfg.numAttrs; ++i) attr[i] = chain[i];
   cfg.attrs = attr;
-  return cudaLaunchKernelEx(&cfg, attn_chunk_kernel<HD, T16>, maps.q, maps.k, maps.v, a, PW, maps.pool_rows);
+  if (parts > 1) {
+    attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+    attr[cfg.numAttrs].val.clusterDim = {static_cast<unsigned>(parts), 1, 1};
+    ++cfg.numAttrs;
+    cfg.gridDim = dim3(static_cast<unsigned>(items) * parts);
+    return cudaLaunchKernelEx(&cfg, attn_chunk_kernel<HD, T16, true>, maps.q, maps.k, maps.v, a, PW, maps.pool_rows, parts);
+  }
+  cfg.gridDim = dim3(static_cast<unsigned>(items < lc.num_sms ? items : lc.num_sms));
+  return cudaLaunchKernelEx(&cfg, attn_chunk_kernel<HD, T16, false>, maps.q, maps.k, maps.v, a, PW, maps.pool_rows, 1);
 }
 
 }  // namespace

@@ -33,6 +33,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "kernels.h"
 
@@ -40,7 +41,6 @@ namespace {
 
 constexpr int THREADS = 384;
 constexpr int KT = 128;  // keys per step
-constexpr int MIN_STEPS = 2;         // steps of a CTA at least, where an item is split
 constexpr float LAG = 4.f;          // how far a maximum that is looked at may exceed m (log2)
 constexpr float SUM_MAX = 16384.f;  // largest sum of a row's 128 probabilities
 
@@ -244,11 +244,20 @@ AXON_DEV Item find_item(const ChunkArgs& p, int PC, long long item) {
   return r;
 }
 
+// Into how many parts an item of `steps` key steps is split by a cluster of `parts` CTAs. A
+// step takes 1.3 us and joining the parts 6 us (8B width): 16 rows after 1000 cached tokens, 8
+// steps, unsplit / 2 / 4 parts 15.9 / 16.5 / 13.4 us; after 500, 12.4 / 15.7; after 2000 (8
+// parts) 26.0 / 15.5; 120 rows after 2000 31.1 / 20.2 (4 parts).
+__host__ __device__ inline int split_of(int steps, int parts) {
+  while (parts > 1 && steps < (parts == 2 ? 10 : 2 * parts)) parts >>= 1;
+  return parts;
+}
+
 // Which blocks an item's tiles see: `ns` blocks of sinks, then those from `jlo` on. This CTA
 // takes them from number `base` on, nb(w) of them for tile w; clears(w): among them is the block with
 // the last token, and slots after it.
 struct Span {
-  int nw, jlo, ns, pend, base;
+  int nw, jlo, ns, pend, base, parts;  // parts: how many CTAs have a share
   int nb0, nb1;
   bool clears0, clears1;
   AXON_DEV int nb(int w) const { return w ? nb1 : nb0; }
@@ -265,8 +274,9 @@ AXON_DEV Span span_of(const ChunkArgs& p, const Item& it, int PW, int part, int 
   const int pend0 = it.past + min(it.p0 + PW, it.S);
   const int n0 = s.ns + ((pend0 + 15) >> 4) - s.jlo, n1 = s.ns + ((s.pend + 15) >> 4) - s.jlo;
   const int all = s.nw == 2 ? n1 : n0, steps = (all + 7) >> 3;
-  s.base = 8 * (steps * part / parts);
-  const int end = min(all, 8 * (steps * (part + 1) / parts));
+  s.parts = split_of(steps, parts);
+  s.base = part < s.parts ? 8 * (steps * part / s.parts) : all;
+  const int end = part < s.parts ? min(all, 8 * (steps * (part + 1) / s.parts)) : all;
   const bool last = (s.pend & 15) && end == all && end > s.base;
   s.clears0 = last && n0 == all;
   s.clears1 = last && n1 == all;
@@ -389,7 +399,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (item.b < 0) break;
         const Span sp = span_of(p, item, PW, part, SPLIT ? parts : 1);
         for (int w = 0; w < sp.nw; ++w) {
-          if (SPLIT && !sp.nb(w)) continue;
+          if (!sp.nb(w)) continue;
           ok = __all_sync(0xffffffffu, wait_bar(q_empty(w), (iq[w] & 1) ^ 1, p.err));
           if (!ok) break;
           if (lane == 0) {
@@ -484,7 +494,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         const Span sp = span_of(p, item, PW, part, SPLIT ? parts : 1);
         const int nb = same(w < sp.nw ? sp.nb(w) : 0), nt = (nb + 7) >> 3;  // of this tile
         const int nt_all = same(sp.steps(sp.nw - 1));
-        if (SPLIT && !nt_all) break;  // no keys for this CTA
+        if (!nt_all) break;  // a CTA of a cluster without a share
         bool ok = wait_all(kv_full(st), ph) && (!nt || wait_all(q_full(w), ph_q)) && my_turn();
         if (!ok) break;
         tc_fence_after();
@@ -558,7 +568,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       if (item.b < 0) break;
       const Span sp = span_of(p, item, PW, part, SPLIT ? parts : 1);
       const int nt_all = sp.steps(sp.nw - 1);
-      if (!SPLIT && w >= sp.nw) {
+      if (sp.parts == 1 && (w >= sp.nw || !nt_all)) {
         it += 2 * nt_all;
         continue;
       }
@@ -679,7 +689,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         l2 = add2(l2, sum[0]);
       }
       it += 2 * nt_all;
-      if (SPLIT) {
+      if (SPLIT && sp.parts > 1) {
         // the row's state into the stages that the keys and values no longer need
         if (nt && ok) ok = __all_sync(0xffffffffu, wait_bar(o_full(w), 0, p.err));
         tc_fence_after();
@@ -746,14 +756,16 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
     }
   }
-  if (SPLIT) {
-    // each CTA of the cluster joins a share of the 256 rows (those without an item have nothing in
-    // the stages and write nothing)
+  // whether the cluster shares its item is the same for all of its CTAs and threads
+  const int* const d = reinterpret_cast<const int*>(smem_raw + (items - raw));
+  if (SPLIT) __syncthreads();  // the item's descriptor
+  const int shares = SPLIT && d[0] >= 0 ? span_of(p, Item{d[0], d[1], d[2], d[3], d[4], d[5]}, PW, part, parts).parts : 1;
+  if (SPLIT && shares > 1) {
+    // each of its CTAs joins a share of the 256 rows
     __syncwarp();
     cluster_sync();
-    const int* d = reinterpret_cast<const int*>(smem_raw + (items - raw));
-    if (warp < 8 && d[0] >= 0) {
-      const int rows = 256 / parts;        // 32 .. 128: a row per 256 / rows threads
+    if (warp < 8 && part < shares) {
+      const int rows = 256 / shares;       // 32 .. 128: a row per 256 / rows threads
       const int per = 256 / rows, R = part * rows + threadIdx.x / per;
       const int w = R >> 7, i = R & 127, pl = i / HPG, h = i - pl * HPG, ip = d[2] + w * PW + pl;
       if (i < HPG * PW && ip < d[4]) {
@@ -761,13 +773,13 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
         for (int x = 0; x < 8; ++x) {
           f[x] = -INFINITY;
-          if (x < parts) f[x] = ld_cluster(sKV + (w * 128 + i) * 8, x);
+          if (x < shares) f[x] = ld_cluster(sKV + (w * 128 + i) * 8, x);
           M = fmaxf(M, f[x]);
         }
 #pragma unroll
         for (int x = 0; x < 8; ++x) {
           f[x] = M == -INFINITY ? 0.f : ex2(f[x] - M);
-          if (x < parts) L += f[x] * ld_cluster(sKV + (w * 128 + i) * 8 + 4, x);
+          if (x < shares) L += f[x] * ld_cluster(sKV + (w * 128 + i) * 8 + 4, x);
         }
         const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
         T16* const dst = static_cast<T16*>(p.o) + (static_cast<long long>(d[3]) + ip) * p.o_row + (d[1] * HPG + h) * p.o_head;
@@ -776,7 +788,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           const uint32_t at = sKV + 2048 + ((w * 128 + i) * (HD / 4) + (c ^ (i & (HD / 4 - 1)))) * 16;
 #pragma unroll
           for (int x = 0; x < 8; ++x) {
-            if (x < parts) {
+            if (x < shares) {
               const float4 e = ld_cluster4(at, x);
               v = make_float4(v.x + f[x] * e.x, v.y + f[x] * e.y, v.z + f[x] * e.z, v.w + f[x] * e.w);
             }
@@ -803,22 +815,49 @@ cudaError_t prepare_hd() {
   return e == cudaSuccess ? cudaFuncSetAttribute(attn_chunk_kernel<HD, T16, true>, attr, KCfg<HD>::SMEM) : e;
 }
 
-// CTAs that share an item: as many as leave none without an SM, where each has two steps
-// of keys at least for the longest row that the table allows.
-int parts_for(const ChunkArgs& a, int PC, int num_sms) {
-  const long long items = (static_cast<long long>(a.T) / PC + a.B) * a.G;  // at most
+// Clusters of 2, 4 and 8 CTAs that run at the same time (a GPC's SMs are no multiple of
+// eight), by device.
+std::atomic<int> g_clusters[64][4];
+
+template <int HD, typename T16>
+cudaError_t count_clusters() {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  for (int i = 1; i < 4 && e == cudaSuccess; ++i) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim = {1u << i, 1, 1};
+    cfg.gridDim = dim3(1u << i);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = KCfg<HD>::SMEM;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    e = cudaOccupancyMaxActiveClusters(&n, attn_chunk_kernel<HD, T16, true>, &cfg);
+    g_clusters[dev & 63][i].store(n, std::memory_order_relaxed);
+  }
+  return e;
+}
+
+// CTAs that share an item: the most whose clusters all run at once, for the longest row that
+// the table allows (a shorter one is split less, on the device).
+int parts_for(const ChunkArgs& a, long long items, int PC) {
   long long keys = a.blocks_per_seq * 16ll;
   if (a.window > 0) keys = std::min(keys, a.window + PC + a.sinks + 0ll);
-  int parts = 1;
-  while (parts < 8 && items * parts * 2 <= num_sms && keys >= parts * 2 * MIN_STEPS * KT) parts *= 2;
-  return parts;
+  const int steps = static_cast<int>(std::min((keys + KT - 1) / KT, 1ll << 20));
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return 1;
+  for (int i = 3; i > 0; --i)
+    if (items <= g_clusters[dev & 63][i].load(std::memory_order_relaxed) && split_of(steps, 1 << i) == 1 << i) return 1 << i;
+  return 1;
 }
 
 template <int HD, typename T16>
 cudaError_t launch_hd(const LaunchCtx& lc, const ChunkArgs& a, const AttnMaps& maps) {
   const int PW = attn_tile_positions(a.H, a.G), PC = 2 * PW;
   const long long items = (static_cast<long long>(a.T) / PC + a.B) * a.G;  // at most
-  const int parts = parts_for(a, PC, lc.num_sms);
+  const int parts = parts_for(a, items, PC);
   cudaLaunchConfig_t cfg = {};
   cfg.blockDim = dim3(THREADS);
   cfg.dynamicSmemBytes = KCfg<HD>::SMEM;
@@ -845,6 +884,7 @@ cudaError_t prepare_attn_chunk_kernels() {
   if (e == cudaSuccess) e = prepare_hd<64, f16>();
   if (e == cudaSuccess) e = prepare_hd<128, bf16>();
   if (e == cudaSuccess) e = prepare_hd<128, f16>();
+  if (e == cudaSuccess) e = count_clusters<128, f16>();  // (all of them hold a whole SM per CTA)
   return e;
 }
 

@@ -262,6 +262,41 @@ def test_prefill_long_context_behind_a_short_chunk(ax):
     check_prefill(ax, Case(8, 1, 128, "bf16", [2000, 1500], [5, 30], 600, 20, seed=2))
 
 
+@pytest.mark.parametrize("past,new", [([1030], [3]), ([1300, 900], [17, 40]), ([2040, 5, 1100], [9, 30, 1]), ([4000], [100]),
+                                      ([3000, 1279], [1, 1])])
+@pytest.mark.parametrize("H,G,d,window,sinks", [(8, 2, 128, 0, 0), (9, 3, 64, 0, 0), (14, 2, 64, 1500, 20), (5, 5, 128, 2500, 3)])
+def test_prefill_few_rows_behind_long_contexts(ax, past, new, H, G, d, window, sinks):
+    """Items that a cluster of 2, 4 or 8 CTAs shares, beside ones that are too short for it."""
+    check_prefill(ax, Case(H, G, d, "fp16", past, new, window, sinks, seed=sum(past)))
+
+
+def test_prefill_short_rows_in_a_wide_table(ax):
+    check_prefill(ax, Case(8, 2, 64, "bf16", [0, 60, 1200], [20, 1, 5], 0, 0, seed=3, per=400))
+
+
+def test_prefill_is_the_same_every_time(ax):
+    c = Case(8, 2, 128, "bf16", [2500, 1100], [30, 9], 0, 0, seed=9)
+    a = check_prefill(ax, c)
+    for _ in range(3):
+        assert torch.equal(a, check_prefill(ax, c))
+
+
+def test_prefill_shows_a_score_far_above_the_first_ones(ax):
+    """The bound of a row's scores comes from its first step: later keys that exceed it by hundreds have to raise it."""
+    for past, new in (([0], [700]), ([1800], [4])):
+        c = Case(4, 2, 128, "fp16", past, new, 0, 0, seed=5)
+        for b, t in ((0, 200), (0, 201), (0, past[0] + new[0] - 2)):
+            blk = int(c.table[b, t // 16])
+            c.k[1, blk, :, t % 16] *= 40.0
+            c.keys[b][t] = c.k[1, blk, :, t % 16].double().cpu().numpy()
+        out = torch.full_like(c.q, float("nan"))
+        cache = ax.make_kv_cache(c.k, c.v)
+        ax.axon_attn_prefill(cache, 1, c.q, c.cu, c.ctx, max(c.new), out, block_table=c.bt, err=c.err)
+        # scores of up to 40 * 30: off by 40 times as much, where neighbours are that close
+        close(out, c.reference()[0], 40 * c.vmax(), ULP["fp16"], PROB["fp16"] / 40)
+        assert ax.axon_check_error(c.err) == (0, 0)
+
+
 def test_prefill_contiguous_rows(ax):
     check_prefill(ax, Case(4, 2, 64, "bf16", [10, 0], [30, 64], 20, 1, seed=6, paged=False))
 

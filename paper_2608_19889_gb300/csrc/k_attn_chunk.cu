@@ -592,33 +592,36 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll 1
         for (int round = 0; round < 2; ++round) {
           if (look) {
-            // hidden scores to -inf (written back), the step's maximum, and m raised to it where it is far
-            // below: a rolled loop, for the few steps that need it
+            // Hidden scores to -inf (written back), and m raised to the step's maximum where it is far
+            // below: a rolled loop over 32 columns, for the few steps that need it. Columns without a
+            // mask are passed over once every row has a bound (a first step takes it from the first keys
+            // that each row sees; should later ones exceed it by far, the sum tells).
             float mx = -INFINITY;
 #pragma unroll 1
-            for (int c = 0; c < KT; c += 64) {
-              float s[64];
+            for (int c = 0; c < KT; c += 32) {
+              uint32_t see = 0;
+#pragma unroll
+              for (int x = 0; x < 2; ++x) {
+                const int blk = sp.base + t * 8 + c / 16 + x, at = blk < sp.ns ? blk * 16 : tok0 + c + x * 16;
+                see |= (bits16(at, lo, pos + 1) | bits16(at, 0, min(p.sinks, pos + 1))) << (16 * x);
+              }
+              const bool mask = !round && __any_sync(0xffffffffu, valid && see != 0xffffffffu);
+              if (!mask && !round && !__any_sync(0xffffffffu, fmaxf(m, mx) == -INFINITY)) continue;
+              float s[32];
               ld32(tS + c, reinterpret_cast<uint32_t*>(s));
-              ld32(tS + c + 32, reinterpret_cast<uint32_t*>(s) + 32);
               tmem_wait_ld();
-              if (!round) {
+              if (mask) {
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                  const int blk = sp.base + t * 8 + c / 16 + x, at = blk < sp.ns ? blk * 16 : tok0 + c + x * 16;
-                  const uint32_t see = bits16(at, lo, pos + 1) | bits16(at, 0, min(p.sinks, pos + 1));
-#pragma unroll
-                  for (int u = 0; u < 16; ++u) s[x * 16 + u] = (see >> u) & 1 ? s[x * 16 + u] : -INFINITY;
-                }
+                for (int u = 0; u < 32; ++u) s[u] = (see >> u) & 1 ? s[u] : -INFINITY;
                 st32(tS + c, reinterpret_cast<uint32_t*>(s));
-                st32(tS + c + 32, reinterpret_cast<uint32_t*>(s) + 32);
               }
               float m4[4] = {mx, s[0], s[1], s[2]};
 #pragma unroll
-              for (int u = 3; u < 59; u += 8) {
+              for (int u = 3; u < 27; u += 8) {
 #pragma unroll
                 for (int y = 0; y < 4; ++y) m4[y] = max3(m4[y], s[u + y], s[u + 4 + y]);
               }
-              mx = max3(max3(m4[0], s[59], s[60]), max3(m4[1], s[61], s[62]), max3(m4[2], m4[3], s[63]));
+              mx = max3(max3(m4[0], s[27], s[28]), max3(m4[1], s[29], s[30]), max3(m4[2], m4[3], s[31]));
             }
             wait_st();
             const float mt = mx * sl2;
@@ -665,7 +668,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           sum[0] = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
           float sa, sb;
           upk2(sum[0], sa, sb);
-          if (look || !__any_sync(0xffffffffu, valid && !(sa + sb <= SUM_MAX))) break;
+          if (round || !__any_sync(0xffffffffu, valid && !(sa + sb <= SUM_MAX))) break;
           look = true;  // a score far above m: raise it and take the step again
         }
         st32(tS, pr);

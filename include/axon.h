@@ -440,8 +440,10 @@ int axon_attn_decode_workspace(const axon_kv_cache* cache, int32_t num_heads, in
  * d_q and d_out (T rows in all; a chunk may be empty), its row i stands at
  * position context_lens[b] + i, and the chunk's keys and values are in the
  * cache already. max_chunk bounds the longest chunk. context_lens is not
- * advanced. Slots past a row's last token never reach an output, whatever they
- * hold; a later token of the same chunk that is not finite may reach earlier rows. */
+ * advanced. num_blocks * num_kv_heads * 16 stays below 2^31. Slots past a chunk's
+ * last token never reach an output, whatever they hold. Tokens that the mask hides
+ * from some rows only (later ones of the chunk, ones before a window in a block that it
+ * reaches) have to be finite: the products add zero times their values. */
 int axon_attn_prefill(const axon_kv_cache* cache, int32_t layer, const void* d_q, int64_t q_row_stride,
                       int64_t q_head_stride, int32_t B, int32_t T, int32_t num_heads, const int32_t* d_cu_seqlens,
                       const int32_t* d_context_lens, int32_t max_chunk, const int32_t* d_block_table,

@@ -1213,6 +1213,7 @@ int axon_model_create(const axon_config* cfg, const axon_tensor* weights, int32_
   if (rc) return rc;
   axon_model* m = new axon_model();
   m->cfg = *cfg;
+  m->cfg.sink_tokens = std::min(cfg->sink_tokens, cfg->max_context);  // (kernels round them up to blocks)
   if (m->cfg.max_prefill_tokens <= 0) m->cfg.max_prefill_tokens = cfg->max_batch * cfg->max_context;
   m->L = cfg->num_hidden_layers;
   m->D = cfg->hidden_size;

@@ -378,9 +378,12 @@ __global__ void __launch_bounds__(THREADS, 1)
   // (or a wait ran out).
   auto take_item = [&](int k) {
     Item it;
-    const bool ok = __all_sync(0xffffffffu, wait_bar(item_full(k & 1), (k >> 1) & 1, p.err));
     it.b = -1;
-    if (!ok) return it;
+    if (SPLIT) {
+      if (k > 0) return it;  // the cluster's one item, found before the roles part
+    } else if (!__all_sync(0xffffffffu, wait_bar(item_full(k & 1), (k >> 1) & 1, p.err))) {
+      return it;
+    }
     const int* d = reinterpret_cast<const int*>(smem_raw + (items - raw) + 32 * (k & 1));
     it.b = d[0];
     it.g = d[1];
@@ -389,28 +392,38 @@ __global__ void __launch_bounds__(THREADS, 1)
     it.S = d[4];
     it.past = d[5];
     __syncwarp();
-    if (lane == 0) mbar_arrive(item_empty(k & 1));
+    if (!SPLIT && lane == 0) mbar_arrive(item_empty(k & 1));
     return it;
   };
+  auto put_item = [&](int k, const Item& it) {
+    int* d = reinterpret_cast<int*>(smem_raw + (items - raw) + 32 * (k & 1));
+    d[0] = it.b;
+    d[1] = it.g;
+    d[2] = it.p0;
+    d[3] = it.row0;
+    d[4] = it.S;
+    d[5] = it.past;
+  };
+  if (SPLIT) {
+    // every thread knows it, without a wait that could run out: they meet at barriers
+    if (warp == 10) {
+      const Item it = find_item(p, 2 * PW, blockIdx.x / parts);
+      if (lane == 0) put_item(0, it);
+    }
+    __syncthreads();
+  }
 
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == 10) {
       // -------------------------------------------------------------- items
-      for (int k = 0;; ++k) {
+      for (int k = 0; !SPLIT; ++k) {
         // there and back over the CTAs, since items get shorter along a sequence
         const unsigned at = k & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
-        Item it = find_item(p, 2 * PW, SPLIT ? blockIdx.x / parts : at + static_cast<long long>(k) * gridDim.x);
-        if (SPLIT && k > 0) it.b = -1;
+        const Item it = find_item(p, 2 * PW, at + static_cast<long long>(k) * gridDim.x);
         if (!__all_sync(0xffffffffu, wait_bar(item_empty(k & 1), ((k >> 1) & 1) ^ 1, p.err))) break;
         if (lane == 0) {
-          int* d = reinterpret_cast<int*>(smem_raw + (items - raw) + 32 * (k & 1));
-          d[0] = it.b;
-          d[1] = it.g;
-          d[2] = it.p0;
-          d[3] = it.row0;
-          d[4] = it.S;
-          d[5] = it.past;
+          put_item(k, it);
           mbar_arrive(item_full(k & 1));
         }
         __syncwarp();
@@ -805,7 +818,6 @@ __global__ void __launch_bounds__(THREADS, 1)
   }
   // whether the cluster shares its item is the same for all of its CTAs and threads
   const int* const d = reinterpret_cast<const int*>(smem_raw + (items - raw));
-  if (SPLIT) __syncthreads();  // the item's descriptor
   const int shares = SPLIT && d[0] >= 0 ? span_of(p, Item{d[0], d[1], d[2], d[3], d[4], d[5]}, PW, part, parts).parts : 1;
   if (SPLIT && shares > 1) {
     // each of its CTAs joins a share of the 256 rows
@@ -891,7 +903,7 @@ cudaError_t count_clusters() {
 // the table allows (a shorter one is split less, on the device).
 int parts_for(const ChunkArgs& a, long long items, int PC) {
   long long keys = a.blocks_per_seq * 16ll;
-  if (a.window > 0) keys = std::min(keys, a.window + PC + a.sinks + 0ll);
+  if (a.window > 0) keys = std::min(keys, 0ll + a.window + PC + a.sinks);
   const int steps = static_cast<int>(std::min((keys + KT - 1) / KT, 1ll << 20));
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return 1;

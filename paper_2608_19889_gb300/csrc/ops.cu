@@ -100,6 +100,12 @@ int check_attn(const axon_kv_cache* c, int layer, const void* q, const void* out
   return AXON_OK;
 }
 
+// Sinks that a row of `blocks` blocks can have (kernels round them up to blocks).
+int clamp_sinks(int sinks, int blocks) {
+  const int most = blocks * 16;  // blocks <= MAX_BLOCKS_PER_SEQ
+  return sinks < most ? sinks : most;
+}
+
 float scale_log2(float scale, int d) {
   const double s = scale > 0.f ? static_cast<double>(scale) : 1.0 / sqrt(static_cast<double>(d));
   return static_cast<float>(s * 1.4426950408889634);
@@ -187,7 +193,7 @@ int axon_attn_decode(const axon_kv_cache* cache, int32_t layer, const void* d_q,
   a.G = cache->num_kv_heads;
   a.d = cache->head_dim;
   a.window = window;
-  a.sinks = window > 0 ? sinks : 0;
+  a.sinks = window > 0 ? clamp_sinks(sinks, blocks_per_seq) : 0;
   a.scale_log2 = scale_log2(scale, cache->head_dim);
   a.o = d_out;
   a.o_row = out_row_stride;
@@ -235,7 +241,7 @@ int axon_attn_prefill(const axon_kv_cache* cache, int32_t layer, const void* d_q
   a.G = G;
   a.d = d;
   a.window = window;
-  a.sinks = window > 0 ? sinks : 0;
+  a.sinks = window > 0 ? clamp_sinks(sinks, blocks_per_seq) : 0;
   a.scale_log2 = scale_log2(scale, d);
   a.o = d_out;
   a.o_row = out_row_stride;
@@ -288,7 +294,7 @@ int axon_kv_release(const axon_kv_cache* cache, const axon_kv_seqs* seqs, const 
   if (n < 0 || n > a.R || window < 0 || sinks < 0) return AXON_ERR_INVALID_ARG;
   if (n == 0) return AXON_OK;
   if ((rc = launch_ctx(cache, stream, &lc))) return rc;
-  return status(launch_pages_release(lc, a, d_rows, n, window > 0 ? window : -1, sinks));
+  return status(launch_pages_release(lc, a, d_rows, n, window > 0 ? window : -1, clamp_sinks(sinks, a.P)));
 }
 
 int axon_kv_reserve(const axon_kv_cache* cache, const axon_kv_seqs* seqs, const int32_t* d_rows,

@@ -38,6 +38,8 @@ class PagedSeqs:
     def extend(self, ids, lengths, logits=None, next_tokens=None):
         """Append chunk b of `ids` (int32 [sum(lengths)], packed) to sequence b: axon_prefill_varlen after taking the
         blocks. lengths: one positive host integer per row."""
+        if len(lengths) != self.rows or min(lengths) < 1 or ids.numel() != sum(lengths):
+            raise ValueError(f"{self.rows} positive lengths that sum to the {ids.numel()} ids are wanted, got {lengths}")
         new = torch.tensor(lengths, dtype=torch.int32, device="cuda")
         cu = torch.nn.functional.pad(new.cumsum(0, dtype=torch.int32), (1, 0))
         ax.axon_kv_reserve(self.cache, self.seqs, self.all, new, self.work, err=self.err)

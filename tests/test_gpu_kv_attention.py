@@ -198,6 +198,30 @@ def test_decode_strides_and_another_stream(ax):
     assert (out == 7.0).all()
 
 
+@pytest.mark.parametrize("window,sinks", [(2 ** 31 - 1, 2 ** 31 - 1), (20, 2 ** 31 - 1), (2 ** 31 - 1, 3)])
+def test_largest_windows_and_sinks(ax, window, sinks):
+    c = Case(4, 2, 64, "bf16", [100, 30], [1, 1], 0, 0, seed=7)
+    c.window, c.sinks = window, sinks
+    check_decode(ax, c)
+    check_prefill(ax, c)
+
+
+def test_heads_before_rows(ax):
+    """Queries and outputs stored [heads, rows, head_dim], and every second row of a buffer."""
+    c = Case(8, 2, 64, "fp16", [40, 9, 0], [1, 1, 1], 0, 0, seed=17)
+    want = c.reference()[0]
+    q = c.q.transpose(0, 1).contiguous().transpose(0, 1)
+    out = torch.full((8, 3, 64), float("nan"), dtype=c.q.dtype, device="cuda").transpose(0, 1)
+    assert q.stride() == (64, 192, 1)
+    close(run_decode(ax, c, q=q, out=out)[0], want, c.vmax(), ULP["fp16"])
+    out.fill_(float("nan"))
+    check_prefill(ax, c, q=q, out=out)
+    wide = torch.full((6, 8, 64), float("nan"), dtype=c.q.dtype, device="cuda")
+    wide[::2] = c.q
+    check_prefill(ax, c, q=wide[::2], out=torch.empty_like(wide)[::2])
+    close(run_decode(ax, c, q=wide[::2], out=torch.empty_like(wide)[::2])[0], want, c.vmax(), ULP["fp16"])
+
+
 def test_decode_shows_an_infinite_value(ax):
     """An infinite value at a visible token: its dim of the output is not finite, the others are untouched."""
     c = Case(4, 1, 64, "bf16", [40], [1], 0, 0, seed=11)

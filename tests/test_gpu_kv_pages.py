@@ -146,7 +146,8 @@ def test_release_whole_rows(ax):
     c.check()
 
 
-@pytest.mark.parametrize("window,sinks", [(1, 0), (16, 0), (17, 1), (20, 16), (33, 17), (64, 4), (5, 1000), (10000, 4)])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (16, 0), (17, 1), (20, 16), (33, 17), (64, 4), (5, 1000), (10000, 4), (9, 2 ** 31 - 1),
+                                          (2 ** 31 - 1, 2 ** 31 - 1)])
 def test_release_what_a_window_has_passed(ax, window, sinks):
     lens = [0, 1, 16, 31, 32, 33, 47, 48, 64, 65, 127, 128, 129, 200]
     c = Cache(ax, lens, 100, 14)

@@ -126,6 +126,18 @@ def test_managed_blocks_give_what_a_roomy_cache_gives(prec):
         ax.axon_free(m)
 
 
+def test_more_sinks_than_positions_are_no_window():
+    """Sinks that cover the context: the plain causal mask, whatever the window."""
+    ax = _ax()
+    w = gpu_weights(SINK)
+    out = []
+    for shape in (dict(SINK, sinks=2 ** 31 - 1), dict(SINK, window=2 ** 31 - 1)):
+        m = create(shape, w, max_batch=1, max_context=128)
+        out.append(run_prefill(m, si.make_ids(1, 90, SINK["V"], seed=3), ax.AXON_LOGITS_ALL, SINK["V"])[0])
+        ax.axon_free(m)
+    assert np.array_equal(out[0], out[1])
+
+
 def test_paged_seqs_refuses():
     from paper_2608_19889_gb300 import paged
     ax = _ax()

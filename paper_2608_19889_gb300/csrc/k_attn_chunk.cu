@@ -223,9 +223,10 @@ struct Item {
   int b, g, p0, row0, S, past;  // b < 0: none
 };
 
-// Item `item` of the launch: sequences in order, a sequence's position pairs from the
-// end (those with the most keys first), the kv heads of a pair together. Offsets and lengths that do not
-// fit are reported and give no items.
+// Item `item` of the launch: sequences whose chunks fill both tiles before the others (single
+// tokens of a mixed batch, whose items are shorter), else in order; a sequence's position
+// pairs from the end (those with the most keys first), the kv heads of a pair together.
+// Offsets and lengths that do not fit are reported and give no items.
 AXON_DEV Item find_item(const ChunkArgs& p, int PC, long long item) {
   Item r;
   r.b = -1;
@@ -233,7 +234,12 @@ AXON_DEV Item find_item(const ChunkArgs& p, int PC, long long item) {
   const long long pair = item / p.G;
   const int lane = threadIdx.x & 31;
   long long before = 0;
-  for (int b0 = 0; b0 < p.B; b0 += 32) {
+  for (int b0 = 0, rest = 0; rest < 2; b0 += 32) {
+    if (b0 >= p.B) {  // once more, for the others
+      b0 = -32;
+      ++rest;
+      continue;
+    }
     int r0 = 0, len = 0, ps = 0;
     if (b0 + lane < p.B) {
       r0 = p.cu ? p.cu[b0 + lane] : (b0 + lane) * p.max_chunk;
@@ -248,7 +254,7 @@ AXON_DEV Item find_item(const ChunkArgs& p, int PC, long long item) {
       }
       if ((b0 + lane == 0 && r0 != 0) || (b0 + lane == p.B - 1 && r1 != p.T)) set_err(p.err, DEVERR_SEQ);
     }
-    const int mine = (len + PC - 1) / PC;
+    const int mine = (2 * len > PC) == (rest == 0) ? (len + PC - 1) / PC : 0;
     int end = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {

@@ -376,7 +376,8 @@ int axon_moe_routing_record(axon_model* m, int32_t* d_experts, int32_t rows);
  * Workspaces are device memory, 16-byte aligned, of at least the size that
  * the matching query returns. The attention's must be zero before its first
  * use and every call leaves it fit for the next one; the block operators' may
- * hold anything. Calls that may overlap (different streams) need their own. */
+ * hold anything. Calls that may overlap (different streams) need their own. The first
+ * attention call on a device sets its kernels' limits: make it before a stream capture. */
 
 /* The pools of all layers: [num_layers][num_blocks][num_kv_heads][16][head_dim],
  * keys after RoPE, 16-byte aligned. Block numbers are common to all layers. */
@@ -400,7 +401,7 @@ typedef struct axon_kv_seqs {
   int32_t* block_table;   /* [max_seqs][blocks_per_seq] block numbers, -1: none */
   int32_t* context_lens;  /* [max_seqs] tokens in the cache, as axon_decode_step advances them */
   int32_t* refs;          /* [num_blocks] */
-  int32_t max_seqs;       /* at most 8192 */
+  int32_t max_seqs;       /* at most 8192; times blocks_per_seq below 2^31 */
   int32_t blocks_per_seq;
 } axon_kv_seqs;
 

@@ -39,8 +39,8 @@
 // the last step, output rows stored 32 lines at a time) 10000 beside 33 such steps. 8191 positions
 // under a 4096-key window with sinks, 32 query heads, 8 kv heads: 293 to 308 us over the boxes,
 // 1.34 to 1.41 PFLOP/s, 70 to 74 % of the burst rate of cuBLAS (1.90) and 79 to 83 % of its rate
-// under the power cap (1.70), with clocks at 1.9 GHz. The model's prefill kernel takes 476 with
-// the same arguments. Instruction counts and fetches of the issuers decide: waits inlined with
+// under the power cap (1.70), with clocks at 1.9 GHz. The model's prefill kernel, given sinks, took
+// 476. Instruction counts and fetches of the issuers decide: waits inlined with
 // long loops (122 KB of code) 372 -> 369 us without them, issuers in uniform registers and in
 // turns 369 -> 336, items in an order that evens out 336 -> 317, no local memory 309 -> 297.
 #include <math.h>

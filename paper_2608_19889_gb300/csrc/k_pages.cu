@@ -471,8 +471,8 @@ cudaError_t launch_pages_copy(const LaunchCtx& lc, const PagesArgs& a, const int
 }
 
 cudaError_t launch_pages_release(const LaunchCtx& lc, const PagesArgs& a, const int* rows, int n, int window, int sinks) {
-  const unsigned y = static_cast<unsigned>((a.P + 4 * CT - 1) / (4 * CT));
-  return launch_k(lc, release_kernel, dim3(n, y), CT, 0, a, rows, window, sinks);
+  const int y = (a.P + 4 * CT - 1) / (4 * CT);  // (the kernel takes what is left in turns)
+  return launch_k(lc, release_kernel, dim3(n, y < 64 ? y : 64), CT, 0, a, rows, window, sinks);
 }
 
 cudaError_t launch_pages_reserve(const LaunchCtx& lc, const PagesArgs& a, const int* rows, const int* more, int n) {

@@ -125,7 +125,9 @@ int pages_args(const axon_kv_cache* c, const axon_kv_seqs* s, void* work, int64_
   if (!s) return AXON_OK;
   if (!s->block_table || !s->context_lens || !s->refs || s->max_seqs < 1 || s->blocks_per_seq < 1)
     return AXON_ERR_INVALID_ARG;
-  if (s->max_seqs > MAX_ROWS || s->blocks_per_seq > MAX_BLOCKS_PER_SEQ) return AXON_ERR_UNSUPPORTED;
+  if (s->max_seqs > MAX_ROWS || s->blocks_per_seq > MAX_BLOCKS_PER_SEQ ||
+      static_cast<long long>(s->max_seqs) * s->blocks_per_seq > INT_MAX)
+    return AXON_ERR_UNSUPPORTED;
   a->table = s->block_table;
   a->ctx = s->context_lens;
   a->refs = s->refs;

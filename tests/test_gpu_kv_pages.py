@@ -157,6 +157,15 @@ def test_release_what_a_window_has_passed(ax, window, sinks):
     c.check()
 
 
+def test_release_a_wide_row(ax):
+    """More entries than the launch covers at once."""
+    c = Cache(ax, [100, 1200000], 75100, 75010, (1, 1, 64))
+    c.release([1, 0], 600000, 20)
+    c.check()
+    c.release([1])
+    c.check()
+
+
 def test_release_reports(ax):
     c = Cache(ax, [37, 16], 8, 4)
     c.ax.axon_kv_release(c.cache, c.seqs, c.ints([2, 1]), err=c.err)

@@ -107,6 +107,8 @@ def test_block_operators_refuse(ax):
     for change in (dict(block_table=None), dict(context_lens=None), dict(refs=None), dict(max_seqs=0), dict(blocks_per_seq=0)):
         assert L.axon_kv_release(C, ctypes.byref(seqs(ax, **change)), FAKE, 1, 0, 0, None, None) == bad
     assert L.axon_kv_release(C, ctypes.byref(seqs(ax, max_seqs=8193)), FAKE, 1, 0, 0, None, None) == ax.AXON_ERR_UNSUPPORTED
+    assert L.axon_kv_release(C, ctypes.byref(seqs(ax, max_seqs=8192, blocks_per_seq=1 << 18)), FAKE, 1, 0, 0, None, None) == \
+        ax.AXON_ERR_UNSUPPORTED
     # nothing to do
     assert L.axon_kv_fork(C, S, None, None, 0, FAKE, W, None, None) == 0
     assert L.axon_kv_release(C, S, None, 0, 0, 0, None, None) == 0

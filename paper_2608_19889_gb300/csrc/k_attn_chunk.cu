@@ -16,7 +16,15 @@
 //   9, 11       MMA issuers of tile 0 and 1: S = Q K^T into TMEM, O += P V with P read back
 //               from TMEM;
 //   10          finds the items, two ahead, and publishes them.
-// The 512 TMEM columns hold S0, S1 (128 each, later P in the first 64) and O0, O1.
+// The 512 TMEM columns hold S0, S1 (128 each, later both terms of P, 64 each) and O0, O1.
+//
+// A probability enters the product in two 16-bit terms, p and what its rounding lost: 2^-17 of
+// it is left out (bf16), so the output's own rounding is the only one that counts. Error against 64
+// bits over that of a result rounded once, 64 and 128 dims, 16 to 2500 keys: 1.000 in both types;
+// with one term 1.07 to 1.35, which is also more than the model's prefill kernel (k_attn_tc.cu,
+// second terms for 16 keys of a step) loses, so that a model would have paid for its sinks in
+// precision. The price is half as many products again: 8191 positions 391 us against 303,
+// a mixed batch 39.8 against 32.3, 16 tokens 8 either way.
 //
 // m is not the running maximum but a bound that lags: the maximum of a row's first visible step,
 // raised (and O rescaled) only when it has become too small. Rounding to 16 bits is
@@ -24,24 +32,15 @@
 // none overflows, and the row sum of a step, which is needed anyway, tells: above 2^14 the
 // step is taken again with m raised. So the usual step reads its scores once and
 // computes no maximum. Steps under a mask, and a row's first, pass over the scores
-// before that. The row sum is fp32: of the unrounded probabilities, which costs half the
-// additions and where keys are many differs by the mean of many roundings; in those few steps of
-// tiles with at most 512 keys, of the rounded ones (error against 64 bits over that of
-// a result rounded once, worst of 28 drawn calls: 1.5 without, 1.35 with; mean 1.02).
+// before that. The row sum is fp32, of the unrounded probabilities.
 //
-// Bound: a 128 x 128 tile at head_dim 128 takes 1024 tensor cycles (2 x 2 x 128^3
-// operations at 8192 per cycle), and per scheduler 512 cycles of the exponential
-// unit and about 340 issue slots, so two tiles in turn can keep the tensor pipe
-// busy while the softmax of one takes no longer than the products of the other.
-// Measured in steady state (clocks read in the kernel): softmax 1160 cycles, from the last
-// probability to the first product 180, 16 products and their completion 1150, so a step of both
-// tiles 2500 to 2800 cycles for 2048 of the pipe; an item's start and end (first bound, mask of
-// the last step, output rows stored 32 lines at a time) 10000 beside 33 such steps. 8191 positions
-// under a 4096-key window with sinks, 32 query heads, 8 kv heads: 293 to 308 us over the boxes,
-// 1.34 to 1.41 PFLOP/s, 70 to 74 % of the burst rate of cuBLAS (1.90) and 79 to 83 % of its rate
-// under the power cap (1.70), with clocks at 1.9 GHz. The model's prefill kernel, given sinks, took
-// 476. Instruction counts and fetches of the issuers decide: waits inlined with
-// long loops (122 KB of code) 372 -> 369 us without them, issuers in uniform registers and in
+// Bound: the tensor pipe. A 128 x 128 tile at head_dim 128 takes 1536 tensor cycles (2 x 3 x 128^3
+// operations at 8192 per cycle), 3072 for both, and per scheduler 512 cycles of the exponential
+// unit and about 600 issue slots; the softmax of one tile runs under the products of the other.
+// 8191 positions under a 4096-key window with sinks, 32 query heads, 8 kv heads: 391 us, 1.06
+// PFLOP/s of the formula's operations and 1.58 of the pipe's, 83 % of the burst rate of cuBLAS
+// (1.90). Instruction counts and fetches of the issuers matter (measured with one term): waits
+// inlined with long loops 372 -> 369 us without them, issuers in uniform registers and in
 // turns 369 -> 336, items in an order that evens out 336 -> 317, no local memory 309 -> 297.
 #include <math.h>
 
@@ -54,7 +53,6 @@ namespace {
 
 constexpr int THREADS = 384;
 constexpr int KT = 128;  // keys per step
-constexpr int FEW = 4;              // steps of a tile whose rows may have few keys
 constexpr float LAG = 4.f;          // how far a maximum that is looked at may exceed m (log2)
 constexpr float SUM_MAX = 16384.f;  // largest sum of a row's 128 probabilities
 
@@ -190,17 +188,14 @@ template <> AXON_DEV uint32_t pack_p<f16>(float lo, float hi) {
   __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<uint32_t*>(&h);
 }
-// lo += the low, hi += the high 16-bit value of p.
-template <typename T> AXON_DEV void add_p(float& lo, float& hi, uint32_t p);
-template <> AXON_DEV void add_p<bf16>(float& lo, float& hi, uint32_t p) {
-  asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n add.f32.bf16 %0, l, %0;\n add.f32.bf16 %1, h, %1;\n}"
-      : "+f"(lo), "+f"(hi)
-      : "r"(p));
+// What the two 16-bit roundings in p lost of a and e.
+template <typename T> AXON_DEV uint32_t pack_rest(float a, float e, uint32_t p);
+template <> AXON_DEV uint32_t pack_rest<bf16>(float a, float e, uint32_t p) {
+  return pack_bf2(a - bf_lo(p), e - bf_hi(p));
 }
-template <> AXON_DEV void add_p<f16>(float& lo, float& hi, uint32_t p) {
-  asm("{\n .reg .f16 l, h;\n mov.b32 {l, h}, %2;\n add.f32.f16 %0, l, %0;\n add.f32.f16 %1, h, %1;\n}"
-      : "+f"(lo), "+f"(hi)
-      : "r"(p));
+template <> AXON_DEV uint32_t pack_rest<f16>(float a, float e, uint32_t p) {
+  const float2 r = __half22float2(*reinterpret_cast<__half2*>(&p));
+  return pack_p<f16>(a - r.x, e - r.y);
 }
 // The V tile as the B operand of P V: N = dims (contiguous in memory), K = tokens at
 // 128-byte pitch; 8-token groups 1024 bytes apart, the second 64 dims one chunk further.
@@ -276,8 +271,8 @@ AXON_DEV Item find_item(const ChunkArgs& p, int PC, long long item) {
   return r;
 }
 
-// Into how many parts an item of `steps` key steps is split by a cluster of `parts` CTAs. A
-// step takes 1.3 us and joining the parts 6 us (8B width): 16 rows after 1000 cached tokens, 8
+// Into how many parts an item of `steps` key steps is split by a cluster of `parts` CTAs. With
+// one-term probabilities a step took 1.3 us and joining the parts 6 us (8B width): 16 rows after 1000 cached tokens, 8
 // steps, unsplit / 2 / 4 parts 15.9 / 16.5 / 13.4 us; after 500, 12.4 / 15.7; after 2000 (8
 // parts) 26.0 / 15.5; 120 rows after 2000 31.1 / 20.2 (4 parts).
 __host__ __device__ inline int split_of(int steps, int parts) {
@@ -564,12 +559,18 @@ __global__ void __launch_bounds__(THREADS, 1)
             if (t != 0 && blocks >= 8) {
               if (lead) {
 #pragma unroll
-                for (int x = 0; x < 8; ++x) mma_ts(tO, tS + x * 8, vd + x * 128, id_o, 1u);
+                for (int x = 0; x < 8; ++x) {
+                  mma_ts(tO, tS + x * 8, vd + x * 128, id_o, 1u);
+                  mma_ts(tO, tS + KT / 2 + x * 8, vd + x * 128, id_o, 1u);
+                }
               }
             } else if (lead) {
               // the first step starts the sums; blocks past the last hold no values
 #pragma unroll 1
-              for (int x = 0; x < min(8, blocks); ++x) mma_ts(tO, tS + x * 8, vd + x * 128, id_o, (t | x) != 0 ? 1u : 0u);
+              for (int x = 0; x < min(8, blocks); ++x) {
+                mma_ts(tO, tS + x * 8, vd + x * 128, id_o, (t | x) != 0 ? 1u : 0u);
+                mma_ts(tO, tS + KT / 2 + x * 8, vd + x * 128, id_o, 1u);
+              }
             }
             // MMAs run in issue order: the next scores may overwrite the probabilities just
             // issued, and s_full implies that O is up to date
@@ -632,7 +633,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (!ok) break;
         ++ns_;
         tc_fence_after();
-        uint32_t pr[KT / 2];
+        uint32_t pr[KT / 2], rest[KT / 2];
         uint64_t sum[4];
 #pragma unroll 1
         for (int round = 0; round < 2; ++round) {
@@ -713,6 +714,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             a = ex2(a);
             e = ex2(e);
             pr[c] = pack_p<T16>(a, e);
+            rest[c] = pack_rest<T16>(a, e, pr[c]);
             sum[c & 3] = add2(sum[c & 3], pk2(a, e));
           }
           sum[0] = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
@@ -723,6 +725,8 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         st32(tS, pr);
         st32(tS + 32, pr + 32);
+        st32(tS + 64, rest);
+        st32(tS + 96, rest + 32);
         // the slots past the last token, before the product reads them
         if (sp.clears(w) && t == nt - 1) {
           const int iv = it + 2 * t + 1, sv = iv % NS;
@@ -737,19 +741,6 @@ __global__ void __launch_bounds__(THREADS, 1)
           fence_proxy_async();
         }
         wait_st();
-        if (look && nt <= FEW) {
-          // rows with few keys: the sum of the rounded probabilities, whose errors the product shares
-          float a[2] = {0.f, 0.f};
-#pragma unroll 1
-          for (int c = 0; c < KT / 2; c += 32) {
-            uint32_t q[32];
-            ld32(tS + c, q);
-            tmem_wait_ld();
-#pragma unroll
-            for (int u = 0; u < 32; ++u) add_p<T16>(a[0], a[1], q[u]);
-          }
-          sum[0] = pk2(a[0], a[1]);
-        }
         tc_fence_before();
         mbar_arrive(p_full(w));
         l2 = add2(l2, sum[0]);

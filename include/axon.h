@@ -375,9 +375,10 @@ int axon_moe_routing_record(axon_model* m, int32_t* d_experts, int32_t rows);
  *
  * Workspaces are device memory, 16-byte aligned, of at least the size that
  * the matching query returns. The attention's must be zero before its first
- * use and every call leaves it fit for the next one; the block operators' may
- * hold anything. Calls that may overlap (different streams) need their own. The first
- * attention call on a device sets its kernels' limits: make it before a stream capture. */
+ * use and every call leaves it fit for the next one, of any shape and batch that
+ * it is large enough for; the block operators' may hold anything. Calls that may
+ * overlap (different streams) need their own. The first attention call on a device
+ * sets its kernels' limits: make it before a stream capture. */
 
 /* The pools of all layers: [num_layers][num_blocks][num_kv_heads][16][head_dim],
  * keys after RoPE, 16-byte aligned. Block numbers are common to all layers. */

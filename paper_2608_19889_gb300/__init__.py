@@ -359,7 +359,7 @@ def make_kv_seqs(block_table, context_lens, refs) -> axon_kv_seqs:
 
 
 def make_attn_workspace(cache, rows, heads):
-    """Zeroed workspace of axon_attn_decode for up to `rows` rows of `heads` heads."""
+    """Zeroed workspace of axon_attn_decode for `heads` heads on this cache, or for any call that needs no larger one."""
     n = ctypes.c_int64(0)
     _check("axon_attn_decode_workspace", lib().axon_attn_decode_workspace(cache.ref, heads, rows, ctypes.byref(n)))
     return _torch.zeros(n.value, dtype=_torch.uint8, device="cuda")

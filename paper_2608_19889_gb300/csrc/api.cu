@@ -428,8 +428,8 @@ PagedAttnArgs sink_decode(const axon_model* m, const AttnArgs& at, int B) {
   a.window = at.window;
   a.sinks = m->cfg.sink_tokens;
   a.scale_log2 = at.scale_log2;
-  a.part = static_cast<float*>(m->sink_work);
-  a.ticket = reinterpret_cast<int*>(static_cast<char*>(m->sink_work) + paged_attn_part_bytes(m->H, m->G, m->d, m->num_sms));
+  a.ticket = static_cast<int*>(m->sink_work);
+  a.part = reinterpret_cast<float*>(static_cast<char*>(m->sink_work) + paged_attn_ticket_bytes(m->num_sms));
   a.err = m->err;
   return a;
 }
@@ -1551,8 +1551,7 @@ int axon_model_create(const axon_config* cfg, const axon_tensor* weights, int32_
   if ((rc = dev_alloc(m, &p, static_cast<size_t>(dec_b) * m->G * 4))) return fail(rc);
   m->attn_cnt = static_cast<int*>(p);
   if (cfg->sink_tokens > 0) {
-    const size_t bytes = paged_attn_part_bytes(m->H, m->G, m->d, m->num_sms) +
-                         4 * paged_attn_tickets(dec_b, m->H, m->G, m->num_sms);
+    const size_t bytes = paged_attn_ticket_bytes(m->num_sms) + paged_attn_part_bytes(m->H, m->G, m->d, m->num_sms);
     if ((rc = dev_alloc(m, &m->sink_work, bytes))) return fail(rc);
     if (cudaMemsetAsync(m->sink_work, 0, bytes, st) != cudaSuccess) return fail(AXON_ERR_CUDA);
   }

@@ -424,7 +424,6 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
       }
     }
     group_sync(group, gs);
-    const long long item = static_cast<long long>(b) * p.G + g;
     const bool whole = off == 0 && cnt == rp.n;
     const float* const gstate = state + group * gs * C::STATE;
     const int gl = wg * 32 + lane;
@@ -538,12 +537,12 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
       if (parts > radix) {
         // two levels: the last of each `radix` neighbours joins them, the last of these joins the results
         const int j = static_cast<int>(wid - first) / radix * radix, n = min(radix, parts - j);
-        joiner = last_of(p.ticket + p.B * p.G + slot(first + j), n);
+        joiner = last_of(p.ticket + gridDim.x * DW + slot(first + j), n);
         if (joiner) join(first + j, n, 1, false);
         step = radix;
         count = (parts + radix - 1) / radix;
       }
-      if (joiner && last_of(p.ticket + item, count)) join(first, count, step, true);
+      if (joiner && last_of(p.ticket + first, count)) join(first, count, step, true);
       group_sync(group, gs);
     }
     u += cnt;
@@ -593,16 +592,15 @@ cudaError_t launch_hd(const LaunchCtx& lc, const PagedAttnArgs& a) {
 
 }  // namespace
 
-// Partial states first, then the tickets (zero between calls).
 size_t paged_attn_part_bytes(int H, int G, int d, int num_sms) {
   const bool two = H / G > 8;
   const size_t workers = static_cast<size_t>(num_sms) * (two ? 2 : 3) * DW;
   return 2 * 2 * workers * (two ? 16 : 8) * (d + 2) * 4;
 }
-// A ticket per item and per worker's slot.
-size_t paged_attn_tickets(int B, int H, int G, int num_sms) {
-  return static_cast<size_t>(B) * G + 2 * static_cast<size_t>(num_sms) * (H / G > 8 ? 2 : 3) * DW;
-}
+// A ticket per cut item, which goes by its first worker (no other cut item begins there), and one per
+// worker's slot. They stand in front of the states and their number goes by the SMs alone,
+// so that no call's states lie where another shape or batch has its tickets.
+size_t paged_attn_ticket_bytes(int num_sms) { return 4 * 3 * static_cast<size_t>(num_sms) * 3 * DW; }
 
 cudaError_t prepare_attn_paged_kernels() {
   cudaError_t e = prepare_hd<64, bf16>();

@@ -224,12 +224,12 @@ struct PagedAttnArgs {
   long long o_row, o_head;
   void* o_lo;   // optional second term of o, same strides (with q_lo only)
   float* lse;   // optional [B][H], natural logarithm
+  int* ticket;  // paged_attn_ticket_bytes, zero between calls; a workspace begins with them
   float* part;  // paged_attn_part_bytes
-  int* ticket;  // paged_attn_tickets, zero between calls
   int* err;
 };
 size_t paged_attn_part_bytes(int H, int G, int d, int num_sms);
-size_t paged_attn_tickets(int B, int H, int G, int num_sms);
+size_t paged_attn_ticket_bytes(int num_sms);  // a multiple of 16
 // Pages that can be visible to B rows, times the kv heads; at most 2^31 - 1 are supported.
 inline long long paged_attn_most_pages(int B, int G, int blocks_per_seq, int window, int sinks) {
   long long row = blocks_per_seq;

@@ -153,8 +153,8 @@ int axon_attn_decode_workspace(const axon_kv_cache* cache, int32_t num_heads, in
   if (num_heads / cache->num_kv_heads > 16 || B > PAGED_ATTN_MAX_B) return AXON_ERR_UNSUPPORTED;
   LaunchCtx lc;
   if ((rc = launch_ctx(cache, nullptr, &lc))) return rc;
-  *bytes = static_cast<int64_t>(paged_attn_part_bytes(num_heads, cache->num_kv_heads, cache->head_dim, lc.num_sms)) +
-           4 * static_cast<int64_t>(paged_attn_tickets(B, num_heads, cache->num_kv_heads, lc.num_sms));
+  *bytes = static_cast<int64_t>(paged_attn_ticket_bytes(lc.num_sms) +
+                                paged_attn_part_bytes(num_heads, cache->num_kv_heads, cache->head_dim, lc.num_sms));
   return AXON_OK;
 }
 
@@ -174,10 +174,9 @@ int axon_attn_decode(const axon_kv_cache* cache, int32_t layer, const void* d_q,
   if (!d_block_table && static_cast<long long>(B) * blocks_per_seq > cache->num_blocks) return AXON_ERR_INVALID_ARG;
   LaunchCtx lc;
   if ((rc = launch_ctx(cache, stream, &lc))) return rc;
-  const int64_t part =
-      static_cast<int64_t>(paged_attn_part_bytes(num_heads, cache->num_kv_heads, cache->head_dim, lc.num_sms));
-  if (workspace_bytes <
-      part + 4 * static_cast<int64_t>(paged_attn_tickets(B, num_heads, cache->num_kv_heads, lc.num_sms)))
+  const size_t tickets = paged_attn_ticket_bytes(lc.num_sms);
+  if (workspace_bytes < static_cast<int64_t>(
+                            tickets + paged_attn_part_bytes(num_heads, cache->num_kv_heads, cache->head_dim, lc.num_sms)))
     return AXON_ERR_INVALID_ARG;
   PagedAttnArgs a;
   memset(&a, 0, sizeof(a));
@@ -201,8 +200,8 @@ int axon_attn_decode(const axon_kv_cache* cache, int32_t layer, const void* d_q,
   a.o_row = out_row_stride;
   a.o_head = out_head_stride;
   a.lse = d_lse;
-  a.part = static_cast<float*>(d_workspace);
-  a.ticket = reinterpret_cast<int*>(static_cast<char*>(d_workspace) + part);
+  a.ticket = static_cast<int*>(d_workspace);
+  a.part = reinterpret_cast<float*>(static_cast<char*>(d_workspace) + tickets);
   a.err = d_err;
   return status(with_limits([&] { return launch_attn_paged_decode(lc, a); }));
 }

@@ -85,11 +85,12 @@ class AxonError(RuntimeError):
 _lib = None
 _torch = None  # imported with the library
 _raw_stream = None  # (device index) -> the current stream's handle
+_current_device = None  # () -> index of the device that launches go to
 
 
 def lib() -> ctypes.CDLL:
     """Load the CUDA library (raises if it has not been built)."""
-    global _lib, _torch, _raw_stream
+    global _lib, _torch, _raw_stream, _current_device
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} is missing: build it with paper_2608_19889_gb300.build.build()")
@@ -136,6 +137,7 @@ def lib() -> ctypes.CDLL:
         _torch = torch
         # a handle without the Stream object around it (0.1 us against 3 us), where this torch has the call
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         _lib = L
     return _lib
 
@@ -198,6 +200,7 @@ def axon_model_create(cfg: axon_config, weights: dict, stream=None) -> ctypes.c_
     h = ctypes.c_void_p()
     _check("axon_model_create", lib().axon_model_create(ctypes.byref(cfg), arr, len(names), _stream(stream),
                                                         ctypes.byref(h)))
+    h.device = torch.cuda.current_device()
     return h
 
 
@@ -294,30 +297,46 @@ def axon_free(m):
 # Small calls are bound by the host: what a wrapper reads of a tensor costs 0.05 to 0.15 us apiece.
 
 
-def _want(t, dtype, what, n):
-    """Address of a dense device tensor of n elements; refuse what the C call could not tell from one."""
-    if t.dtype is dtype and t.is_cuda and t.is_contiguous() and t.numel() == n:
+def _want(t, dtype, what, n, device):
+    """Address of a dense tensor of n elements on the device; refuse what the C call could not tell from one."""
+    if t.dtype is dtype and t.get_device() == device and t.is_contiguous() and t.numel() == n:
         return t.data_ptr()
-    raise TypeError(f"{what}: a dense {dtype} device tensor of {n} elements is wanted, got {t.dtype} {tuple(t.shape)} "
-                    f"with strides {t.stride()} on {t.device}")
+    raise TypeError(f"{what}: a dense {dtype} tensor of {n} elements on cuda:{max(device, 0)} is wanted, got {t.dtype} "
+                    f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
 
 
-def _list(t, what):
+def _list(t, what, device):
     """Address and length of a dense int32 device vector."""
     if t.dim() != 1:
         raise TypeError(f"{what}: a vector is wanted, got {tuple(t.shape)}")
     n = t.numel()
-    return _want(t, _torch.int32, what, n), n
+    return _want(t, _torch.int32, what, n, device), n
 
 
-def _word(err):
-    return None if err is None else _want(err, _torch.int32, "err", 1)
+def _word(err, device):
+    return None if err is None else _want(err, _torch.int32, "err", 1, device)
 
 
-def _handle(stream, t):
-    """The stream's handle; None: the current one of the tensor's device."""
-    if stream is None and _raw_stream is not None:
-        return _raw_stream(t.get_device())
+def _space(t, device):
+    """Address of a workspace."""
+    if t.get_device() == device:
+        return t.data_ptr()
+    raise TypeError(f"workspace: memory of cuda:{device} is wanted, got {t.device}")
+
+
+def _current(device):
+    """Kernels go to the current device, which has to be the operands'."""
+    if _current_device() != device:
+        raise ValueError(f"operands are on cuda:{device}, the current device is cuda:{_current_device()}")
+
+
+def _handle(stream, device):
+    """The stream's handle; None: the device's current one."""
+    _current(device)
+    if stream is None:
+        return _raw_stream(device) if _raw_stream is not None else _stream(None)
+    if getattr(stream, "device_index", device) != device:
+        raise ValueError(f"operands are on cuda:{device}, the stream is on cuda:{stream.device_index}")
     return _stream(stream)
 
 
@@ -330,11 +349,20 @@ def make_kv_cache(k, v) -> axon_kv_cache:
         raise TypeError(f"k, v: bf16, fp16 or fp32 tensors of the same 5 dimensions are wanted, got {k.dtype} "
                         f"{tuple(k.shape)} and {v.dtype} {tuple(v.shape)}")
     L, N, G, bs, d = k.shape
-    return _described(axon_kv_cache(_want(k, k.dtype, "k", k.numel()), _want(v, k.dtype, "v", k.numel()), L, N, G, bs, d, prec))
+    n, dev = k.numel(), _on(k, "k")
+    return _described(axon_kv_cache(_want(k, k.dtype, "k", n, dev), _want(v, k.dtype, "v", n, dev), L, N, G, bs, d, prec), dev)
 
 
-def _described(c):
+def _on(t, what):
+    """Index of a tensor's device."""
+    if not t.is_cuda:
+        raise TypeError(f"{what}: device memory is wanted, got a tensor on {t.device}")
+    return t.get_device()
+
+
+def _described(c, device):
     """What the wrappers read of a descriptor at every call, as plain attributes."""
+    c.device = device
     c.dtype = {AXON_BF16: _torch.bfloat16, AXON_FP16: _torch.float16, AXON_FP32_DEBUG: _torch.float32}[c.precision]
     c.blocks, c.dim, c.ref = c.num_blocks, c.head_dim, ctypes.byref(c)
     return c
@@ -344,7 +372,7 @@ def axon_kv_cache_get(m) -> axon_kv_cache:
     """Descriptor of a model's own cache."""
     c = axon_kv_cache()
     _check("axon_kv_cache_get", lib().axon_kv_cache_get(m, ctypes.byref(c)))
-    return _described(c)
+    return _described(c, getattr(m, "device", _current_device()))
 
 
 def make_kv_seqs(block_table, context_lens, refs) -> axon_kv_seqs:
@@ -352,41 +380,44 @@ def make_kv_seqs(block_table, context_lens, refs) -> axon_kv_seqs:
     their addresses: keep the tensors."""
     lib()
     R, P = block_table.shape
-    s = axon_kv_seqs(_want(block_table, _torch.int32, "block_table", R * P), _want(context_lens, _torch.int32, "context_lens", R),
-                     _list(refs, "refs")[0], R, P)
-    s.blocks, s.ref = refs.numel(), ctypes.byref(s)
+    dev = _on(block_table, "block_table")
+    s = axon_kv_seqs(_want(block_table, _torch.int32, "block_table", R * P, dev),
+                     _want(context_lens, _torch.int32, "context_lens", R, dev), _list(refs, "refs", dev)[0], R, P)
+    s.device, s.blocks, s.ref = dev, refs.numel(), ctypes.byref(s)
     return s
 
 
 def make_attn_workspace(cache, rows, heads):
     """Zeroed workspace of axon_attn_decode for `heads` heads on this cache, or for any call that needs no larger one."""
     n = ctypes.c_int64(0)
+    _current(cache.device)
     _check("axon_attn_decode_workspace", lib().axon_attn_decode_workspace(cache.ref, heads, rows, ctypes.byref(n)))
-    return _torch.zeros(n.value, dtype=_torch.uint8, device="cuda")
+    return _torch.zeros(n.value, dtype=_torch.uint8, device=_torch.device("cuda", cache.device))
 
 
 def make_kv_workspace(cache, seqs):
     """Workspace of axon_kv_fork, axon_kv_reserve and axon_kv_compact."""
     n = ctypes.c_int64(0)
     _check("axon_kv_workspace", lib().axon_kv_workspace(cache.ref, seqs.ref, ctypes.byref(n)))
-    return _torch.empty(n.value, dtype=_torch.uint8, device="cuda")
+    return _torch.empty(n.value, dtype=_torch.uint8, device=_torch.device("cuda", cache.device))
 
 
 def _rows(q, out, cache):
     """(rows, heads, row stride, head stride of q, of out) of [rows, heads, head_dim] tensors of the cache's type."""
     shape, qs, os_ = q.shape, q.stride(), out.stride()
     if (len(shape) != 3 or out.shape != shape or shape[2] != cache.dim or q.dtype is not cache.dtype or
-            out.dtype is not cache.dtype or qs[2] != 1 or os_[2] != 1 or not q.is_cuda or not out.is_cuda):
-        raise TypeError(f"q, out: {cache.dtype} device tensors [rows, heads, {cache.dim}] with a dense last dimension are "
-                        f"wanted, got {q.dtype} {tuple(shape)} on {q.device}, {out.dtype} {tuple(out.shape)} on {out.device}")
+            out.dtype is not cache.dtype or qs[2] != 1 or os_[2] != 1 or q.get_device() != cache.device or
+            out.get_device() != cache.device):
+        raise TypeError(f"q, out: {cache.dtype} tensors [rows, heads, {cache.dim}] on cuda:{cache.device} with a dense last "
+                        f"dimension are wanted, got {q.dtype} {tuple(shape)} on {q.device}, {out.dtype} {tuple(out.shape)} on {out.device}")
     return shape[0], shape[1], qs[0], qs[1], os_[0], os_[1]
 
 
-def _table(block_table, blocks_per_seq, rows):
+def _table(block_table, blocks_per_seq, rows, device):
     if block_table is None:
         return None, blocks_per_seq
     per = block_table.shape[-1]
-    return _want(block_table, _torch.int32, "block_table", rows * per), per
+    return _want(block_table, _torch.int32, "block_table", rows * per, device), per
 
 
 def axon_attn_decode(cache, layer, q, context_lens, out, workspace, block_table=None, blocks_per_seq=0, window=0, sinks=0,
@@ -395,11 +426,13 @@ def axon_attn_decode(cache, layer, q, context_lens, out, workspace, block_table=
     context_lens: int32 [B]; block_table: int32 [B, blocks], or None with blocks_per_seq for contiguous rows;
     workspace: make_attn_workspace; lse: fp32 [B, heads] or None; err: int32 [1] error word or None."""
     B, H, qr, qh, orow, ohead = _rows(q, out, cache)
-    table, per = _table(block_table, blocks_per_seq, B)
+    dev = cache.device
+    table, per = _table(block_table, blocks_per_seq, B, dev)
     rc = _lib.axon_attn_decode(
-        cache.ref, layer, q.data_ptr(), qr, qh, B, H, _want(context_lens, _torch.int32, "context_lens", B), table, per, window,
-        sinks, scale, out.data_ptr(), orow, ohead, None if lse is None else _want(lse, _torch.float32, "lse", B * H),
-        workspace.data_ptr(), workspace.nbytes, None if err is None else _word(err), _handle(stream, q))
+        cache.ref, layer, q.data_ptr(), qr, qh, B, H, _want(context_lens, _torch.int32, "context_lens", B, dev), table, per,
+        window, sinks, scale, out.data_ptr(), orow, ohead,
+        None if lse is None else _want(lse, _torch.float32, "lse", B * H, dev), _space(workspace, dev), workspace.nbytes,
+        None if err is None else _word(err, dev), _handle(stream, dev))
     if rc:
         raise AxonError("axon_attn_decode", rc)
 
@@ -409,12 +442,13 @@ def axon_attn_prefill(cache, layer, q, cu_seqlens, context_lens, max_chunk, out,
     """Attention of packed chunks (see include/axon.h). q, out: [T, heads, head_dim]; cu_seqlens: int32 [B+1];
     context_lens: int32 [B] tokens before each chunk (not advanced); the rest as in axon_attn_decode."""
     T, H, qr, qh, orow, ohead = _rows(q, out, cache)
-    past, B = _list(context_lens, "context_lens")
-    table, per = _table(block_table, blocks_per_seq, B)
+    dev = cache.device
+    past, B = _list(context_lens, "context_lens", dev)
+    table, per = _table(block_table, blocks_per_seq, B, dev)
     rc = _lib.axon_attn_prefill(
-        cache.ref, layer, q.data_ptr(), qr, qh, B, T, H, _want(cu_seqlens, _torch.int32, "cu_seqlens", B + 1), past, max_chunk,
-        table, per, window, sinks, scale, out.data_ptr(), orow, ohead, None if err is None else _word(err),
-        _handle(stream, q))
+        cache.ref, layer, q.data_ptr(), qr, qh, B, T, H, _want(cu_seqlens, _torch.int32, "cu_seqlens", B + 1, dev), past,
+        max_chunk, table, per, window, sinks, scale, out.data_ptr(), orow, ohead, None if err is None else _word(err, dev),
+        _handle(stream, dev))
     if rc:
         raise AxonError("axon_attn_prefill", rc)
 
@@ -422,50 +456,57 @@ def axon_attn_prefill(cache, layer, q, cu_seqlens, context_lens, max_chunk, out,
 def _same_pool(cache, seqs):
     if cache.blocks != seqs.blocks:
         raise TypeError(f"refs: {cache.blocks} counts are wanted, one per block, got {seqs.blocks}")
+    if cache.device != seqs.device:
+        raise TypeError(f"tables on cuda:{cache.device} are wanted, got cuda:{seqs.device}")
+    return cache.device
 
 
 def axon_kv_copy_blocks(cache, src, dst, err=None, stream=None):
     """Copy blocks src[i] to dst[i] (int32 [n]) in all layers."""
-    s, n = _list(src, "src")
-    _check("axon_kv_copy_blocks", _lib.axon_kv_copy_blocks(cache.ref, s, _want(dst, _torch.int32, "dst", n), n, _word(err),
-                                                           _handle(stream, src)))
+    dev = cache.device
+    s, n = _list(src, "src", dev)
+    _check("axon_kv_copy_blocks", _lib.axon_kv_copy_blocks(cache.ref, s, _want(dst, _torch.int32, "dst", n, dev), n,
+                                                           _word(err, dev), _handle(stream, dev)))
 
 
 def axon_kv_fork(cache, seqs, src, dst, workspace, err=None, stream=None):
     """Rows dst[i] take over what rows src[i] hold (int32 [n]); workspace: make_kv_workspace."""
-    _same_pool(cache, seqs)
-    s, n = _list(src, "src")
-    _check("axon_kv_fork", _lib.axon_kv_fork(cache.ref, seqs.ref, s, _want(dst, _torch.int32, "dst", n), n,
-                                             workspace.data_ptr(), workspace.nbytes, _word(err), _handle(stream, src)))
+    dev = _same_pool(cache, seqs)
+    s, n = _list(src, "src", dev)
+    _check("axon_kv_fork", _lib.axon_kv_fork(cache.ref, seqs.ref, s, _want(dst, _torch.int32, "dst", n, dev), n,
+                                             _space(workspace, dev), workspace.nbytes, _word(err, dev), _handle(stream, dev)))
 
 
 def axon_kv_release(cache, seqs, rows, window=0, sinks=0, err=None, stream=None):
     """Rows (int32 [n]) give back everything, or with a window what no later query sees."""
-    _same_pool(cache, seqs)
-    r, n = _list(rows, "rows")
-    _check("axon_kv_release", _lib.axon_kv_release(cache.ref, seqs.ref, r, n, window, sinks, _word(err), _handle(stream, rows)))
+    dev = _same_pool(cache, seqs)
+    r, n = _list(rows, "rows", dev)
+    _check("axon_kv_release", _lib.axon_kv_release(cache.ref, seqs.ref, r, n, window, sinks, _word(err, dev),
+                                                   _handle(stream, dev)))
 
 
 def axon_kv_reserve(cache, seqs, rows, new_tokens, workspace, err=None, stream=None):
     """Rows (int32 [n]) take blocks for new_tokens (int32 [n]) more tokens; workspace: make_kv_workspace."""
-    _same_pool(cache, seqs)
-    r, n = _list(rows, "rows")
-    _check("axon_kv_reserve", _lib.axon_kv_reserve(cache.ref, seqs.ref, r, _want(new_tokens, _torch.int32, "new_tokens", n), n,
-                                                   workspace.data_ptr(), workspace.nbytes, _word(err), _handle(stream, rows)))
+    dev = _same_pool(cache, seqs)
+    r, n = _list(rows, "rows", dev)
+    _check("axon_kv_reserve", _lib.axon_kv_reserve(
+        cache.ref, seqs.ref, r, _want(new_tokens, _torch.int32, "new_tokens", n, dev), n, _space(workspace, dev),
+        workspace.nbytes, _word(err, dev), _handle(stream, dev)))
 
 
 def axon_kv_compact(cache, seqs, workspace, moved=None, live=None, err=None, stream=None):
     """Move the blocks in use to the front of the pool. moved: int32 [blocks] each block's number afterwards (-1: free);
     live: int32 [1] their count; workspace: make_kv_workspace."""
-    _same_pool(cache, seqs)
+    dev = _same_pool(cache, seqs)
     _check("axon_kv_compact", _lib.axon_kv_compact(
-        cache.ref, seqs.ref, None if moved is None else _want(moved, _torch.int32, "moved", cache.blocks),
-        None if live is None else _want(live, _torch.int32, "live", 1), workspace.data_ptr(), workspace.nbytes, _word(err),
-        _handle(stream, workspace)))
+        cache.ref, seqs.ref, None if moved is None else _want(moved, _torch.int32, "moved", cache.blocks, dev),
+        None if live is None else _want(live, _torch.int32, "live", 1, dev), _space(workspace, dev), workspace.nbytes,
+        _word(err, dev), _handle(stream, dev)))
 
 
 def axon_check_error(err, stream=None) -> tuple[int, int]:
     """(status, bits) of an operator's error word (int32 [1]) after synchronising the stream; the word is cleared."""
     bits = ctypes.c_int32(0)
-    rc = lib().axon_check_error(_want(err, _torch.int32, "err", 1), _stream(stream), ctypes.byref(bits))
+    dev = _on(err, "err")
+    rc = lib().axon_check_error(_word(err, dev), _handle(stream, dev), ctypes.byref(bits))
     return rc, bits.value

@@ -319,9 +319,10 @@ def _word(err, device):
 
 def _space(t, device):
     """Address of a workspace."""
-    if t.get_device() == device:
+    if t.get_device() == device and t.is_contiguous():
         return t.data_ptr()
-    raise TypeError(f"workspace: memory of cuda:{device} is wanted, got {t.device}")
+    raise TypeError(f"workspace: dense memory of cuda:{device} is wanted, got {tuple(t.shape)} with strides {t.stride()} on "
+                    f"{t.device}")
 
 
 def _current(device):

@@ -160,3 +160,11 @@ def test_workspaces_are_made_where_the_cache_is(ax, monkeypatch):
     ax.make_attn_workspace(c, 3, 4)
     ax.make_kv_workspace(c, ax.make_kv_seqs(i32(3, 2, device=1), i32(3, device=1), i32(8, device=1)))
     assert made == [torch.device("cuda", 1)] * 2
+
+def test_a_workspace_that_is_not_dense_is_refused(ax):
+    work = Tensor((1 << 20,), torch.uint8)
+    work.is_contiguous = lambda: False
+    for op in ("decode", "fork", "reserve", "compact"):
+        with pytest.raises(TypeError):
+            calls(ax, work=work)[op]()
+    assert not ax._calls

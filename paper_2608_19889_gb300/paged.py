@@ -2,8 +2,8 @@
 
 `PagedSeqs` keeps what the block operators work on (block table, lengths, counts, workspace, error word) for the cache of
 a model created with AXON_KV_PAGED, and steps the model with it: blocks are taken before tokens are appended, shared by
-forks, and given back when a sequence ends or, under a sliding window, when they have slid out of it. Nothing here waits
-for the GPU except `check` and `lengths`.
+forks, and given back when a sequence ends or, under a sliding window, when they have slid out of it. `check`, `lengths`
+and `blocks_in_use` wait for the GPU, `extend` for the copy of its lengths; nothing else does.
 """
 from __future__ import annotations
 
@@ -36,12 +36,15 @@ class PagedSeqs:
         self.unused = torch.empty(rows, **dev)  # greedy tokens that nobody asked for
 
     def extend(self, ids, lengths, logits=None, next_tokens=None):
-        """Append chunk b of `ids` (int32 [sum(lengths)], packed) to sequence b: axon_prefill_varlen after taking the
-        blocks. lengths: one positive host integer per row."""
+        """Append chunk b of `ids` (int32 [sum(lengths)], packed) to sequence b: axon_prefill_varlen after blocks that slid
+        out of the window are given back and the chunk's taken. lengths: one positive host integer per row. Under a window a
+        long prompt that is fed in pieces holds no more than a piece, the window and the sinks reach."""
         if len(lengths) != self.rows or min(lengths) < 1 or ids.numel() != sum(lengths):
             raise ValueError(f"{self.rows} positive lengths that sum to the {ids.numel()} ids are wanted, got {lengths}")
         new = torch.tensor(lengths, dtype=torch.int32, device="cuda")
         cu = torch.nn.functional.pad(new.cumsum(0, dtype=torch.int32), (1, 0))
+        if self.window:
+            ax.axon_kv_release(self.cache, self.seqs, self.all, window=self.window, sinks=self.sinks, err=self.err)
         ax.axon_kv_reserve(self.cache, self.seqs, self.all, new, self.work, err=self.err)
         ax.axon_prefill_varlen(self.model, ids, cu, self.lens, max(lengths), block_table=self.table, logits=logits,
                                next_tokens=next_tokens)

@@ -35,26 +35,34 @@ class PagedSeqs:
         self.one = torch.ones(rows, **dev)
         self.unused = torch.empty(rows, **dev)  # greedy tokens that nobody asked for
 
+    def _first(self, n):
+        if not 1 <= n <= self.rows:
+            raise ValueError(f"1 .. {self.rows} rows are wanted, got {n}")
+        if self.window:
+            ax.axon_kv_release(self.cache, self.seqs, self.all[:n], window=self.window, sinks=self.sinks, err=self.err)
+
     def extend(self, ids, lengths, logits=None, next_tokens=None):
         """Append chunk b of `ids` (int32 [sum(lengths)], packed) to sequence b: axon_prefill_varlen after blocks that slid
-        out of the window are given back and the chunk's taken. lengths: one positive host integer per row. Under a window a
-        long prompt that is fed in pieces holds no more than a piece, the window and the sinks reach."""
-        if len(lengths) != self.rows or min(lengths) < 1 or ids.numel() != sum(lengths):
-            raise ValueError(f"{self.rows} positive lengths that sum to the {ids.numel()} ids are wanted, got {lengths}")
+        out of the window are given back and the chunk's taken. lengths: one positive host integer for each of the first
+        rows; the others stay as they are. Under a window a long prompt that is fed in pieces holds no more than a piece, the
+        window and the sinks reach."""
+        n = len(lengths)
+        if n and (min(lengths) < 1 or ids.numel() != sum(lengths)):
+            raise ValueError(f"positive lengths that sum to the {ids.numel()} ids are wanted, got {lengths}")
+        self._first(n)
         new = torch.tensor(lengths, dtype=torch.int32, device="cuda")
         cu = torch.nn.functional.pad(new.cumsum(0, dtype=torch.int32), (1, 0))
-        if self.window:
-            ax.axon_kv_release(self.cache, self.seqs, self.all, window=self.window, sinks=self.sinks, err=self.err)
-        ax.axon_kv_reserve(self.cache, self.seqs, self.all, new, self.work, err=self.err)
+        ax.axon_kv_reserve(self.cache, self.seqs, self.all[:n], new, self.work, err=self.err)
         ax.axon_prefill_varlen(self.model, ids, cu, self.lens, max(lengths), block_table=self.table, logits=logits,
                                next_tokens=next_tokens)
 
     def step(self, tokens, logits=None, next_tokens=None):
-        """One decode step of every row: blocks that slid out of the window are given back, one is taken where the token
-        begins it."""
-        if self.window:
-            ax.axon_kv_release(self.cache, self.seqs, self.all, window=self.window, sinks=self.sinks, err=self.err)
-        ax.axon_kv_reserve(self.cache, self.seqs, self.all, self.one, self.work, err=self.err)
+        """One decode step of the first rows, one for each token; the others stay as they are (a row that ended takes no
+        blocks if the live ones are kept in front: fork the last of them over it). Blocks that slid out of the window are
+        given back, one is taken where the token begins it."""
+        n = tokens.numel()
+        self._first(n)
+        ax.axon_kv_reserve(self.cache, self.seqs, self.all[:n], self.one[:n], self.work, err=self.err)
         ax.axon_decode_step(self.model, tokens, self.lens, block_table=self.table, logits=logits,
                             next_tokens=self.unused if next_tokens is None else next_tokens)
 

@@ -24,7 +24,7 @@ def seqs_of(shape, rows, blocks, max_context=512, max_batch=None):
     ax = _ax()
     w = gpu_weights(shape)
     cfg = ax.make_config(shape, max_batch or rows, max_context, kv_layout=ax.AXON_KV_PAGED, kv_num_blocks=blocks,
-                         max_prefill_tokens=64)
+                         max_prefill_tokens=128)
     m = ax.axon_model_create(cfg, w)
     return m, paged.PagedSeqs(m, cfg, rows), w
 
@@ -62,5 +62,40 @@ def test_a_long_prompt_in_pieces_needs_no_more_than_its_window(window, sinks):
         seqs.check()
         for b in range(2):
             assert np.abs(logits[b].cpu().numpy() - last_logits(shape, w, text[b])).max() <= tiny_tol("bf16")
+    finally:
+        ax.axon_free(m)
+
+def test_rows_past_the_tokens_are_left_as_they_are():
+    """A step and a piece for the first rows only: an ended row takes no blocks, a waiting one keeps its own."""
+    shape = dict(TINY, window=64, sinks=4)
+    ax = _ax()
+    m, seqs, w = seqs_of(shape, 3, 40)
+    try:
+        text = [si.make_ids(1, n, shape["V"], seed=n)[0] for n in (30, 21, 17)]
+        seqs.extend(ints(np.concatenate(text)), [30, 21, 17])
+        seqs.release(ints([2]))
+        held = seqs.table[1:].clone()
+        logits = torch.empty(1, shape["V"], device="cuda")
+        for i in range(20):
+            text[0] = np.append(text[0], i)
+            seqs.step(ints([i]), logits=logits)
+        seqs.check()
+        assert seqs.lengths() == [50, 21, 0]
+        assert torch.equal(seqs.table[1:], held) and int((held[1] >= 0).sum()) == 0
+        assert seqs.blocks_in_use() == 4 + 2
+        assert np.abs(logits[0].cpu().numpy() - last_logits(shape, w, text[0])).max() <= tiny_tol("bf16")
+        # the other rows go on from there
+        seqs.extend(ints([7, 8, 9]), [1, 2], logits=torch.empty(2, shape["V"], device="cuda"))
+        both = torch.empty(2, shape["V"], device="cuda")
+        seqs.step(ints([3, 4]), logits=both)
+        seqs.check()
+        assert seqs.lengths() == [52, 24, 0]
+        for b, tail in ((0, [7, 3]), (1, [8, 9, 4])):
+            want = last_logits(shape, w, np.append(text[b], tail))
+            assert np.abs(both[b].cpu().numpy() - want).max() <= tiny_tol("bf16")
+        with pytest.raises(ValueError):
+            seqs.step(ints([1, 2, 3, 4]))
+        with pytest.raises(ValueError):
+            seqs.extend(ints([]), [])
     finally:
         ax.axon_free(m)

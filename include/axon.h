@@ -330,7 +330,8 @@ int axon_profile_prefill(axon_model* m, const int32_t* d_ids, int32_t B, int32_t
  * that loads the library until the process exits) instead of from memory
  * allocated per call. It calls no cudaMalloc, cudaFree or graph
  * instantiation.
- *   Limits: B * num_key_value_heads <= 256 and head_dim <= 128, else
+ *   Limits: B * num_key_value_heads <= 256 (not with sink_tokens, whose
+ *   attention merges in the model's own memory) and head_dim <= 128, else
  *   AXON_ERR_UNSUPPORTED; the 16-bit modes AXON_BF16 and AXON_FP16 only
  *   (AXON_ERR_UNSUPPORTED in AXON_FP32_DEBUG). The attention keeps at most
  *   256 / (B * num_key_value_heads) key splits per sequence and kv head.
@@ -340,7 +341,8 @@ int axon_profile_prefill(axon_model* m, const int32_t* d_ids, int32_t B, int32_t
  *   call before any stream capture.
  *   Every call shares the one array and clears the parts that must start
  *   at zero: calls that overlap on the GPU (different streams, or several
- *   models at once) race on it and must be serialised by the caller.
+ *   models at once) race on it and must be serialised by the caller. (With
+ *   sink_tokens that holds for the calls of one model.)
  * The key-split count may differ from axon_decode_step's, so logits can
  * differ from it by floating-point rounding of the merge. */
 int axon_decode_step_noalloc(axon_model* m, const int32_t* d_tokens, int32_t B, int32_t* d_context_lens,

@@ -1153,12 +1153,13 @@ launch_chain:
 }  // namespace
 
 // Direct-launch decode step with caller-supplied attention merge scratch
-// (used by the allocation-free entry point in noalloc.cu). Not exported.
+// (used by the allocation-free entry point in noalloc.cu). *merge_rows: slots of it per
+// token at least; none with attention sinks, whose attention has its own workspace. Not exported.
 int axon_internal_decode_direct(axon_model* m, const int32_t* tokens, int B, int32_t* ctx, const int32_t* bt,
                                 float* logits, int32_t* next, cudaStream_t st, float* attn_part, int* attn_cnt,
-                                int attn_rows_cap, int* head_dim, int* kv_heads) {
+                                int attn_rows_cap, int* head_dim, int* merge_rows) {
   if (head_dim) *head_dim = m->d;
-  if (kv_heads) *kv_heads = m->G;
+  if (merge_rows) *merge_rows = m->cfg.sink_tokens ? 0 : m->G;
   if (!tokens) return AXON_OK;  // query only
   return enqueue_decode(m, tokens, B, ctx, bt, logits, next, st, nullptr, 0, attn_part, attn_cnt, attn_rows_cap);
 }

@@ -21,7 +21,7 @@
 
 int axon_internal_decode_direct(axon_model* m, const int32_t* tokens, int B, int32_t* ctx, const int32_t* bt,
                                 float* logits, int32_t* next, cudaStream_t st, float* attn_part, int* attn_cnt,
-                                int attn_rows_cap, int* head_dim, int* kv_heads);
+                                int attn_rows_cap, int* head_dim, int* merge_rows);
 int axon_internal_decode_args_ok(const axon_model* m, const int32_t* d_tokens, int32_t B, const int32_t* d_ctx,
                                  const int32_t* d_block_table, const int32_t* d_next);
 
@@ -101,17 +101,17 @@ extern "C" int axon_decode_step_noalloc(axon_model* m, const int32_t* d_tokens, 
                                         void* stream) {
   int rc = axon_internal_decode_args_ok(m, d_tokens, B, d_context_lens, d_block_table, d_next);
   if (rc != AXON_OK) return rc;
-  int head_dim = 0, kv_heads = 0;
+  int head_dim = 0, merge_rows = 0;
   axon_internal_decode_direct(m, nullptr, 0, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, 0,
-                              &head_dim, &kv_heads);
-  if (head_dim > NOALLOC_MAX_HEAD_DIM || B * kv_heads > NOALLOC_ROWS) return AXON_ERR_UNSUPPORTED;
+                              &head_dim, &merge_rows);
+  if (head_dim > NOALLOC_MAX_HEAD_DIM || B * merge_rows > NOALLOC_ROWS) return AXON_ERR_UNSUPPORTED;
   float* part = scratch_on_current_device(&rc);
   if (!part) return rc;
   int* tickets = reinterpret_cast<int*>(part + NOALLOC_PART_FLOATS);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   // Tickets must start at zero; the partial states are always written before
   // they are read, so they need no clearing.
-  if (cudaMemsetAsync(tickets, 0, static_cast<size_t>(B) * kv_heads * sizeof(int), st) != cudaSuccess) {
+  if (merge_rows && cudaMemsetAsync(tickets, 0, static_cast<size_t>(B) * merge_rows * sizeof(int), st) != cudaSuccess) {
     cudaGetLastError();
     return AXON_ERR_CUDA;
   }

@@ -333,9 +333,9 @@ def _current(device):
 
 def _handle(stream, device):
     """The stream's handle; None: the device's current one."""
+    if stream is None and _raw_stream is not None and _current_device() == device:
+        return _raw_stream(device)
     _current(device)
-    if stream is None:
-        return _raw_stream(device) if _raw_stream is not None else _stream(None)
     if getattr(stream, "device_index", device) != device:
         raise ValueError(f"operands are on cuda:{device}, the stream is on cuda:{stream.device_index}")
     return _stream(stream)

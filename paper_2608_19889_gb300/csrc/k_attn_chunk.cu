@@ -181,7 +181,8 @@ AXON_DEV float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-// Probabilities lie in [0, 2^8]: no saturation needed.
+// A probability is at most the sum of its step, SUM_MAX: no saturation needed.
+static_assert(SUM_MAX < 65504.f, "probabilities have to fit fp16");
 template <typename T> AXON_DEV uint32_t pack_p(float lo, float hi);
 template <> AXON_DEV uint32_t pack_p<bf16>(float lo, float hi) { return pack_bf2(lo, hi); }
 template <> AXON_DEV uint32_t pack_p<f16>(float lo, float hi) {

@@ -97,8 +97,8 @@ AXON_DEV RowPages row_pages(const PagedAttnArgs& p, int pos) {
 }
 // Position of row b's query; -1: the row sees nothing.
 AXON_DEV int row_pos(const PagedAttnArgs& p, int b) {
-  const long long pos = static_cast<long long>(p.ctx[b]) + p.pos_add;
-  if (pos < p.blocks_per_seq * 16ll) return pos < 0 ? -1 : static_cast<int>(pos);
+  const int pos = p.ctx[b];
+  if (pos < p.blocks_per_seq * 16ll) return max(pos, -1);
   set_err(p.err, DEVERR_POS);
   return -1;
 }

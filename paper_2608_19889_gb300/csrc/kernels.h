@@ -213,8 +213,7 @@ struct PagedAttnArgs {
   const void* q_lo;  // optional second term of q, same strides
   const void* k;     // layer pool [num_blocks][G][16][d]
   const void* v;
-  const int* ctx;  // row b's query is at position ctx[b] + pos_add; negative: the row is idle
-  int pos_add;
+  const int* ctx;  // row b's query is at position ctx[b]; negative: the row is idle
   const int* block_table;  // [B][blocks_per_seq], or null: blocks b * blocks_per_seq + j
   int blocks_per_seq, num_blocks;
   int B, H, G, d;

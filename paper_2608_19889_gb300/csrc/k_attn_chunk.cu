@@ -47,6 +47,7 @@
 #include <algorithm>
 #include <atomic>
 
+#include "attn_tc.cuh"
 #include "kernels.h"
 
 namespace {
@@ -80,44 +81,6 @@ AXON_DEV bool wait_bar(uint32_t bar, uint32_t parity, int* err) {
   }
   return true;
 }
-AXON_DEV void tma_load_3d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
-          dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
-      : "memory");
-}
-// D[tmem] (+)= A[tmem] * B[smem desc] (A: 128 lanes, two 16-bit values per column).
-AXON_DEV void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(
-          d_tmem),
-      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-AXON_DEV void ld32(uint32_t taddr, uint32_t* r) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,"
-      "%30,%31}, [%32];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-      : "r"(taddr)
-      : "memory");
-}
-AXON_DEV void st32(uint32_t taddr, const uint32_t* r) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,"
-      "%30,%31,%32};" ::"r"(taddr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
-      "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
-      "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-      : "memory");
-}
 AXON_DEV void st_global32(void* at, const uint32_t* v) {
   asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
                "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
@@ -148,29 +111,6 @@ AXON_DEV bool elect_one() {
   asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(r));
   return r != 0;
 }
-AXON_DEV void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-AXON_DEV float ex2(float v) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-  return r;
-}
-// Two fp32 values in one 64-bit register: one issue slot for both.
-AXON_DEV uint64_t pk2(float a, float b) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-AXON_DEV void upk2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-AXON_DEV uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-AXON_DEV uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
 AXON_DEV uint64_t add2(uint64_t a, uint64_t b) {
   uint64_t r;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
@@ -181,32 +121,8 @@ AXON_DEV float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-// A probability is at most the sum of its step, SUM_MAX: no saturation needed.
+// A probability is at most the sum of its step, SUM_MAX: none saturates.
 static_assert(SUM_MAX < 65504.f, "probabilities have to fit fp16");
-template <typename T> AXON_DEV uint32_t pack_p(float lo, float hi);
-template <> AXON_DEV uint32_t pack_p<bf16>(float lo, float hi) { return pack_bf2(lo, hi); }
-template <> AXON_DEV uint32_t pack_p<f16>(float lo, float hi) {
-  __half2 h = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<uint32_t*>(&h);
-}
-// What the two 16-bit roundings in p lost of a and e.
-template <typename T> AXON_DEV uint32_t pack_rest(float a, float e, uint32_t p);
-template <> AXON_DEV uint32_t pack_rest<bf16>(float a, float e, uint32_t p) {
-  return pack_bf2(a - bf_lo(p), e - bf_hi(p));
-}
-template <> AXON_DEV uint32_t pack_rest<f16>(float a, float e, uint32_t p) {
-  const float2 r = __half22float2(*reinterpret_cast<__half2*>(&p));
-  return pack_p<f16>(a - r.x, e - r.y);
-}
-// The V tile as the B operand of P V: N = dims (contiguous in memory), K = tokens at
-// 128-byte pitch; 8-token groups 1024 bytes apart, the second 64 dims one chunk further.
-template <int HD>
-AXON_DEV uint64_t v_desc(uint32_t addr) {
-  uint64_t d = smem_desc_sw128(addr);
-  d &= ~(static_cast<uint64_t>(0x3FFFu) << 16);
-  d |= static_cast<uint64_t>(KCfg<HD>::CHUNK >> 4) << 16;
-  return d;
-}
 
 // Bits c of 0 .. 15 with lo <= base + c < hi.
 AXON_DEV uint32_t bits16(int base, int lo, int hi) {
@@ -496,7 +412,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       const bool lead = elect_one();
       constexpr uint32_t id_s = idesc_f32acc(128, KT, MmaFmt<T16>::v);
       constexpr uint32_t id_o = idesc_f32acc(128, HD, MmaFmt<T16>::v) | (1u << 16);  // B stored N-contiguous
-      const uint64_t dQ = smem_desc_sw128(sQ + w * C::TILE), dK = smem_desc_sw128(sKV), dV = v_desc<HD>(sKV);
+      const uint64_t dQ = smem_desc_sw128(sQ + w * C::TILE), dK = smem_desc_sw128(sKV), dV = v_desc<C::CHUNK>(sKV);
       const uint32_t tS = tmem + w * KT, tO = tmem + 2 * KT + w * HD;
       uint32_t st = 0, ph = 0;  // ring: next stage and its phase
       auto next_stage = [&]() {
@@ -561,16 +477,16 @@ __global__ void __launch_bounds__(THREADS, 1)
               if (lead) {
 #pragma unroll
                 for (int x = 0; x < 8; ++x) {
-                  mma_ts(tO, tS + x * 8, vd + x * 128, id_o, 1u);
-                  mma_ts(tO, tS + KT / 2 + x * 8, vd + x * 128, id_o, 1u);
+                  tc_mma_f16_ts(tO, tS + x * 8, vd + x * 128, id_o, 1u);
+                  tc_mma_f16_ts(tO, tS + KT / 2 + x * 8, vd + x * 128, id_o, 1u);
                 }
               }
             } else if (lead) {
               // the first step starts the sums; blocks past the last hold no values
 #pragma unroll 1
               for (int x = 0; x < min(8, blocks); ++x) {
-                mma_ts(tO, tS + x * 8, vd + x * 128, id_o, (t | x) != 0 ? 1u : 0u);
-                mma_ts(tO, tS + KT / 2 + x * 8, vd + x * 128, id_o, 1u);
+                tc_mma_f16_ts(tO, tS + x * 8, vd + x * 128, id_o, (t | x) != 0 ? 1u : 0u);
+                tc_mma_f16_ts(tO, tS + KT / 2 + x * 8, vd + x * 128, id_o, 1u);
               }
             }
             // MMAs run in issue order: the next scores may overwrite the probabilities just
@@ -656,16 +572,16 @@ __global__ void __launch_bounds__(THREADS, 1)
               const bool mask = !round && __any_sync(0xffffffffu, valid && all != 0xffffu);
               if (!mask && !round && !__any_sync(0xffffffffu, fmaxf(m, mx) == -INFINITY)) continue;
               float s[64];
-              ld32(tS + c, reinterpret_cast<uint32_t*>(s));
-              ld32(tS + c + 32, reinterpret_cast<uint32_t*>(s) + 32);
+              tmem_ld32(tS + c, reinterpret_cast<uint32_t*>(s));
+              tmem_ld32(tS + c + 32, reinterpret_cast<uint32_t*>(s) + 32);
               tmem_wait_ld();
               if (mask) {
 #pragma unroll
                 for (int x = 0; x < 4; ++x)
 #pragma unroll
                   for (int u = 0; u < 16; ++u) s[x * 16 + u] = (see[x] >> u) & 1 ? s[x * 16 + u] : -INFINITY;
-                st32(tS + c, reinterpret_cast<uint32_t*>(s));
-                st32(tS + c + 32, reinterpret_cast<uint32_t*>(s) + 32);
+                tmem_st32(tS + c, reinterpret_cast<uint32_t*>(s));
+                tmem_st32(tS + c + 32, reinterpret_cast<uint32_t*>(s) + 32);
               }
               float m4[4] = {mx, s[0], s[1], s[2]};
 #pragma unroll
@@ -675,7 +591,7 @@ __global__ void __launch_bounds__(THREADS, 1)
               }
               mx = max3(max3(m4[0], s[59], s[60]), max3(m4[1], s[61], s[62]), max3(m4[2], m4[3], s[63]));
             }
-            wait_st();
+            tmem_wait_st();
             const float mt = mx * sl2;
             const bool up = valid && mt > (m == -INFINITY ? m : m + LAG);
             if (__any_sync(0xffffffffu, up)) {
@@ -687,24 +603,24 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll 1
                 for (int c = 0; c < HD; c += 32) {
                   float o[32];
-                  ld32(tO + c, reinterpret_cast<uint32_t*>(o));
+                  tmem_ld32(tO + c, reinterpret_cast<uint32_t*>(o));
                   tmem_wait_ld();
 #pragma unroll
                   for (int u = 0; u < 32; u += 2) upk2(mul2(pk2(o[u], o[u + 1]), f2), o[u], o[u + 1]);
-                  st32(tO + c, reinterpret_cast<uint32_t*>(o));
+                  tmem_st32(tO + c, reinterpret_cast<uint32_t*>(o));
                 }
-                wait_st();
+                tmem_wait_st();
               }
             }
           }
           const float nb = m == -INFINITY ? 0.f : -m;
           const uint64_t nbp = pk2(nb, nb);
           float s[KT];
-          ld32(tS, reinterpret_cast<uint32_t*>(s));
-          ld32(tS + 32, reinterpret_cast<uint32_t*>(s) + 32);
+          tmem_ld32(tS, reinterpret_cast<uint32_t*>(s));
+          tmem_ld32(tS + 32, reinterpret_cast<uint32_t*>(s) + 32);
           tmem_wait_ld();
-          ld32(tS + 64, reinterpret_cast<uint32_t*>(s) + 64);
-          ld32(tS + 96, reinterpret_cast<uint32_t*>(s) + 96);
+          tmem_ld32(tS + 64, reinterpret_cast<uint32_t*>(s) + 64);
+          tmem_ld32(tS + 96, reinterpret_cast<uint32_t*>(s) + 96);
 #pragma unroll
           for (int x = 0; x < 4; ++x) sum[x] = 0;  // pairs of 0.f
 #pragma unroll
@@ -724,10 +640,10 @@ __global__ void __launch_bounds__(THREADS, 1)
           if (round || !__any_sync(0xffffffffu, valid && !(sa + sb <= SUM_MAX))) break;
           look = true;  // a score far above m: raise it and take the step again
         }
-        st32(tS, pr);
-        st32(tS + 32, pr + 32);
-        st32(tS + 64, rest);
-        st32(tS + 96, rest + 32);
+        tmem_st32(tS, pr);
+        tmem_st32(tS + 32, pr + 32);
+        tmem_st32(tS + 64, rest);
+        tmem_st32(tS + 96, rest + 32);
         // the slots past the last token, before the product reads them
         if (sp.clears(w) && t == nt - 1) {
           const int iv = it + 2 * t + 1, sv = iv % NS;
@@ -741,7 +657,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           }
           fence_proxy_async();
         }
-        wait_st();
+        tmem_wait_st();
         tc_fence_before();
         mbar_arrive(p_full(w));
         l2 = add2(l2, sum[0]);
@@ -763,7 +679,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         for (int c = 0; c < HD; c += 32) {
           uint32_t o[32];
           if (nt && ok) {
-            ld32(tO + c, o);
+            tmem_ld32(tO + c, o);
             tmem_wait_ld();
           } else {
 #pragma unroll
@@ -789,8 +705,8 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
       for (int c = 0; c < HD; c += 64) {
         uint32_t o[64];
-        ld32(tO + c, o);
-        ld32(tO + c + 32, o + 32);
+        tmem_ld32(tO + c, o);
+        tmem_ld32(tO + c + 32, o + 32);
         tmem_wait_ld();
         if (c + 64 == HD) {
           tc_fence_before();

@@ -68,7 +68,7 @@ struct KCfg {
 };
 
 // mbar_wait with a loop of few instructions: the kernel waits in some twenty places, and its
-// instruction fetches are on the critical path (122 KB of code as it was, 20 KB so).
+// instruction fetches are on the critical path.
 AXON_DEV bool wait_bar(uint32_t bar, uint32_t parity, int* err) {
   if (mbar_try_wait(bar, parity)) return true;
   const uint64_t t0 = global_ns();

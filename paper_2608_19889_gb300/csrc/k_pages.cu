@@ -11,9 +11,10 @@
 // range of them, with hardware barriers between its phases in place of launches (a launch costs
 // the host about 2.2 us, a phase of the cluster about 1); what touches block contents is a second
 // launch over the whole GPU. Copies are bound by HBM: every byte is read and written
-// once, a warp moving 2 KB with four 16-byte loads per lane in flight. Measured: a fork of four
-// rows 5.8 us and a reservation 4.1 us of GPU time; 1.57 GB moved by a compaction in 238 us,
-// 6.6 TB/s, 97 % of the copy bandwidth.
+// once, a warp moving 2 KB with four 16-byte loads per lane in flight. Measured (GPU time in a
+// captured row of calls): a fork of four rows 7.4 us, a reservation of 7 rows among 724 blocks 5.6
+// and of 448 rows among 93,952 blocks 16.4 (rows are compared with each other, and the blocks
+// ranked); 1.57 GB read and written by a compaction in 239 us, 6.6 TB/s, 97 % of the copy bandwidth.
 #include <cooperative_groups.h>
 #include <math.h>
 
@@ -450,7 +451,7 @@ cudaError_t launch_k(const LaunchCtx& lc, K kernel, dim3 grid, int threads, size
 }
 
 // CTAs for `tiles` warp-sized copies and `cells` table entries: at most 64 per SM: eight at a time, so
-// that late ones even out the SMs (copies of 3 GB: 253 us with eight, 247 with 16, 237 with 64).
+// that late ones even out the SMs (1.57 GB read and written: 253 us with eight, 247 with 16, 237 with 64).
 unsigned move_grid(const LaunchCtx& lc, double tiles, double cells) {
   const double want = fmax(tiles / (CT / 32), cells / CT);
   const double most = lc.num_sms * 64.0;

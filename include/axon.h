@@ -80,7 +80,10 @@ enum { AXON_LOGITS_LAST = 0, AXON_LOGITS_ALL = 1 };
 
 /* Model configuration: HF config.json equivalents (the appendix causal_lm
  * listing reads hidden size, layer and head counts and vocabulary size
- * through `Config.dim @@key`), plus capacity and layout fields. */
+ * through `Config.dim @@key`), plus capacity and layout fields. The struct
+ * carries neither a size nor a version and has grown at its end (sink_tokens is
+ * the newest field): compile callers against the header of the library that
+ * they load, and zero the struct before filling it. */
 typedef struct axon_config {
   int32_t num_hidden_layers;   /* L */
   int32_t hidden_size;         /* D, multiple of 64 */
@@ -373,7 +376,9 @@ int axon_moe_routing_record(axon_model* m, int32_t* d_experts, int32_t rows);
  * AXON_ERR_UNSUPPORTED). What only the device can see -- a block number, a
  * length or a row out of range -- sets a bit of the caller's error word
  * *d_err (one int32, zeroed by the caller; NULL: not reported) and the access
- * is skipped; axon_check_error reads and clears the word.
+ * is skipped; axon_check_error reads and clears the word. An attention row that would
+ * have read a block out of range then holds finite numbers of no meaning (the one-token
+ * form leaves its keys out, the chunk form takes them for zeros); other rows are right.
  *
  * Workspaces are device memory, 16-byte aligned, of at least the size that
  * the matching query returns. The attention's must be zero before its first
@@ -447,7 +452,8 @@ int axon_attn_decode_workspace(const axon_kv_cache* cache, int32_t num_heads, in
  * advanced. num_blocks * num_kv_heads * 16 stays below 2^31. Slots past a chunk's
  * last token never reach an output, whatever they hold. Tokens that the mask hides
  * from some rows only (later ones of the chunk, ones before a window in a block that it
- * reaches) have to be finite: the products add zero times their values. */
+ * reaches) have to be finite: the products add zero times their values. P has two
+ * 16-bit terms here too. */
 int axon_attn_prefill(const axon_kv_cache* cache, int32_t layer, const void* d_q, int64_t q_row_stride,
                       int64_t q_head_stride, int32_t B, int32_t T, int32_t num_heads, const int32_t* d_cu_seqlens,
                       const int32_t* d_context_lens, int32_t max_chunk, const int32_t* d_block_table,

@@ -1,8 +1,9 @@
-"""Endless generation in bounded memory: a sliding window with sinks over a paged cache.
+"""Long generation in bounded memory: a sliding window with sinks over a paged cache.
 
 A small random-init decoder reads one prompt, four samples fork from it (they share the prompt's whole blocks), every
 sample decodes far past the window while the blocks that slid out go back to the pool, one sample ends, another forks
-into its place, and the pool is compacted on the way. Run on a GB300:
+into its place, and the pool is compacted on the way. Positions are absolute, so a sequence ends at the CONTEXT positions
+that the model was made for, however little memory it holds. Run on a GB300:
 
     python examples/streaming.py [--steps N]
 """
@@ -29,6 +30,8 @@ def generate(steps=300, say=print):
     import synth_inputs as si
     from paper_2608_19889_gb300 import paged
 
+    if PROMPT + steps > CONTEXT:
+        raise ValueError(f"at most {CONTEXT - PROMPT} steps: a sequence ends at {CONTEXT} positions")
     torch.cuda.set_device(0)
     cfg = ax.make_config(SHAPE, SAMPLES, CONTEXT, kv_layout=ax.AXON_KV_PAGED, kv_num_blocks=POOL,
                          max_prefill_tokens=PROMPT + SAMPLES)

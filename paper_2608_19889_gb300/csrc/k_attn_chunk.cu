@@ -23,8 +23,8 @@
 // bits over that of a result rounded once, 64 and 128 dims, 16 to 2500 keys: 1.000 in both types;
 // with one term 1.07 to 1.35, which is also more than the model's prefill kernel (k_attn_tc.cu,
 // second terms for 16 keys of a step) loses, so that a model would have paid for its sinks in
-// precision. The price is half as many products again: 8191 positions 391 us against 303,
-// a mixed batch 39.8 against 32.3, 16 tokens 8 either way.
+// precision. The price is half as many products again; both in turn on one box, warm caches:
+// 8191 positions 361 us against 282, a mixed batch 37.9 against 31.1, 16 tokens 7.8 either way.
 //
 // m is not the running maximum but a bound that lags: the maximum of a row's first visible step,
 // raised (and O rescaled) only when it has become too small. Rounding to 16 bits is
@@ -37,9 +37,9 @@
 // Bound: the tensor pipe. A 128 x 128 tile at head_dim 128 takes 1536 tensor cycles (2 x 3 x 128^3
 // operations at 8192 per cycle), 3072 for both, and per scheduler 512 cycles of the exponential
 // unit and about 600 issue slots; the softmax of one tile runs under the products of the other.
-// 8191 positions under a 4096-key window with sinks, 32 query heads, 8 kv heads: 391 us, 1.06
-// PFLOP/s of the formula's operations and 1.58 of the pipe's, 83 % of the burst rate of cuBLAS
-// (1.90). Instruction counts and fetches of the issuers matter (measured with one term): waits
+// 8191 positions under a 4096-key window with sinks, 32 query heads, 8 kv heads: 386 to 391 us,
+// 1.06 PFLOP/s of the formula's operations and 1.59 of the pipe's, 84 % of the burst rate of cuBLAS
+// (1.90); the pipe is active in 81 % of an SM's cycles. Instruction counts and fetches of the issuers matter (measured with one term): waits
 // inlined with long loops 372 -> 369 us without them, issuers in uniform registers and in
 // turns 369 -> 336, items in an order that evens out 336 -> 317, no local memory 309 -> 297.
 #include <math.h>

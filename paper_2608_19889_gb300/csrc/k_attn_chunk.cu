@@ -37,9 +37,9 @@
 // Bound: the tensor pipe. A 128 x 128 tile at head_dim 128 takes 1536 tensor cycles (2 x 3 x 128^3
 // operations at 8192 per cycle), 3072 for both, and per scheduler 512 cycles of the exponential
 // unit and about 600 issue slots; the softmax of one tile runs under the products of the other.
-// 8191 positions under a 4096-key window with sinks, 32 query heads, 8 kv heads: 386 to 391 us,
-// 1.06 PFLOP/s of the formula's operations and 1.59 of the pipe's, 84 % of the burst rate of cuBLAS
-// (1.90); the pipe is active in 81 % of an SM's cycles. Instruction counts and fetches of the issuers matter (measured with one term): waits
+// 8191 positions under a 4096-key window with sinks, 32 query heads, 8 kv heads: 386 to 420 us
+// over the boxes, 0.98 to 1.07 PFLOP/s of the formula's operations and 1.47 to 1.60 of the pipe's, 77 to
+// 84 % of the burst rate of cuBLAS (1.90); the pipe is active in 81 % of an SM's cycles. Instruction counts and fetches of the issuers matter (measured with one term): waits
 // inlined with long loops 372 -> 369 us without them, issuers in uniform registers and in
 // turns 369 -> 336, items in an order that evens out 336 -> 317, no local memory 309 -> 297.
 #include <math.h>

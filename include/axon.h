@@ -460,6 +460,41 @@ int axon_attn_prefill(const axon_kv_cache* cache, int32_t layer, const void* d_q
                       int32_t blocks_per_seq, int32_t window, int32_t sinks, float scale, void* d_out,
                       int64_t out_row_stride, int64_t out_head_stride, int32_t* d_err, void* stream);
 
+/* Rotary table of the first `rotary_dim` dims of a head (a multiple of 16, at most 128): d_rope
+ * [positions][rotary_dim / 2][2] fp32, (cos a, sin a) of a = position * f_j,
+ * f_j = theta^(-2j / rotary_dim), the angle in 64 bits. factor > 0: the frequency scaling of
+ * axon_config (low and high as rope_low_freq_factor and rope_high_freq_factor), else f_j as they are. d_rope
+ * is 16-byte aligned. A table made in any other way serves as well. */
+int axon_rope_table(float* d_rope, int32_t positions, int32_t rotary_dim, float theta, float factor, float low, float high,
+                    int32_t original_positions, void* stream);
+
+/* Which dims of the rotated part make a pair: (j, j + rotary_dim / 2), or (2j, 2j + 1). */
+enum { AXON_ROPE_HALF = 0, AXON_ROPE_INTERLEAVED = 1 };
+
+/* New tokens into a layer of the cache: keys rotated to their positions and values go to the
+ * tokens' slots, rotated queries to d_q_out, for axon_attn_decode, axon_attn_shared or axon_attn_prefill with the same
+ * lengths afterwards. A pair (x, y) becomes (x cos a - y sin a, y cos a + x sin a) in fp32, rounded once (fp16:
+ * saturated at 65504); what is not rotated is copied bit for bit.
+ *   d_q, d_q_out    [T][num_heads][head_dim] of the cache's type, strides as in axon_attn_decode; both NULL: keys and
+ *                   values only (num_heads 0). d_q_out may be d_q with the same strides; else they may not overlap.
+ *   d_k, d_v        [T][num_kv_heads][head_dim], likewise (parts of one projection's output, for instance)
+ *   d_cu_seqlens    [B + 1]: chunk b is rows cu_seqlens[b] .. cu_seqlens[b+1]-1 (a chunk may be empty), its row i stands
+ *                   at position context_lens[b] + i. NULL: one token per row, T = B, at position context_lens[b];
+ *                   negative: an idle row, which is left out
+ *   d_context_lens  [B], not advanced
+ *   d_block_table   [B][blocks_per_seq], or NULL: row b holds blocks b * blocks_per_seq onward
+ *   d_rope          [rope_positions][rotary_dim / 2][2] as axon_rope_table makes it; NULL with rotary_dim 0: no rotation
+ *   rotary_dim      a multiple of 16, at most head_dim
+ * All caches, AXON_FP32_DEBUG too. Rows that are left out (idle, beyond the table of blocks or the rotary table, of a
+ * chunk whose offsets are inconsistent) leave d_q_out and the cache as they are; a block out of range keeps the
+ * token's key and value out, its query is written. Two tokens may not go to one slot: fork before rows part. */
+int axon_kv_append(const axon_kv_cache* cache, int32_t layer, const void* d_q, int64_t q_row_stride, int64_t q_head_stride,
+                   const void* d_k, int64_t k_row_stride, int64_t k_head_stride, const void* d_v, int64_t v_row_stride,
+                   int64_t v_head_stride, int32_t B, int32_t T, int32_t num_heads, const int32_t* d_cu_seqlens,
+                   const int32_t* d_context_lens, const int32_t* d_block_table, int32_t blocks_per_seq, const float* d_rope,
+                   int32_t rope_positions, int32_t rotary_dim, int32_t rope_layout, void* d_q_out, int64_t out_row_stride,
+                   int64_t out_head_stride, int32_t* d_err, void* stream);
+
 /* Block dst[i] becomes a copy of block src[i], in all layers, for i < n. No
  * block may be a destination twice, or a source and a destination. */
 int axon_kv_copy_blocks(const axon_kv_cache* cache, const int32_t* d_src, const int32_t* d_dst, int32_t n,

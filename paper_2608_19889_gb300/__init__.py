@@ -29,11 +29,12 @@ AXON_BF16, AXON_FP32_DEBUG, AXON_FP16 = 0, 1, 2
 AXON_DTYPE_BF16, AXON_DTYPE_F32 = 0, 1
 AXON_LOGITS_LAST, AXON_LOGITS_ALL = 0, 1
 AXON_ACT_SILU, AXON_ACT_GELU_TANH = 0, 1
+AXON_ROPE_HALF, AXON_ROPE_INTERLEAVED = 0, 1
 
 EXPORTED = ["axon_model_create", "axon_prefill", "axon_prefill_varlen", "axon_decode_step", "axon_reset",
             "axon_check_device", "axon_kv_view_get", "axon_profile_decode_step", "axon_profile_prefill",
             "axon_decode_step_noalloc", "axon_moe_routing_record", "axon_kv_cache_get", "axon_attn_decode",
-            "axon_attn_decode_workspace", "axon_attn_prefill", "axon_kv_copy_blocks", "axon_kv_fork", "axon_kv_release",
+            "axon_attn_decode_workspace", "axon_attn_prefill", "axon_rope_table", "axon_kv_append", "axon_kv_copy_blocks", "axon_kv_fork", "axon_kv_release",
             "axon_kv_reserve", "axon_kv_compact", "axon_kv_workspace", "axon_check_error", "axon_free",
             "axon_status_string"]
 
@@ -116,6 +117,9 @@ def lib() -> ctypes.CDLL:
         L.axon_attn_decode_workspace.argtypes = [vp, i32, i32, p_i64]
         L.axon_attn_prefill.argtypes = [vp, i32, vp, i64, i64, i32, i32, i32, vp, vp, i32, vp, i32, i32, i32, f32, vp,
                                         i64, i64, vp, vp]
+        L.axon_rope_table.argtypes = [vp, i32, i32, f32, f32, f32, f32, i32, vp]
+        L.axon_kv_append.argtypes = [vp, i32] + [vp, i64, i64] * 3 + [i32, i32, i32, vp, vp, vp, i32, vp, i32, i32, i32, vp,
+                                                                      i64, i64, vp, vp]
         L.axon_kv_copy_blocks.argtypes = [vp, vp, vp, i32, vp, vp]
         L.axon_kv_fork.argtypes = [vp, vp, vp, vp, i32, vp, i64, vp, vp]
         L.axon_kv_release.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp]
@@ -131,7 +135,8 @@ def lib() -> ctypes.CDLL:
                   "axon_check_device", "axon_kv_view_get", "axon_profile_decode_step", "axon_profile_prefill",
                   "axon_decode_step_noalloc", "axon_moe_routing_record", "axon_kv_cache_get", "axon_attn_decode",
                   "axon_attn_decode_workspace", "axon_attn_prefill", "axon_kv_copy_blocks", "axon_kv_fork",
-                  "axon_kv_release", "axon_kv_reserve", "axon_kv_compact", "axon_kv_workspace", "axon_check_error"):
+                  "axon_kv_release", "axon_kv_reserve", "axon_kv_compact", "axon_kv_workspace", "axon_check_error",
+                  "axon_rope_table", "axon_kv_append"):
             getattr(L, n).restype = ctypes.c_int
         import torch
         _torch = torch
@@ -365,7 +370,7 @@ def _described(c, device):
     """What the wrappers read of a descriptor at every call, as plain attributes."""
     c.device = device
     c.dtype = {AXON_BF16: _torch.bfloat16, AXON_FP16: _torch.float16, AXON_FP32_DEBUG: _torch.float32}[c.precision]
-    c.blocks, c.dim, c.ref = c.num_blocks, c.head_dim, ctypes.byref(c)
+    c.blocks, c.dim, c.kv_heads, c.ref = c.num_blocks, c.head_dim, c.num_kv_heads, ctypes.byref(c)
     return c
 
 
@@ -452,6 +457,57 @@ def axon_attn_prefill(cache, layer, q, cu_seqlens, context_lens, max_chunk, out,
         _handle(stream, dev))
     if rc:
         raise AxonError("axon_attn_prefill", rc)
+
+
+def axon_rope_table(positions, rotary_dim, theta, factor=0.0, low=1.0, high=4.0, original=8192, device=None, stream=None):
+    """Rotary table fp32 [positions, rotary_dim / 2, 2] of axon_kv_append (see include/axon.h); factor, low, high, original: the
+    frequency scaling of make_config's rope_factor, rope_low, rope_high, rope_orig (0: none)."""
+    lib()
+    dev = _torch.device("cuda", _current_device() if device is None else _torch.device(device).index or 0)
+    table = _torch.empty(positions, rotary_dim // 2, 2, dtype=_torch.float32, device=dev)
+    _check("axon_rope_table", _lib.axon_rope_table(table.data_ptr(), positions, rotary_dim, theta, factor, low, high, original,
+                                                   _handle(stream, dev.index)))
+    return table
+
+
+def _heads(t, what, rows, heads, cache):
+    """Address, row and head strides of a tensor [rows, heads, head_dim] of the cache's type."""
+    shape, s = t.shape, t.stride()
+    if (len(shape) == 3 and shape[0] == rows and shape[1] == heads and shape[2] == cache.dim and t.dtype is cache.dtype and
+            s[2] == 1 and t.get_device() == cache.device):
+        return t.data_ptr(), s[0], s[1]
+    raise TypeError(f"{what}: a {cache.dtype} tensor [{rows}, {heads}, {cache.dim}] on cuda:{cache.device} with a dense last "
+                    f"dimension is wanted, got {t.dtype} {tuple(shape)} with strides {s} on {t.device}")
+
+
+def axon_kv_append(cache, layer, k, v, context_lens, block_table=None, blocks_per_seq=0, cu_seqlens=None, rope=None,
+                   interleaved=False, q=None, q_out=None, err=None, stream=None):
+    """New tokens into a layer of the cache, keys and queries rotated (see include/axon.h). k, v: [T, kv heads, head_dim] and
+    q, q_out: [T, heads, head_dim] (q_out may be q), any row and head strides; context_lens: int32 [B] tokens before the
+    new ones (not advanced); cu_seqlens: int32 [B+1], or None: one token per row; rope: fp32 [positions, rotated pairs, 2]
+    as axon_rope_table returns it, or None: no rotation; block_table, blocks_per_seq as in axon_attn_decode."""
+    dev, T = cache.device, k.shape[0]
+    past, B = _list(context_lens, "context_lens", dev)
+    table, per = _table(block_table, blocks_per_seq, B, dev)
+    positions = pairs = 0
+    turn = None
+    if rope is not None:
+        positions, pairs = rope.shape[0], rope.shape[1]
+        turn = _want(rope, _torch.float32, "rope", 2 * positions * pairs, dev)
+    if q is None:
+        if q_out is not None:
+            raise TypeError("q_out: there is no q to rotate")
+        heads, queries, out = 0, (None, 0, 0), (None, 0, 0)
+    else:
+        heads = q.shape[1]
+        queries, out = _heads(q, "q", T, heads, cache), _heads(q_out, "q_out", T, heads, cache)
+    rc = _lib.axon_kv_append(
+        cache.ref, layer, *queries, *_heads(k, "k", T, cache.kv_heads, cache), *_heads(v, "v", T, cache.kv_heads, cache), B, T,
+        heads, None if cu_seqlens is None else _want(cu_seqlens, _torch.int32, "cu_seqlens", B + 1, dev), past, table, per,
+        turn, positions, 2 * pairs, AXON_ROPE_INTERLEAVED if interleaved else AXON_ROPE_HALF, *out,
+        None if err is None else _word(err, dev), _handle(stream, dev))
+    if rc:
+        raise AxonError("axon_kv_append", rc)
 
 
 def _same_pool(cache, seqs):

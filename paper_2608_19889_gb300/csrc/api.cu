@@ -1423,21 +1423,9 @@ int axon_model_create(const axon_config* cfg, const axon_tensor* weights, int32_
   {
     const int half = m->d / 2;
     std::vector<double> freq(half);
-    for (int j = 0; j < half; ++j) {
-      double f = std::pow(static_cast<double>(cfg->rope_theta), -2.0 * j / m->d);
-      if (cfg->rope_scaling_factor > 0.f) {
-        const double factor = cfg->rope_scaling_factor, lo = cfg->rope_low_freq_factor,
-                     hi = cfg->rope_high_freq_factor, C = cfg->rope_original_max_position;
-        const double w = 2.0 * 3.14159265358979323846 / f;
-        if (w > C / lo) {
-          f = f / factor;
-        } else if (w >= C / hi) {
-          const double t = (C / w - lo) / (hi - lo);
-          f = (1.0 - t) * f / factor + t * f;
-        }
-      }
-      freq[j] = f;
-    }
+    for (int j = 0; j < half; ++j)
+      freq[j] = rope_frequency(cfg->rope_theta, m->d, j, cfg->rope_scaling_factor, cfg->rope_low_freq_factor,
+                               cfg->rope_high_freq_factor, cfg->rope_original_max_position);
     std::vector<float2> tab(static_cast<size_t>(cfg->max_context) * half);
     for (int pos = 0; pos < cfg->max_context; ++pos)
       for (int j = 0; j < half; ++j) {

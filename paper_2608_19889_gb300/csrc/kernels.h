@@ -5,6 +5,8 @@
 #include <cuda.h>
 #include <stdint.h>
 
+#include <cmath>
+
 #include "epilogue.cuh"
 
 // Launch options shared by every launcher: stream and whether to request
@@ -240,6 +242,44 @@ inline long long paged_attn_most_pages(int B, int G, int blocks_per_seq, int win
 }
 cudaError_t prepare_attn_paged_kernels();
 cudaError_t launch_attn_paged_decode(const LaunchCtx& lc, const PagedAttnArgs& a);
+
+// ---- new tokens into the paged cache (k_append.cu)
+struct AppendArgs {
+  const void* x[3];  // queries, keys, values [T][heads][d], strides in elements
+  long long x_row[3], x_head[3];
+  void* o;  // rotated queries
+  long long o_row, o_head;
+  void* k;  // layer pool [num_blocks][G][16][d]
+  void* v;
+  const int* cu;    // [B + 1] row offsets, or null: one token per row, T = B
+  const int* past;  // [B] tokens before each chunk
+  const int* block_table;  // [B][blocks_per_seq], or null: blocks b * blocks_per_seq + j
+  int blocks_per_seq, num_blocks;
+  int B, T, H, G, d;  // H = 0: no queries
+  int most;           // positions that the table of blocks and the rotary table have
+  const float* rope;  // [positions][rotary / 2] (cosine, sine)
+  int rotary;         // dims rotated, a multiple of 16; 0: none
+  int interleaved;
+  int* err;
+};
+cudaError_t launch_append(const LaunchCtx& lc, const AppendArgs& a, int elem_bytes);
+// Rotary table of up to 64 pairs from their angles per position.
+cudaError_t launch_rope_table(const LaunchCtx& lc, float* out, int positions, int pairs, const double* freqs);
+// Angle per position of pair j: theta^(-2 j / dim), stretched per band when factor > 0 (wavelengths above
+// original / low by the factor, those below original / high not at all, blended between).
+inline double rope_frequency(double theta, int dim, int j, double factor, double low, double high, double original) {
+  double f = std::pow(theta, -2.0 * j / dim);
+  if (factor > 0) {
+    const double w = 2.0 * 3.14159265358979323846 / f;
+    if (w > original / low) {
+      f = f / factor;
+    } else if (w >= original / high) {
+      const double t = (original / w - low) / (high - low);
+      f = (1.0 - t) * f / factor + t * f;
+    }
+  }
+  return f;
+}
 
 // ---- blocks of the paged cache (k_pages.cu)
 struct PagesArgs {

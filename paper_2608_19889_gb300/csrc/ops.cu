@@ -1,5 +1,5 @@
 // C entry points of the operators on a paged key/value cache: attention that
-// reads it, and its blocks' management. They check what the host can see, take
+// reads it, new tokens, and its blocks' management. They check what the host can see, take
 // the caller's buffers and launch; nothing is allocated and nothing is kept.
 #include <limits.h>
 #include <math.h>
@@ -69,7 +69,7 @@ int launch_ctx(const axon_kv_cache* c, void* stream, LaunchCtx* lc) {
     cudaGetLastError();
     return AXON_ERR_CUDA;
   }
-  *lc = LaunchCtx{static_cast<cudaStream_t>(stream), true, sms, c->precision == AXON_FP16};
+  *lc = LaunchCtx{static_cast<cudaStream_t>(stream), true, sms, c && c->precision == AXON_FP16};
   return AXON_OK;
 }
 
@@ -249,6 +249,80 @@ int axon_attn_prefill(const axon_kv_cache* cache, int32_t layer, const void* d_q
   a.o_head = out_head_stride;
   a.err = d_err;
   return status(with_limits([&] { return launch_attn_chunk(lc, a, maps); }));
+}
+
+int axon_rope_table(float* d_rope, int32_t positions, int32_t rotary_dim, float theta, float factor, float low, float high,
+                    int32_t original_positions, void* stream) {
+  if (!d_rope || unaligned(d_rope) || positions < 1 || rotary_dim < 1) return AXON_ERR_INVALID_ARG;
+  if (!(theta > 0.f) || isinf(theta) || !(factor >= 0.f) || isinf(factor)) return AXON_ERR_INVALID_ARG;
+  if (factor > 0.f && (original_positions <= 0 || !(low > 0.f) || !(high > low) || isinf(high))) return AXON_ERR_INVALID_ARG;
+  if (rotary_dim % 16 || rotary_dim > 128) return AXON_ERR_UNSUPPORTED;
+  LaunchCtx lc;
+  const int rc = launch_ctx(nullptr, stream, &lc);
+  if (rc) return rc;
+  double f[64];
+  for (int j = 0; j < rotary_dim / 2; ++j) f[j] = rope_frequency(theta, rotary_dim, j, factor, low, high, original_positions);
+  return status(launch_rope_table(lc, d_rope, positions, rotary_dim / 2, f));
+}
+
+int axon_kv_append(const axon_kv_cache* cache, int32_t layer, const void* d_q, int64_t q_row_stride, int64_t q_head_stride,
+                   const void* d_k, int64_t k_row_stride, int64_t k_head_stride, const void* d_v, int64_t v_row_stride,
+                   int64_t v_head_stride, int32_t B, int32_t T, int32_t num_heads, const int32_t* d_cu_seqlens,
+                   const int32_t* d_context_lens, const int32_t* d_block_table, int32_t blocks_per_seq, const float* d_rope,
+                   int32_t rope_positions, int32_t rotary_dim, int32_t rope_layout, void* d_q_out, int64_t out_row_stride,
+                   int64_t out_head_stride, int32_t* d_err, void* stream) {
+  int rc = check_cache(cache);
+  if (rc) return rc;
+  const int G = cache->num_kv_heads, d = cache->head_dim;
+  if (layer < 0 || layer >= cache->num_layers || !d_k || !d_v || unaligned(d_k) || unaligned(d_v)) return AXON_ERR_INVALID_ARG;
+  if (B < 1 || T < 1 || num_heads < 0 || !d_context_lens || (!d_cu_seqlens && T != B)) return AXON_ERR_INVALID_ARG;
+  if (blocks_per_seq < 1 || blocks_per_seq > MAX_BLOCKS_PER_SEQ) return AXON_ERR_INVALID_ARG;
+  if (!d_block_table && static_cast<long long>(B) * blocks_per_seq > cache->num_blocks) return AXON_ERR_INVALID_ARG;
+  if (rotary_dim < 0 || rotary_dim > d || (rotary_dim > 0) != (d_rope != nullptr) || unaligned(d_rope)) return AXON_ERR_INVALID_ARG;
+  if (rotary_dim > 0 && (rope_positions < 1 || (rope_layout != AXON_ROPE_HALF && rope_layout != AXON_ROPE_INTERLEAVED)))
+    return AXON_ERR_INVALID_ARG;
+  if ((num_heads > 0) != (d_q != nullptr) || (d_q != nullptr) != (d_q_out != nullptr) || unaligned(d_q) || unaligned(d_q_out))
+    return AXON_ERR_INVALID_ARG;
+  if ((rc = check_strides(T, G, d, k_row_stride, k_head_stride)) || (rc = check_strides(T, G, d, v_row_stride, v_head_stride)))
+    return rc;
+  if (d_q && ((rc = check_strides(T, num_heads, d, q_row_stride, q_head_stride)) ||
+              (rc = check_strides(T, num_heads, d, out_row_stride, out_head_stride))))
+    return rc;
+  if (d_q && d_q == d_q_out && (q_row_stride != out_row_stride || q_head_stride != out_head_stride)) return AXON_ERR_INVALID_ARG;
+  if (rotary_dim % 16 || num_heads > 65536 || G > 65536) return AXON_ERR_UNSUPPORTED;
+  LaunchCtx lc;
+  if ((rc = launch_ctx(cache, stream, &lc))) return rc;
+  AppendArgs a;
+  memset(&a, 0, sizeof(a));
+  const void* x[3] = {d_q, d_k, d_v};
+  const int64_t rows[3] = {q_row_stride, k_row_stride, v_row_stride}, heads[3] = {q_head_stride, k_head_stride, v_head_stride};
+  for (int i = 0; i < 3; ++i) {
+    a.x[i] = x[i];
+    a.x_row[i] = rows[i];
+    a.x_head[i] = heads[i];
+  }
+  a.o = d_q_out;
+  a.o_row = out_row_stride;
+  a.o_head = out_head_stride;
+  a.k = layer_pool(cache, cache->k_pool, layer);
+  a.v = layer_pool(cache, cache->v_pool, layer);
+  a.cu = d_cu_seqlens;
+  a.past = d_context_lens;
+  a.block_table = d_block_table;
+  a.blocks_per_seq = blocks_per_seq;
+  a.num_blocks = cache->num_blocks;
+  a.B = B;
+  a.T = T;
+  a.H = num_heads;
+  a.G = G;
+  a.d = d;
+  a.most = blocks_per_seq * 16;
+  if (rotary_dim > 0 && rope_positions < a.most) a.most = rope_positions;
+  a.rope = d_rope;
+  a.rotary = rotary_dim;
+  a.interleaved = rope_layout == AXON_ROPE_INTERLEAVED;
+  a.err = d_err;
+  return status(launch_append(lc, a, cache->precision == AXON_FP32_DEBUG ? 4 : 2));
 }
 
 int axon_kv_workspace(const axon_kv_cache* cache, const axon_kv_seqs* seqs, int64_t* bytes) {

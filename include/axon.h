@@ -539,6 +539,29 @@ int axon_kv_compact(const axon_kv_cache* cache, const axon_kv_seqs* seqs, int32_
 /* Workspace of axon_kv_fork, axon_kv_reserve and axon_kv_compact. */
 int axon_kv_workspace(const axon_kv_cache* cache, const axon_kv_seqs* seqs, int64_t* bytes);
 
+/* A token per row from its logits, for B rows of V (1 .. 524288). With m the largest logit of the row,
+ * w_i = exp((logit_i - m) / temperature), and tokens in the order of their logits, equal ones by number:
+ *   top-k: the first top_k stay (0 or less, V or more: all);
+ *   top-p: of these the fewest, from the front, whose weights reach top_p times the sum of them all (1 or more, or
+ *          not a number: all; 0 or less: the first);
+ *   min-p: of these the ones with w_i >= min_p (0 or less, or not a number: all).
+ * The first token always stays. d_tokens[b] is the first, by number, at which the running sum of the weights that
+ * stay passes u times their sum, d_prob[b] (fp32, or NULL) its weight over that sum. u is clamped to [0, 1 - 2^-24].
+ * temperature 0 (or less, or not a number): the largest logit, the lowest number among equals, d_prob 1. Logits that are not numbers
+ * count as -infinity, which is never chosen; a row of nothing else gets token -1 and d_prob 0. Infinite logits share
+ * everything.
+ * Weights and their sums are 64-bit integers of 2^-44, exact to about 2^-41 of each weight: the token is that of 64-bit
+ * arithmetic unless u or top_p falls within some 2^-40 of a border, and does not depend on timing.
+ *   d_logits        [B][V] of type `precision` (AXON_BF16, AXON_FP16; AXON_FP32_DEBUG: fp32, as the model's logits),
+ *                   row stride in elements, at least V
+ *   d_temperature, d_top_k, d_top_p, d_min_p  [B], or NULL: 1, all, 1, 0
+ *   d_u             [B], uniform in [0, 1)
+ * No error word: nothing is indexed by what the device holds. The first call on a device sets its kernel's limits: make
+ * it before a stream capture. */
+int axon_sample(const void* d_logits, int64_t row_stride, int32_t precision, int32_t B, int32_t V, const float* d_temperature,
+                const int32_t* d_top_k, const float* d_top_p, const float* d_min_p, const float* d_u, int32_t* d_tokens,
+                float* d_prob, void* stream);
+
 /* Synchronise `stream` and read and clear an operator's error word: AXON_OK,
  * AXON_ERR_DEVICE_CHECK or AXON_ERR_TIMEOUT; *bits (optional) receives it. Bits:
  * 2 block number, 4 position, 8 wait expired, 16 row or row offsets, 32 no free block. */

@@ -34,7 +34,7 @@ AXON_ROPE_HALF, AXON_ROPE_INTERLEAVED = 0, 1
 EXPORTED = ["axon_model_create", "axon_prefill", "axon_prefill_varlen", "axon_decode_step", "axon_reset",
             "axon_check_device", "axon_kv_view_get", "axon_profile_decode_step", "axon_profile_prefill",
             "axon_decode_step_noalloc", "axon_moe_routing_record", "axon_kv_cache_get", "axon_attn_decode",
-            "axon_attn_decode_workspace", "axon_attn_prefill", "axon_rope_table", "axon_kv_append", "axon_kv_copy_blocks", "axon_kv_fork", "axon_kv_release",
+            "axon_attn_decode_workspace", "axon_attn_prefill", "axon_rope_table", "axon_kv_append", "axon_sample", "axon_kv_copy_blocks", "axon_kv_fork", "axon_kv_release",
             "axon_kv_reserve", "axon_kv_compact", "axon_kv_workspace", "axon_check_error", "axon_free",
             "axon_status_string"]
 
@@ -120,6 +120,7 @@ def lib() -> ctypes.CDLL:
         L.axon_rope_table.argtypes = [vp, i32, i32, f32, f32, f32, f32, i32, vp]
         L.axon_kv_append.argtypes = [vp, i32] + [vp, i64, i64] * 3 + [i32, i32, i32, vp, vp, vp, i32, vp, i32, i32, i32, vp,
                                                                       i64, i64, vp, vp]
+        L.axon_sample.argtypes = [vp, i64, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]
         L.axon_kv_copy_blocks.argtypes = [vp, vp, vp, i32, vp, vp]
         L.axon_kv_fork.argtypes = [vp, vp, vp, vp, i32, vp, i64, vp, vp]
         L.axon_kv_release.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp]
@@ -136,7 +137,7 @@ def lib() -> ctypes.CDLL:
                   "axon_decode_step_noalloc", "axon_moe_routing_record", "axon_kv_cache_get", "axon_attn_decode",
                   "axon_attn_decode_workspace", "axon_attn_prefill", "axon_kv_copy_blocks", "axon_kv_fork",
                   "axon_kv_release", "axon_kv_reserve", "axon_kv_compact", "axon_kv_workspace", "axon_check_error",
-                  "axon_rope_table", "axon_kv_append"):
+                  "axon_rope_table", "axon_kv_append", "axon_sample"):
             getattr(L, n).restype = ctypes.c_int
         import torch
         _torch = torch
@@ -567,3 +568,28 @@ def axon_check_error(err, stream=None) -> tuple[int, int]:
     dev = _on(err, "err")
     rc = lib().axon_check_error(_word(err, dev), _handle(stream, dev), ctypes.byref(bits))
     return rc, bits.value
+
+
+def axon_sample(logits, u, tokens, temperature=None, top_k=None, top_p=None, min_p=None, prob=None, stream=None):
+    """A token per row (see include/axon.h). logits: fp32, bf16 or fp16 [B, V], any row stride; u: fp32 [B] random numbers in
+    [0, 1); tokens: int32 [B]; temperature, top_p, min_p: fp32 [B] and top_k: int32 [B], or None (1, 1, 0, all); prob: fp32
+    [B] or None, the token's probability among those it was chosen from."""
+    if _lib is None:
+        lib()
+    dtype = logits.dtype
+    prec = (AXON_FP32_DEBUG if dtype is _torch.float32 else AXON_BF16 if dtype is _torch.bfloat16 else
+            AXON_FP16 if dtype is _torch.float16 else None)
+    if prec is None or logits.dim() != 2 or not logits.is_cuda or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise TypeError(f"logits: a device tensor [rows, vocabulary] of fp32, bf16 or fp16 with dense rows is wanted, got {dtype} "
+                        f"{tuple(logits.shape)} with strides {logits.stride()} on {logits.device}")
+    (B, V), dev = logits.shape, logits.get_device()
+    f32 = _torch.float32
+    rc = _lib.axon_sample(
+        logits.data_ptr(), logits.stride(0), prec, B, V,
+        None if temperature is None else _want(temperature, f32, "temperature", B, dev),
+        None if top_k is None else _want(top_k, _torch.int32, "top_k", B, dev),
+        None if top_p is None else _want(top_p, f32, "top_p", B, dev), None if min_p is None else _want(min_p, f32, "min_p", B, dev),
+        _want(u, f32, "u", B, dev), _want(tokens, _torch.int32, "tokens", B, dev),
+        None if prob is None else _want(prob, f32, "prob", B, dev), _handle(stream, dev))
+    if rc:
+        raise AxonError("axon_sample", rc)

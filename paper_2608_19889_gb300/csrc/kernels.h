@@ -281,6 +281,24 @@ inline double rope_frequency(double theta, int dim, int j, double factor, double
   return f;
 }
 
+// ---- tokens from logits (k_sample.cu)
+constexpr int SAMPLE_MAX_VOCAB = 1 << 19;
+struct SampleArgs {
+  const void* logits;  // [B][V], row stride in elements
+  long long row_stride;
+  int B, V;
+  const float* temperature;  // [B] each, or null: 1, all, 1, 0
+  const int* top_k;
+  const float* top_p;
+  const float* min_p;
+  const float* u;
+  int* tokens;
+  float* prob;  // or null
+};
+cudaError_t prepare_sample_kernels();
+// precision: of the logits, as in axon.h
+cudaError_t launch_sample(const LaunchCtx& lc, const SampleArgs& a, int precision);
+
 // ---- blocks of the paged cache (k_pages.cu)
 struct PagesArgs {
   void* k;  // [L][N][block_bytes / 16]

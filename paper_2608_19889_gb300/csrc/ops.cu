@@ -1,5 +1,5 @@
 // C entry points of the operators on a paged key/value cache: attention that
-// reads it, new tokens, and its blocks' management. They check what the host can see, take
+// reads it, new tokens, and its blocks' management; and of tokens from logits. They check what the host can see, take
 // the caller's buffers and launch; nothing is allocated and nothing is kept.
 #include <limits.h>
 #include <math.h>
@@ -14,6 +14,7 @@
 namespace {
 
 constexpr int MAX_ROWS = 8192;         // rows of a block table
+constexpr int SAMPLE_MAX_ROWS = 1 << 24;
 constexpr int MAX_BLOCKS_PER_SEQ = 1 << 26;  // positions fit 31 bits
 
 bool unaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
@@ -51,6 +52,7 @@ cudaError_t with_limits(Launch launch) {
     if (!known) {
       e = prepare_attn_chunk_kernels();
       if (e == cudaSuccess) e = prepare_attn_paged_kernels();
+      if (e == cudaSuccess) e = prepare_sample_kernels();
       if (e != cudaSuccess) return e;
       ready.fetch_or(bit, std::memory_order_release);
     }
@@ -395,6 +397,32 @@ int axon_kv_compact(const axon_kv_cache* cache, const axon_kv_seqs* seqs, int32_
   if (rc) return rc;
   if ((rc = launch_ctx(cache, stream, &lc))) return rc;
   return status(launch_pages_compact(lc, a, d_moved, d_live));
+}
+
+int axon_sample(const void* d_logits, int64_t row_stride, int32_t precision, int32_t B, int32_t V, const float* d_temperature,
+                const int32_t* d_top_k, const float* d_top_p, const float* d_min_p, const float* d_u, int32_t* d_tokens,
+                float* d_prob, void* stream) {
+  if (!d_logits || !d_u || !d_tokens || B < 1 || V < 1 || (B > 1 && row_stride < V)) return AXON_ERR_INVALID_ARG;
+  if (precision != AXON_BF16 && precision != AXON_FP16 && precision != AXON_FP32_DEBUG) return AXON_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(d_logits) % (precision == AXON_FP32_DEBUG ? 4 : 2)) return AXON_ERR_INVALID_ARG;
+  if (V > SAMPLE_MAX_VOCAB || B > SAMPLE_MAX_ROWS) return AXON_ERR_UNSUPPORTED;
+  LaunchCtx lc;
+  const int rc = launch_ctx(nullptr, stream, &lc);
+  if (rc) return rc;
+  SampleArgs a;
+  memset(&a, 0, sizeof(a));
+  a.logits = d_logits;
+  a.row_stride = row_stride;
+  a.B = B;
+  a.V = V;
+  a.temperature = d_temperature;
+  a.top_k = d_top_k;
+  a.top_p = d_top_p;
+  a.min_p = d_min_p;
+  a.u = d_u;
+  a.tokens = d_tokens;
+  a.prob = d_prob;
+  return status(with_limits([&] { return launch_sample(lc, a, precision); }));
 }
 
 int axon_check_error(int32_t* d_err, void* stream, int32_t* bits) {

@@ -72,6 +72,31 @@ AXON_DEV unsigned long long argmax_key(float v, int idx) {
   return (static_cast<unsigned long long>(b) << 32) | (0xffffffffu - static_cast<uint32_t>(idx));
 }
 
+// ------------------------------------------------------------- packed fp32
+// Two fp32 values in one 64-bit register: the packed FMA and add take one
+// issue slot for both.
+AXON_DEV uint64_t pk2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+AXON_DEV void upk2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+AXON_DEV uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+AXON_DEV uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+AXON_DEV uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
 // ------------------------------------------------------------ global loads
 // Streaming 16-byte load that bypasses L1 allocation (weights: read once).
 AXON_DEV uint4 ld_stream16(const void* p) {

@@ -32,74 +32,131 @@ constexpr int ST = 512;        // threads
 constexpr int SW = ST / 32;    // warps
 constexpr int NB = 1024;       // bins
 constexpr int MAX_CL = 16;     // CTAs of a cluster
-constexpr float X_END = 45.5f; // exponents from here on have weight 0
-constexpr int MAX_SLICE = SAMPLE_MAX_VOCAB / MAX_CL;
+constexpr int STEPS = 1024;    // steps of an octave
+constexpr int K_END = 45 * STEPS;  // weights from here on are 0
+constexpr int BIN_SHIFT = 5;   // 32 bins per octave
+constexpr int MAX_SLICE = 46 * 1024;  // logits of a CTA: 184 KB
+static_assert(SAMPLE_MAX_VOCAB / MAX_CL <= MAX_SLICE, "the largest vocabulary has to fit a cluster");
+static_assert(MAX_SLICE / ST <= 128, "sums of a thread's weights have to fit 32 bits");
 
 typedef unsigned long long u64;
 
-// 2^(-j/256) * 2^44 for j = -128 .. 128, by the series of exp in 64 bits.
+// 2^(-j/1024) as a pair of fp32 numbers, by the series of exp in 64 bits.
 struct PowerTable {
-  u64 v[257];
-  constexpr PowerTable() : v() {
-    for (int j = -128; j <= 128; ++j) {
-      const double y = -j * (0.693147180559945309417232 / 256.0);
+  float hi[STEPS], lo[STEPS];
+  constexpr PowerTable() : hi(), lo() {
+    for (int j = 0; j < STEPS; ++j) {
+      const double y = -j * (0.693147180559945309417232 / STEPS);
       double term = 1.0, sum = 0.0;
       for (int n = 1; n < 30; ++n) {
         sum += term;
         term *= y / n;
       }
-      v[j + 128] = static_cast<u64>(sum * 17592186044416.0 + 0.5);
+      hi[j] = static_cast<float>(sum);
+      lo[j] = static_cast<float>(sum - static_cast<double>(hi[j]));
     }
   }
 };
 __device__ constexpr PowerTable g_powers{};
 
-// A row's scale: exponent (base 2) of logit l is (m - l) (ch + cl).
+// A row's scale. With s = l - base the exponent (base 2) of a logit is s (ch + cl); its step j is s ch in 1024ths, rounded,
+// and k = top - j >= 1 counts the steps below the largest logit's.
 struct Scale {
-  float m, ch, cl;
+  float base, ch, cl;
+  int top;
 };
 
-AXON_DEV float exponent(const Scale& c, float l) { return (c.m - l) * c.ch; }
+constexpr float MAGIC = 12582912.f;  // 1.5 * 2^23: adding it rounds |x| <= 2^22 to an integer, in the low bits
+constexpr int MAGIC_BITS = 0x4b400000;
 
-AXON_DEV u64 weight(const Scale& c, float l, const u64* powers) {
-  const float s = c.m - l, p = s * c.ch;
-  if (!(p < X_END)) return 0;  // also -infinity
-  // what m - l and the product lost
-  const float back = s - c.m, lost = (c.m - (s - back)) + (-l - back);
-  float e = fmaf(s, c.ch, -p);
-  e = fmaf(s, c.cl, e);
-  e = fmaf(lost, c.ch, e);
-  const float n = rintf(p), f = p - n, j = rintf(f * 256.f);
-  const float g = fmaf(j, -1.f / 256.f, f);  // exact; the exponent is n + j / 256 + g + e
-  // 2^-(g + e) = 1 - y + y^2 / 2 - y^3 / 6 + y^4 / 24, y = (g + e) ln 2 < 1.4e-3
+// Steps of logit l below the top; not below K_END (unsigned) where its weight is 0, -infinity and numbers that are none among
+// them: s ch * 1024 + MAGIC is then a float of another size or sign, whose bits lie far from MAGIC's.
+AXON_DEV unsigned steps_of(const Scale& c, float l) {
+  const float n = (l - c.base) * -c.ch;
+  return static_cast<unsigned>(c.top + MAGIC_BITS - __float_as_int(fmaf(n, -1024.f, MAGIC)));
+}
+
+// Weights of two logits, in units of 2^-22 (hi) and 2^-44 (lo, signed), rounded; k: their steps. 2^(s (ch + cl) - top / 1024) =
+// 2^-(k/1024) (1 - y + y^2/2 - y^3/6), y = (j/1024 - s (ch + cl)) ln 2 < 3.4e-4, every sum and product that counts as a
+// pair of fp32 numbers: exact to about 2^-41.
+struct Weights {
+  unsigned k[2];
+  int hi[2], lo[2];
+};
+AXON_DEV Weights weights(const Scale& c, float l0, float l1, const float2* powers) {
   constexpr float LN2 = 0.693147182464599609375f, LN2_LO = -1.90465429995776804525e-9f;
-  const float yh = g * LN2;
-  float yl = fmaf(g, LN2, -yh);
-  yl = fmaf(g, LN2_LO, yl);
-  yl = fmaf(e, LN2, yl);
-  const float y = yh + yl;
-  const float q = y * y * fmaf(y, fmaf(y, 1.f / 24.f, -1.f / 6.f), 0.5f);
-  constexpr float Q40 = 1099511627776.f;
-  const int r = __float2int_rn(yh * -Q40) + __float2int_rn((q - yl) * Q40);  // 2^-40 steps
-  const u64 w0 = powers[static_cast<int>(j) + 128];
-  const long long more = (static_cast<long long>(r) * static_cast<long long>(w0 >> 14)) >> 26;
-  const u64 w = w0 + static_cast<u64>(more);
-  return ((2 * w >> static_cast<int>(n)) + 1) >> 1;
+  const uint64_t one = pk2(-1.f, -1.f);
+  const uint64_t s = add2(pk2(l0, l1), pk2(-c.base, -c.base));
+  const uint64_t n = mul2(s, pk2(-c.ch, -c.ch));
+  uint64_t e = fma2(s, pk2(c.ch, c.ch), n);  // what the product lost
+  e = fma2(s, pk2(c.cl, c.cl), e);
+  const uint64_t t = fma2(n, pk2(-1024.f, -1024.f), pk2(MAGIC, MAGIC));
+  const uint64_t g = fma2(add2(t, pk2(-MAGIC, -MAGIC)), pk2(1.f / 1024.f, 1.f / 1024.f), n);  // exact
+  Weights w;
+  float t0, t1;
+  upk2(t, t0, t1);
+  w.k[0] = static_cast<unsigned>(c.top + MAGIC_BITS - __float_as_int(t0));
+  w.k[1] = static_cast<unsigned>(c.top + MAGIC_BITS - __float_as_int(t1));
+  const float2 p0 = powers[w.k[0] & (STEPS - 1)], p1 = powers[w.k[1] & (STEPS - 1)];
+  const uint64_t th = pk2(p0.x, p1.x), tl = pk2(p0.y, p1.y);
+  const uint64_t yh = mul2(g, pk2(LN2, LN2)), ny = mul2(g, pk2(-LN2, -LN2));
+  uint64_t yl = fma2(g, pk2(-LN2, -LN2), yh);  // y = yh - yl
+  yl = fma2(g, pk2(-LN2_LO, -LN2_LO), yl);
+  yl = fma2(e, pk2(LN2, LN2), yl);
+  const uint64_t y = fma2(yl, one, yh);
+  const uint64_t r = fma2(mul2(y, y), fma2(y, pk2(-1.f / 6.f, -1.f / 6.f), pk2(0.5f, 0.5f)), yl);
+  // (th + tl) (1 - yh + r) = vh + vl
+  const uint64_t q = mul2(th, yh), vh = fma2(q, one, th);
+  const uint64_t lost = fma2(q, one, fma2(vh, one, th));
+  const uint64_t vl = add2(fma2(th, r, fma2(th, ny, q)), add2(lost, fma2(tl, ny, tl)));
+  // times 2^22 of the octave, in two integers
+  const uint64_t sc = pk2(__uint_as_float((149u - (w.k[0] >> 10)) << 23), __uint_as_float((149u - (w.k[1] >> 10)) << 23));
+  const uint64_t a = mul2(vh, sc), whole = add2(fma2(vl, sc, a), pk2(MAGIC, MAGIC));
+  const uint64_t rest = fma2(vl, sc, fma2(add2(whole, pk2(-MAGIC, -MAGIC)), one, a));
+  float h0, h1, r0, r1;
+  upk2(whole, h0, h1);
+  upk2(fma2(rest, pk2(4194304.f, 4194304.f), pk2(MAGIC, MAGIC)), r0, r1);
+  w.hi[0] = __float_as_int(h0) - MAGIC_BITS;
+  w.hi[1] = __float_as_int(h1) - MAGIC_BITS;
+  w.lo[0] = __float_as_int(r0) - MAGIC_BITS;
+  w.lo[1] = __float_as_int(r1) - MAGIC_BITS;
+  return w;
+}
+AXON_DEV u64 joined(int hi, int lo) { return (static_cast<u64>(static_cast<unsigned>(hi)) << 22) + static_cast<u64>(static_cast<long long>(lo)); }
+AXON_DEV u64 weight(const Scale& c, float l, const float2* powers) {
+  const Weights w = weights(c, l, l, powers);
+  return w.k[0] < K_END ? joined(w.hi[0], w.lo[0]) : 0;
+}
+
+// v in [0, 1) in units of 2^-64, rounded down; 0 for what is not above 0. (Integer code on purpose, here and for
+// the scale: an SM does two 64-bit floating-point operations per cycle, and a division by all threads took 4 us.)
+AXON_DEV u64 fraction64(float v) {
+  if (!(v > 0.f)) return 0;
+  const unsigned b = __float_as_uint(v);
+  const u64 digits = (b & 0x7fffffu) | 0x800000u;  // v = digits * 2^(exponent - 150); below 2^-126 next to nothing
+  const int up = static_cast<int>(b >> 23) - 86;
+  return up >= 0 ? digits << up : up > -24 ? digits >> -up : 0;
 }
 
 // Floats as integers of the same order.
 AXON_DEV unsigned key_of(float v) {
-  const unsigned b = __float_as_uint(v);
+  const unsigned b = __float_as_uint(v + 0.f);  // -0 is 0
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 AXON_DEV float of_key(unsigned k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 
+constexpr int FEW = 256;    // logits among which one CTA settles everything
+constexpr int LIST = 512;   // a CTA's part of a list
+constexpr int SOME = 1024;  // logits of a bin among which the cut is found without more bins
 struct Shared {
-  unsigned hist[2][3][NB];  // low and high words of the amounts, counts; used in turn
-  u64 powers[257];
+  unsigned hist[2][2][NB];  // low and high words of the amounts; used in turn
+  float2 powers[STEPS];
+  uint2 mine[LIST];         // this CTA's list: key, number
+  uint2 all[SOME];          // all CTAs' lists, in the first one
+  unsigned mine_n;
   u64 cta[2];               // what the cluster exchanges, in turn
   u64 warp[SW];
-  u64 found[3];             // the crossing bin: number, what is needed of it, its count
+  u64 found[3];             // the crossing bin: number, what is needed of it, all of it
   unsigned ends[2];
 };
 
@@ -126,13 +183,24 @@ struct Row {
   int rank, CL;
   int turn = 0;      // exchanges so far
   int pass = 0;      // histograms so far
-  int seg;           // elements per warp, a multiple of 32
+  int end;           // n rounded up to 128; there it holds NaN, which is never kept
+  int seg;           // elements per warp, a multiple of 128
   Scale c;
+  float m;           // the largest logit
+  float share = 1.f;       // top-p, below 1: asked for
+  u64 least = 0;     // min-p: the smallest weight that may stay
+  u64 target = 0;    // what the last crossing's running sum had to reach
   // what is kept: logits above vcut, and equal ones up to number icut
   float vcut = -INFINITY;
   int icut = 0x7fffffff;
 
-  AXON_DEV bool kept(float l, int i) const { return l > vcut || (l == vcut && first + i <= icut); }
+  AXON_DEV bool kept(float l, int i) const {
+    return l >= vcut && (icut == 0x7fffffff || l > vcut || first + i <= icut);  // icut: the same for all
+  }
+  AXON_DEV void cut_at(float v, int number) {
+    vcut = v;
+    icut = number;
+  }
 
   // v (the same in all threads of a CTA): summed over the CTAs before this one, and over all.
   AXON_DEV void exchange(u64 v, u64& before, u64& all) {
@@ -147,59 +215,42 @@ struct Row {
   }
 
   // Adds to bin b of the current histogram.
-  AXON_DEV void add(int b, u64 amount, bool mass, bool count) {
+  template <bool MASS>
+  AXON_DEV void add(int b, u64 amount) {
     unsigned* h = &sh.hist[pass & 1][0][b];
-    if (mass) {
-      const unsigned lo = static_cast<unsigned>(amount), hi = static_cast<unsigned>(amount >> 32);
-      const unsigned up = hi + (atomicAdd(h, lo) > ~lo);
+    if (MASS) {
+      const unsigned lo = static_cast<unsigned>(amount);
+      const unsigned up = static_cast<unsigned>(amount >> 32) + (atomicAdd(h, lo) > ~lo);
       if (up) atomicAdd(h + NB, up);
-      if (count) atomicAdd(h + 2 * NB, 1u);
     } else {
       atomicAdd(h, 1u);
     }
   }
   AXON_DEV void clear(int which) {
-    for (int i = threadIdx.x; i < 3 * NB; i += ST) (&sh.hist[which][0][0])[i] = 0;
+    for (int i = threadIdx.x; i < 2 * NB; i += ST) (&sh.hist[which][0][0])[i] = 0;
   }
 
-  // The bins of all CTAs; the first at which the running sum reaches the target goes to sh.found.
-  // share: the target is this part of the sum, else `target`. Returns whether there is one.
-  AXON_DEV bool crossing(bool mass, bool count, float share, u64 target) {
-    cg::cluster_group cluster = cg::this_cluster();
-    cluster.sync();
-    const int which = pass & 1, t = threadIdx.x, lane = t & 31, warp = t >> 5;
-    ++pass;
-    // this thread's bins: 2t, 2t + 1
-    u64 a[2] = {0, 0};
-    unsigned m[2] = {0, 0};
-    for (int r = 0; r < CL; ++r) {
-      const unsigned* h = cluster.map_shared_rank(&sh.hist[which][0][0], r);
-      const uint2 lo = reinterpret_cast<const uint2*>(h)[t];
-      a[0] += lo.x;
-      a[1] += lo.y;
-      if (mass) {
-        const uint2 hi = reinterpret_cast<const uint2*>(h + NB)[t];
-        a[0] += static_cast<u64>(hi.x) << 32;
-        a[1] += static_cast<u64>(hi.y) << 32;
-        if (count) {
-          const uint2 k = reinterpret_cast<const uint2*>(h + 2 * NB)[t];
-          m[0] += k.x;
-          m[1] += k.y;
-        }
-      }
-    }
+  // The smallest whole number that is at least part * sum, and at least 1; part < 1.
+  AXON_DEV static u64 share_of(float part, u64 sum) {
+    const u64 f = fraction64(part);
+    return max(u64{1}, __umul64hi(f, sum) + (f * sum != 0));
+  }
+  // floor(u * sum) for u clamped to [0, 1)
+  AXON_DEV static u64 draw(float u, u64 sum) {
+    return u > 0.f ? __umul64hi(fraction64(fminf(u, 0.999999940395355224609375f)), sum) : 0;
+  }
+
+  // The first of the bins at which the running sum reaches the target goes to sh.found; a: this thread's bins 2t and 2t + 1.
+  // part_of >= 0: the target is this part of the sum, else `goal`. Returns whether there is one.
+  AXON_DEV bool scan_bins(const u64 (&a)[2], float part_of, u64 goal) {
+    const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
     const u64 inc = warp_scan64(a[0] + a[1]);
     if (lane == 31) sh.warp[warp] = inc;
-    clear(which ^ 1);  // everybody has read it before the barrier above
     __syncthreads();
     const u64 x = lane < SW ? sh.warp[lane] : 0;
     const u64 all = warp_sum64(x);
     u64 sum = warp_sum64(lane < warp ? x : 0) + inc - a[0] - a[1];
-    if (share >= 0.f) {
-      const u64 part = static_cast<u64>(static_cast<double>(share) * 18446744073709551616.0);  // share < 1
-      target = __umul64hi(part, all) + (part * all != 0);
-      if (target == 0) target = 1;
-    }
+    target = part_of >= 0.f ? share_of(part_of, all) : goal;
     const bool any = all >= target;
     if (any) {
 #pragma unroll
@@ -207,7 +258,7 @@ struct Row {
         if (sum < target && sum + a[i] >= target) {
           sh.found[0] = 2 * t + i;
           sh.found[1] = target - sum;
-          sh.found[2] = mass ? m[i] : a[i];
+          sh.found[2] = a[i];
         }
         sum += a[i];
       }
@@ -215,18 +266,45 @@ struct Row {
     __syncthreads();
     return any;
   }
+  // The same for the sums of all CTAs' bins; clears the other histogram, which everybody has read.
+  template <bool MASS>
+  AXON_DEV bool crossing(float part_of, u64 goal) {
+    cg::cluster_group cluster = cg::this_cluster();
+    cluster.sync();
+    const int which = pass & 1, t = threadIdx.x;
+    ++pass;
+    u64 a[2] = {0, 0};
+    for (int r0 = 0; r0 < CL; r0 += 4) {
+      uint2 lo[4], hi[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        lo[r] = hi[r] = make_uint2(0, 0);
+        if (r0 + r < CL) {
+          const unsigned* h = cluster.map_shared_rank(&sh.hist[which][0][0], r0 + r);
+          lo[r] = reinterpret_cast<const uint2*>(h)[t];
+          if (MASS) hi[r] = reinterpret_cast<const uint2*>(h + NB)[t];
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        a[0] += (static_cast<u64>(hi[r].x) << 32) + lo[r].x;
+        a[1] += (static_cast<u64>(hi[r].y) << 32) + lo[r].y;
+      }
+    }
+    clear(which ^ 1);
+    return scan_bins(a, part_of, goal);
+  }
 
-  AXON_DEV int bin_of(float x) const { return min(static_cast<int>(x * (NB / X_END)), NB - 1); }
+  AXON_DEV static int bin_of(unsigned k) { return min(static_cast<int>(k) >> BIN_SHIFT, NB - 1); }
 
-  // The smallest key whose bin is at most b; called by a whole warp.
-  AXON_DEV unsigned lowest_key(int b) const {
-    unsigned lo = 0, hi = key_of(c.m);  // hi: bin 0
+  // The smallest key for which in(logit) holds, if it holds from some logit to the largest; called by a whole warp.
+  template <typename F>
+  AXON_DEV unsigned lowest_key(F in) const {
+    unsigned lo = 0, hi = key_of(m);
     const int lane = threadIdx.x & 31;
     while (lo < hi) {
       const unsigned step = (hi - lo) / 32 + 1, at = min(hi, lo + lane * step);  // (hi - lo) < 2^32 - 32
-      const float x = exponent(c, of_key(at));
-      const bool in = x < X_END && bin_of(x) <= b;  // monotone: false, then true
-      const unsigned hits = __ballot_sync(0xffffffffu, in);
+      const unsigned hits = __ballot_sync(0xffffffffu, in(of_key(at)));
       const int f = hits ? __ffs(hits) - 1 : 32;
       const unsigned top = f < 32 ? min(hi, lo + f * step) : hi;
       lo = f > 0 ? min(hi, lo + (f - 1) * step) + 1 : lo;
@@ -234,21 +312,64 @@ struct Row {
     }
     return lo;
   }
+  // ... whose bin is at most b.
+  AXON_DEV unsigned lowest_in(int b) const {
+    return lowest_key([&](float l) {
+      const unsigned k = steps_of(c, l);
+      return k < K_END && bin_of(k) <= b;
+    });
+  }
 
-  // Sum of `amount(l, i)` over this warp's part of the slice; in every lane.
+  // f(in, l, i, k, hi, lo) for the logits val[i], i0 <= i < i1 (multiples of 128; the slice is padded), by this warp, with
+  // their steps and weights; in: kept, and of a weight. Where no lane keeps one of four, they are passed over.
   template <typename F>
-  AXON_DEV u64 warp_amount(int i0, int i1, F amount) {
-    u64 s = 0;
-    for (int i = i0 + (threadIdx.x & 31); i < i1; i += 32) s += amount(val[i], i);
-    return warp_sum64(s);
+  AXON_DEV void each(int i0, int i1, F f) {
+    const bool some = vcut > -INFINITY;
+    for (int i = i0 + (threadIdx.x & 31) * 4; i < i1; i += 128) {
+      const float4 v = *reinterpret_cast<const float4*>(val + i);
+      const float l[4] = {v.x, v.y, v.z, v.w};
+      if (some && !__any_sync(0xffffffffu, fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)) >= vcut)) continue;
+#pragma unroll
+      for (int x = 0; x < 4; x += 2) {
+        const Weights w = weights(c, l[x], l[x + 1], sh.powers);
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+          f(w.k[y] < K_END && kept(l[x + y], i + x + y), l[x + y], i + x + y, w.k[y], w.hi[y], w.lo[y]);
+      }
+    }
+  }
+  // f(in, l, i), without weights; in: kept.
+  template <typename F>
+  AXON_DEV void each_plain(int i0, int i1, F f) {
+    for (int i = i0 + (threadIdx.x & 31) * 4; i < i1; i += 128) {
+      const float4 v = *reinterpret_cast<const float4*>(val + i);
+      const float l[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int x = 0; x < 4; ++x) f(kept(l[x], i + x), l[x], i + x);
+    }
+  }
+  // The amount of elements i0 .. i1 - 1 in every lane of the warp that calls it: how many equal v, or the sum of weights.
+  template <bool TIES>
+  AXON_DEV u64 amount(int i0, int i1, float v) {
+    if (TIES) {
+      unsigned n = 0;
+      each_plain(i0, i1, [&](bool in, float l, int) { n += in && l == v; });
+      return __reduce_add_sync(0xffffffffu, n);
+    }
+    int hi = 0, lo = 0;  // at most MAX_SLICE / ST elements per thread
+    each(i0, i1, [&](bool in, float, int, unsigned, int h, int l) {
+      hi += in ? h : 0;
+      lo += in ? l : 0;
+    });
+    return warp_sum64(joined(hi, lo));
   }
 
   // The first token, by number, at which the running sum of the amounts passes t(sum of all): its number, and
   // its amount, in the threads of one warp of the cluster; -1 in the others.
-  template <typename F, typename T>
-  AXON_DEV int locate(F amount, T t, u64& its, u64& all) {
+  template <bool TIES, typename T>
+  AXON_DEV int locate(float v, T t, u64& its, u64& all) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const u64 mine = warp_amount(warp * seg, min(n, warp * seg + seg), amount);
+    const u64 mine = amount<TIES>(warp * seg, min(end, warp * seg + seg), v);
     if (lane == 0) sh.warp[warp] = mine;
     __syncthreads();
     u64 x = lane < SW ? sh.warp[lane] : 0, before;
@@ -261,8 +382,8 @@ struct Row {
     int at = __ffs(__ballot_sync(0xffffffffu, inc > rest)) - 1;  // the warp's part that it falls into
     rest -= __shfl_sync(0xffffffffu, inc - x, at);
     // which all warps share
-    const int i0 = at * seg, i1 = min(n, i0 + seg), sub = (seg / 32 + SW - 1) / SW * 32;
-    const u64 part = warp_amount(i0 + warp * sub, min(i1, i0 + warp * sub + sub), amount);
+    const int i0 = at * seg, i1 = min(end, i0 + seg), sub = (seg / 128 + SW - 1) / SW * 128;
+    const u64 part = amount<TIES>(i0 + warp * sub, min(i1, i0 + warp * sub + sub), v);
     __syncthreads();
     if (lane == 0) sh.warp[warp] = part;
     __syncthreads();
@@ -272,7 +393,9 @@ struct Row {
     if (at != warp) return -1;
     rest -= __shfl_sync(0xffffffffu, inc - x, at);
     for (int i = i0 + warp * sub; i < i1; i += 32) {
-      const u64 a = i + lane < i1 ? amount(val[i + lane], i + lane) : 0;
+      u64 a = 0;
+      if (kept(val[i + lane], i + lane))
+        a = TIES ? static_cast<u64>(val[i + lane] == v) : weight(c, val[i + lane], sh.powers);
       const u64 sum = warp_scan64(a);
       const unsigned hit = __ballot_sync(0xffffffffu, sum > rest);
       if (hit) {
@@ -285,75 +408,215 @@ struct Row {
     return -1;
   }
 
-  // Cuts what is kept to its first k (share < 0), or to the fewest whose weights reach this share.
-  AXON_DEV void cut(float share, u64 k) {
-    const bool mass = share >= 0.f;
-    const int i0 = (threadIdx.x >> 5) * seg + (threadIdx.x & 31), i1 = min(n, ((threadIdx.x >> 5) + 1) * seg);
-    __syncthreads();  // the histogram is cleared
-    for (int i = i0; i < i1; i += 32) {
-      const float l = val[i], x = exponent(c, l);
-      if (x < X_END && kept(l, i)) add(bin_of(x), mass ? weight(c, l, sh.powers) : 1, mass, false);
+  // The logits that are kept and in bins b0 .. b1, all CTAs': how many; and, if they are at most `most` and no CTA has more
+  // than its list holds, in the first one's sh.all.
+  AXON_DEV int gather(int b0, int b1, int most) {
+    cg::cluster_group cluster = cg::this_cluster();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (tid == 0) sh.mine_n = 0;
+    __syncthreads();
+    each_plain(warp * seg, min(end, warp * seg + seg), [&](bool in, float l, int i) {
+      const unsigned s = steps_of(c, l);
+      if (in && s < K_END && bin_of(s) <= b1 && bin_of(s) >= b0) {
+        const unsigned at = atomicAdd(&sh.mine_n, 1u);
+        if (at < LIST) sh.mine[at] = make_uint2(key_of(l), first + i);
+      }
+    });
+    cluster.sync();
+    const unsigned here = lane < CL ? *cluster.map_shared_rank(&sh.mine_n, lane) : 0;
+    const int nc = __any_sync(0xffffffffu, here > LIST) ? 0x7fffffff : static_cast<int>(__reduce_add_sync(0xffffffffu, here));
+    if (nc <= most && rank == 0) {
+      for (int r = warp; r < CL; r += SW) {
+        const unsigned count = __shfl_sync(0xffffffffu, here, r);
+        const unsigned before = __reduce_add_sync(0xffffffffu, lane < r ? here : 0);
+        const uint2* from = cluster.map_shared_rank(&sh.mine[0], r);
+        for (unsigned i = lane; i < count; i += 32) sh.all[before + i] = from[i];
+      }
     }
-    if (!crossing(mass, false, share, k)) return;
+    __syncthreads();
+    return nc;
+  }
+
+  // All that matters is among the nc logits in the first CTA's sh.all: the first k of them
+  // stay (k > 0) and then the share, or those that the running sum of all weights needs to reach the target (k = 0); min-p; the draw.
+  AXON_DEV void settle(int nc, u64 k, float u, int* token, float* prob) {
+    // two threads per logit; the weights are where the histograms were
+    const int tid = threadIdx.x, i = tid >> 1;
+    u64* const w = reinterpret_cast<u64*>(&sh.hist[0][0][0]);
+    const uint2 me = i < nc ? sh.all[i] : make_uint2(0, 0);
+    const u64 mine = i < nc ? weight(c, of_key(me.x), sh.powers) : 0;
+    if (i < nc && !(tid & 1)) w[i] = mine;
+    __syncthreads();
+    unsigned ahead = 0;
+    u64 sum = 0;
+    for (int j = tid & 1; j < nc; j += 2) {
+      const uint2 x = sh.all[j];
+      const bool in = x.x > me.x || (x.x == me.x && x.y < me.y);
+      ahead += in;
+      sum += in ? w[j] : 0;
+    }
+    ahead += __shfl_xor_sync(0xffffffffu, ahead, 1);
+    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+    bool stays = i < nc && (k == 0 || ahead < k);
+    u64 goal = target;
+    if (k > 0 && share < 1.f) goal = share_of(fmaxf(share, 0.f), cta_sum(stays && !(tid & 1) ? mine : 0));
+    if (k == 0 || share < 1.f) stays = stays && sum < goal;
+    stays = stays && (ahead == 0 || mine >= least);
+    __syncthreads();
+    if (i < nc && !(tid & 1) && !stays) w[i] = 0;
+    const u64 total = cta_sum(stays && !(tid & 1) ? mine : 0), t = draw(u, total);
+    sum = 0;
+    for (int j = tid & 1; j < nc; j += 2) sum += sh.all[j].y < me.y ? w[j] : 0;
+    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+    if (stays && !(tid & 1) && sum <= t && t - sum < mine) {
+      *token = static_cast<int>(me.y);
+      if (prob) *prob = static_cast<float>(static_cast<double>(mine) / static_cast<double>(total));
+    }
+  }
+  // The cut among the nc logits in the first CTA's sh.all: key and, in the low word, the last number of it that stays. By bins
+  // of this CTA alone, until one key is left.
+  template <bool MASS>
+  AXON_DEV u64 cut_list(int nc, u64 need) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    unsigned lo = 0xffffffffu, hi = 0;
+    for (int i = tid; i < nc; i += ST) {
+      lo = min(lo, sh.all[i].x);
+      hi = max(hi, sh.all[i].x);
+    }
+    lo = __reduce_min_sync(0xffffffffu, lo);
+    hi = __reduce_max_sync(0xffffffffu, hi);
+    if (lane == 0) sh.warp[warp] = (static_cast<u64>(hi) << 32) | lo;
+    for (int w = 0; w < 2; ++w) clear(w);
+    __syncthreads();
+    const u64 x = sh.warp[lane & (SW - 1)];
+    lo = __reduce_min_sync(0xffffffffu, static_cast<unsigned>(x));
+    hi = __reduce_max_sync(0xffffffffu, static_cast<unsigned>(x >> 32));
+    u64 amount = ~u64{0};
+    for (;;) {
+      const int shift = max(0, 32 - __clz(hi - lo) - 10);
+      __syncthreads();
+      for (int i = tid; i < nc; i += ST) {
+        const unsigned key = sh.all[i].x;
+        if (key >= lo && key <= hi) add<MASS>((hi - key) >> shift, MASS ? weight(c, of_key(key), sh.powers) : 1);
+      }
+      __syncthreads();
+      const int which = pass & 1;
+      const uint2 l = reinterpret_cast<const uint2*>(&sh.hist[which][0][0])[tid], h = reinterpret_cast<const uint2*>(&sh.hist[which][1][0])[tid];
+      const u64 a[2] = {(static_cast<u64>(h.x) << 32) + l.x, (static_cast<u64>(h.y) << 32) + l.y};
+      scan_bins(a, -1.f, need);
+      hi -= static_cast<unsigned>(sh.found[0]) << shift;
+      lo = max(lo, hi - min(hi, (1u << shift) - 1));
+      need = sh.found[1];
+      amount = sh.found[2];
+      clear(which);
+      __syncthreads();
+      if (lo == hi) break;
+    }
+    const u64 one = MASS ? weight(c, of_key(lo), sh.powers) : 1;
+    if (amount == one) return (static_cast<u64>(lo) << 32) | 0x7fffffffu;
+    const u64 which = (need + one - 1) / one;  // of the equal ones, by number
+    for (int i = tid; i < nc; i += ST) {
+      if (sh.all[i].x != lo) continue;
+      unsigned n = 1;
+      for (int j = 0; j < nc; ++j) n += sh.all[j].x == lo && sh.all[j].y < sh.all[i].y;
+      if (n == which) sh.found[0] = (static_cast<u64>(lo) << 32) | sh.all[i].y;
+    }
+    __syncthreads();
+    return sh.found[0];
+  }
+  // v summed over the CTA
+  AXON_DEV u64 cta_sum(u64 v) {
+    const int lane = threadIdx.x & 31;
+    v = warp_sum64(v);
+    __syncthreads();
+    if (lane == 0) sh.warp[threadIdx.x >> 5] = v;
+    __syncthreads();
+    return warp_sum64(lane < SW ? sh.warp[lane] : 0);
+  }
+
+  // Cuts what is kept to its first k, or (MASS, k = 0) to the fewest whose weights reach the share. true: the token is written.
+  template <bool MASS>
+  AXON_DEV bool cut(u64 k, float u, int* token, float* prob) {
+    const int tid = threadIdx.x, i0 = (tid >> 5) * seg, i1 = min(end, i0 + seg);
+    __syncthreads();  // the histogram is cleared
+    if (MASS)
+      each(i0, i1, [&](bool in, float, int, unsigned s, int hi, int lo) {
+        if (in) add<true>(bin_of(s), joined(hi, lo));
+      });
+    else
+      each_plain(i0, i1, [&](bool in, float l, int) {
+        const unsigned s = steps_of(c, l);
+        if (in && s < K_END) add<false>(bin_of(s), 1);
+      });
+    if (!crossing<MASS>(MASS ? fmaxf(share, 0.f) : -1.f, k)) return false;
     const int b = static_cast<int>(sh.found[0]);
-    u64 need = sh.found[1], count = mass ? 0 : sh.found[2];
+    u64 need = sh.found[1], amount = sh.found[2];
+    // Few in these bins? (How many is known of a count; of weights, that they are no fewer than the sum takes of the largest.)
+    if (MASS ? (target >> 44) < FEW : k - need + amount <= FEW) {
+      const int nc = gather(0, b, FEW);
+      if (nc <= FEW) {
+        if (rank == 0) settle(nc, k, u, token, prob);
+        return true;
+      }
+      cg::this_cluster().sync();  // the counts are read before the next list begins
+    }
+    const int nc = gather(b, b, SOME);
+    if (nc <= SOME) {
+      u64 at = rank == 0 ? cut_list<MASS>(nc, need) : 0, before, all;
+      if (rank)
+        for (int w = 0; w < 2; ++w) clear(w);
+      exchange(at, before, all);
+      const float v = of_key(static_cast<unsigned>(all >> 32));
+      cut_at(v, min(static_cast<int>(all & 0x7fffffffu), v == vcut ? icut : 0x7fffffff));
+      return false;
+    }
+    for (int w = 0; w < 2; ++w) clear(w);
     // keys of the bin
-    if (threadIdx.x < 32) {
-      const unsigned lo = lowest_key(b), hi = b > 0 ? lowest_key(b - 1) - 1 : key_of(c.m);
-      if (threadIdx.x == 0) {
+    if (tid < 32) {
+      const unsigned lo = lowest_in(b), hi = b > 0 ? lowest_in(b - 1) - 1 : key_of(m);
+      if (tid == 0) {
         sh.ends[0] = lo;
         sh.ends[1] = hi;
       }
     }
     __syncthreads();
     unsigned lo = sh.ends[0], hi = sh.ends[1];
-    while (lo < hi && !(mass ? count == 1 : need == count)) {
+    while (lo < hi && (MASS || need < amount)) {
       const unsigned width = hi - lo;  // less one
       const int shift = max(0, 32 - __clz(width) - 10);
-      for (int i = i0; i < i1; i += 32) {
-        const float l = val[i];
+      each_plain(i0, i1, [&](bool in, float l, int) {
         const unsigned key = key_of(l);
-        if (key >= lo && key <= hi && kept(l, i))
-          add((hi - key) >> shift, mass ? weight(c, l, sh.powers) : 1, mass, true);
-      }
-      crossing(mass, true, -1.f, need);
+        if (in && key >= lo && key <= hi) add<MASS>((hi - key) >> shift, MASS ? weight(c, l, sh.powers) : 1);
+      });
+      crossing<MASS>(-1.f, need);
       hi -= static_cast<unsigned>(sh.found[0]) << shift;
       lo = max(lo, hi - min(hi, (1u << shift) - 1));
       need = sh.found[1];
-      count = sh.found[2];
+      amount = sh.found[2];
     }
     const float v = of_key(lo);
-    if (mass ? count == 1 : need == count) {
-      if (v != vcut) icut = 0x7fffffff;
-      vcut = v;
-      return;
+    if (!MASS && need == amount) {
+      cut_at(v, v == vcut ? icut : 0x7fffffff);
+      return false;
     }
     // one logit, of which the first some are kept
-    if (mass) {
+    if (MASS) {
       const u64 w = weight(c, v, sh.powers);
       need = (need + w - 1) / w;
     }
     u64 its, all, before;
-    const float was = vcut;
-    const int was_i = icut;
-    const int at = locate([&](float l, int i) -> u64 { return l == v && (l > was || first + i <= was_i); },
-                          [&](u64) { return need - 1; }, its, all);
+    const int at = locate<true>(v, [&](u64) { return need - 1; }, its, all);
     __syncthreads();
-    if (threadIdx.x == 0) sh.found[0] = 0;
+    if (tid == 0) sh.found[0] = 0;
     __syncthreads();
-    if (at >= 0 && (threadIdx.x & 31) == 0) sh.found[0] = at + 1;
+    if (at >= 0 && (tid & 31) == 0) sh.found[0] = at + 1;
     __syncthreads();
     exchange(sh.found[0], before, all);
-    vcut = v;
-    icut = static_cast<int>(all) - 1;
+    cut_at(v, static_cast<int>(all) - 1);
+    return false;
   }
 };
 
-template <typename TL>
-AXON_DEV float logit(const TL* x) {
-  const float v = to_f(*x);
-  return v == v ? v + 0.f : -INFINITY;  // -0 becomes 0
-}
 template <typename TL> AXON_DEV void unpack16(const uint4& w, float* f);
 template <> AXON_DEV void unpack16<float>(const uint4& w, float* f) {
   f[0] = __uint_as_float(w.x); f[1] = __uint_as_float(w.y); f[2] = __uint_as_float(w.z); f[3] = __uint_as_float(w.w);
@@ -379,22 +642,15 @@ __global__ void __launch_bounds__(ST) sample_kernel(const SampleArgs p, int CL, 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int b = blockIdx.x / CL, rank = blockIdx.x % CL;
   cg::cluster_group cluster = cg::this_cluster();
-  for (int i = tid; i < 257; i += ST) sh.powers[i] = g_powers.v[i];
-  for (int i = tid; i < 6 * NB; i += ST) (&sh.hist[0][0][0])[i] = 0;
+  for (int i = tid; i < STEPS; i += ST) sh.powers[i] = make_float2(g_powers.hi[i], g_powers.lo[i]);
+  for (int i = tid; i < 4 * NB; i += ST) (&sh.hist[0][0][0])[i] = 0;
   grid_dep_launch();
   grid_dep_wait();
 
-  // ---- the slice, and the largest logit with the lowest number
+  // ---- the slice, and the largest logit (maxima pass over what is not a number)
   const int first = min(rank * slice, p.V), n = min(slice, p.V - first);
   const TL* const x = static_cast<const TL*>(p.logits) + b * p.row_stride + first;
   float best = -INFINITY;
-  int at = 0;
-  auto take = [&](float v, int i) {
-    if (v > best) {
-      best = v;
-      at = i;
-    }
-  };
   constexpr int PER = 16 / sizeof(TL);
   int done = 0;
   if ((reinterpret_cast<uintptr_t>(x) & 15) == 0) {
@@ -412,103 +668,114 @@ __global__ void __launch_bounds__(ST) sample_kernel(const SampleArgs p, int CL, 
         float f[PER];
         unpack16<TL>(w[k], f);
 #pragma unroll
-        for (int e = 0; e < PER; ++e) {
-          f[e] = f[e] == f[e] ? f[e] + 0.f : -INFINITY;
-          take(f[e], i + e);
-        }
+        for (int e = 0; e < PER; ++e) best = fmaxf(best, f[e]);
 #pragma unroll
         for (int e = 0; e < PER; e += 4) *reinterpret_cast<float4*>(val + i + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
       }
     }
   }
   for (int i = done + tid; i < n; i += ST) {
-    const float v = logit(x + i);
-    take(v, i);
-    val[i] = v;
+    val[i] = to_f(x[i]);
+    best = fmaxf(best, val[i]);
   }
-  u64 key = best > -INFINITY ? argmax_key(best, first + at) : 0;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) key = max(key, __shfl_xor_sync(0xffffffffu, key, o));
-  if (lane == 0) sh.warp[warp] = key;
+  const int end = (n + 127) & ~127;
+  for (int i = n + tid; i < end; i += ST) val[i] = __int_as_float(0x7fffffff);
+  Row row{p, sh, val, n, first, rank, CL};
+  row.end = end;
+  row.seg = ((slice + SW - 1) / SW + 127) / 128 * 128;
+  u64 all = key_of(warp_max(best));
+  if (lane == 0) sh.warp[warp] = all;
   __syncthreads();
-  if (tid == 0) {
-    for (int w = 1; w < SW; ++w) key = max(key, sh.warp[w]);
-    sh.cta[1] = key;
-  }
+  all = key_of(warp_max(lane < SW ? of_key(static_cast<unsigned>(sh.warp[lane])) : -INFINITY));
+  if (tid == 0) sh.cta[1] = all;
   cluster.sync();
-  key = lane < CL ? *cluster.map_shared_rank(&sh.cta[1], lane) : 0;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) key = max(key, __shfl_xor_sync(0xffffffffu, key, o));
-  const int top = static_cast<int>(0xffffffffu - static_cast<unsigned>(key));
+  float m = warp_max(lane < CL ? of_key(static_cast<unsigned>(*cluster.map_shared_rank(&sh.cta[1], lane))) : -INFINITY);
 
   const float temp = p.temperature ? p.temperature[b] : 1.f;
-  if (key == 0 || !(temp > 0.f)) {
-    // nothing to choose from, or the largest
-    if (rank == 0 && tid == 0) {
-      p.tokens[b] = key ? top : -1;
-      if (p.prob) p.prob[b] = key ? 1.f : 0.f;
+  const float low = p.min_p ? p.min_p[b] : 0.f;
+  const bool nothing = m == -INFINITY, greedy = nothing || !(temp > 0.f);
+  if (greedy || low > 1.f) {
+    // the first of the largest alone
+    int at = 0x7fffffff;
+    for (int i = tid; i < n; i += ST)
+      if (val[i] == m) at = min(at, first + i);
+    at = __reduce_min_sync(0xffffffffu, at);
+    __syncthreads();
+    if (lane == 0) sh.warp[warp] = at;
+    __syncthreads();
+    if (tid == 0) {
+      for (int w = 0; w < SW; ++w) at = min(at, static_cast<int>(sh.warp[w]));
+      sh.cta[0] = at;
+    }
+    cluster.sync();
+    if (rank == 0 && warp == 0) {
+      at = __reduce_min_sync(0xffffffffu, lane < CL ? static_cast<int>(*cluster.map_shared_rank(&sh.cta[0], lane)) : 0x7fffffff);
+      if (lane == 0) {
+        p.tokens[b] = nothing ? -1 : at;
+        if (p.prob) p.prob[b] = nothing ? 0.f : 1.f;
+      }
     }
     cluster.sync();  // nobody's shared memory goes away while another reads it
     return;
   }
-  float m = of_key(static_cast<unsigned>(key >> 32));
   if (m == INFINITY) {  // infinite logits share everything
     for (int i = tid; i < n; i += ST) val[i] = val[i] == INFINITY ? 0.f : -INFINITY;
     m = 0.f;
   }
-  const double scale = 1.4426950408889634074 / static_cast<double>(temp);
-  Row row{p, sh, val, n, first, rank, CL};
-  row.seg = ((slice + SW - 1) / SW + 31) / 32 * 32;
-  row.c.m = m;
-  row.c.ch = static_cast<float>(fmin(scale, 3e38));
-  row.c.cl = static_cast<float>(fmin(scale, 3e38) - row.c.ch);
+  // log2(e) / temperature as a pair: the quotient, and the quotient of what it left
+  constexpr float LOG2E = 1.44269502162933349609375f, LOG2E_LO = 1.92596299112661746887e-8f;
+  row.c.ch = fminf(LOG2E / temp, 3e38f);
+  row.c.cl = 0.f;
+  if (temp > 1e-30f && temp < 1e30f) row.c.cl = (fmaf(-row.c.ch, temp, LOG2E) + LOG2E_LO) / temp;
+  row.m = m;
+  // Far from 0 the logits that count lie within a factor of two of the largest: their distance from it is exact.
+  row.c.base = fabsf(m) * row.c.ch < 128.f ? 0.f : m;
+  row.c.top = 0;
+  row.c.top = 1 - static_cast<int>(steps_of(row.c, m));
   __syncthreads();
 
   const int k = p.top_k ? p.top_k[b] : 0;
-  if (k > 0 && k < p.V) row.cut(-1.f, k);
-  const float share = p.top_p ? p.top_p[b] : 1.f;
-  if (share < 1.f) row.cut(fmaxf(share, 0.f), 0);
-  const float low = p.min_p ? p.min_p[b] : 0.f;
+  const float share = p.top_p ? p.top_p[b] : 1.f, random = p.u[b];
+  if (share < 1.f) row.share = share;
   if (low > 0.f) {
-    // w >= min_p is l >= m + temperature ln(min_p), rounded up to a float
-    const float v = __double2float_ru(static_cast<double>(m) + static_cast<double>(temp) * log(static_cast<double>(low)));
-    if (v > row.vcut) {
-      row.vcut = v;
-      row.icut = 0x7fffffff;
-    }
-    if (v > m) {  // the first is kept in any case
-      row.vcut = m;
-      row.icut = top;
-    }
+    const u64 most = weight(row.c, m, sh.powers);
+    row.least = low < 1.f ? Row::share_of(low, most) : most;
   }
-  const float random = p.u[b];
-  u64 its = 0, all = 0;
-  const int token = row.locate(
-      [&](float l, int i) -> u64 { return row.kept(l, i) ? weight(row.c, l, sh.powers) : 0; },
-      [&](u64 sum) {
-        if (!(random > 0.f)) return u64{0};
-        const float under = fminf(random, 0.999999940395355224609375f);
-        return __umul64hi(static_cast<u64>(static_cast<double>(under) * 18446744073709551616.0), sum);
-      },
-      its, all);
-  if (token >= 0 && lane == 0) {
-    p.tokens[b] = token;
-    if (p.prob) p.prob[b] = static_cast<float>(static_cast<double>(its) / static_cast<double>(all));
+  int* const token = p.tokens + b;
+  float* const prob = p.prob ? p.prob + b : nullptr;
+  if ((k > 0 && k < p.V && row.cut<false>(k, random, token, prob)) || (row.share < 1.f && row.cut<true>(0, random, token, prob))) {
+    cluster.sync();
+    return;
+  }
+  if (row.least) {
+    if (warp == 0) {
+      const unsigned key = row.lowest_key([&](float l) { return l > -INFINITY && weight(row.c, l, sh.powers) >= row.least; });
+      if (lane == 0) sh.ends[0] = key;
+    }
+    __syncthreads();
+    const float v = of_key(sh.ends[0]);
+    if (v > row.vcut) row.cut_at(v, 0x7fffffff);
+  }
+  u64 its = 0;
+  const int at = row.locate<false>(0.f, [&](u64 sum) { return Row::draw(random, sum); }, its, all);
+  if (at >= 0 && lane == 0) {
+    *token = at;
+    if (prob) *prob = static_cast<float>(static_cast<double>(its) / static_cast<double>(all));
   }
   cluster.sync();
 }
 
-// CTAs per row.
+// CTAs per row: as many as run at once (two per SM), and slices of no more than 24K logits.
 int cluster_for(const LaunchCtx& lc, int B, int V) {
   int CL = 1;
-  while (CL < MAX_CL && ((V + CL - 1) / CL > MAX_SLICE || (static_cast<long long>(B) * CL < 2 * lc.num_sms && V / CL > 2 * ST))) CL *= 2;
+  while (CL < MAX_CL && (V > CL * 24 * 1024 || (2ll * B * CL <= 2 * lc.num_sms && V / CL > 2 * ST))) CL *= 2;
   return CL;
 }
 
 template <typename TL>
 cudaError_t launch_type(const LaunchCtx& lc, const SampleArgs& a) {
   const int CL = cluster_for(lc, a.B, a.V);
-  const int slice = ((a.V + CL - 1) / CL + 7) & ~7;
+  const int slice = ((a.V + CL - 1) / CL + 127) & ~127;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(a.B) * CL);
   cfg.blockDim = dim3(ST);
@@ -526,7 +793,7 @@ cudaError_t launch_type(const LaunchCtx& lc, const SampleArgs& a) {
 
 template <typename TL>
 cudaError_t prepare_type() {
-  cudaError_t e = cudaFuncSetAttribute(sample_kernel<TL>, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SLICE * 4 + 32);
+  cudaError_t e = cudaFuncSetAttribute(sample_kernel<TL>, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SLICE * 4);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(sample_kernel<TL>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   return e;
 }

@@ -444,7 +444,26 @@ int axon_attn_decode(const axon_kv_cache* cache, int32_t layer, const void* d_q,
                      int64_t workspace_bytes, int32_t* d_err, void* stream);
 int axon_attn_decode_workspace(const axon_kv_cache* cache, int32_t num_heads, int32_t B, int64_t* bytes);
 
-/* The same for chunks of tokens, packed row after row as in
+/* axon_attn_decode for rows that come in groups whose first blocks are the same: samples of one prompt or beams
+ * (axon_kv_fork), requests with one system prompt. The blocks that all live rows of a group see whole are read once for
+ * the group, the rest row by row; the result is axon_attn_decode's but for the order of its sums.
+ *   d_group_offsets [num_groups + 1], ascending: group n is rows group_offsets[n] .. group_offsets[n+1]-1 (a group may be
+ *                   empty); rows of no group share nothing. Inconsistent offsets are reported and nothing is shared
+ *   d_prefix_lens   [num_groups] tokens whose whole blocks (prefix_lens / 16, rounded down) the tables of the
+ *                   group's live rows name alike, in all their rows: the first live row's entries are read for all, which the call
+ *                   does not check. It may be longer than a row's context; negative: reported, nothing is shared
+ *   num_groups      1 .. 1024
+ *   d_block_table   [B][blocks_per_seq]; entries of shared blocks that only idle rows (context_lens negative) hold may be anything
+ * The rest as in axon_attn_decode, the workspace among it: one of axon_attn_shared_workspace's size serves axon_attn_decode
+ * of the same heads and cache too. num_blocks * num_kv_heads * 16 stays below 2^31. */
+int axon_attn_shared(const axon_kv_cache* cache, int32_t layer, const void* d_q, int64_t q_row_stride, int64_t q_head_stride,
+                     int32_t B, int32_t num_heads, const int32_t* d_context_lens, const int32_t* d_block_table,
+                     int32_t blocks_per_seq, const int32_t* d_group_offsets, const int32_t* d_prefix_lens, int32_t num_groups,
+                     int32_t window, int32_t sinks, float scale, void* d_out, int64_t out_row_stride, int64_t out_head_stride,
+                     float* d_lse, void* d_workspace, int64_t workspace_bytes, int32_t* d_err, void* stream);
+int axon_attn_shared_workspace(const axon_kv_cache* cache, int32_t num_heads, int32_t B, int64_t* bytes);
+
+/* axon_attn_decode for chunks of tokens, packed row after row as in
  * axon_prefill_varlen: chunk b is rows cu_seqlens[b] .. cu_seqlens[b+1]-1 of
  * d_q and d_out (T rows in all; a chunk may be empty), its row i stands at
  * position context_lens[b] + i, and the chunk's keys and values are in the

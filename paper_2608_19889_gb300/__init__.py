@@ -34,7 +34,7 @@ AXON_ROPE_HALF, AXON_ROPE_INTERLEAVED = 0, 1
 EXPORTED = ["axon_model_create", "axon_prefill", "axon_prefill_varlen", "axon_decode_step", "axon_reset",
             "axon_check_device", "axon_kv_view_get", "axon_profile_decode_step", "axon_profile_prefill",
             "axon_decode_step_noalloc", "axon_moe_routing_record", "axon_kv_cache_get", "axon_attn_decode",
-            "axon_attn_decode_workspace", "axon_attn_prefill", "axon_rope_table", "axon_kv_append", "axon_sample", "axon_kv_copy_blocks", "axon_kv_fork", "axon_kv_release",
+            "axon_attn_decode_workspace", "axon_attn_prefill", "axon_attn_shared", "axon_attn_shared_workspace", "axon_rope_table", "axon_kv_append", "axon_sample", "axon_kv_copy_blocks", "axon_kv_fork", "axon_kv_release",
             "axon_kv_reserve", "axon_kv_compact", "axon_kv_workspace", "axon_check_error", "axon_free",
             "axon_status_string"]
 
@@ -117,6 +117,9 @@ def lib() -> ctypes.CDLL:
         L.axon_attn_decode_workspace.argtypes = [vp, i32, i32, p_i64]
         L.axon_attn_prefill.argtypes = [vp, i32, vp, i64, i64, i32, i32, i32, vp, vp, i32, vp, i32, i32, i32, f32, vp,
                                         i64, i64, vp, vp]
+        L.axon_attn_shared.argtypes = [vp, i32, vp, i64, i64, i32, i32, vp, vp, i32, vp, vp, i32, i32, i32, f32, vp, i64, i64,
+                                       vp, vp, i64, vp, vp]
+        L.axon_attn_shared_workspace.argtypes = [vp, i32, i32, p_i64]
         L.axon_rope_table.argtypes = [vp, i32, i32, f32, f32, f32, f32, i32, vp]
         L.axon_kv_append.argtypes = [vp, i32] + [vp, i64, i64] * 3 + [i32, i32, i32, vp, vp, vp, i32, vp, i32, i32, i32, vp,
                                                                       i64, i64, vp, vp]
@@ -137,7 +140,8 @@ def lib() -> ctypes.CDLL:
                   "axon_decode_step_noalloc", "axon_moe_routing_record", "axon_kv_cache_get", "axon_attn_decode",
                   "axon_attn_decode_workspace", "axon_attn_prefill", "axon_kv_copy_blocks", "axon_kv_fork",
                   "axon_kv_release", "axon_kv_reserve", "axon_kv_compact", "axon_kv_workspace", "axon_check_error",
-                  "axon_rope_table", "axon_kv_append", "axon_sample"):
+                  "axon_rope_table", "axon_kv_append", "axon_sample", "axon_attn_shared",
+                  "axon_attn_shared_workspace"):
             getattr(L, n).restype = ctypes.c_int
         import torch
         _torch = torch
@@ -402,6 +406,14 @@ def make_attn_workspace(cache, rows, heads):
     return _torch.zeros(n.value, dtype=_torch.uint8, device=_torch.device("cuda", cache.device))
 
 
+def make_shared_workspace(cache, rows, heads):
+    """Zeroed workspace of axon_attn_shared for up to `rows` rows of `heads` heads on this cache; it serves axon_attn_decode too."""
+    n = ctypes.c_int64(0)
+    _current(cache.device)
+    _check("axon_attn_shared_workspace", lib().axon_attn_shared_workspace(cache.ref, heads, rows, ctypes.byref(n)))
+    return _torch.zeros(n.value, dtype=_torch.uint8, device=_torch.device("cuda", cache.device))
+
+
 def make_kv_workspace(cache, seqs):
     """Workspace of axon_kv_fork, axon_kv_reserve and axon_kv_compact."""
     n = ctypes.c_int64(0)
@@ -442,6 +454,24 @@ def axon_attn_decode(cache, layer, q, context_lens, out, workspace, block_table=
         None if err is None else _word(err, dev), _handle(stream, dev))
     if rc:
         raise AxonError("axon_attn_decode", rc)
+
+
+def axon_attn_shared(cache, layer, q, context_lens, group_offsets, prefix_lens, out, workspace, block_table, window=0,
+                     sinks=0, scale=0.0, lse=None, err=None, stream=None):
+    """axon_attn_decode for rows in groups whose first blocks are the same (see include/axon.h). group_offsets: int32
+    [groups + 1], rows of the groups; prefix_lens: int32 [groups], tokens whose whole blocks they share; workspace:
+    make_shared_workspace; the rest as in axon_attn_decode."""
+    B, H, qr, qh, orow, ohead = _rows(q, out, cache)
+    dev = cache.device
+    table, per = _table(block_table, 0, B, dev)
+    prefix, N = _list(prefix_lens, "prefix_lens", dev)
+    rc = _lib.axon_attn_shared(
+        cache.ref, layer, q.data_ptr(), qr, qh, B, H, _want(context_lens, _torch.int32, "context_lens", B, dev), table, per,
+        _want(group_offsets, _torch.int32, "group_offsets", N + 1, dev), prefix, N, window, sinks, scale, out.data_ptr(), orow,
+        ohead, None if lse is None else _want(lse, _torch.float32, "lse", B * H, dev), _space(workspace, dev), workspace.nbytes,
+        None if err is None else _word(err, dev), _handle(stream, dev))
+    if rc:
+        raise AxonError("axon_attn_shared", rc)
 
 
 def axon_attn_prefill(cache, layer, q, cu_seqlens, context_lens, max_chunk, out, block_table=None, blocks_per_seq=0,

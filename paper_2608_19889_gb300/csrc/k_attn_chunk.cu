@@ -67,25 +67,6 @@ struct KCfg {
   static constexpr int SMEM = 2 * TILE + STAGES * TILE + 8 * BARS + 2 * 32 + 16 + 1024;
 };
 
-// mbar_wait with a loop of few instructions: the kernel waits in some twenty places, and its
-// instruction fetches are on the critical path.
-AXON_DEV bool wait_bar(uint32_t bar, uint32_t parity, int* err) {
-  if (mbar_try_wait(bar, parity)) return true;
-  const uint64_t t0 = global_ns();
-#pragma unroll 1
-  while (!mbar_try_wait(bar, parity)) {
-    if (global_ns() - t0 > 2000000000ull) {
-      set_err(err, DEVERR_TIMEOUT);
-      return false;
-    }
-  }
-  return true;
-}
-AXON_DEV void st_global32(void* at, const uint32_t* v) {
-  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
-               "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
-               : "memory");
-}
 AXON_DEV void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
@@ -105,16 +86,6 @@ AXON_DEV float4 ld_cluster4(uint32_t at, int rank) {
                : "r"(at), "r"(rank)
                : "memory");
   return v;
-}
-AXON_DEV bool elect_one() {
-  uint32_t r;
-  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(r));
-  return r != 0;
-}
-AXON_DEV float max3(float a, float b, float c) {
-  float r;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
 }
 // A probability is at most the sum of its step, SUM_MAX: none saturates.
 static_assert(SUM_MAX < 65504.f, "probabilities have to fit fp16");

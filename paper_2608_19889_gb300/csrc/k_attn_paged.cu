@@ -32,6 +32,7 @@
 // that the output's only rounding that counts is its own.
 #include <math.h>
 
+#include "attn_shared.cuh"
 #include "kernels.h"
 
 namespace {
@@ -78,21 +79,24 @@ template <> AXON_DEV uint32_t pack_prob<f16>(float a, float b, float& ra, float&
   return *reinterpret_cast<uint32_t*>(&h);
 }
 
-// Pages of a row: `sink` pages from the front, then those from page `first` on.
+// Pages of a row: `sink` pages from the front, then those from page `first` on, without the `gap` pages from
+// `gap_at` on, which the row's group has in common.
 struct RowPages {
-  int pos, lo, sink, first, n;
+  int pos, lo, sink, first, n, gap_at, gap;
 };
-AXON_DEV RowPages row_pages(const PagedAttnArgs& p, int pos) {
+AXON_DEV RowPages row_pages(const PagedAttnArgs& p, int pos, int2 common = make_int2(INT_MAX, INT_MAX)) {
   RowPages r;
   r.pos = pos;
+  r.gap_at = common.x;
+  r.gap = common.y - common.x;
   if (pos < 0) {
-    r.lo = r.sink = r.first = r.n = 0;
+    r.lo = r.sink = r.first = r.n = r.gap = 0;
     return r;
   }
   r.lo = (p.window > 0 && pos >= p.window) ? pos - p.window + 1 : 0;
   r.first = r.lo >> 4;
   r.sink = min((min(p.sinks, pos + 1) + 15) >> 4, r.first);
-  r.n = r.sink + (pos >> 4) + 1 - r.first;
+  r.n = r.sink + (pos >> 4) + 1 - r.first - r.gap;
   return r;
 }
 // Position of row b's query; -1: the row sees nothing.
@@ -103,9 +107,10 @@ AXON_DEV int row_pos(const PagedAttnArgs& p, int b) {
   return -1;
 }
 
-// LO: q has a second 16-bit term, and o one too where o_lo is given.
-template <int HD, typename T16, int NT, bool LO>
-__global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_kernel(const PagedAttnArgs p) {
+// LO: q has a second 16-bit term, and o one too where o_lo is given. SH: without the pages that a row's group has in
+// common; a row that has some leaves its state for the join.
+template <int HD, typename T16, int NT, bool LO, bool SH>
+AXON_DEV void paged_decode(const PagedAttnArgs& p, const SharedGroups& sg) {
   using C = DCfg<HD, NT>;
   constexpr int KI = HD / 32;  // 16-byte pieces per key row and lane
   constexpr int VI = HD / 64;  // 16-byte pieces per value row and lane
@@ -118,13 +123,28 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, c = lane & 3;
   const int HPG = p.H / p.G;
   grid_dep_launch();
-  grid_dep_wait();
+  // (SH: the prefix pass before this kernel lets it start once its inputs are there)
+  if (!SH) grid_dep_wait();
+  GroupPlan gp{};
+  if constexpr (SH) {
+    int* const at = rpos + p.B;
+    gp = GroupPlan{at, at + sg.N, at + 2 * sg.N, at + 3 * sg.N};
+    plan_groups<DW * 32>(p, sg, gp, false);
+  }
+  // the pages that row b has in common with others
+  auto common = [&](int b) {
+    if constexpr (SH) {
+      const int n = group_of(sg, b);
+      if (n >= 0 && gp.c1[n] > gp.c0[n]) return make_int2(gp.c0[n], gp.c1[n]);
+    }
+    return make_int2(INT_MAX, INT_MAX);
+  };
 
   // ---- pages before each row
   if (p.B <= 32) {
     if (warp == 0) {
       const int pos = lane < p.B ? row_pos(p, lane) : -1;
-      const int n = row_pages(p, pos).n;
+      const int n = row_pages(p, pos, SH && pos >= 0 ? common(lane) : make_int2(INT_MAX, INT_MAX)).n;
       int inc = n;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -142,7 +162,7 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
     for (int b0 = 0; b0 < p.B; b0 += DW * 32) {
       const int b = b0 + tid;
       const int pos = b < p.B ? row_pos(p, b) : -1;
-      const int n = row_pages(p, pos).n;
+      const int n = row_pages(p, pos, SH && pos >= 0 ? common(b) : make_int2(INT_MAX, INT_MAX)).n;
       int inc = n;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -172,6 +192,15 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
   // ---- rows that see nothing
   for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
     if (before[b + 1] != before[b]) continue;
+    if (SH && row_pages(p, rpos[b], common(b)).gap > 0) {
+      // everything that the row sees is in common
+      for (int i = tid; i < p.H * (HD / 4); i += DW * 32) {
+        const long long at = static_cast<long long>(b) * p.H + i / (HD / 4);
+        reinterpret_cast<float4*>(sg.state)[static_cast<long long>(b) * p.H * (HD / 4) + i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (i % (HD / 4) == 0) sg.state_stats[at] = make_float2(-INFINITY, 0.f);
+      }
+      continue;
+    }
     for (int i = tid; i < p.H * (HD / 8); i += DW * 32) {
       const int h = i / (HD / 8), x = i % (HD / 8);
       const long long at = b * p.o_row + h * p.o_head + x * 8;
@@ -216,7 +245,7 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
 
   for (unsigned u = u0; u < u1;) {
     while (before[b + 1] * p.G <= u) ++b;
-    const RowPages rp = row_pages(p, rpos[b]);
+    const RowPages rp = row_pages(p, rpos[b], SH ? common(b) : make_int2(INT_MAX, INT_MAX));
     const unsigned row0 = before[b] * p.G;
     const int g = static_cast<int>((u - row0) / rp.n);
     const unsigned item0 = row0 + static_cast<unsigned>(g) * rp.n;
@@ -227,7 +256,8 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
     const int pages = cnt > wg ? (cnt - wg + gs - 1) / gs : 0;
     auto logical = [&](int k) {  // page of the row that is this warp's k-th
       const int i = off + wg + k * gs;
-      return i < rp.sink ? i : i - rp.sink + rp.first;
+      const int j = i < rp.sink ? i : i - rp.sink + rp.first;
+      return SH && j >= rp.gap_at ? j + rp.gap : j;
     };
     auto entries = [&](int k0) {  // pool blocks of this warp's pages k0 .. k0 + 31, one per lane
       const int k = k0 + lane;
@@ -429,6 +459,12 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
     const int gl = wg * 32 + lane;
     constexpr int PX = HD / 4;  // 4-dim pieces of a head
     auto finish = [&](int h, int x, float4 v, float M, float L) {
+      if (SH && rp.gap > 0) {
+        const long long at = static_cast<long long>(b) * p.H + g * HPG + h;
+        *reinterpret_cast<float4*>(sg.state + at * HD + x * 4) = v;
+        if (x == 0) sg.state_stats[at] = make_float2(M, L);
+        return;
+      }
       const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
       const long long at = b * p.o_row + (g * HPG + h) * p.o_head + x * 4;
       v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
@@ -549,6 +585,16 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
   }
 }
 
+template <int HD, typename T16, int NT, bool LO>
+__global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_kernel(const PagedAttnArgs p) {
+  paged_decode<HD, T16, NT, LO, false>(p, SharedGroups{});
+}
+template <int HD, typename T16, int NT>
+__global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_own_kernel(const PagedAttnArgs p, const SharedGroups sg) {
+  paged_decode<HD, T16, NT, false, true>(p, sg);
+  grid_dep_wait();  // this kernel's end means the prefix pass's too, for the join
+}
+
 template <int HD, int NT>
 constexpr size_t smem_bytes(int B) {
   return static_cast<size_t>(DW) * DCfg<HD, NT>::STATE * 4 + (2 * static_cast<size_t>(B) + 1) * 4;
@@ -562,12 +608,15 @@ cudaError_t prepare_hd() {
   if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_paged_decode_kernel<HD, T16, 1, true>, attr, one);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_paged_decode_kernel<HD, T16, 2, false>, attr, two);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_paged_decode_kernel<HD, T16, 2, true>, attr, two);
+  constexpr int plan = 16 * SHARED_MAX_GROUPS;
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_paged_own_kernel<HD, T16, 1>, attr, one + plan);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_paged_own_kernel<HD, T16, 2>, attr, two + plan);
   return e;
 }
 
 template <int HD, typename T16, int NT, bool LO>
-cudaError_t launch_nt(const LaunchCtx& lc, const PagedAttnArgs& a) {
-  const size_t smem = smem_bytes<HD, NT>(a.B);
+cudaError_t launch_nt(const LaunchCtx& lc, const PagedAttnArgs& a, const SharedGroups* sg = nullptr) {
+  const size_t smem = smem_bytes<HD, NT>(a.B) + (sg ? 16 * static_cast<size_t>(sg->N) : 0);
   // no more CTAs than pages that can be visible, at a page per warp
   const long long pages = paged_attn_most_pages(a.B, a.G, a.blocks_per_seq, a.window, a.sinks);
   const long long most = static_cast<long long>(lc.num_sms) * (NT == 1 ? 3 : 2);
@@ -581,7 +630,13 @@ cudaError_t launch_nt(const LaunchCtx& lc, const PagedAttnArgs& a) {
   cudaLaunchAttribute attr[2];
   cfg.numAttrs = chain_attrs(lc, attr);
   cfg.attrs = attr;
+  if (sg) return cudaLaunchKernelEx(&cfg, attn_paged_own_kernel<HD, T16, NT>, a, *sg);
   return cudaLaunchKernelEx(&cfg, attn_paged_decode_kernel<HD, T16, NT, LO>, a);
+}
+
+template <int HD, typename T16>
+cudaError_t launch_own_hd(const LaunchCtx& lc, const PagedAttnArgs& a, const SharedGroups& sg) {
+  return a.H / a.G <= 8 ? launch_nt<HD, T16, 1, false>(lc, a, &sg) : launch_nt<HD, T16, 2, false>(lc, a, &sg);
 }
 
 template <int HD, typename T16>
@@ -615,5 +670,12 @@ cudaError_t launch_attn_paged_decode(const LaunchCtx& lc, const PagedAttnArgs& a
     return cudaErrorInvalidValue;
   if (a.d == 64) return lc.f16 ? launch_hd<64, f16>(lc, a) : launch_hd<64, bf16>(lc, a);
   if (a.d == 128) return lc.f16 ? launch_hd<128, f16>(lc, a) : launch_hd<128, bf16>(lc, a);
+  return cudaErrorInvalidValue;
+}
+
+cudaError_t launch_attn_paged_own(const LaunchCtx& lc, const PagedAttnArgs& a, const SharedGroups& s) {
+  if (a.H / a.G > 16 || a.B < 1 || a.B > PAGED_ATTN_MAX_B || a.q_lo || s.N > SHARED_MAX_GROUPS) return cudaErrorInvalidValue;
+  if (a.d == 64) return lc.f16 ? launch_own_hd<64, f16>(lc, a, s) : launch_own_hd<64, bf16>(lc, a, s);
+  if (a.d == 128) return lc.f16 ? launch_own_hd<128, f16>(lc, a, s) : launch_own_hd<128, bf16>(lc, a, s);
   return cudaErrorInvalidValue;
 }

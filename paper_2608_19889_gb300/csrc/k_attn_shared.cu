@@ -1,0 +1,624 @@
+// Attention of one new token per row where rows share the first blocks of their context: the
+// prefix pass over the blocks in common, once per group, and the join with each row's own part,
+// which the one-token kernel (k_attn_paged.cu) takes.
+//
+//   o = sum over parts of 2^(m_i - m) O_i / sum of 2^(m_i - m) l_i,  m = max m_i
+//   (m_i, l_i, O_i): a part's maximum, sum of 2^(s - m_i) and sum of 2^(s - m_i) v
+//
+// The blocks in common are read once for all rows of a group and hold no masked token, so that the prefix
+// pass is a plain product: a tile is 128 (row, query head) pairs of one kv head, PW = 128 / (H/G) rows; an item is
+// two tiles of a group and a kv head, which share the keys, 128 per step (eight blocks). The steps of all
+// items form one line, which the CTAs (one per SM) split evenly: an item's parts go to the workspace, as many as
+// CTAs have a share of it, and the join adds them up in their order, so that results do not depend on timing.
+// Warps:
+//   0..3, 4..7  softmax of tile 0 and 1, one thread per (row, head);
+//   8           TMA producer: queries of an item, keys and values through a ring of tiles;
+//   9, 11       MMA issuers of tile 0 and 1 (S = Q K^T into TMEM, O += P V with P from TMEM).
+// P enters the product in two 16-bit terms, as in the other attention kernels.
+#include <math.h>
+
+#include <algorithm>
+
+#include "attn_shared.cuh"
+#include "attn_tc.cuh"
+#include "kernels.h"
+
+namespace {
+
+constexpr int THREADS = 384;
+constexpr int KT = 128;    // keys per step
+constexpr float LAG = 4.f; // how far a row's scores may exceed its m (log2)
+constexpr int MAX_N = SHARED_MAX_GROUPS;
+
+template <int HD>
+struct SCfg {
+  static constexpr int CH = HD / 64;                // 64-dim chunks (128-byte swizzled rows)
+  static constexpr int CHUNK = 128 * 128;           // bytes of one 128-row chunk
+  static constexpr int TILE = CH * CHUNK;           // Q, K or V tile
+  static constexpr int STAGES = HD == 128 ? 4 : 8;  // K and V tiles in flight
+  static constexpr int BARS = 2 * STAGES + 14;
+  static constexpr int PLAN = 4 * (5 * MAX_N + 4);
+  static constexpr int SMEM = 2 * TILE + STAGES * TILE + 8 * BARS + 16 + PLAN + 1024;
+};
+
+// How the steps are dealt: `workers` CTAs, the first `extra` of them one step more than `share`.
+struct Deal {
+  unsigned total, workers, share, extra;
+  AXON_DEV unsigned begin(unsigned w) const { return w * share + min(w, extra); }
+  AXON_DEV unsigned worker_of(unsigned u) const {
+    const unsigned cut = extra * (share + 1);
+    return u < cut ? u / (share + 1) : extra + (u - cut) / share;
+  }
+};
+AXON_DEV Deal deal(unsigned total, unsigned ctas, unsigned least) {
+  Deal d;
+  d.total = total;
+  d.workers = min(ctas, max(1u, total / least));
+  d.share = total / d.workers;
+  d.extra = total - d.share * d.workers;
+  return d;
+}
+
+// A CTA's share of an item.
+struct Part {
+  int group, g;       // group, kv head
+  int r0, p0, rows;   // the group's first row, the item's first row in the group, rows of the item
+  int page0, pages;   // blocks
+  int lead;
+  long long at;       // its first (row, head) in the workspace
+  unsigned steps;
+};
+
+// In front of the parts' first (row, head): those of the items before it, which all lie inside B * H, and 256 for each
+// CTA before, since an item has that many (row, head) pairs at most and each CTA adds a part at most.
+AXON_DEV long long part_at(int r0, int rows, int g, int p0, int H, int HPG, unsigned worker) {
+  return static_cast<long long>(r0) * H + (static_cast<long long>(g) * rows + p0) * HPG + 256ll * worker;
+}
+
+template <int HD, typename T16>
+__global__ void __launch_bounds__(THREADS, 1)
+    attn_prefix_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                       const __grid_constant__ CUtensorMap tmV, const PagedAttnArgs p, const SharedGroups sg, int PW, int pool_rows) {
+  using C = SCfg<HD>;
+  constexpr int NS = C::STAGES;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  const uint32_t sQ = base, sKV = base + 2 * C::TILE, bars = sKV + NS * C::TILE;
+  auto kv_full = [&](int s) { return bars + 8 * s; };
+  auto kv_empty = [&](int s) { return bars + 8 * (NS + s); };
+  const uint32_t more = bars + 8 * (2 * NS);
+  auto q_full = [&](int w) { return more + 8 * w; };
+  auto q_empty = [&](int w) { return more + 8 * (2 + w); };
+  auto s_full = [&](int w) { return more + 8 * (4 + w); };
+  auto p_full = [&](int w) { return more + 8 * (6 + w); };
+  auto o_full = [&](int w) { return more + 8 * (8 + w); };
+  auto o_empty = [&](int w) { return more + 8 * (10 + w); };
+  auto turn = [&](int w) { return more + 8 * (12 + w); };
+  const uint32_t tmem_slot = bars + 8 * C::BARS;
+  int* const plan = reinterpret_cast<int*>(smem_raw + (tmem_slot + 16 - raw));
+  const GroupPlan gp{plan, plan + MAX_N, plan + 2 * MAX_N, plan + 3 * MAX_N};
+  unsigned* const before = reinterpret_cast<unsigned*>(plan + 4 * MAX_N);  // [N + 1] steps of the groups before
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const int HPG = p.H / p.G, PC = 2 * PW;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < NS; ++s) {
+      mbar_init(kv_full(s), 1);
+      mbar_init(kv_empty(s), 2);  // both issuers
+    }
+    for (int w = 0; w < 2; ++w) {
+      mbar_init(q_full(w), 1);
+      mbar_init(q_empty(w), 1);
+      mbar_init(s_full(w), 1);
+      mbar_init(p_full(w), 128);
+      mbar_init(o_full(w), 1);
+      mbar_init(o_empty(w), 128);
+      mbar_init(turn(w), 1);
+    }
+    fence_mbar_init();
+    fence_proxy_async();
+    tma_prefetch_desc(&tmQ);
+    tma_prefetch_desc(&tmK);
+    tma_prefetch_desc(&tmV);
+  }
+  if (warp == 9) {
+    tmem_alloc(tmem_slot, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *reinterpret_cast<const uint32_t*>(smem_raw + (tmem_slot - raw));
+  grid_dep_wait();
+  grid_dep_launch();  // the rows' own parts, which wait for nothing of this kernel
+
+  // ---- what is in common, and the line of steps
+  plan_groups<THREADS>(p, sg, gp, blockIdx.x == 0);
+  if (warp == 0) {
+    unsigned sum = 0;
+    for (int i0 = 0; i0 < sg.N; i0 += 32) {
+      const int i = i0 + lane;
+      unsigned n = 0;
+      if (i < sg.N && gp.c1[i] > gp.c0[i])
+        n = static_cast<unsigned>((gp.c1[i] - gp.c0[i] + 7) >> 3) * ((sg.offsets[i + 1] - sg.offsets[i] + PC - 1) / PC) * p.G;
+      unsigned inc = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const unsigned t = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += t;
+      }
+      if (i < sg.N) before[i] = sum + inc - n;
+      sum += __shfl_sync(0xffffffffu, inc, 31);
+    }
+    if (lane == 0) before[sg.N] = sum;
+  }
+  __syncthreads();
+  const Deal d = deal(before[sg.N], gridDim.x, sg.least_steps);
+  if (blockIdx.x == 0) {
+    // for the join
+    for (int i = threadIdx.x; i < sg.N; i += THREADS)
+      sg.plan[1 + i] = make_int4(gp.c0[i], gp.c1[i], static_cast<int>(before[i]), 0);
+    if (threadIdx.x == 0) sg.plan[0] = make_int4(static_cast<int>(d.total), static_cast<int>(gridDim.x), sg.least_steps, 0);
+  }
+  const unsigned u1 = blockIdx.x < d.workers && d.total ? d.begin(blockIdx.x + 1) : 0;
+  // The part that begins at step u (< u1) of the line; the same in all lanes.
+  auto part_of = [&](unsigned u) {
+    int lo = 0, hi = sg.N - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (before[mid] <= u) lo = mid; else hi = mid - 1;
+    }
+    Part t;
+    t.group = lo;
+    t.r0 = sg.offsets[lo];
+    const int rows = sg.offsets[lo + 1] - t.r0, pages = gp.c1[lo] - gp.c0[lo], pairs = (rows + PC - 1) / PC;
+    const unsigned steps = (pages + 7) >> 3, off = u - before[lo], item = off / steps, first = off - item * steps;
+    t.g = static_cast<int>(item) / pairs;
+    t.p0 = (static_cast<int>(item) - t.g * pairs) * PC;
+    t.rows = min(PC, rows - t.p0);
+    t.steps = min(steps - first, u1 - u);
+    t.page0 = gp.c0[lo] + 8 * static_cast<int>(first);
+    t.pages = min(gp.c1[lo] - t.page0, 8 * static_cast<int>(t.steps));
+    t.lead = gp.lead[lo];
+    t.at = part_at(t.r0, rows, t.g, t.p0, p.H, HPG, blockIdx.x);
+    return t;
+  };
+  const unsigned u0 = u1 ? d.begin(blockIdx.x) : 0;
+
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if (warp == 8) {
+      // ----------------------------------------------------------- producer
+      int iq[2] = {0, 0}, it = 0;
+      bool ok = true;
+      for (unsigned u = u0; u < u1 && ok;) {
+        const Part t = part_of(u);
+        u += t.steps;
+        for (int w = 0; w < 2 && w * PW < t.rows; ++w) {
+          ok = __all_sync(0xffffffffu, wait_bar(q_empty(w), (iq[w] & 1) ^ 1, p.err));
+          if (!ok) break;
+          if (lane == 0) {
+            mbar_arrive_expect_tx(q_full(w), HPG * PW * HD * 2);
+            for (int c = 0; c < C::CH; ++c)
+              tma_load_3d(sQ + w * C::TILE + c * C::CHUNK, &tmQ, q_full(w), c * 64, t.g * HPG, t.r0 + t.p0 + w * PW);
+          }
+          ++iq[w];
+        }
+        // pool row of this lane's block of step s; past the last block and for table entries
+        // out of range (reported) the row lies outside the pool, where a box reads zeros
+        auto pool_row = [&](unsigned s) {
+          const int i = static_cast<int>(s) * 8 + lane;
+          if (lane >= 8 || i >= t.pages) return pool_rows;
+          const int blk = p.block_table[static_cast<long long>(t.lead) * p.blocks_per_seq + t.page0 + i];
+          if (blk < 0 || blk >= p.num_blocks) {
+            set_err(p.err, DEVERR_BLOCK);
+            return pool_rows;
+          }
+          return (blk * p.G + t.g) * 16;
+        };
+        int next = pool_row(0);
+        for (unsigned s = 0; s < t.steps && ok; ++s) {
+          const int y = next;
+          next = pool_row(s + 1);
+          for (int kv = 0; kv < 2; ++kv, ++it) {
+            const int st = it % NS;
+            ok = __all_sync(0xffffffffu, wait_bar(kv_empty(st), ((it / NS) & 1) ^ 1, p.err));
+            if (!ok) break;
+            if (lane == 0) mbar_arrive_expect_tx(kv_full(st), C::TILE);
+            __syncwarp();
+            if (lane < 8)
+              for (int c = 0; c < C::CH; ++c)
+                tma_load_2d(sKV + st * C::TILE + c * C::CHUNK + lane * 2048, kv ? &tmV : &tmK, kv_full(st), c * 64, y);
+          }
+        }
+      }
+      // every copy lands before the CTA's shared memory goes away
+      for (int w = 0; w < 2; ++w)
+        if (iq[w] > 0) wait_bar(q_full(w), (iq[w] - 1) & 1, p.err);
+      for (int i = it > NS ? it - NS : 0; i < it; ++i) wait_bar(kv_full(i % NS), (i / NS) & 1, p.err);
+    } else if (warp != 10) {
+      // -------------------------------------------------------- MMA issuers
+      // A warp per tile, in turns: one tile's products run under the other's softmax.
+      const int w = warp == 9 ? 0 : 1;
+      const bool leader = elect_one();
+      constexpr uint32_t id_s = idesc_f32acc(128, KT, MmaFmt<T16>::v);
+      constexpr uint32_t id_o = idesc_f32acc(128, HD, MmaFmt<T16>::v) | (1u << 16);  // B stored N-contiguous
+      const uint64_t dQ = smem_desc_sw128(sQ + w * C::TILE), dK = smem_desc_sw128(sKV), dV = v_desc<C::CHUNK>(sKV);
+      const uint32_t tS = tmem + w * KT, tO = tmem + 2 * KT + w * HD;
+      uint32_t st = 0, ph = 0;  // ring: next stage and its phase
+      auto next_stage = [&]() {
+        st = st + 1 == NS ? 0 : st + 1;
+        ph ^= st == 0;
+      };
+      auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_bar(bar, parity, p.err)) != 0; };
+      uint32_t ph_q = 0, ph_p = 0;  // phases of this tile's parts and steps
+      uint32_t turns = 0;
+      auto my_turn = [&]() { return wait_all(turn(w), (turns & 1) ^ (w ^ 1)); };
+      // scores from the keys in stage st; the turn passes two products before the end
+      auto scores = [&](bool last) {
+        const uint64_t kd = dK + st * (C::TILE >> 4);
+        if (leader) {
+#pragma unroll
+          for (int k = 0; k < HD / 16; ++k) {
+            const int off = ((k >> 2) * C::CHUNK + (k & 3) * 32) >> 4;
+            if (k == HD / 16 - 2) mbar_arrive(turn(w ^ 1));
+            tc_mma_f16(tS, dQ + off, kd + off, id_s, k != 0);
+          }
+          tc_commit(s_full(w));
+          if (last) tc_commit(q_empty(w));
+        }
+        ++turns;
+      };
+      auto pass_turn = [&]() {
+        if (leader) mbar_arrive(turn(w ^ 1));
+        ++turns;
+      };
+      for (unsigned u = u0; u < u1;) {
+        const Part t = part_of(u);
+        u += t.steps;
+        const int nt_all = __shfl_sync(0xffffffffu, static_cast<int>(t.steps), 0), pages = __shfl_sync(0xffffffffu, t.pages, 0);
+        const int nt = w * PW < t.rows ? nt_all : 0;
+        bool ok = wait_all(kv_full(st), ph) && (!nt || wait_all(q_full(w), ph_q)) && my_turn();
+        if (!ok) break;
+        tc_fence_after();
+        if (nt)
+          scores(nt == 1);
+        else
+          pass_turn();
+        if (leader) tc_commit(kv_empty(st));
+        next_stage();
+        for (int s = 0; s < nt_all; ++s) {
+          const bool keys = s + 1 < nt_all;
+          const uint32_t sv = st, phv = ph;
+          next_stage();
+          ok = wait_all(kv_full(sv), phv) && (!keys || wait_all(kv_full(st), ph)) &&
+               (!nt || s != 0 || wait_all(o_empty(w), ph_q ^ 1)) && my_turn() && (!nt || wait_all(p_full(w), ph_p));
+          if (!ok) break;
+          tc_fence_after();
+          if (nt) {
+            const uint64_t vd = dV + sv * (C::TILE >> 4);
+            ph_p ^= 1;
+            const int blocks = min(8, pages - 8 * s);
+            if (s != 0 && blocks == 8) {
+              if (leader) {
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                  tc_mma_f16_ts(tO, tS + x * 8, vd + x * 128, id_o, 1u);
+                  tc_mma_f16_ts(tO, tS + KT / 2 + x * 8, vd + x * 128, id_o, 1u);
+                }
+              }
+            } else if (leader) {
+              // the first step starts the sums; blocks past the last hold no values
+#pragma unroll 1
+              for (int x = 0; x < blocks; ++x) {
+                tc_mma_f16_ts(tO, tS + x * 8, vd + x * 128, id_o, (s | x) != 0 ? 1u : 0u);
+                tc_mma_f16_ts(tO, tS + KT / 2 + x * 8, vd + x * 128, id_o, 1u);
+              }
+            }
+            // MMAs run in issue order: the next scores may overwrite the probabilities just
+            // issued, and s_full implies that O is up to date
+            if (keys) {
+              scores(s + 2 == nt);
+            } else {
+              pass_turn();
+              if (leader) tc_commit(o_full(w));
+            }
+          } else {
+            pass_turn();
+          }
+          if (leader) tc_commit(kv_empty(sv));
+          if (keys) {
+            if (leader) tc_commit(kv_empty(st));
+            next_stage();
+          }
+        }
+        if (!ok) break;
+        if (nt) ph_q ^= 1;
+      }
+    }
+    __syncwarp();
+  } else {
+    // --------------------------------------------------------------- softmax
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    const int w = warp >> 2;
+    const int i = threadIdx.x & 127;  // row of the tile
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t tS = tmem + lanes + w * KT, tO = tmem + lanes + 2 * KT + w * HD;
+    const float sl2 = p.scale_log2;
+    const uint64_t sl2p = pk2(sl2, sl2);
+    int ns_ = 0, no = 0;  // scores and outputs taken
+    bool ok = true;
+    for (unsigned u = u0; u < u1 && ok;) {
+      const Part t = part_of(u);
+      u += t.steps;
+      if (w * PW >= t.rows) continue;
+      const bool valid = i < HPG * PW && w * PW * HPG + i < t.rows * HPG;
+      float m = valid ? -INFINITY : 0.f;
+      uint64_t l2 = pk2(0.f, 0.f);
+      for (int s_ = 0; s_ < static_cast<int>(t.steps); ++s_) {
+        ok = __all_sync(0xffffffffu, wait_bar(s_full(w), ns_ & 1, p.err));
+        if (!ok) break;
+        ++ns_;
+        tc_fence_after();
+        float s[KT];
+        tmem_ld32(tS, reinterpret_cast<uint32_t*>(s));
+        tmem_ld32(tS + 32, reinterpret_cast<uint32_t*>(s) + 32);
+        tmem_ld32(tS + 64, reinterpret_cast<uint32_t*>(s) + 64);
+        tmem_ld32(tS + 96, reinterpret_cast<uint32_t*>(s) + 96);
+        tmem_wait_ld();
+        const int cols = (t.pages - 8 * s_) * 16;  // keys of the step
+        if (cols < KT) {
+#pragma unroll
+          for (int c = 16; c < KT; ++c) s[c] = c < cols ? s[c] : -INFINITY;
+        }
+        float m4[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+        for (int c = 4; c < 124; c += 8) {
+#pragma unroll
+          for (int y = 0; y < 4; ++y) m4[y] = max3(m4[y], s[c + y], s[c + 4 + y]);
+        }
+        const float mx = max3(max3(m4[0], s[124], s[125]), max3(m4[1], s[126], s[127]), max3(m4[2], m4[3], m4[3])) * sl2;
+        const bool up = valid && mx > (m == -INFINITY ? m : m + LAG);
+        if (__any_sync(0xffffffffu, up)) {
+          const float f = up ? (m == -INFINITY ? 0.f : ex2(m - mx)) : 1.f;
+          m = up ? mx : m;
+          const uint64_t f2 = pk2(f, f);
+          l2 = mul2(l2, f2);
+          if (s_ > 0) {
+#pragma unroll 1
+            for (int c = 0; c < HD; c += 32) {
+              float o[32];
+              tmem_ld32(tO + c, reinterpret_cast<uint32_t*>(o));
+              tmem_wait_ld();
+#pragma unroll
+              for (int x = 0; x < 32; x += 2) upk2(mul2(pk2(o[x], o[x + 1]), f2), o[x], o[x + 1]);
+              tmem_st32(tO + c, reinterpret_cast<uint32_t*>(o));
+            }
+            tmem_wait_st();
+          }
+        }
+        const float nb = m == -INFINITY ? 0.f : -m;
+        const uint64_t nbp = pk2(nb, nb);
+        uint32_t pr[KT / 2], rest[KT / 2];
+        uint64_t sum[4] = {0, 0, 0, 0};  // pairs of 0.f
+#pragma unroll
+        for (int c = 0; c < KT / 2; ++c) {
+          float a, e;
+          upk2(fma2(pk2(s[2 * c], s[2 * c + 1]), sl2p, nbp), a, e);
+          a = ex2(a);
+          e = ex2(e);
+          pr[c] = pack_p<T16>(a, e);
+          rest[c] = pack_rest<T16>(a, e, pr[c]);
+          sum[c & 3] = add2(sum[c & 3], pk2(a, e));
+        }
+        tmem_st32(tS, pr);
+        tmem_st32(tS + 32, pr + 32);
+        tmem_st32(tS + 64, rest);
+        tmem_st32(tS + 96, rest + 32);
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(p_full(w));
+        l2 = add2(l2, add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])));
+      }
+      if (!ok) break;
+      ok = __all_sync(0xffffffffu, wait_bar(o_full(w), no & 1, p.err));
+      if (!ok) break;
+      ++no;
+      tc_fence_after();
+      const long long at = t.at + w * PW * HPG + i;
+      float* const dst = sg.part + at * HD;
+#pragma unroll 1
+      for (int c = 0; c < HD; c += 32) {
+        uint32_t o[32];
+        tmem_ld32(tO + c, o);
+        tmem_wait_ld();
+        if (c + 32 == HD) {
+          tc_fence_before();
+          mbar_arrive(o_empty(w));
+        }
+        if (valid) {
+#pragma unroll
+          for (int x = 0; x < 32; x += 8) st_global32(dst + c + x, o + x);
+        }
+      }
+      if (valid) {
+        float la, lb;
+        upk2(l2, la, lb);
+        sg.stats[at] = make_float2(m, la + lb);
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+constexpr int JT = 128;  // threads of the join
+
+// One CTA per row and query head: the parts of its item, in order, and the row's own.
+template <int HD, typename T16>
+__global__ void __launch_bounds__(JT) attn_join_kernel(const PagedAttnArgs p, const SharedGroups sg, int PC) {
+  __shared__ float s_f[1024 + 1];
+  __shared__ float s_red[2][JT / 32];
+  __shared__ float4 s_o[JT];
+  grid_dep_launch();
+  const int b = blockIdx.x, h = blockIdx.y, tid = threadIdx.x;
+  grid_dep_wait();
+  if (live_pos(p, b) < 0) return;
+  const int n = group_of(sg, b);
+  if (n < 0) return;
+  const int4 gp = sg.plan[1 + n], all = sg.plan[0];
+  if (gp.y <= gp.x) return;
+  const Deal d = deal(static_cast<unsigned>(all.x), static_cast<unsigned>(all.y), static_cast<unsigned>(all.z));
+  const int HPG = p.H / p.G, g = h / HPG, r0 = sg.offsets[n], rows = sg.offsets[n + 1] - r0, pairs = (rows + PC - 1) / PC;
+  const int pair = (b - r0) / PC;
+  const unsigned steps = (gp.y - gp.x + 7) >> 3, first = static_cast<unsigned>(gp.z) + (static_cast<unsigned>(g) * pairs + pair) * steps;
+  const unsigned w0 = d.worker_of(first);
+  const int parts = static_cast<int>(d.worker_of(first + steps - 1) - w0) + 1;
+  const long long at = part_at(r0, rows, g, pair * PC, p.H, HPG, w0) + (b - r0 - pair * PC) * HPG + h - g * HPG;
+  const long long own = static_cast<long long>(b) * p.H + h;
+
+  // factors: the parts', and the row's own last
+  float2 st[1 + 1024 / JT];
+  float M = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < 1 + 1024 / JT; ++k) {
+    const int i = tid + k * JT;
+    st[k] = make_float2(-INFINITY, 0.f);
+    if (i <= parts) st[k] = i < parts ? __ldcg(sg.stats + at + 256ll * i) : __ldcg(sg.state_stats + own);
+    M = fmaxf(M, st[k].x);
+  }
+  M = warp_max(M);
+  if ((tid & 31) == 0) s_red[0][tid >> 5] = M;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < JT / 32; ++k) M = fmaxf(M, s_red[0][k]);
+  const float top = M == -INFINITY ? 0.f : M;
+  float L = 0.f;
+#pragma unroll
+  for (int k = 0; k < 1 + 1024 / JT; ++k) {
+    const int i = tid + k * JT;
+    if (i > parts) break;
+    const float f = exp2f(st[k].x - top);
+    s_f[i] = f;
+    L += f * st[k].y;
+  }
+  L = warp_sum(L);
+  if ((tid & 31) == 0) s_red[1][tid >> 5] = L;
+  __syncthreads();
+  L = 0.f;
+#pragma unroll
+  for (int k = 0; k < JT / 32; ++k) L += s_red[1][k];
+
+  constexpr int X = HD / 4, PG = JT / X;  // 16-byte pieces of a row; threads that share them
+  const int x = tid % X, pg = tid / X;
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i0 = pg; i0 <= parts; i0 += 8 * PG) {
+    float4 o[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int i = i0 + k * PG;
+      o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (i <= parts)
+        o[k] = __ldcg(reinterpret_cast<const float4*>(i < parts ? sg.part + (at + 256ll * i) * HD : sg.state + own * HD) + x);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int i = i0 + k * PG;
+      const float f = i <= parts ? s_f[i] : 0.f;
+      if (f != 0.f) v = make_float4(v.x + f * o[k].x, v.y + f * o[k].y, v.z + f * o[k].z, v.w + f * o[k].w);
+    }
+  }
+  s_o[tid] = v;
+  __syncthreads();
+  if (pg) return;
+#pragma unroll
+  for (int k = 1; k < PG; ++k) {
+    const float4 e = s_o[k * X + x];
+    v = make_float4(v.x + e.x, v.y + e.y, v.z + e.z, v.w + e.w);
+  }
+  const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
+  *reinterpret_cast<uint2*>(static_cast<T16*>(p.o) + b * p.o_row + h * p.o_head + x * 4) =
+      make_uint2(pack2<T16>(v.x * inv, v.y * inv), pack2<T16>(v.z * inv, v.w * inv));
+  if (p.lse && x == 0) p.lse[own] = (M + log2f(L)) * 0.69314718055994531f;
+}
+
+template <int HD, typename T16>
+cudaError_t prepare_hd() {
+  return cudaFuncSetAttribute(attn_prefix_kernel<HD, T16>, cudaFuncAttributeMaxDynamicSharedMemorySize, SCfg<HD>::SMEM);
+}
+
+template <int HD, typename T16>
+cudaError_t launch_prefix_hd(const LaunchCtx& lc, const PagedAttnArgs& a, const SharedGroups& s, const AttnMaps& maps) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.blockDim = dim3(THREADS);
+  cfg.gridDim = dim3(lc.num_sms);
+  cfg.dynamicSmemBytes = SCfg<HD>::SMEM;
+  cfg.stream = lc.stream;
+  cudaLaunchAttribute attr[2];
+  cfg.numAttrs = chain_attrs(lc, attr);
+  cfg.attrs = attr;
+  return cudaLaunchKernelEx(&cfg, attn_prefix_kernel<HD, T16>, maps.q, maps.k, maps.v, a, s, attn_tile_positions(a.H, a.G),
+                            maps.pool_rows);
+}
+template <int HD, typename T16>
+cudaError_t launch_join_hd(const LaunchCtx& lc, const PagedAttnArgs& a, const SharedGroups& s) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.blockDim = dim3(JT);
+  cfg.gridDim = dim3(a.B, a.H);
+  cfg.stream = lc.stream;
+  cudaLaunchAttribute attr[2];
+  cfg.numAttrs = chain_attrs(lc, attr);
+  cfg.attrs = attr;
+  return cudaLaunchKernelEx(&cfg, attn_join_kernel<HD, T16>, a, s, 2 * attn_tile_positions(a.H, a.G));
+}
+
+template <int HD, typename T16>
+cudaError_t launch_hd(const LaunchCtx& lc, const PagedAttnArgs& a, const SharedGroups& s, const AttnMaps& maps) {
+  cudaError_t e = launch_prefix_hd<HD, T16>(lc, a, s, maps);
+  if (e == cudaSuccess) e = launch_attn_paged_own(lc, a, s);
+  return e == cudaSuccess ? launch_join_hd<HD, T16>(lc, a, s) : e;
+}
+
+constexpr size_t ALIGN = 256;
+size_t aligned(size_t n) { return (n + ALIGN - 1) / ALIGN * ALIGN; }
+
+}  // namespace
+
+cudaError_t prepare_attn_shared_kernels() {
+  cudaError_t e = prepare_hd<64, bf16>();
+  if (e == cudaSuccess) e = prepare_hd<64, f16>();
+  if (e == cudaSuccess) e = prepare_hd<128, bf16>();
+  if (e == cudaSuccess) e = prepare_hd<128, f16>();
+  return e;
+}
+
+// Plan, the rows' own states, the prefix pass's parts, from a multiple of 256 bytes on.
+size_t shared_attn_bytes(int B, int H, int d, int num_sms) {
+  const size_t own = static_cast<size_t>(B) * H, parts = own + 256 * static_cast<size_t>(num_sms);
+  return ALIGN + aligned(16 * (1 + MAX_N)) + aligned(8 * own) + aligned(8 * parts) + 4 * static_cast<size_t>(d) * (own + parts);
+}
+void shared_attn_carve(SharedGroups* s, void* work, int B, int H, int d, int num_sms) {
+  const size_t own = static_cast<size_t>(B) * H, parts = own + 256 * static_cast<size_t>(num_sms);
+  char* at = reinterpret_cast<char*>(aligned(reinterpret_cast<uintptr_t>(work)));
+  s->plan = reinterpret_cast<int4*>(at);
+  at += aligned(16 * (1 + MAX_N));
+  s->state_stats = reinterpret_cast<float2*>(at);
+  at += aligned(8 * own);
+  s->stats = reinterpret_cast<float2*>(at);
+  at += aligned(8 * parts);
+  s->state = reinterpret_cast<float*>(at);
+  s->part = s->state + own * d;
+}
+
+cudaError_t launch_attn_shared(const LaunchCtx& lc, const PagedAttnArgs& a, const SharedGroups& s, const AttnMaps& maps) {
+  if (a.H / a.G > 16 || a.B < 1 || a.B > PAGED_ATTN_MAX_B || s.N < 1 || s.N > MAX_N || !a.block_table || lc.num_sms > 1024)
+    return cudaErrorInvalidValue;
+  if (a.d == 64) return lc.f16 ? launch_hd<64, f16>(lc, a, s, maps) : launch_hd<64, bf16>(lc, a, s, maps);
+  if (a.d == 128) return lc.f16 ? launch_hd<128, f16>(lc, a, s, maps) : launch_hd<128, bf16>(lc, a, s, maps);
+  return cudaErrorInvalidValue;
+}

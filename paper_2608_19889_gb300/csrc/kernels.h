@@ -243,6 +243,27 @@ inline long long paged_attn_most_pages(int B, int G, int blocks_per_seq, int win
 cudaError_t prepare_attn_paged_kernels();
 cudaError_t launch_attn_paged_decode(const LaunchCtx& lc, const PagedAttnArgs& a);
 
+// ---- the same for rows in groups whose first blocks are the same (k_attn_shared.cu)
+constexpr int SHARED_MAX_GROUPS = 1024;
+struct SharedGroups {
+  const int* offsets;  // [N + 1] rows of the groups
+  const int* prefix;   // [N] tokens whose whole blocks are the same
+  int N;
+  int least;        // blocks in common below which a group shares nothing
+  int least_steps;  // of 8 blocks, for a CTA
+  int4* plan;          // [1 + SHARED_MAX_GROUPS], written by the prefix pass
+  float2* state_stats; // [B][H] maximum and sum of the rows' own parts
+  float* state;        // [B][H][d] their outputs, not divided
+  float2* stats;       // of the prefix pass's parts
+  float* part;
+};
+size_t shared_attn_bytes(int B, int H, int d, int num_sms);
+void shared_attn_carve(SharedGroups* s, void* work, int B, int H, int d, int num_sms);
+cudaError_t prepare_attn_shared_kernels();
+// Three launches: prefix pass, the rows' own parts, the join.
+cudaError_t launch_attn_shared(const LaunchCtx& lc, const PagedAttnArgs& a, const SharedGroups& s, const AttnMaps& maps);
+cudaError_t launch_attn_paged_own(const LaunchCtx& lc, const PagedAttnArgs& a, const SharedGroups& s);
+
 // ---- new tokens into the paged cache (k_append.cu)
 struct AppendArgs {
   const void* x[3];  // queries, keys, values [T][heads][d], strides in elements

@@ -52,6 +52,7 @@ cudaError_t with_limits(Launch launch) {
     if (!known) {
       e = prepare_attn_chunk_kernels();
       if (e == cudaSuccess) e = prepare_attn_paged_kernels();
+      if (e == cudaSuccess) e = prepare_attn_shared_kernels();
       if (e == cudaSuccess) e = prepare_sample_kernels();
       if (e != cudaSuccess) return e;
       ready.fetch_or(bit, std::memory_order_release);
@@ -146,25 +147,18 @@ int pages_args(const axon_kv_cache* c, const axon_kv_seqs* s, void* work, int64_
 
 }  // namespace
 
-extern "C" {
+namespace {
 
-int axon_attn_decode_workspace(const axon_kv_cache* cache, int32_t num_heads, int32_t B, int64_t* bytes) {
-  int rc = check_cache(cache);
-  if (rc) return rc;
-  if (!bytes || num_heads < 1 || num_heads % cache->num_kv_heads || B < 1) return AXON_ERR_INVALID_ARG;
-  if (num_heads / cache->num_kv_heads > 16 || B > PAGED_ATTN_MAX_B) return AXON_ERR_UNSUPPORTED;
-  LaunchCtx lc;
-  if ((rc = launch_ctx(cache, nullptr, &lc))) return rc;
-  *bytes = static_cast<int64_t>(paged_attn_ticket_bytes(lc.num_sms) +
-                                paged_attn_part_bytes(num_heads, cache->num_kv_heads, cache->head_dim, lc.num_sms));
-  return AXON_OK;
+// Bytes of axon_attn_decode's part of a workspace.
+size_t decode_bytes(const axon_kv_cache* c, int H, int sms) {
+  return paged_attn_ticket_bytes(sms) + paged_attn_part_bytes(H, c->num_kv_heads, c->head_dim, sms);
 }
 
-int axon_attn_decode(const axon_kv_cache* cache, int32_t layer, const void* d_q, int64_t q_row_stride,
-                     int64_t q_head_stride, int32_t B, int32_t num_heads, const int32_t* d_context_lens,
-                     const int32_t* d_block_table, int32_t blocks_per_seq, int32_t window, int32_t sinks, float scale,
-                     void* d_out, int64_t out_row_stride, int64_t out_head_stride, float* d_lse, void* d_workspace,
-                     int64_t workspace_bytes, int32_t* d_err, void* stream) {
+// What the one-token forms have in common: checks and arguments, but for the workspace.
+int decode_args(const axon_kv_cache* cache, int layer, const void* d_q, int64_t q_row_stride, int64_t q_head_stride, int B,
+                int num_heads, const int32_t* d_context_lens, const int32_t* d_block_table, int blocks_per_seq, int window,
+                int sinks, float scale, void* d_out, int64_t out_row_stride, int64_t out_head_stride, float* d_lse,
+                void* d_workspace, int32_t* d_err, void* stream, LaunchCtx* lc, PagedAttnArgs* out) {
   int rc = check_attn(cache, layer, d_q, d_out, num_heads, blocks_per_seq, window, sinks, scale);
   if (rc) return rc;
   if (!d_context_lens || !d_workspace || unaligned(d_workspace) || B < 1) return AXON_ERR_INVALID_ARG;
@@ -174,13 +168,8 @@ int axon_attn_decode(const axon_kv_cache* cache, int32_t layer, const void* d_q,
       (rc = check_strides(B, num_heads, cache->head_dim, out_row_stride, out_head_stride)))
     return rc;
   if (!d_block_table && static_cast<long long>(B) * blocks_per_seq > cache->num_blocks) return AXON_ERR_INVALID_ARG;
-  LaunchCtx lc;
-  if ((rc = launch_ctx(cache, stream, &lc))) return rc;
-  const size_t tickets = paged_attn_ticket_bytes(lc.num_sms);
-  if (workspace_bytes < static_cast<int64_t>(
-                            tickets + paged_attn_part_bytes(num_heads, cache->num_kv_heads, cache->head_dim, lc.num_sms)))
-    return AXON_ERR_INVALID_ARG;
-  PagedAttnArgs a;
+  if ((rc = launch_ctx(cache, stream, lc))) return rc;
+  PagedAttnArgs& a = *out;
   memset(&a, 0, sizeof(a));
   a.q = d_q;
   a.q_row = q_row_stride;
@@ -203,9 +192,79 @@ int axon_attn_decode(const axon_kv_cache* cache, int32_t layer, const void* d_q,
   a.o_head = out_head_stride;
   a.lse = d_lse;
   a.ticket = static_cast<int*>(d_workspace);
-  a.part = reinterpret_cast<float*>(static_cast<char*>(d_workspace) + tickets);
+  a.part = reinterpret_cast<float*>(static_cast<char*>(d_workspace) + paged_attn_ticket_bytes(lc->num_sms));
   a.err = d_err;
+  return AXON_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int axon_attn_decode_workspace(const axon_kv_cache* cache, int32_t num_heads, int32_t B, int64_t* bytes) {
+  int rc = check_cache(cache);
+  if (rc) return rc;
+  if (!bytes || num_heads < 1 || num_heads % cache->num_kv_heads || B < 1) return AXON_ERR_INVALID_ARG;
+  if (num_heads / cache->num_kv_heads > 16 || B > PAGED_ATTN_MAX_B) return AXON_ERR_UNSUPPORTED;
+  LaunchCtx lc;
+  if ((rc = launch_ctx(cache, nullptr, &lc))) return rc;
+  *bytes = static_cast<int64_t>(decode_bytes(cache, num_heads, lc.num_sms));
+  return AXON_OK;
+}
+
+int axon_attn_decode(const axon_kv_cache* cache, int32_t layer, const void* d_q, int64_t q_row_stride,
+                     int64_t q_head_stride, int32_t B, int32_t num_heads, const int32_t* d_context_lens,
+                     const int32_t* d_block_table, int32_t blocks_per_seq, int32_t window, int32_t sinks, float scale,
+                     void* d_out, int64_t out_row_stride, int64_t out_head_stride, float* d_lse, void* d_workspace,
+                     int64_t workspace_bytes, int32_t* d_err, void* stream) {
+  LaunchCtx lc;
+  PagedAttnArgs a;
+  const int rc = decode_args(cache, layer, d_q, q_row_stride, q_head_stride, B, num_heads, d_context_lens, d_block_table,
+                             blocks_per_seq, window, sinks, scale, d_out, out_row_stride, out_head_stride, d_lse, d_workspace,
+                             d_err, stream, &lc, &a);
+  if (rc) return rc;
+  if (workspace_bytes < static_cast<int64_t>(decode_bytes(cache, num_heads, lc.num_sms))) return AXON_ERR_INVALID_ARG;
   return status(with_limits([&] { return launch_attn_paged_decode(lc, a); }));
+}
+
+int axon_attn_shared_workspace(const axon_kv_cache* cache, int32_t num_heads, int32_t B, int64_t* bytes) {
+  int64_t own = 0;
+  int rc = axon_attn_decode_workspace(cache, num_heads, B, bytes ? &own : nullptr);
+  if (rc) return rc;
+  LaunchCtx lc;
+  if ((rc = launch_ctx(cache, nullptr, &lc))) return rc;
+  *bytes = own + static_cast<int64_t>(shared_attn_bytes(B, num_heads, cache->head_dim, lc.num_sms));
+  return AXON_OK;
+}
+
+int axon_attn_shared(const axon_kv_cache* cache, int32_t layer, const void* d_q, int64_t q_row_stride, int64_t q_head_stride,
+                     int32_t B, int32_t num_heads, const int32_t* d_context_lens, const int32_t* d_block_table,
+                     int32_t blocks_per_seq, const int32_t* d_group_offsets, const int32_t* d_prefix_lens, int32_t num_groups,
+                     int32_t window, int32_t sinks, float scale, void* d_out, int64_t out_row_stride, int64_t out_head_stride,
+                     float* d_lse, void* d_workspace, int64_t workspace_bytes, int32_t* d_err, void* stream) {
+  if (!d_block_table || !d_group_offsets || !d_prefix_lens || num_groups < 1) return AXON_ERR_INVALID_ARG;
+  if (num_groups > SHARED_MAX_GROUPS) return AXON_ERR_UNSUPPORTED;
+  LaunchCtx lc;
+  PagedAttnArgs a;
+  const int rc = decode_args(cache, layer, d_q, q_row_stride, q_head_stride, B, num_heads, d_context_lens, d_block_table,
+                             blocks_per_seq, window, sinks, scale, d_out, out_row_stride, out_head_stride, d_lse, d_workspace,
+                             d_err, stream, &lc, &a);
+  if (rc) return rc;
+  const size_t own = decode_bytes(cache, num_heads, lc.num_sms);
+  if (workspace_bytes < static_cast<int64_t>(own + shared_attn_bytes(B, num_heads, a.d, lc.num_sms))) return AXON_ERR_INVALID_ARG;
+  AttnMaps maps;
+  if (!make_attn_maps_strided(&maps, d_q, B, a.q_row, a.q_head, a.k, a.v, static_cast<long long>(cache->num_blocks) * a.G * 16,
+                              num_heads, a.G, a.d, lc.f16))
+    return AXON_ERR_UNSUPPORTED;
+  SharedGroups s;
+  memset(&s, 0, sizeof(s));
+  s.offsets = d_group_offsets;
+  s.prefix = d_prefix_lens;
+  s.N = num_groups;
+  s.least = 8;
+  s.least_steps = 2;
+  shared_attn_carve(&s, static_cast<char*>(d_workspace) + own, B, num_heads, a.d, lc.num_sms);
+  return status(with_limits([&] { return launch_attn_shared(lc, a, s, maps); }));
 }
 
 int axon_attn_prefill(const axon_kv_cache* cache, int32_t layer, const void* d_q, int64_t q_row_stride,

@@ -124,17 +124,19 @@ AXON_DEV void paged_decode(const PagedAttnArgs& p, const SharedGroups& sg) {
   const int HPG = p.H / p.G;
   grid_dep_launch();
   // (SH: the prefix pass before this kernel lets it start once its inputs are there)
-  if (!SH) grid_dep_wait();
-  GroupPlan gp{};
+  if (!SH || sg.alone) grid_dep_wait();
+  const GroupPlan gp(rpos + p.B, SH ? sg.N : 0);
   if constexpr (SH) {
-    int* const at = rpos + p.B;
-    gp = GroupPlan{at, at + sg.N, at + 2 * sg.N, at + 3 * sg.N};
-    plan_groups<DW * 32>(p, sg, gp, false);
+    if (sg.alone) {
+      if (blockIdx.x == 0) check_groups<DW * 32>(p, sg);
+    } else {
+      plan_groups<DW * 32, 0>(p, sg, gp, false);
+    }
   }
   // the pages that row b has in common with others
   auto common = [&](int b) {
     if constexpr (SH) {
-      const int n = group_of(sg, b);
+      const int n = sg.alone ? -1 : group_of(gp, sg.N, b);
       if (n >= 0 && gp.c1[n] > gp.c0[n]) return make_int2(gp.c0[n], gp.c1[n]);
     }
     return make_int2(INT_MAX, INT_MAX);
@@ -608,7 +610,7 @@ cudaError_t prepare_hd() {
   if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_paged_decode_kernel<HD, T16, 1, true>, attr, one);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_paged_decode_kernel<HD, T16, 2, false>, attr, two);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_paged_decode_kernel<HD, T16, 2, true>, attr, two);
-  constexpr int plan = 16 * SHARED_MAX_GROUPS;
+  constexpr int plan = 4 * (GroupPlan::INTS * SHARED_MAX_GROUPS + 2);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_paged_own_kernel<HD, T16, 1>, attr, one + plan);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_paged_own_kernel<HD, T16, 2>, attr, two + plan);
   return e;
@@ -616,7 +618,7 @@ cudaError_t prepare_hd() {
 
 template <int HD, typename T16, int NT, bool LO>
 cudaError_t launch_nt(const LaunchCtx& lc, const PagedAttnArgs& a, const SharedGroups* sg = nullptr) {
-  const size_t smem = smem_bytes<HD, NT>(a.B) + (sg ? 16 * static_cast<size_t>(sg->N) : 0);
+  const size_t smem = smem_bytes<HD, NT>(a.B) + (sg ? 4 * (GroupPlan::INTS * static_cast<size_t>(sg->N) + 2) : 0);
   // no more CTAs than pages that can be visible, at a page per warp
   const long long pages = paged_attn_most_pages(a.B, a.G, a.blocks_per_seq, a.window, a.sinks);
   const long long most = static_cast<long long>(lc.num_sms) * (NT == 1 ? 3 : 2);

@@ -7,15 +7,20 @@
 //
 // The blocks in common are read once for all rows of a group and hold no masked token, so that the prefix
 // pass is a plain product: a tile is 128 (row, query head) pairs of one kv head, PW = 128 / (H/G) rows; an item is
-// two tiles of a group and a kv head, which share the keys, 128 per step (eight blocks). The steps of all
+// two tiles of a group and a kv head, which share the keys, 128 per step (eight blocks). Where the rows fill one tile
+// only, both pipelines take it, every other step each: else its products would wait for its softmax. The steps of all
 // items form one line, which the CTAs (one per SM) split evenly: an item's parts go to the workspace, as many as
 // CTAs have a share of it, and the join adds them up in their order, so that results do not depend on timing.
 // Warps:
 //   0..3, 4..7  softmax of tile 0 and 1, one thread per (row, head);
-//   8           TMA producer: queries of an item, keys and values through a ring of tiles;
+//   8, 10       TMA producers, of queries and keys, and of values, through a ring of tiles (16 boxes of 2 KB per tile take
+//               one warp 1100 cycles to ask for);
 //   9, 11       MMA issuers of tile 0 and 1 (S = Q K^T into TMEM, O += P V with P from TMEM).
+// The softmax warps first run a step on nothing, while the others work out what is in common: its 1500 instructions
+// come from memory the first time, which took 9000 cycles instead of 1600, and most launches take ten or twenty steps.
 // P enters the product in two 16-bit terms, as in the other attention kernels.
 #include <math.h>
+#include <stdlib.h>
 
 #include <algorithm>
 
@@ -36,12 +41,16 @@ struct SCfg {
   static constexpr int CHUNK = 128 * 128;           // bytes of one 128-row chunk
   static constexpr int TILE = CH * CHUNK;           // Q, K or V tile
   static constexpr int STAGES = HD == 128 ? 4 : 8;  // K and V tiles in flight
-  static constexpr int BARS = 2 * STAGES + 14;
-  static constexpr int PLAN = 4 * (5 * MAX_N + 4);
+  static constexpr int BARS = 2 * STAGES + 16;
+  static constexpr int PLAN = 4 * ((GroupPlan::INTS + 1) * MAX_N + 4);
   static constexpr int SMEM = 2 * TILE + STAGES * TILE + 8 * BARS + 16 + PLAN + 1024;
 };
 
-// How the steps are dealt: `workers` CTAs, the first `extra` of them one step more than `share`.
+// What a step costs on the line: 3500 cycles with two tiles (the tensor pipe's 3072), 2800 with one (64 KB from HBM).
+constexpr unsigned COST_TWO = 5, COST_ONE = 4;
+
+// How the line is dealt: `workers` CTAs, the first `extra` of them one more than `share`; a CTA takes the steps that begin
+// in its range, which holds one at least.
 struct Deal {
   unsigned total, workers, share, extra;
   AXON_DEV unsigned begin(unsigned w) const { return w * share + min(w, extra); }
@@ -50,29 +59,49 @@ struct Deal {
     return u < cut ? u / (share + 1) : extra + (u - cut) / share;
   }
 };
-AXON_DEV Deal deal(unsigned total, unsigned ctas, unsigned least) {
+AXON_DEV Deal deal(unsigned total, unsigned ctas, unsigned least_steps) {
   Deal d;
   d.total = total;
-  d.workers = min(ctas, max(1u, total / least));
+  d.workers = min(ctas, max(1u, total / (COST_TWO * least_steps)));
   d.share = total / d.workers;
   d.extra = total - d.share * d.workers;
   return d;
 }
 
-// A CTA's share of an item.
-struct Part {
-  int group, g;       // group, kv head
-  int r0, p0, rows;   // the group's first row, the item's first row in the group, rows of the item
-  int page0, pages;   // blocks
-  int lead;
-  long long at;       // its first (row, head) in the workspace
-  unsigned steps;
+// A group on the line.
+struct Span {
+  int rows, pages, pairs;
+  unsigned steps, last_cost;  // of an item; the cost of a step of the last pair, the others' is COST_TWO
+  unsigned per_head;          // cost of a kv head's items
+  AXON_DEV Span(int rows_, int pages_, int PW) : rows(rows_), pages(pages_) {
+    pairs = (rows + 2 * PW - 1) / (2 * PW);
+    steps = static_cast<unsigned>(pages + 7) >> 3;
+    last_cost = rows - (pairs - 1) * 2 * PW > PW ? COST_TWO : COST_ONE;
+    per_head = steps * ((pairs - 1) * COST_TWO + last_cost);
+  }
+  AXON_DEV unsigned cost(int pair) const { return pair == pairs - 1 ? last_cost : COST_TWO; }
+  AXON_DEV unsigned item(int g, int pair) const { return g * per_head + pair * steps * COST_TWO; }
 };
 
-// In front of the parts' first (row, head): those of the items before it, which all lie inside B * H, and 256 for each
-// CTA before, since an item has that many (row, head) pairs at most and each CTA adds a part at most.
-AXON_DEV long long part_at(int r0, int rows, int g, int p0, int H, int HPG, unsigned worker) {
-  return static_cast<long long>(r0) * H + (static_cast<long long>(g) * rows + p0) * HPG + 256ll * worker;
+// A CTA's share of an item.
+struct Part {
+  int g, r0, p0, rows;  // kv head, the group's first row, the item's first row in it, rows of the item
+  int page0, pages;     // blocks
+  int lead;
+  bool one;             // one tile, in both pipelines
+  int at;               // its first (row, head) in the workspace
+  int steps;
+  unsigned next;        // where the next part begins
+  // steps of pipeline w
+  AXON_DEV int count(int w, int PW) const { return one ? (steps + 1 - w) >> 1 : w * PW < rows ? steps : 0; }
+};
+
+// In front of the parts' first (row, head): twice those of the items before it, which all lie inside B * H, and 256 for each
+// CTA before, since an item has that many (row, head) pairs at most (twice those of its tile, if it has one) and
+// each CTA adds a part at most.
+// (Below 2^31: the launcher saw to it.)
+AXON_DEV int part_at(int r0, int rows, int g, int p0, int H, int HPG, unsigned worker) {
+  return 2 * (r0 * H + (g * rows + p0) * HPG) + 256 * static_cast<int>(worker);
 }
 
 template <int HD, typename T16>
@@ -95,10 +124,11 @@ __global__ void __launch_bounds__(THREADS, 1)
   auto o_full = [&](int w) { return more + 8 * (8 + w); };
   auto o_empty = [&](int w) { return more + 8 * (10 + w); };
   auto turn = [&](int w) { return more + 8 * (12 + w); };
+  auto warm = [&](int w) { return more + 8 * (14 + w); };
   const uint32_t tmem_slot = bars + 8 * C::BARS;
   int* const plan = reinterpret_cast<int*>(smem_raw + (tmem_slot + 16 - raw));
-  const GroupPlan gp{plan, plan + MAX_N, plan + 2 * MAX_N, plan + 3 * MAX_N};
-  unsigned* const before = reinterpret_cast<unsigned*>(plan + 4 * MAX_N);  // [N + 1] steps of the groups before
+  const GroupPlan gp(plan, sg.N);
+  unsigned* const before = reinterpret_cast<unsigned*>(plan + GroupPlan::INTS * sg.N + 2);  // [N + 1] cost of the groups before
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int HPG = p.H / p.G, PC = 2 * PW;
 
@@ -115,6 +145,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       mbar_init(o_full(w), 1);
       mbar_init(o_empty(w), 128);
       mbar_init(turn(w), 1);
+      mbar_init(warm(w), 128);
     }
     fence_mbar_init();
     fence_proxy_async();
@@ -130,85 +161,92 @@ __global__ void __launch_bounds__(THREADS, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *reinterpret_cast<const uint32_t*>(smem_raw + (tmem_slot - raw));
-  grid_dep_wait();
-  grid_dep_launch();  // the rows' own parts, which wait for nothing of this kernel
-
-  // ---- what is in common, and the line of steps
-  plan_groups<THREADS>(p, sg, gp, blockIdx.x == 0);
-  if (warp == 0) {
-    unsigned sum = 0;
-    for (int i0 = 0; i0 < sg.N; i0 += 32) {
-      const int i = i0 + lane;
-      unsigned n = 0;
-      if (i < sg.N && gp.c1[i] > gp.c0[i])
-        n = static_cast<unsigned>((gp.c1[i] - gp.c0[i] + 7) >> 3) * ((sg.offsets[i + 1] - sg.offsets[i] + PC - 1) / PC) * p.G;
-      unsigned inc = n;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const unsigned t = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += t;
-      }
-      if (i < sg.N) before[i] = sum + inc - n;
-      sum += __shfl_sync(0xffffffffu, inc, 31);
-    }
-    if (lane == 0) before[sg.N] = sum;
-  }
-  __syncthreads();
-  const Deal d = deal(before[sg.N], gridDim.x, sg.least_steps);
-  if (blockIdx.x == 0) {
-    // for the join
-    for (int i = threadIdx.x; i < sg.N; i += THREADS)
-      sg.plan[1 + i] = make_int4(gp.c0[i], gp.c1[i], static_cast<int>(before[i]), 0);
-    if (threadIdx.x == 0) sg.plan[0] = make_int4(static_cast<int>(d.total), static_cast<int>(gridDim.x), sg.least_steps, 0);
-  }
-  const unsigned u1 = blockIdx.x < d.workers && d.total ? d.begin(blockIdx.x + 1) : 0;
-  // The part that begins at step u (< u1) of the line; the same in all lanes.
-  auto part_of = [&](unsigned u) {
-    int lo = 0, hi = sg.N - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (before[mid] <= u) lo = mid; else hi = mid - 1;
-    }
-    Part t;
-    t.group = lo;
-    t.r0 = sg.offsets[lo];
-    const int rows = sg.offsets[lo + 1] - t.r0, pages = gp.c1[lo] - gp.c0[lo], pairs = (rows + PC - 1) / PC;
-    const unsigned steps = (pages + 7) >> 3, off = u - before[lo], item = off / steps, first = off - item * steps;
-    t.g = static_cast<int>(item) / pairs;
-    t.p0 = (static_cast<int>(item) - t.g * pairs) * PC;
-    t.rows = min(PC, rows - t.p0);
-    t.steps = min(steps - first, u1 - u);
-    t.page0 = gp.c0[lo] + 8 * static_cast<int>(first);
-    t.pages = min(gp.c1[lo] - t.page0, 8 * static_cast<int>(t.steps));
-    t.lead = gp.lead[lo];
-    t.at = part_at(t.r0, rows, t.g, t.p0, p.H, HPG, blockIdx.x);
-    return t;
+  // what the parts' owners need to know is there once `ready` lets them pass
+  auto ready = [&]() { asm volatile("barrier.cta.sync 1, 384;" ::: "memory"); };
+  Deal d{};
+  unsigned u0 = 0, u1 = 0;
+  auto take_share = [&]() {
+    d = deal(before[sg.N], gridDim.x, sg.least_steps);
+    u1 = blockIdx.x < d.workers && d.total ? d.begin(blockIdx.x + 1) : 0;
+    u0 = u1 ? d.begin(blockIdx.x) : 0;
   };
-  const unsigned u0 = u1 ? d.begin(blockIdx.x) : 0;
+  // The part with the first step that begins at u or after it (u < u1); no steps: none does. The same in all lanes.
+  auto part_of = [&](unsigned u) {
+    Part t;
+    for (;;) {
+      int lo = 0, hi = sg.N - 1;  // the last group that begins at u or before it
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (before[mid] <= u) lo = mid; else hi = mid - 1;
+      }
+      const Span s(gp.from[lo + 1] - gp.from[lo], gp.c1[lo] - gp.c0[lo], PW);
+      const unsigned off = u - before[lo];
+      t.g = static_cast<int>(off / s.per_head);
+      const unsigned in = off - t.g * s.per_head;
+      const int pair = min(static_cast<int>(in / (s.steps * COST_TWO)), s.pairs - 1);
+      const unsigned cost = s.cost(pair), begin = before[lo] + s.item(t.g, pair), first = (u - begin + cost - 1) / cost;
+      if (first >= s.steps) {  // the rest of a step that the CTA before has
+        u = begin + s.steps * cost;
+        if (u < u1) continue;
+        t.steps = 0;
+        t.next = u1;
+        return t;
+      }
+      // steps that begin before u1
+      const unsigned last = begin + first * cost < u1 ? min(s.steps, (u1 - begin + cost - 1) / cost) : first;
+      t.steps = static_cast<int>(last - first);
+      t.next = begin + last * cost;
+      t.r0 = gp.from[lo];
+      t.p0 = pair * PC;
+      t.rows = min(PC, s.rows - t.p0);
+      t.one = t.rows <= PW;
+      t.page0 = gp.c0[lo] + 8 * static_cast<int>(first);
+      t.pages = min(gp.c1[lo] - t.page0, 8 * t.steps);
+      t.lead = gp.lead[lo];
+      t.at = part_at(t.r0, s.rows, t.g, t.p0, p.H, HPG, blockIdx.x);
+      return t;
+    }
+  };
 
   if (warp >= 8) {
+    // Before `ready`, since the softmax warps wait for these registers; and once for all that these warps do, since what
+    // follows a place where the branches meet may be given registers that only the softmax warps have.
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    grid_dep_wait();
+    grid_dep_launch();  // the rows' own parts, which wait for nothing of this kernel
+    plan_groups<128, 256>(p, sg, gp, blockIdx.x == 0);
     if (warp == 8) {
-      // ----------------------------------------------------------- producer
-      int iq[2] = {0, 0}, it = 0;
+      unsigned sum = 0;
+      for (int i0 = 0; i0 < sg.N; i0 += 32) {
+        const int i = i0 + lane;
+        unsigned n = 0;
+        if (i < sg.N && gp.c1[i] > gp.c0[i]) n = Span(gp.from[i + 1] - gp.from[i], gp.c1[i] - gp.c0[i], PW).per_head * p.G;
+        unsigned inc = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const unsigned t = __shfl_up_sync(0xffffffffu, inc, o);
+          if (lane >= o) inc += t;
+        }
+        if (i < sg.N) before[i] = sum + inc - n;
+        sum += __shfl_sync(0xffffffffu, inc, 31);
+      }
+      if (lane == 0) before[sg.N] = sum;
+    }
+    ready();
+    take_share();
+    if (!(warp & 1)) {
+      // ---------------------------------------------------------- producers
+      const int kv = warp == 8 ? 0 : 1;
+      int iq[2] = {0, 0}, it = kv;  // queries; tiles of the ring, this warp's every other one
       bool ok = true;
       for (unsigned u = u0; u < u1 && ok;) {
         const Part t = part_of(u);
-        u += t.steps;
-        for (int w = 0; w < 2 && w * PW < t.rows; ++w) {
-          ok = __all_sync(0xffffffffu, wait_bar(q_empty(w), (iq[w] & 1) ^ 1, p.err));
-          if (!ok) break;
-          if (lane == 0) {
-            mbar_arrive_expect_tx(q_full(w), HPG * PW * HD * 2);
-            for (int c = 0; c < C::CH; ++c)
-              tma_load_3d(sQ + w * C::TILE + c * C::CHUNK, &tmQ, q_full(w), c * 64, t.g * HPG, t.r0 + t.p0 + w * PW);
-          }
-          ++iq[w];
-        }
+        u = t.next;
+        if (!t.steps) break;
         // pool row of this lane's block of step s; past the last block and for table entries
         // out of range (reported) the row lies outside the pool, where a box reads zeros
-        auto pool_row = [&](unsigned s) {
-          const int i = static_cast<int>(s) * 8 + lane;
+        auto pool_row = [&](int s) {
+          const int i = s * 8 + lane;
           if (lane >= 8 || i >= t.pages) return pool_rows;
           const int blk = p.block_table[static_cast<long long>(t.lead) * p.blocks_per_seq + t.page0 + i];
           if (blk < 0 || blk >= p.num_blocks) {
@@ -218,26 +256,51 @@ __global__ void __launch_bounds__(THREADS, 1)
           return (blk * p.G + t.g) * 16;
         };
         int next = pool_row(0);
-        for (unsigned s = 0; s < t.steps && ok; ++s) {
-          const int y = next;
-          next = pool_row(s + 1);
-          for (int kv = 0; kv < 2; ++kv, ++it) {
-            const int st = it % NS;
-            ok = __all_sync(0xffffffffu, wait_bar(kv_empty(st), ((it / NS) & 1) ^ 1, p.err));
-            if (!ok) break;
-            if (lane == 0) mbar_arrive_expect_tx(kv_full(st), C::TILE);
-            __syncwarp();
-            if (lane < 8)
-              for (int c = 0; c < C::CH; ++c)
-                tma_load_2d(sKV + st * C::TILE + c * C::CHUNK + lane * 2048, kv ? &tmV : &tmK, kv_full(st), c * 64, y);
+        for (int w = 0; w < 2 && !kv; ++w) {
+          if (!t.count(w, PW)) continue;
+          ok = __all_sync(0xffffffffu, wait_bar(q_empty(w), (iq[w] & 1) ^ 1, p.err));
+          if (!ok) break;
+          if (lane == 0) {
+            mbar_arrive_expect_tx(q_full(w), HPG * PW * HD * 2);
+            for (int c = 0; c < C::CH; ++c)
+              tma_load_3d(sQ + w * C::TILE + c * C::CHUNK, &tmQ, q_full(w), c * 64, t.g * HPG, t.r0 + t.p0 + (t.one ? 0 : w * PW));
           }
+          ++iq[w];
+        }
+        for (int s = 0; s < t.steps && ok; ++s, it += 2) {
+          const int y = next, st = it % NS;
+          next = pool_row(s + 1);
+          ok = __all_sync(0xffffffffu, wait_bar(kv_empty(st), ((it / NS) & 1) ^ 1, p.err));
+          if (!ok) break;
+          if (lane == 0) mbar_arrive_expect_tx(kv_full(st), C::TILE);
+          __syncwarp();
+          if (lane < 8)
+            for (int c = 0; c < C::CH; ++c)
+              tma_load_2d(sKV + st * C::TILE + c * C::CHUNK + lane * 2048, kv ? &tmV : &tmK, kv_full(st), c * 64, y);
         }
       }
-      // every copy lands before the CTA's shared memory goes away
+      if (kv && blockIdx.x == 0) {
+        // what the join has to know of the rows
+        if (lane == 0) sg.plan[0] = make_int4(static_cast<int>(d.total), static_cast<int>(gridDim.x), sg.least_steps, 0);
+        for (int b = lane; b < p.B; b += 32) {
+          const int n = live_pos(p, b) >= 0 ? group_of(gp, sg.N, b) : -1;
+          sg.plan[1 + b] = n >= 0 && gp.c1[n] > gp.c0[n]
+                               ? make_int4(gp.c1[n] - gp.c0[n], static_cast<int>(before[n]), gp.from[n], gp.from[n + 1] - gp.from[n])
+                               : make_int4(0, 0, 0, 0);
+        }
+      }
+      // Nothing may be on its way to the CTA's shared memory when it goes away: neither copies nor the arrivals that the
+      // tensor pipe makes for the issuers' last commits, which come after the one that lets the softmax warps finish. (A
+      // stage that is given back was filled.)
       for (int w = 0; w < 2; ++w)
-        if (iq[w] > 0) wait_bar(q_full(w), (iq[w] - 1) & 1, p.err);
-      for (int i = it > NS ? it - NS : 0; i < it; ++i) wait_bar(kv_full(i % NS), (i / NS) & 1, p.err);
-    } else if (warp != 10) {
+        if (iq[w] > 0) wait_bar(q_empty(w), (iq[w] - 1) & 1, p.err);
+      for (int i = max(it - NS, kv); i < it; i += 2) wait_bar(kv_empty(i % NS), (i / NS) & 1, p.err);
+      if (!ok) {
+        for (int w = 0; w < 2; ++w)
+          if (iq[w] > 0) wait_bar(q_full(w), (iq[w] - 1) & 1, p.err);
+        for (int i = max(it - NS, kv); i < it; i += 2) wait_bar(kv_full(i % NS), (i / NS) & 1, p.err);
+      }
+    } else {
       // -------------------------------------------------------- MMA issuers
       // A warp per tile, in turns: one tile's products run under the other's softmax.
       const int w = warp == 9 ? 0 : 1;
@@ -254,6 +317,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_bar(bar, parity, p.err)) != 0; };
       uint32_t ph_q = 0, ph_p = 0;  // phases of this tile's parts and steps
       uint32_t turns = 0;
+      wait_all(warm(w), 0);  // (nothing of the step on nothing is read; its stores are done)
       auto my_turn = [&]() { return wait_all(turn(w), (turns & 1) ^ (w ^ 1)); };
       // scores from the keys in stage st; the turn passes two products before the end
       auto scores = [&](bool last) {
@@ -274,11 +338,77 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (leader) mbar_arrive(turn(w ^ 1));
         ++turns;
       };
+      auto products = [&](uint32_t sv, int blocks, bool first) {
+        const uint64_t vd = dV + sv * (C::TILE >> 4);
+        if (!first && blocks == 8) {
+          if (leader) {
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+              tc_mma_f16_ts(tO, tS + x * 8, vd + x * 128, id_o, 1u);
+              tc_mma_f16_ts(tO, tS + KT / 2 + x * 8, vd + x * 128, id_o, 1u);
+            }
+          }
+        } else if (leader) {
+          // the first step starts the sums; blocks past the last hold no values
+#pragma unroll 1
+          for (int x = 0; x < blocks; ++x) {
+            tc_mma_f16_ts(tO, tS + x * 8, vd + x * 128, id_o, !first || x != 0 ? 1u : 0u);
+            tc_mma_f16_ts(tO, tS + KT / 2 + x * 8, vd + x * 128, id_o, 1u);
+          }
+        }
+      };
       for (unsigned u = u0; u < u1;) {
         const Part t = part_of(u);
-        u += t.steps;
-        const int nt_all = __shfl_sync(0xffffffffu, static_cast<int>(t.steps), 0), pages = __shfl_sync(0xffffffffu, t.pages, 0);
-        const int nt = w * PW < t.rows ? nt_all : 0;
+        u = t.next;
+        if (!t.steps) break;
+        const int nt_all = __shfl_sync(0xffffffffu, t.steps, 0), pages = __shfl_sync(0xffffffffu, t.pages, 0);
+        const int nt = __shfl_sync(0xffffffffu, t.count(w, PW), 0);
+        if (__shfl_sync(0xffffffffu, static_cast<int>(t.one), 0)) {
+          // every other step; nobody else uses its stages, so that each is given back for both issuers
+          const uint32_t st0 = st, ph0 = ph;
+          auto stage_of = [&](int s, int kv, uint32_t& phase) {
+            const uint32_t at = st0 + 2 * s + kv;
+            phase = ph0 ^ ((at / NS) & 1);
+            return at % NS;
+          };
+          bool ok = !nt || wait_all(q_full(w), ph_q);
+          for (int k = 0; k < nt && ok; ++k) {
+            const int s = 2 * k + w;
+            uint32_t phk, phv;
+            const uint32_t sk = stage_of(s, 0, phk), sv = stage_of(s, 1, phv);
+            ok = wait_all(kv_full(sk), phk);
+            if (!ok) break;
+            tc_fence_after();
+            if (leader) {
+              const uint64_t kd = dK + sk * (C::TILE >> 4);
+#pragma unroll
+              for (int x = 0; x < HD / 16; ++x) {
+                const int off = ((x >> 2) * C::CHUNK + (x & 3) * 32) >> 4;
+                tc_mma_f16(tS, dQ + off, kd + off, id_s, x != 0);
+              }
+              tc_commit(s_full(w));
+              if (k + 1 == nt) tc_commit(q_empty(w));
+              tc_commit(kv_empty(sk));
+              tc_commit(kv_empty(sk));
+            }
+            ok = wait_all(kv_full(sv), phv) && (k != 0 || wait_all(o_empty(w), ph_q ^ 1)) && wait_all(p_full(w), ph_p);
+            if (!ok) break;
+            tc_fence_after();
+            ph_p ^= 1;
+            products(sv, min(8, pages - 8 * s), k == 0);
+            if (leader) {
+              if (k + 1 == nt) tc_commit(o_full(w));
+              tc_commit(kv_empty(sv));
+              tc_commit(kv_empty(sv));
+            }
+          }
+          if (!ok) break;
+          if (nt) ph_q ^= 1;
+          const uint32_t at = st0 + 2 * nt_all;
+          ph = ph0 ^ ((at / NS) & 1);
+          st = at % NS;
+          continue;
+        }
         bool ok = wait_all(kv_full(st), ph) && (!nt || wait_all(q_full(w), ph_q)) && my_turn();
         if (!ok) break;
         tc_fence_after();
@@ -297,25 +427,8 @@ __global__ void __launch_bounds__(THREADS, 1)
           if (!ok) break;
           tc_fence_after();
           if (nt) {
-            const uint64_t vd = dV + sv * (C::TILE >> 4);
             ph_p ^= 1;
-            const int blocks = min(8, pages - 8 * s);
-            if (s != 0 && blocks == 8) {
-              if (leader) {
-#pragma unroll
-                for (int x = 0; x < 8; ++x) {
-                  tc_mma_f16_ts(tO, tS + x * 8, vd + x * 128, id_o, 1u);
-                  tc_mma_f16_ts(tO, tS + KT / 2 + x * 8, vd + x * 128, id_o, 1u);
-                }
-              }
-            } else if (leader) {
-              // the first step starts the sums; blocks past the last hold no values
-#pragma unroll 1
-              for (int x = 0; x < blocks; ++x) {
-                tc_mma_f16_ts(tO, tS + x * 8, vd + x * 128, id_o, (s | x) != 0 ? 1u : 0u);
-                tc_mma_f16_ts(tO, tS + KT / 2 + x * 8, vd + x * 128, id_o, 1u);
-              }
-            }
+            products(sv, min(8, pages - 8 * s), s == 0);
             // MMAs run in issue order: the next scores may overwrite the probabilities just
             // issued, and s_full implies that O is up to date
             if (keys) {
@@ -349,17 +462,35 @@ __global__ void __launch_bounds__(THREADS, 1)
     const uint64_t sl2p = pk2(sl2, sl2);
     int ns_ = 0, no = 0;  // scores and outputs taken
     bool ok = true;
-    for (unsigned u = u0; u < u1 && ok;) {
-      const Part t = part_of(u);
-      u += t.steps;
-      if (w * PW >= t.rows) continue;
-      const bool valid = i < HPG * PW && w * PW * HPG + i < t.rows * HPG;
+    unsigned u = 0;
+    // the first round: a step on nothing
+    for (bool dry = true; ok; dry = false) {
+      int nt = 0, left = KT, stride = 0;  // steps; keys from a step on, and to the next one
+      bool valid = false;
+      int at = 0;
+      if (!dry) {
+        if (u >= u1) break;
+        const Part t = part_of(u);
+        if (!t.steps) break;
+        u = t.next;
+        nt = t.count(w, PW);
+        stride = t.one ? 2 * KT : KT;
+        left = 16 * t.pages - (t.one ? w * KT : 0);
+        valid = i < HPG * PW && (t.one ? 0 : w * PW * HPG) + i < t.rows * HPG;
+        at = t.at + w * (t.one ? t.rows : PW) * HPG + i;
+        if (!nt) {
+          if (t.one && valid) sg.stats[at] = make_float2(-INFINITY, 0.f);  // nothing for the second pipeline
+          continue;
+        }
+      }
       float m = valid ? -INFINITY : 0.f;
       uint64_t l2 = pk2(0.f, 0.f);
-      for (int s_ = 0; s_ < static_cast<int>(t.steps); ++s_) {
-        ok = __all_sync(0xffffffffu, wait_bar(s_full(w), ns_ & 1, p.err));
-        if (!ok) break;
-        ++ns_;
+      for (int s_ = dry ? -1 : 0; s_ < nt; ++s_, left -= stride) {
+        if (!dry) {
+          ok = __all_sync(0xffffffffu, wait_bar(s_full(w), ns_ & 1, p.err));
+          if (!ok) break;
+          ++ns_;
+        }
         tc_fence_after();
         float s[KT];
         tmem_ld32(tS, reinterpret_cast<uint32_t*>(s));
@@ -367,10 +498,9 @@ __global__ void __launch_bounds__(THREADS, 1)
         tmem_ld32(tS + 64, reinterpret_cast<uint32_t*>(s) + 64);
         tmem_ld32(tS + 96, reinterpret_cast<uint32_t*>(s) + 96);
         tmem_wait_ld();
-        const int cols = (t.pages - 8 * s_) * 16;  // keys of the step
-        if (cols < KT) {
+        if (left < KT) {
 #pragma unroll
-          for (int c = 16; c < KT; ++c) s[c] = c < cols ? s[c] : -INFINITY;
+          for (int c = 16; c < KT; ++c) s[c] = c < left ? s[c] : -INFINITY;
         }
         float m4[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
@@ -418,16 +548,21 @@ __global__ void __launch_bounds__(THREADS, 1)
         tmem_st32(tS + 96, rest + 32);
         tmem_wait_st();
         tc_fence_before();
-        mbar_arrive(p_full(w));
+        mbar_arrive(dry ? warm(w) : p_full(w));
         l2 = add2(l2, add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])));
+      }
+      if (dry) {
+        ready();
+        take_share();
+        u = u0;
+        continue;
       }
       if (!ok) break;
       ok = __all_sync(0xffffffffu, wait_bar(o_full(w), no & 1, p.err));
       if (!ok) break;
       ++no;
       tc_fence_after();
-      const long long at = t.at + w * PW * HPG + i;
-      float* const dst = sg.part + at * HD;
+      float* const dst = sg.part + static_cast<long long>(at) * HD;
 #pragma unroll 1
       for (int c = 0; c < HD; c += 32) {
         uint32_t o[32];
@@ -458,38 +593,39 @@ __global__ void __launch_bounds__(THREADS, 1)
 }
 
 constexpr int JT = 128;  // threads of the join
+constexpr int MAX_SMS = 512, MAX_PARTS = 2 * MAX_SMS;
 
 // One CTA per row and query head: the parts of its item, in order, and the row's own.
 template <int HD, typename T16>
-__global__ void __launch_bounds__(JT) attn_join_kernel(const PagedAttnArgs p, const SharedGroups sg, int PC) {
-  __shared__ float s_f[1024 + 1];
+__global__ void __launch_bounds__(JT) attn_join_kernel(const PagedAttnArgs p, const SharedGroups sg, int PW) {
+  __shared__ float s_f[MAX_PARTS + 1];
   __shared__ float s_red[2][JT / 32];
   __shared__ float4 s_o[JT];
   grid_dep_launch();
   const int b = blockIdx.x, h = blockIdx.y, tid = threadIdx.x;
   grid_dep_wait();
-  if (live_pos(p, b) < 0) return;
-  const int n = group_of(sg, b);
-  if (n < 0) return;
-  const int4 gp = sg.plan[1 + n], all = sg.plan[0];
-  if (gp.y <= gp.x) return;
+  const int4 gp = __ldcg(sg.plan + 1 + b), all = __ldcg(sg.plan);
+  if (!gp.x) return;
   const Deal d = deal(static_cast<unsigned>(all.x), static_cast<unsigned>(all.y), static_cast<unsigned>(all.z));
-  const int HPG = p.H / p.G, g = h / HPG, r0 = sg.offsets[n], rows = sg.offsets[n + 1] - r0, pairs = (rows + PC - 1) / PC;
-  const int pair = (b - r0) / PC;
-  const unsigned steps = (gp.y - gp.x + 7) >> 3, first = static_cast<unsigned>(gp.z) + (static_cast<unsigned>(g) * pairs + pair) * steps;
-  const unsigned w0 = d.worker_of(first);
-  const int parts = static_cast<int>(d.worker_of(first + steps - 1) - w0) + 1;
-  const long long at = part_at(r0, rows, g, pair * PC, p.H, HPG, w0) + (b - r0 - pair * PC) * HPG + h - g * HPG;
+  const Span sp(gp.w, gp.x, PW);
+  const int HPG = p.H / p.G, g = h / HPG, r0 = gp.z, pair = (b - r0) / (2 * PW), p0 = pair * 2 * PW;
+  const unsigned begin = static_cast<unsigned>(gp.y) + sp.item(g, pair);
+  const unsigned w0 = d.worker_of(begin);
+  const int ctas = static_cast<int>(d.worker_of(begin + (sp.steps - 1) * sp.cost(pair)) - w0) + 1;
+  // one tile: two parts of each CTA
+  const int rows = min(2 * PW, sp.rows - p0), two = rows <= PW ? 1 : 0, parts = ctas << two;
+  const int at = part_at(r0, sp.rows, g, p0, p.H, HPG, w0) + (b - r0 - p0) * HPG + h - g * HPG;
   const long long own = static_cast<long long>(b) * p.H + h;
+  auto place = [&](int i) { return at + 256 * (i >> two) + (two & i) * rows * HPG; };
 
   // factors: the parts', and the row's own last
-  float2 st[1 + 1024 / JT];
+  float2 st[MAX_PARTS / JT + 1];
   float M = -INFINITY;
 #pragma unroll
-  for (int k = 0; k < 1 + 1024 / JT; ++k) {
+  for (int k = 0; k < MAX_PARTS / JT + 1; ++k) {
     const int i = tid + k * JT;
     st[k] = make_float2(-INFINITY, 0.f);
-    if (i <= parts) st[k] = i < parts ? __ldcg(sg.stats + at + 256ll * i) : __ldcg(sg.state_stats + own);
+    if (i <= parts) st[k] = i < parts ? __ldcg(sg.stats + place(i)) : __ldcg(sg.state_stats + own);
     M = fmaxf(M, st[k].x);
   }
   M = warp_max(M);
@@ -500,7 +636,7 @@ __global__ void __launch_bounds__(JT) attn_join_kernel(const PagedAttnArgs p, co
   const float top = M == -INFINITY ? 0.f : M;
   float L = 0.f;
 #pragma unroll
-  for (int k = 0; k < 1 + 1024 / JT; ++k) {
+  for (int k = 0; k < MAX_PARTS / JT + 1; ++k) {
     const int i = tid + k * JT;
     if (i > parts) break;
     const float f = exp2f(st[k].x - top);
@@ -524,7 +660,7 @@ __global__ void __launch_bounds__(JT) attn_join_kernel(const PagedAttnArgs p, co
       const int i = i0 + k * PG;
       o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
       if (i <= parts)
-        o[k] = __ldcg(reinterpret_cast<const float4*>(i < parts ? sg.part + (at + 256ll * i) * HD : sg.state + own * HD) + x);
+        o[k] = __ldcg(reinterpret_cast<const float4*>(i < parts ? sg.part + static_cast<long long>(place(i)) * HD : sg.state + own * HD) + x);
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
@@ -556,7 +692,10 @@ template <int HD, typename T16>
 cudaError_t launch_prefix_hd(const LaunchCtx& lc, const PagedAttnArgs& a, const SharedGroups& s, const AttnMaps& maps) {
   cudaLaunchConfig_t cfg = {};
   cfg.blockDim = dim3(THREADS);
-  cfg.gridDim = dim3(lc.num_sms);
+  // no more CTAs than the longest rows that the table allows could keep busy
+  const long long items = (static_cast<long long>(a.B) / (2 * attn_tile_positions(a.H, a.G)) + std::min(s.N, a.B / 2)) * a.G;
+  const long long steps = items * ((a.blocks_per_seq + 7) / 8) / s.least_steps;
+  cfg.gridDim = dim3(static_cast<unsigned>(std::max(1ll, std::min<long long>(lc.num_sms, steps))));
   cfg.dynamicSmemBytes = SCfg<HD>::SMEM;
   cfg.stream = lc.stream;
   cudaLaunchAttribute attr[2];
@@ -574,11 +713,12 @@ cudaError_t launch_join_hd(const LaunchCtx& lc, const PagedAttnArgs& a, const Sh
   cudaLaunchAttribute attr[2];
   cfg.numAttrs = chain_attrs(lc, attr);
   cfg.attrs = attr;
-  return cudaLaunchKernelEx(&cfg, attn_join_kernel<HD, T16>, a, s, 2 * attn_tile_positions(a.H, a.G));
+  return cudaLaunchKernelEx(&cfg, attn_join_kernel<HD, T16>, a, s, attn_tile_positions(a.H, a.G));
 }
 
 template <int HD, typename T16>
 cudaError_t launch_hd(const LaunchCtx& lc, const PagedAttnArgs& a, const SharedGroups& s, const AttnMaps& maps) {
+  if (s.alone) return launch_attn_paged_own(lc, a, s);
   cudaError_t e = launch_prefix_hd<HD, T16>(lc, a, s, maps);
   if (e == cudaSuccess) e = launch_attn_paged_own(lc, a, s);
   return e == cudaSuccess ? launch_join_hd<HD, T16>(lc, a, s) : e;
@@ -599,14 +739,14 @@ cudaError_t prepare_attn_shared_kernels() {
 
 // Plan, the rows' own states, the prefix pass's parts, from a multiple of 256 bytes on.
 size_t shared_attn_bytes(int B, int H, int d, int num_sms) {
-  const size_t own = static_cast<size_t>(B) * H, parts = own + 256 * static_cast<size_t>(num_sms);
-  return ALIGN + aligned(16 * (1 + MAX_N)) + aligned(8 * own) + aligned(8 * parts) + 4 * static_cast<size_t>(d) * (own + parts);
+  const size_t own = static_cast<size_t>(B) * H, parts = 2 * own + 256 * static_cast<size_t>(num_sms);
+  return ALIGN + aligned(16 * (1 + PAGED_ATTN_MAX_B)) + aligned(8 * own) + aligned(8 * parts) + 4 * static_cast<size_t>(d) * (own + parts);
 }
 void shared_attn_carve(SharedGroups* s, void* work, int B, int H, int d, int num_sms) {
-  const size_t own = static_cast<size_t>(B) * H, parts = own + 256 * static_cast<size_t>(num_sms);
+  const size_t own = static_cast<size_t>(B) * H, parts = 2 * own + 256 * static_cast<size_t>(num_sms);
   char* at = reinterpret_cast<char*>(aligned(reinterpret_cast<uintptr_t>(work)));
   s->plan = reinterpret_cast<int4*>(at);
-  at += aligned(16 * (1 + MAX_N));
+  at += aligned(16 * (1 + PAGED_ATTN_MAX_B));
   s->state_stats = reinterpret_cast<float2*>(at);
   at += aligned(8 * own);
   s->stats = reinterpret_cast<float2*>(at);
@@ -615,8 +755,25 @@ void shared_attn_carve(SharedGroups* s, void* work, int B, int H, int d, int num
   s->part = s->state + own * d;
 }
 
+// Blocks read again come from L2, at some 10 TB/s, and the prefix pass and the join take some 13 us: less than 128 MB of
+// them is faster read again. GPU time of rows with 16 to 64 tokens of their own, 32 / 8 heads of 128, shared / each for
+// itself: 4 rows on 4096 tokens (50 MB spared) 19 / 17 us, 8 groups of 4 on 1024 (100 MB) 36 / 25, 16 rows on 4096 (251 MB)
+// 23 / 35, 8 groups of 4 on 4096 (403 MB) 54 / 83. AXON_SHARED_MIN_BYTES sets another limit, for measurements and for
+// tests of small cases.
+void shared_attn_rules(SharedGroups* s, const PagedAttnArgs& a) {
+  const long long block = 64ll * a.d * a.G;  // bytes of a block's keys and values
+  const long long row = paged_attn_most_pages(1, 1, a.blocks_per_seq, a.window, a.sinks);
+  s->least = 8;
+  const char* const limit = getenv("AXON_SHARED_MIN_BYTES");
+  const long long bytes = limit ? std::max(0ll, atoll(limit)) : 128ll << 20;
+  s->least_spared = static_cast<int>(std::min((bytes + block - 1) / block, 1ll << 20));
+  s->least_steps = 2;
+  s->alone = row * (a.B - 1) < s->least_spared;
+}
+
 cudaError_t launch_attn_shared(const LaunchCtx& lc, const PagedAttnArgs& a, const SharedGroups& s, const AttnMaps& maps) {
-  if (a.H / a.G > 16 || a.B < 1 || a.B > PAGED_ATTN_MAX_B || s.N < 1 || s.N > MAX_N || !a.block_table || lc.num_sms > 1024)
+  if (a.H / a.G > 16 || a.B < 1 || a.B > PAGED_ATTN_MAX_B || s.N < 1 || s.N > MAX_N || !a.block_table || lc.num_sms > MAX_SMS ||
+      2ll * a.B * a.H + 256ll * lc.num_sms > INT_MAX)
     return cudaErrorInvalidValue;
   if (a.d == 64) return lc.f16 ? launch_hd<64, f16>(lc, a, s, maps) : launch_hd<64, bf16>(lc, a, s, maps);
   if (a.d == 128) return lc.f16 ? launch_hd<128, f16>(lc, a, s, maps) : launch_hd<128, bf16>(lc, a, s, maps);

@@ -28,6 +28,12 @@ def ax():
     return ax
 
 
+@pytest.fixture(autouse=True)
+def small_cases_share_too(monkeypatch):
+    """Sharing saves too little in cases of this size to be taken by itself."""
+    monkeypatch.setenv("AXON_SHARED_MIN_BYTES", "0")
+
+
 class Case:
     """groups: (tokens whose whole blocks are shared, positions of the rows' queries, None: idle; grouped or loose)."""
 
@@ -281,3 +287,66 @@ def test_same_bits_every_time_captured_and_on_another_stream(ax):
     want, _ = c.reference(range(len(c.pos)))
     off = np.abs(out.double().cpu().numpy() - want) - ULP["bf16"] * np.abs(want)
     assert off.max() <= 5e-4 * max(np.abs(v).max() for v in c.values)
+
+
+def test_where_sharing_does_not_pay_by_itself(ax, monkeypatch):
+    """The library's own limit: no prefix pass for tables so narrow (alone), none for rows so short (found on the device)."""
+    monkeypatch.delenv("AXON_SHARED_MIN_BYTES")
+    groups = [(300, [310, 320, 330]), (200, [250, None]), (400, [470, 410, 399, 500])]
+    for per in (0, 4096):
+        c = Case(32, 8, 128, "bf16", groups, seed=13)
+        if per:
+            c.bt = torch.nn.functional.pad(c.bt, (0, per - c.per), value=-1)
+        check(ax, c)
+        plain = torch.empty_like(c.q)
+        cache = ax.make_kv_cache(c.k, c.v)
+        ax.axon_attn_decode(cache, c.layer, c.q, c.ctx, plain, ax.make_attn_workspace(cache, len(c.pos), 32), block_table=c.bt)
+        assert torch.equal(run(ax, c)[0], plain)
+    c.offsets[1] = 100
+    check(ax, c, err=(8, 16))
+    c = Case(32, 8, 128, "bf16", groups, seed=13)
+    c.offsets[1], c.prefix[2] = -1, -7
+    check(ax, c, err=(8, 20))
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (3000, 4)])
+def test_where_it_does(ax, monkeypatch, window, sinks):
+    """40 rows on 4096 tokens, by the library's own limit, against the one-token form."""
+    monkeypatch.delenv("AXON_SHARED_MIN_BYTES")
+    r = np.random.default_rng(14)
+    B, G, d, per, whole = 43, 8, 128, 300, 256
+    N = whole + B * (per - whole)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(14)
+    k, v = (torch.empty(1, N, G, 16, d, dtype=torch.bfloat16, device=DEV).normal_(generator=g) for _ in range(2))
+    q = torch.empty(B, 32, d, dtype=torch.bfloat16, device=DEV).normal_(generator=g) * 1.6
+    table = np.concatenate([np.tile(np.arange(whole), (B, 1)), whole + np.arange(B * (per - whole)).reshape(B, -1)], 1)
+    bt = torch.from_numpy(table.astype(np.int32)).to(DEV)
+    ctx = torch.from_numpy(r.integers(whole * 16, per * 16, B).astype(np.int32)).to(DEV)
+    cache = ax.make_kv_cache(k, v)
+    work = ax.make_shared_workspace(cache, B, 32)
+    a, b = torch.empty_like(q), torch.empty_like(q)
+    la, lb = torch.empty(B, 32, device=DEV), torch.empty(B, 32, device=DEV)
+    offsets, prefix = (torch.tensor(x, dtype=torch.int32, device=DEV) for x in ([0, 40, 43], [4096, 16]))
+    ax.axon_attn_shared(cache, 0, q, ctx, offsets, prefix, a, work, bt, window=window, sinks=sinks, lse=la)
+    ax.axon_attn_decode(cache, 0, q, ctx, b, work, block_table=bt, window=window, sinks=sinks, lse=lb)
+    assert not torch.equal(a, b)  # other sums: the prefix pass ran
+    vmax = float(v.abs().max())
+    assert ((a.double() - b.double()).abs() <= 5e-4 * vmax + 2.0 ** -7 * b.double().abs()).all()
+    assert float((la - lb).abs().max()) <= 5e-4
+
+
+def test_thousands_of_calls_in_a_row(ax):
+    """Nothing of a call is on its way when its blocks end: three states in turn, the same bits every time."""
+    cases = [Case(32, 8, 128, t, [(300 + 16 * i, [420 + 3 * j for j in range(w)]) for i, w in enumerate((4, 3, 40))], seed=20 + n,
+                  layers=1, layer=0) for n, t in enumerate(("fp16", "bf16", "fp16"))]
+    state = []
+    for c in cases:
+        cache = ax.make_kv_cache(c.k, c.v)
+        work = ax.make_shared_workspace(cache, len(c.pos), 32)
+        state.append((c, cache, work, torch.empty_like(c.q), run(ax, c, work=work)[0]))
+    for i in range(6000):
+        c, cache, work, out, _ = state[i % 3]
+        ax.axon_attn_shared(cache, 0, c.q, c.ctx, c.offsets, c.prefix, out, work, c.bt)
+    for c, cache, work, out, want in state:
+        assert torch.equal(out, want)

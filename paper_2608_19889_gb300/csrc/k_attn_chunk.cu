@@ -369,6 +369,8 @@ __global__ void __launch_bounds__(THREADS, 1)
       for (int w = 0; w < 2; ++w)
         if (iq[w] > 0) wait_bar(q_full(w), (iq[w] - 1) & 1, p.err);
       for (int i = it > NS ? it - NS : 0; i < it; ++i) wait_bar(kv_full(i % NS), (i / NS) & 1, p.err);
+      // and so do the arrivals of the issuers' last commits, which come after the one that the softmax warps wait for
+      for (int i = ok && it > NS ? it - NS : 0; ok && i < it; ++i) wait_bar(kv_empty(i % NS), (i / NS) & 1, p.err);
     } else if (warp != 10) {
       // -------------------------------------------------------- MMA issuers
       // A warp per tile. What an issuer itself executes is on the critical path (a product takes 64

@@ -218,6 +218,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     // unless a wait ran out)
     mbar_wait(q_full, 0, p.err);
     for (int i = it > NS ? it - NS : 0; i < it; ++i) mbar_wait(kv_full(i % NS), (i / NS) & 1, p.err);
+    // and so do the arrivals of the issuer's last commits, which come after the one that the softmax warps wait for
+    for (int i = ok && it > NS ? it - NS : 0; ok && i < it; ++i) mbar_wait(kv_empty(i % NS), (i / NS) & 1, p.err);
   } else if (warp == 9) {
     // ------------------------------------------------------------ MMA issuer
     if (lane == 0) {

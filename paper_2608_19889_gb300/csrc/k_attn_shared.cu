@@ -41,7 +41,7 @@ struct SCfg {
   static constexpr int CHUNK = 128 * 128;           // bytes of one 128-row chunk
   static constexpr int TILE = CH * CHUNK;           // Q, K or V tile
   static constexpr int STAGES = HD == 128 ? 4 : 8;  // K and V tiles in flight
-  static constexpr int BARS = 2 * STAGES + 16;
+  static constexpr int BARS = 2 * STAGES + 18;
   static constexpr int PLAN = 4 * ((GroupPlan::INTS + 1) * MAX_N + 4);
   static constexpr int SMEM = 2 * TILE + STAGES * TILE + 8 * BARS + 16 + PLAN + 1024;
 };
@@ -89,11 +89,12 @@ struct Part {
   int page0, pages;     // blocks
   int lead;
   bool one;             // one tile, in both pipelines
+  int odd;              // one: the pipeline that takes its first step, since a stage of the ring is always the same one's
   int at;               // its first (row, head) in the workspace
   int steps;
   unsigned next;        // where the next part begins
   // steps of pipeline w
-  AXON_DEV int count(int w, int PW) const { return one ? (steps + 1 - w) >> 1 : w * PW < rows ? steps : 0; }
+  AXON_DEV int count(int w, int PW) const { return one ? (steps + 1 - (w ^ odd)) >> 1 : w * PW < rows ? steps : 0; }
 };
 
 // In front of the parts' first (row, head): twice those of the items before it, which all lie inside B * H, and 256 for each
@@ -125,6 +126,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   auto o_empty = [&](int w) { return more + 8 * (10 + w); };
   auto turn = [&](int w) { return more + 8 * (12 + w); };
   auto warm = [&](int w) { return more + 8 * (14 + w); };
+  auto met = [&](int w) { return more + 8 * (16 + w); };
   const uint32_t tmem_slot = bars + 8 * C::BARS;
   int* const plan = reinterpret_cast<int*>(smem_raw + (tmem_slot + 16 - raw));
   const GroupPlan gp(plan, sg.N);
@@ -146,6 +148,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       mbar_init(o_empty(w), 128);
       mbar_init(turn(w), 1);
       mbar_init(warm(w), 128);
+      mbar_init(met(w), 1);
     }
     fence_mbar_init();
     fence_proxy_async();
@@ -171,8 +174,10 @@ __global__ void __launch_bounds__(THREADS, 1)
     u0 = u1 ? d.begin(blockIdx.x) : 0;
   };
   // The part with the first step that begins at u or after it (u < u1); no steps: none does. The same in all lanes.
-  auto part_of = [&](unsigned u) {
+  // done: steps of the CTA before it.
+  auto part_of = [&](unsigned u, int done) {
     Part t;
+    t.odd = done & 1;
     for (;;) {
       int lo = 0, hi = sg.N - 1;  // the last group that begins at u or before it
       while (lo < hi) {
@@ -240,7 +245,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       int iq[2] = {0, 0}, it = kv;  // queries; tiles of the ring, this warp's every other one
       bool ok = true;
       for (unsigned u = u0; u < u1 && ok;) {
-        const Part t = part_of(u);
+        const Part t = part_of(u, it >> 1);
         u = t.next;
         if (!t.steps) break;
         // pool row of this lane's block of step s; past the last block and for table entries
@@ -357,14 +362,21 @@ __global__ void __launch_bounds__(THREADS, 1)
           }
         }
       };
+      int done = 0;
+      bool apart = false;  // the issuers have gone through the ring each on its own
+      uint32_t meetings = 0;
       for (unsigned u = u0; u < u1;) {
-        const Part t = part_of(u);
+        const Part t = part_of(u, done);
         u = t.next;
         if (!t.steps) break;
+        done += t.steps;
         const int nt_all = __shfl_sync(0xffffffffu, t.steps, 0), pages = __shfl_sync(0xffffffffu, t.pages, 0);
         const int nt = __shfl_sync(0xffffffffu, t.count(w, PW), 0);
         if (__shfl_sync(0xffffffffu, static_cast<int>(t.one), 0)) {
-          // every other step; nobody else uses its stages, so that each is given back for both issuers
+          // Every other step; nobody else uses its stages, so that each is given back for both issuers. A stage has the same
+          // issuer in all such parts: an issuer that came to a stage of the other one could take the fill before the last
+          // for the one that it waits for, their parities being the same.
+          apart = true;
           const uint32_t st0 = st, ph0 = ph;
           auto stage_of = [&](int s, int kv, uint32_t& phase) {
             const uint32_t at = st0 + 2 * s + kv;
@@ -373,7 +385,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           };
           bool ok = !nt || wait_all(q_full(w), ph_q);
           for (int k = 0; k < nt && ok; ++k) {
-            const int s = 2 * k + w;
+            const int s = 2 * k + (w ^ t.odd);
             uint32_t phk, phv;
             const uint32_t sk = stage_of(s, 0, phk), sv = stage_of(s, 1, phv);
             ok = wait_all(kv_full(sk), phk);
@@ -409,7 +421,15 @@ __global__ void __launch_bounds__(THREADS, 1)
           st = at % NS;
           continue;
         }
-        bool ok = wait_all(kv_full(st), ph) && (!nt || wait_all(q_full(w), ph_q)) && my_turn();
+        bool ok = true;
+        if (apart) {
+          // for the same reason both have seen the fills of all stages so far before they go through the ring together
+          apart = false;
+          if (leader) mbar_arrive(met(w ^ 1));
+          ok = wait_all(met(w), meetings & 1);
+          ++meetings;
+        }
+        ok = ok && wait_all(kv_full(st), ph) && (!nt || wait_all(q_full(w), ph_q)) && my_turn();
         if (!ok) break;
         tc_fence_after();
         if (nt)
@@ -463,23 +483,32 @@ __global__ void __launch_bounds__(THREADS, 1)
     int ns_ = 0, no = 0;  // scores and outputs taken
     bool ok = true;
     unsigned u = 0;
-    // the first round: a step on nothing
+    int done = 0;  // steps
+    {
+      uint32_t zero[32];
+#pragma unroll
+      for (int c = 0; c < 32; ++c) zero[c] = 0;
+      for (int c = 0; c < KT; c += 32) tmem_st32(tS + c, zero);
+      tmem_wait_st();
+    }
+    // the first round: a step on nothing (zeros)
     for (bool dry = true; ok; dry = false) {
       int nt = 0, left = KT, stride = 0;  // steps; keys from a step on, and to the next one
       bool valid = false;
       int at = 0;
       if (!dry) {
         if (u >= u1) break;
-        const Part t = part_of(u);
+        const Part t = part_of(u, done);
         if (!t.steps) break;
         u = t.next;
+        done += t.steps;
         nt = t.count(w, PW);
         stride = t.one ? 2 * KT : KT;
-        left = 16 * t.pages - (t.one ? w * KT : 0);
+        left = 16 * t.pages - (t.one ? (w ^ t.odd) * KT : 0);
         valid = i < HPG * PW && (t.one ? 0 : w * PW * HPG) + i < t.rows * HPG;
         at = t.at + w * (t.one ? t.rows : PW) * HPG + i;
         if (!nt) {
-          if (t.one && valid) sg.stats[at] = make_float2(-INFINITY, 0.f);  // nothing for the second pipeline
+          if (t.one && valid) sg.stats[at] = make_float2(-INFINITY, 0.f);  // one step: nothing for this pipeline
           continue;
         }
       }

@@ -32,16 +32,16 @@ constexpr int ST = 512;        // threads
 constexpr int SW = ST / 32;    // warps
 constexpr int NB = 1024;       // bins
 constexpr int MAX_CL = 16;     // CTAs of a cluster
-constexpr int STEPS = 1024;    // steps of an octave
+constexpr int STEPS = 512;     // steps of an octave
 constexpr int K_END = 45 * STEPS;  // weights from here on are 0
-constexpr int BIN_SHIFT = 5;   // 32 bins per octave
+constexpr int BIN_SHIFT = 4;   // 32 bins per octave
 constexpr int MAX_SLICE = 46 * 1024;  // logits of a CTA: 184 KB
 static_assert(SAMPLE_MAX_VOCAB / MAX_CL <= MAX_SLICE, "the largest vocabulary has to fit a cluster");
 static_assert(MAX_SLICE / ST <= 128, "sums of a thread's weights have to fit 32 bits");
 
 typedef unsigned long long u64;
 
-// 2^(-j/1024) as a pair of fp32 numbers, by the series of exp in 64 bits.
+// 2^(-j/512) as a pair of fp32 numbers, by the series of exp in 64 bits.
 struct PowerTable {
   float hi[STEPS], lo[STEPS];
   constexpr PowerTable() : hi(), lo() {
@@ -59,7 +59,7 @@ struct PowerTable {
 };
 __device__ constexpr PowerTable g_powers{};
 
-// A row's scale. With s = l - base the exponent (base 2) of a logit is s (ch + cl); its step j is s ch in 1024ths, rounded,
+// A row's scale. With s = l - base the exponent (base 2) of a logit is s (ch + cl); its step j is s ch in 512ths, rounded,
 // and k = top - j >= 1 counts the steps below the largest logit's.
 struct Scale {
   float base, ch, cl;
@@ -70,14 +70,14 @@ constexpr float MAGIC = 12582912.f;  // 1.5 * 2^23: adding it rounds |x| <= 2^22
 constexpr int MAGIC_BITS = 0x4b400000;
 
 // Steps of logit l below the top; not below K_END (unsigned) where its weight is 0, -infinity and numbers that are none among
-// them: s ch * 1024 + MAGIC is then a float of another size or sign, whose bits lie far from MAGIC's.
+// them: s ch * 512 + MAGIC is then a float of another size or sign, whose bits lie far from MAGIC's.
 AXON_DEV unsigned steps_of(const Scale& c, float l) {
   const float n = (l - c.base) * -c.ch;
-  return static_cast<unsigned>(c.top + MAGIC_BITS - __float_as_int(fmaf(n, -1024.f, MAGIC)));
+  return static_cast<unsigned>(c.top + MAGIC_BITS - __float_as_int(fmaf(n, -static_cast<float>(STEPS), MAGIC)));
 }
 
-// Weights of two logits, in units of 2^-22 (hi) and 2^-44 (lo, signed), rounded; k: their steps. 2^(s (ch + cl) - top / 1024) =
-// 2^-(k/1024) (1 - y + y^2/2 - y^3/6), y = (j/1024 - s (ch + cl)) ln 2 < 3.4e-4, every sum and product that counts as a
+// Weights of two logits, in units of 2^-22 (hi) and 2^-44 (lo, signed), rounded; k: their steps. 2^(s (ch + cl) - top / 512) =
+// 2^-(k/512) (1 - y + y^2/2 - y^3/6), y = (j/512 - s (ch + cl)) ln 2 < 6.8e-4, every sum and product that counts as a
 // pair of fp32 numbers: exact to about 2^-41.
 struct Weights {
   unsigned k[2];
@@ -90,8 +90,9 @@ AXON_DEV Weights weights(const Scale& c, float l0, float l1, const float2* power
   const uint64_t n = mul2(s, pk2(-c.ch, -c.ch));
   uint64_t e = fma2(s, pk2(c.ch, c.ch), n);  // what the product lost
   e = fma2(s, pk2(c.cl, c.cl), e);
-  const uint64_t t = fma2(n, pk2(-1024.f, -1024.f), pk2(MAGIC, MAGIC));
-  const uint64_t g = fma2(add2(t, pk2(-MAGIC, -MAGIC)), pk2(1.f / 1024.f, 1.f / 1024.f), n);  // exact
+  constexpr float S = static_cast<float>(STEPS);
+  const uint64_t t = fma2(n, pk2(-S, -S), pk2(MAGIC, MAGIC));
+  const uint64_t g = fma2(add2(t, pk2(-MAGIC, -MAGIC)), pk2(1.f / S, 1.f / S), n);  // exact
   Weights w;
   float t0, t1;
   upk2(t, t0, t1);
@@ -110,7 +111,7 @@ AXON_DEV Weights weights(const Scale& c, float l0, float l1, const float2* power
   const uint64_t lost = fma2(q, one, fma2(vh, one, th));
   const uint64_t vl = add2(fma2(th, r, fma2(th, ny, q)), add2(lost, fma2(tl, ny, tl)));
   // times 2^22 of the octave, in two integers
-  const uint64_t sc = pk2(__uint_as_float((149u - (w.k[0] >> 10)) << 23), __uint_as_float((149u - (w.k[1] >> 10)) << 23));
+  const uint64_t sc = pk2(__uint_as_float((149u - w.k[0] / STEPS) << 23), __uint_as_float((149u - w.k[1] / STEPS) << 23));
   const uint64_t a = mul2(vh, sc), whole = add2(fma2(vl, sc, a), pk2(MAGIC, MAGIC));
   const uint64_t rest = fma2(vl, sc, fma2(add2(whole, pk2(-MAGIC, -MAGIC)), one, a));
   float h0, h1, r0, r1;
@@ -138,18 +139,26 @@ AXON_DEV u64 fraction64(float v) {
   return up >= 0 ? digits << up : up > -24 ? digits >> -up : 0;
 }
 
-// Floats as integers of the same order.
-AXON_DEV unsigned key_of(float v) {
+// Logits as integers of the same order: the bits of the float, without those that logits of TL never differ in.
+template <typename TL> struct Key { static constexpr int DROP = 0; };
+template <> struct Key<bf16> { static constexpr int DROP = 16; };
+template <> struct Key<f16> { static constexpr int DROP = 13; };
+template <typename TL> AXON_DEV unsigned sample_key(float v) {
   const unsigned b = __float_as_uint(v + 0.f);  // -0 is 0
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
+  return (b & 0x80000000u ? ~b : b | 0x80000000u) >> Key<TL>::DROP;
 }
-AXON_DEV float of_key(unsigned k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
+template <typename TL> AXON_DEV float sample_value(unsigned k) {
+  constexpr int D = Key<TL>::DROP;
+  k <<= D;
+  return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k & ~((1u << D) - 1));
+}
 
 constexpr int FEW = 256;    // logits among which one CTA settles everything
 constexpr int LIST = 512;   // a CTA's part of a list
 constexpr int SOME = 1024;  // logits of a bin among which the cut is found without more bins
 struct Shared {
-  unsigned hist[2][2][NB];  // low and high words of the amounts; used in turn
+  unsigned hist[2][2][NB];  // amounts, used in turn: as they come, bits 0 .. 15 and 16 .. 31; then 64 bits in two words
+  unsigned high[NB];        // bits from 32 on, as they come
   float2 powers[STEPS];
   uint2 mine[LIST];         // this CTA's list: key, number
   uint2 all[SOME];          // all CTAs' lists, in the first one
@@ -160,10 +169,13 @@ struct Shared {
   unsigned ends[2];
 };
 
+// v < 2^63 summed over the warp, 21 bits at a time; the sum is below 2^63.
 AXON_DEV u64 warp_sum64(u64 v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
+  constexpr unsigned M = (1u << 21) - 1;
+  const unsigned a = __reduce_add_sync(0xffffffffu, static_cast<unsigned>(v) & M);
+  const unsigned b = __reduce_add_sync(0xffffffffu, static_cast<unsigned>(v >> 21) & M);
+  const unsigned c = __reduce_add_sync(0xffffffffu, static_cast<unsigned>(v >> 42));
+  return a + (static_cast<u64>(b) << 21) + (static_cast<u64>(c) << 42);
 }
 AXON_DEV u64 warp_scan64(u64 v) {
   const int lane = threadIdx.x & 31;
@@ -175,7 +187,10 @@ AXON_DEV u64 warp_scan64(u64 v) {
   return v;
 }
 
+template <typename TL>
 struct Row {
+  AXON_DEV static unsigned key_of(float v) { return sample_key<TL>(v); }
+  AXON_DEV static float of_key(unsigned k) { return sample_value<TL>(k); }
   const SampleArgs& p;
   Shared& sh;
   const float* val;  // this CTA's slice
@@ -214,17 +229,30 @@ struct Row {
     ++turn;
   }
 
-  // Adds to bin b of the current histogram.
+  // Adds to bin b of the current histogram. Weights go there 16 bits at a time: no sum of a CTA's at most 2^16 logits
+  // carries into the next word, and nothing has to come back from an atomic (64-bit ones on shared memory are loops).
   template <bool MASS>
   AXON_DEV void add(int b, u64 amount) {
     unsigned* h = &sh.hist[pass & 1][0][b];
+    const unsigned low = static_cast<unsigned>(amount);
     if (MASS) {
-      const unsigned lo = static_cast<unsigned>(amount);
-      const unsigned up = static_cast<unsigned>(amount >> 32) + (atomicAdd(h, lo) > ~lo);
-      if (up) atomicAdd(h + NB, up);
+      atomicAdd(h, low & 0xffffu);
+      atomicAdd(h + NB, low >> 16);
+      if (amount >> 32) atomicAdd(&sh.high[b], static_cast<unsigned>(amount >> 32));
     } else {
-      atomicAdd(h, 1u);
+      atomicAdd(h, low);
     }
+  }
+  // This thread's bins of the current histogram, 2t and 2t + 1, as 64-bit numbers, in place of the words.
+  AXON_DEV void join_words() {
+    uint2* const l = reinterpret_cast<uint2*>(&sh.hist[pass & 1][0][0]) + threadIdx.x;
+    uint2* const m = reinterpret_cast<uint2*>(&sh.hist[pass & 1][1][0]) + threadIdx.x;
+    uint2* const h = reinterpret_cast<uint2*>(&sh.high[0]) + threadIdx.x;
+    const u64 a = l->x + (static_cast<u64>(m->x) << 16) + (static_cast<u64>(h->x) << 32);
+    const u64 b = l->y + (static_cast<u64>(m->y) << 16) + (static_cast<u64>(h->y) << 32);
+    *l = make_uint2(static_cast<unsigned>(a), static_cast<unsigned>(b));
+    *m = make_uint2(static_cast<unsigned>(a >> 32), static_cast<unsigned>(b >> 32));
+    *h = make_uint2(0, 0);
   }
   AXON_DEV void clear(int which) {
     for (int i = threadIdx.x; i < 2 * NB; i += ST) (&sh.hist[which][0][0])[i] = 0;
@@ -270,6 +298,10 @@ struct Row {
   template <bool MASS>
   AXON_DEV bool crossing(float part_of, u64 goal) {
     cg::cluster_group cluster = cg::this_cluster();
+    if (MASS) {
+      __syncthreads();
+      join_words();
+    }
     cluster.sync();
     const int which = pass & 1, t = threadIdx.x;
     ++pass;
@@ -365,7 +397,7 @@ struct Row {
   }
 
   // The first token, by number, at which the running sum of the amounts passes t(sum of all): its number, and
-  // its amount, in the threads of one warp of the cluster; -1 in the others.
+  // its amount, in one thread of the cluster; -1 in the others.
   template <bool TIES, typename T>
   AXON_DEV int locate(float v, T t, u64& its, u64& all) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -392,16 +424,22 @@ struct Row {
     at = __ffs(__ballot_sync(0xffffffffu, inc > rest)) - 1;
     if (at != warp) return -1;
     rest -= __shfl_sync(0xffffffffu, inc - x, at);
-    for (int i = i0 + warp * sub; i < i1; i += 32) {
-      u64 a = 0;
-      if (kept(val[i + lane], i + lane))
-        a = TIES ? static_cast<u64>(val[i + lane] == v) : weight(c, val[i + lane], sh.powers);
-      const u64 sum = warp_scan64(a);
+    for (int i = i0 + warp * sub + 4 * lane; i < i1; i += 128) {
+      const float4 f = *reinterpret_cast<const float4*>(val + i);
+      const float l[4] = {f.x, f.y, f.z, f.w};
+      u64 a[4];
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+        a[y] = !kept(l[y], i + y) ? 0 : TIES ? static_cast<u64>(l[y] == v) : weight(c, l[y], sh.powers);
+      const u64 mine4 = a[0] + a[1] + a[2] + a[3], sum = warp_scan64(mine4);
       const unsigned hit = __ballot_sync(0xffffffffu, sum > rest);
       if (hit) {
-        const int f = __ffs(hit) - 1;
-        its = __shfl_sync(0xffffffffu, a, f);
-        return first + i + f;
+        if (lane != __ffs(hit) - 1) return -1;
+        rest -= sum - mine4;
+        int y = 0;
+        for (; y < 3 && a[y] <= rest; ++y) rest -= a[y];
+        its = y == 0 ? a[0] : y == 1 ? a[1] : y == 2 ? a[2] : a[3];
+        return first + i + y;
       }
       rest -= __shfl_sync(0xffffffffu, sum, 31);
     }
@@ -501,6 +539,7 @@ struct Row {
       }
       __syncthreads();
       const int which = pass & 1;
+      if (MASS) join_words();
       const uint2 l = reinterpret_cast<const uint2*>(&sh.hist[which][0][0])[tid], h = reinterpret_cast<const uint2*>(&sh.hist[which][1][0])[tid];
       const u64 a[2] = {(static_cast<u64>(h.x) << 32) + l.x, (static_cast<u64>(h.y) << 32) + l.y};
       scan_bins(a, -1.f, need);
@@ -609,7 +648,7 @@ struct Row {
     __syncthreads();
     if (tid == 0) sh.found[0] = 0;
     __syncthreads();
-    if (at >= 0 && (tid & 31) == 0) sh.found[0] = at + 1;
+    if (at >= 0) sh.found[0] = at + 1;
     __syncthreads();
     exchange(sh.found[0], before, all);
     cut_at(v, static_cast<int>(all) - 1);
@@ -643,7 +682,7 @@ __global__ void __launch_bounds__(ST) sample_kernel(const SampleArgs p, int CL, 
   const int b = blockIdx.x / CL, rank = blockIdx.x % CL;
   cg::cluster_group cluster = cg::this_cluster();
   for (int i = tid; i < STEPS; i += ST) sh.powers[i] = make_float2(g_powers.hi[i], g_powers.lo[i]);
-  for (int i = tid; i < 4 * NB; i += ST) (&sh.hist[0][0][0])[i] = 0;
+  for (int i = tid; i < 5 * NB; i += ST) (&sh.hist[0][0][0])[i] = 0;  // (high follows)
   grid_dep_launch();
   grid_dep_wait();
 
@@ -680,16 +719,17 @@ __global__ void __launch_bounds__(ST) sample_kernel(const SampleArgs p, int CL, 
   }
   const int end = (n + 127) & ~127;
   for (int i = n + tid; i < end; i += ST) val[i] = __int_as_float(0x7fffffff);
-  Row row{p, sh, val, n, first, rank, CL};
+  Row<TL> row{p, sh, val, n, first, rank, CL};
   row.end = end;
   row.seg = ((slice + SW - 1) / SW + 127) / 128 * 128;
-  u64 all = key_of(warp_max(best));
-  if (lane == 0) sh.warp[warp] = all;
+  best = warp_max(best);
+  if (lane == 0) sh.warp[warp] = __float_as_uint(best);
   __syncthreads();
-  all = key_of(warp_max(lane < SW ? of_key(static_cast<unsigned>(sh.warp[lane])) : -INFINITY));
-  if (tid == 0) sh.cta[1] = all;
+  best = warp_max(lane < SW ? __uint_as_float(static_cast<unsigned>(sh.warp[lane])) : -INFINITY);
+  if (tid == 0) sh.cta[1] = __float_as_uint(best);
   cluster.sync();
-  float m = warp_max(lane < CL ? of_key(static_cast<unsigned>(*cluster.map_shared_rank(&sh.cta[1], lane))) : -INFINITY);
+  float m = warp_max(lane < CL ? __uint_as_float(static_cast<unsigned>(*cluster.map_shared_rank(&sh.cta[1], lane))) : -INFINITY);
+  u64 all = 0;
 
   const float temp = p.temperature ? p.temperature[b] : 1.f;
   const float low = p.min_p ? p.min_p[b] : 0.f;
@@ -739,11 +779,11 @@ __global__ void __launch_bounds__(ST) sample_kernel(const SampleArgs p, int CL, 
   if (share < 1.f) row.share = share;
   if (low > 0.f) {
     const u64 most = weight(row.c, m, sh.powers);
-    row.least = low < 1.f ? Row::share_of(low, most) : most;
+    row.least = low < 1.f ? Row<TL>::share_of(low, most) : most;
   }
   int* const token = p.tokens + b;
   float* const prob = p.prob ? p.prob + b : nullptr;
-  if ((k > 0 && k < p.V && row.cut<false>(k, random, token, prob)) || (row.share < 1.f && row.cut<true>(0, random, token, prob))) {
+  if ((k > 0 && k < p.V && row.template cut<false>(k, random, token, prob)) || (row.share < 1.f && row.template cut<true>(0, random, token, prob))) {
     cluster.sync();
     return;
   }
@@ -753,12 +793,12 @@ __global__ void __launch_bounds__(ST) sample_kernel(const SampleArgs p, int CL, 
       if (lane == 0) sh.ends[0] = key;
     }
     __syncthreads();
-    const float v = of_key(sh.ends[0]);
+    const float v = Row<TL>::of_key(sh.ends[0]);
     if (v > row.vcut) row.cut_at(v, 0x7fffffff);
   }
   u64 its = 0;
-  const int at = row.locate<false>(0.f, [&](u64 sum) { return Row::draw(random, sum); }, its, all);
-  if (at >= 0 && lane == 0) {
+  const int at = row.template locate<false>(0.f, [&](u64 sum) { return Row<TL>::draw(random, sum); }, its, all);
+  if (at >= 0) {
     *token = at;
     if (prob) *prob = static_cast<float>(static_cast<double>(its) / static_cast<double>(all));
   }

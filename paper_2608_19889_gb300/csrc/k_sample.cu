@@ -163,6 +163,7 @@ struct Shared {
   uint2 mine[LIST];         // this CTA's list: key, number
   uint2 all[SOME];          // all CTAs' lists, in the first one
   unsigned mine_n;
+  unsigned estimate;        // of the logits up to the crossing bin
   u64 cta[2];               // what the cluster exchanges, in turn
   u64 warp[SW];
   u64 found[3];             // the crossing bin: number, what is needed of it, all of it
@@ -324,7 +325,22 @@ struct Row {
       }
     }
     clear(which ^ 1);
-    return scan_bins(a, part_of, goal);
+    if (t == 0) sh.estimate = 0;
+    const bool any = scan_bins(a, part_of, goal);
+    if (MASS && part_of >= 0.f && any) {
+      // How many logits there are up to the crossing bin: at least this many, and 2 % more at most, since a bin's weights
+      // are that close to each other.
+      const int b = static_cast<int>(sh.found[0]);
+      unsigned n = 0;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (2 * t + i <= b && 2 * t + i < NB - 1)
+          n += static_cast<unsigned>(fminf(static_cast<float>(a[i]) * exp2f((2 * t + i) * (static_cast<float>(1 << BIN_SHIFT) / STEPS) - 44.f), 1e6f));
+      n = __reduce_add_sync(0xffffffffu, n);
+      if ((t & 31) == 0 && n) atomicAdd(&sh.estimate, n);
+      __syncthreads();
+    }
+    return any;
   }
 
   AXON_DEV static int bin_of(unsigned k) { return min(static_cast<int>(k) >> BIN_SHIFT, NB - 1); }
@@ -590,8 +606,8 @@ struct Row {
     if (!crossing<MASS>(MASS ? fmaxf(share, 0.f) : -1.f, k)) return false;
     const int b = static_cast<int>(sh.found[0]);
     u64 need = sh.found[1], amount = sh.found[2];
-    // Few in these bins? (How many is known of a count; of weights, that they are no fewer than the sum takes of the largest.)
-    if (MASS ? (target >> 44) < FEW : k - need + amount <= FEW) {
+    // Few in these bins? (How many is known of a count, and nearly of weights.)
+    if (MASS ? sh.estimate <= FEW : k - need + amount <= FEW) {
       const int nc = gather(0, b, FEW);
       if (nc <= FEW) {
         if (rank == 0) settle(nc, k, u, token, prob);
@@ -599,18 +615,18 @@ struct Row {
       }
       cg::this_cluster().sync();  // the counts are read before the next list begins
     }
-    const int nc = gather(b, b, SOME);
-    if (nc <= SOME) {
-      u64 at = rank == 0 ? cut_list<MASS>(nc, need) : 0, before, all;
-      if (rank)
-        for (int w = 0; w < 2; ++w) clear(w);
-      exchange(at, before, all);
-      const float v = of_key(static_cast<unsigned>(all >> 32));
-      cut_at(v, min(static_cast<int>(all & 0x7fffffffu), v == vcut ? icut : 0x7fffffff));
-      return false;
+    if ((!MASS && amount <= SOME) || (MASS && static_cast<float>(amount) * exp2f(b * (static_cast<float>(1 << BIN_SHIFT) / STEPS) - 44.f) <= SOME) || b == NB - 1) {
+      const int nc = gather(b, b, SOME);
+      if (nc <= SOME) {
+        u64 before, all;
+        const u64 at = rank == 0 ? cut_list<MASS>(nc, need) : 0;
+        exchange(at, before, all);
+        const float v = of_key(static_cast<unsigned>(all >> 32));
+        cut_at(v, min(static_cast<int>(all & 0x7fffffffu), v == vcut ? icut : 0x7fffffff));
+        return false;
+      }
     }
-    for (int w = 0; w < 2; ++w) clear(w);
-    // keys of the bin
+    // keys of the bin (the next pass's histogram was cleared with the crossing; the others may still read the last one)
     if (tid < 32) {
       const unsigned lo = lowest_in(b), hi = b > 0 ? lowest_in(b - 1) - 1 : key_of(m);
       if (tid == 0) {

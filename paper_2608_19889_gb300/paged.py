@@ -1,9 +1,9 @@
 """Sequences of a paged model whose cache blocks are managed on the device.
 
 `PagedSeqs` keeps what the block operators work on (block table, lengths, counts, workspace, error word) for the cache of
-a model created with AXON_KV_PAGED, and steps the model with it: blocks are taken before tokens are appended, shared by
-forks, and given back when a sequence ends or, under a sliding window, when they have slid out of it. `check`, `lengths`
-and `blocks_in_use` wait for the GPU, `extend` for the copy of its lengths; nothing else does.
+a model created with AXON_KV_PAGED, and steps the model with it, greedily or drawing tokens: blocks are taken before tokens
+are appended, shared by forks, and given back when a sequence ends or, under a sliding window, when they have slid out of
+it. `check`, `lengths` and `blocks_in_use` wait for the GPU, `extend` for the copy of its lengths; nothing else does.
 """
 from __future__ import annotations
 
@@ -34,6 +34,7 @@ class PagedSeqs:
         self.all = torch.arange(rows, **dev)
         self.one = torch.ones(rows, **dev)
         self.unused = torch.empty(rows, **dev)  # greedy tokens that nobody asked for
+        self.vocabulary, self.logits = cfg.vocab_size, None  # logits of `sample`, made with its first call
 
     def _first(self, n):
         if not 1 <= n <= self.rows:
@@ -65,6 +66,15 @@ class PagedSeqs:
         ax.axon_kv_reserve(self.cache, self.seqs, self.all[:n], self.one[:n], self.work, err=self.err)
         ax.axon_decode_step(self.model, tokens, self.lens, block_table=self.table, logits=logits,
                             next_tokens=self.unused if next_tokens is None else next_tokens)
+
+    def sample(self, tokens, u, next_tokens, temperature=None, top_k=None, top_p=None, min_p=None, prob=None):
+        """`step`, and a token for each of its rows drawn from its logits with the random numbers u (fp32, one per row): see
+        axon_sample for these, the settings (device tensors with an entry per row) and prob. next_tokens may be `tokens`."""
+        n = tokens.numel()
+        if self.logits is None:
+            self.logits = torch.empty(self.rows, self.vocabulary, device="cuda")
+        self.step(tokens, logits=self.logits[:n])
+        ax.axon_sample(self.logits[:n], u, next_tokens, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p, prob=prob)
 
     def fork(self, src, dst):
         """Rows dst take over what rows src hold (int32 device tensors)."""

@@ -125,22 +125,22 @@ AXON_DEV void paged_decode(const PagedAttnArgs& p, const SharedGroups& sg) {
   grid_dep_launch();
   // (SH: the prefix pass before this kernel lets it start once its inputs are there)
   if (!SH || sg.alone) grid_dep_wait();
-  const GroupPlan gp(rpos + p.B, SH ? sg.N : 0);
+  // SH: [B] the pages that the row has in common with others, from the first and to the last; then the plan they come from
+  int2* const shared = reinterpret_cast<int2*>(before + 2 * p.B + 2);
   if constexpr (SH) {
+    const GroupPlan gp(reinterpret_cast<int*>(shared + p.B), sg.N);
     if (sg.alone) {
       if (blockIdx.x == 0) check_groups<DW * 32>(p, sg);
     } else {
       plan_groups<DW * 32, 0>(p, sg, gp, false);
     }
-  }
-  // the pages that row b has in common with others
-  auto common = [&](int b) {
-    if constexpr (SH) {
+    for (int b = tid; b < p.B; b += DW * 32) {
       const int n = sg.alone ? -1 : group_of(gp, sg.N, b);
-      if (n >= 0 && gp.c1[n] > gp.c0[n]) return make_int2(gp.c0[n], gp.c1[n]);
+      shared[b] = n >= 0 && gp.c1[n] > gp.c0[n] ? make_int2(gp.c0[n], gp.c1[n]) : make_int2(INT_MAX, INT_MAX);
     }
-    return make_int2(INT_MAX, INT_MAX);
-  };
+    __syncthreads();
+  }
+  auto common = [&](int b) { return SH ? shared[b] : make_int2(INT_MAX, INT_MAX); };
 
   // ---- pages before each row
   if (p.B <= 32) {
@@ -247,7 +247,7 @@ AXON_DEV void paged_decode(const PagedAttnArgs& p, const SharedGroups& sg) {
 
   for (unsigned u = u0; u < u1;) {
     while (before[b + 1] * p.G <= u) ++b;
-    const RowPages rp = row_pages(p, rpos[b], SH ? common(b) : make_int2(INT_MAX, INT_MAX));
+    const RowPages rp = row_pages(p, rpos[b], common(b));
     const unsigned row0 = before[b] * p.G;
     const int g = static_cast<int>((u - row0) / rp.n);
     const unsigned item0 = row0 + static_cast<unsigned>(g) * rp.n;
@@ -602,6 +602,9 @@ constexpr size_t smem_bytes(int B) {
   return static_cast<size_t>(DW) * DCfg<HD, NT>::STATE * 4 + (2 * static_cast<size_t>(B) + 1) * 4;
 }
 
+// What the rows' own parts need beyond it: a pair of words for the alignment, the rows' common pages, the plan.
+size_t shared_smem(int B, int N) { return 4 * (2 + 2 * static_cast<size_t>(B) + GroupPlan::INTS * static_cast<size_t>(N) + 2); }
+
 template <int HD, typename T16>
 cudaError_t prepare_hd() {
   const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
@@ -610,7 +613,7 @@ cudaError_t prepare_hd() {
   if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_paged_decode_kernel<HD, T16, 1, true>, attr, one);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_paged_decode_kernel<HD, T16, 2, false>, attr, two);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_paged_decode_kernel<HD, T16, 2, true>, attr, two);
-  constexpr int plan = 4 * (GroupPlan::INTS * SHARED_MAX_GROUPS + 2);
+  const int plan = static_cast<int>(shared_smem(PAGED_ATTN_MAX_B, SHARED_MAX_GROUPS));
   if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_paged_own_kernel<HD, T16, 1>, attr, one + plan);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_paged_own_kernel<HD, T16, 2>, attr, two + plan);
   return e;
@@ -618,7 +621,7 @@ cudaError_t prepare_hd() {
 
 template <int HD, typename T16, int NT, bool LO>
 cudaError_t launch_nt(const LaunchCtx& lc, const PagedAttnArgs& a, const SharedGroups* sg = nullptr) {
-  const size_t smem = smem_bytes<HD, NT>(a.B) + (sg ? 4 * (GroupPlan::INTS * static_cast<size_t>(sg->N) + 2) : 0);
+  const size_t smem = smem_bytes<HD, NT>(a.B) + (sg ? shared_smem(a.B, sg->N) : 0);
   // no more CTAs than pages that can be visible, at a page per warp
   const long long pages = paged_attn_most_pages(a.B, a.G, a.blocks_per_seq, a.window, a.sinks);
   const long long most = static_cast<long long>(lc.num_sms) * (NT == 1 ? 3 : 2);

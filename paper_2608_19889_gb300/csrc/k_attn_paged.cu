@@ -122,9 +122,9 @@ AXON_DEV void paged_decode(const PagedAttnArgs& p, const SharedGroups& sg) {
   __shared__ int s_scan[DW], s_last[DW];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, c = lane & 3;
   const int HPG = p.H / p.G;
-  grid_dep_launch();
-  // (SH: the prefix pass before this kernel lets it start once its inputs are there)
-  if (!SH || sg.alone) grid_dep_wait();
+  if (!SH || sg.alone) grid_dep_launch();
+  grid_dep_wait();
+  if (SH && !sg.alone) grid_dep_launch();  // the prefix pass, which waits for nothing of this kernel until its end
   // SH: [B] the pages that the row has in common with others, from the first and to the last; then the plan they come from
   int2* const shared = reinterpret_cast<int2*>(before + 2 * p.B + 2);
   if constexpr (SH) {
@@ -594,7 +594,6 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
 template <int HD, typename T16, int NT>
 __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_own_kernel(const PagedAttnArgs p, const SharedGroups sg) {
   paged_decode<HD, T16, NT, false, true>(p, sg);
-  grid_dep_wait();  // this kernel's end means the prefix pass's too, for the join
 }
 
 template <int HD, int NT>

@@ -217,8 +217,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     // Before `ready`, since the softmax warps wait for these registers; and once for all that these warps do, since what
     // follows a place where the branches meet may be given registers that only the softmax warps have.
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-    grid_dep_wait();
-    grid_dep_launch();  // the rows' own parts, which wait for nothing of this kernel
+    grid_dep_launch();
     plan_groups<128, 256>(p, sg, gp, blockIdx.x == 0);
     if (warp == 8) {
       unsigned sum = 0;
@@ -619,6 +618,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
+  grid_dep_wait();  // this kernel's end means the rows' own parts' too, for the join
 }
 
 constexpr int JT = 128;  // threads of the join
@@ -748,8 +748,8 @@ cudaError_t launch_join_hd(const LaunchCtx& lc, const PagedAttnArgs& a, const Sh
 template <int HD, typename T16>
 cudaError_t launch_hd(const LaunchCtx& lc, const PagedAttnArgs& a, const SharedGroups& s, const AttnMaps& maps) {
   if (s.alone) return launch_attn_paged_own(lc, a, s);
-  cudaError_t e = launch_prefix_hd<HD, T16>(lc, a, s, maps);
-  if (e == cudaSuccess) e = launch_attn_paged_own(lc, a, s);
+  cudaError_t e = launch_attn_paged_own(lc, a, s);
+  if (e == cudaSuccess) e = launch_prefix_hd<HD, T16>(lc, a, s, maps);
   return e == cudaSuccess ? launch_join_hd<HD, T16>(lc, a, s) : e;
 }
 

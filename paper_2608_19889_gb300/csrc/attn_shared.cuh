@@ -18,14 +18,80 @@ struct GroupPlan {
   int* said;  // [N] blocks that the caller says are shared
   int* from;  // [N + 1] rows
   int* spared;  // [1]
-  static constexpr int INTS = 6;  // per group, and two more
+  int* pages;   // [1] pages of the rows' own parts, of one kv head
+  int* cost;    // [1] of the prefix pass
+  int* rows;    // [1] rows that see something
+  int* own;     // [1] SMs for the rows' own parts
+  static constexpr int ints(int N) { return 6 * N + 6; }
   AXON_DEV GroupPlan(int* at, int N)
-      : c0(at), c1(at + N), lead(at + 2 * N), live(at + 3 * N), said(at + 4 * N), from(at + 5 * N), spared(at + 6 * N + 1) {}
+      : c0(at), c1(at + N), lead(at + 2 * N), live(at + 3 * N), said(at + 4 * N), from(at + 5 * N), spared(at + 6 * N + 1),
+        pages(spared + 1), cost(spared + 2), rows(spared + 3), own(spared + 4) {}
 };
+
+// Pages of a row: `sink` pages from the front, then those from page `first` on, without the `gap` pages from
+// `gap_at` on, which the row's group has in common.
+struct RowPages {
+  int pos, lo, sink, first, n, gap_at, gap;
+};
+AXON_DEV RowPages row_pages(const PagedAttnArgs& p, int pos, int2 common = make_int2(INT_MAX, INT_MAX)) {
+  RowPages r;
+  r.pos = pos;
+  r.gap_at = common.x;
+  r.gap = common.y - common.x;
+  if (pos < 0) {
+    r.lo = r.sink = r.first = r.n = r.gap = 0;
+    return r;
+  }
+  r.lo = (p.window > 0 && pos >= p.window) ? pos - p.window + 1 : 0;
+  r.first = r.lo >> 4;
+  r.sink = min((min(p.sinks, pos + 1) + 15) >> 4, r.first);
+  r.n = r.sink + (pos >> 4) + 1 - r.first - r.gap;
+  return r;
+}
+
+// What a step of the prefix pass costs, in 0.4 us: 2.05 us with two tiles (the tensor pipe's 1.6), 1.5 with one whose 64 KB come
+// from HBM, 1.25 with one whose keys the group's other items read too.
+constexpr unsigned COST_TWO = 5, COST_ONE = 4, COST_LAST = 3;
+
+// What the rows' own parts take on an SM, in 1/64 of it: a page (of 128 dims; twelve warps share the SM, and each has 1.5 us
+// for a page), and a row's kv head (8 us of a warp: table, first keys, the warps' and parts' states joined); and what they
+// take to begin, once the CTAs of the prefix pass that have nothing to do are gone.
+constexpr unsigned OWN_PAGE = 20, OWN_ROW = 200, OWN_BEGIN = 10;
+
+// A group of the prefix pass: its items are `pairs` per kv head, of two tiles of PW rows; the last one may have one tile.
+struct Span {
+  int rows, pages, pairs;
+  unsigned steps, last_cost;  // of an item; the cost of a step of the last pair, the others' is COST_TWO
+  unsigned per_head;          // cost of a kv head's items
+  AXON_DEV Span(int rows_, int pages_, int PW) : rows(rows_), pages(pages_) {
+    pairs = (rows + 2 * PW - 1) / (2 * PW);
+    steps = static_cast<unsigned>(pages + 7) >> 3;
+    last_cost = rows - (pairs - 1) * 2 * PW > PW ? COST_TWO : pairs > 1 ? COST_LAST : COST_ONE;
+    per_head = steps * ((pairs - 1) * COST_TWO + last_cost);
+  }
+  AXON_DEV unsigned cost(int pair) const { return pair == pairs - 1 ? last_cost : COST_TWO; }
+  AXON_DEV unsigned item(int g, int pair) const { return g * per_head + pair * steps * COST_TWO; }
+};
+
+// The two passes run beside each other, each on SMs of its own: how many of them the rows' own parts take, so that both end
+// together. Called by a warp. (57 rows of 1500 to 5500 tokens, 48 of them on 4001 in common: 74 us, 99 with one pass after the
+// other; 64 rows in groups of 4: 53 and 57.5; 64 rows on 32768 tokens: 85 and 91.)
+AXON_DEV int own_sms(unsigned pages, unsigned rows, unsigned cost, int d, int sms) {
+  if (cost == 0 || sms < 2) return sms;
+  const unsigned long long sum = (static_cast<unsigned long long>(pages) * OWN_PAGE * d / 128 + static_cast<unsigned long long>(rows) * OWN_ROW) >> 6;
+  const unsigned own = static_cast<unsigned>(min(sum, 1ull << 31));
+  unsigned best = 0xffffffffu;
+#pragma unroll 1
+  for (int S = 1 + (threadIdx.x & 31); S < sms; S += 32) {
+    const unsigned t = max(OWN_BEGIN + own / S, max(2 * COST_TWO, cost / (sms - S)));
+    best = min(best, min(t, 0x3fffffu) << 10 | (1023 - S));
+  }
+  return 1023 - static_cast<int>(__reduce_min_sync(0xffffffffu, best) & 1023);
+}
 
 // Position of row b's query; -1: the row sees nothing.
 AXON_DEV int live_pos(const PagedAttnArgs& p, int b) {
-  const int pos = p.ctx[b];
+  const int pos = __ldcg(p.ctx + b);
   return pos < p.blocks_per_seq * 16ll ? max(pos, -1) : -1;
 }
 // The group of row b; -1: none.
@@ -37,6 +103,7 @@ AXON_DEV int group_of(const GroupPlan& g, int N, int b) {
   }
   return lo >= 0 && b < g.from[lo + 1] ? lo : -1;
 }
+// (The prefix pass starts before the kernel in front of it has ended: what it reads comes from L2.)
 // Called by the THREADS threads of the CTA from thread FIRST on, which meet at barrier 2; `report`: sets the error bits.
 // Small calls wait for memory once.
 template <int THREADS, int FIRST>
@@ -45,8 +112,9 @@ AXON_DEV void plan_groups(const PagedAttnArgs& p, const SharedGroups& s, const G
   auto meet = [] { asm volatile("barrier.cta.sync 2, %0;" ::"n"(THREADS) : "memory"); };
   int pos = tid < p.B ? live_pos(p, tid) : -1;
   bool bad = false;
+#pragma unroll 1
   for (int i = tid; i < s.N; i += THREADS) {
-    const int r0 = s.offsets[i], r1 = s.offsets[i + 1], said = s.prefix[i];
+    const int r0 = __ldcg(s.offsets + i), r1 = __ldcg(s.offsets + i + 1), said = __ldcg(s.prefix + i);
     bad |= r0 < 0 || r1 < r0 || r1 > p.B;
     if (said < 0 && report) set_err(p.err, DEVERR_POS);
     g.said[i] = said > 0 ? said >> 4 : 0;
@@ -57,7 +125,7 @@ AXON_DEV void plan_groups(const PagedAttnArgs& p, const SharedGroups& s, const G
     g.lead[i] = INT_MAX;
     g.live[i] = 0;
   }
-  if (tid == 0) *g.spared = 0;
+  if (tid == 0) *g.spared = *g.pages = *g.cost = *g.rows = 0;
   int any = 0;
   asm volatile(
       "{\n .reg .pred a, b;\n setp.ne.s32 a, %1, 0;\n barrier.cta.red.or.pred b, 2, %2, a;\n selp.s32 %0, 1, 0, b;\n}"
@@ -68,13 +136,21 @@ AXON_DEV void plan_groups(const PagedAttnArgs& p, const SharedGroups& s, const G
     // inconsistent offsets: nobody shares anything
     if (report && tid == 0) set_err(p.err, DEVERR_SEQ);
     for (int i = tid; i < s.N; i += THREADS) g.c0[i] = g.c1[i] = 0;
+    if (tid == 0) *g.own = s.sms;
     meet();
     return;
   }
+#pragma unroll 1
   for (int b0 = 0; b0 < p.B; b0 += THREADS) {
     const int b = b0 + tid;
     if (b0) pos = b < p.B ? live_pos(p, b) : -1;
     const int n = pos >= 0 ? group_of(g, s.N, b) : -1;
+    const int pages = __reduce_add_sync(0xffffffffu, row_pages(p, pos).n);
+    const int rows = __popc(__ballot_sync(0xffffffffu, pos >= 0));
+    if ((tid & 31) == 0 && rows) {
+      atomicAdd(g.pages, pages);
+      atomicAdd(g.rows, rows);
+    }
     const int lo = p.window > 0 && pos >= p.window ? pos - p.window + 1 : 0;
     const unsigned in = __ballot_sync(0xffffffffu, n >= 0);
     if (!in) continue;
@@ -97,22 +173,31 @@ AXON_DEV void plan_groups(const PagedAttnArgs& p, const SharedGroups& s, const G
     }
   }
   meet();
+#pragma unroll 1
   for (int i = tid; i < s.N; i += THREADS) {
     int c0 = 0, c1 = 0;
     if (g.live[i] > 1 && g.said[i] > 0) {
       c0 = (g.c0[i] + 15) >> 4;
       c1 = min(g.said[i], (g.c1[i] + 1) >> 4);
       if (c1 - c0 < s.least) c0 = c1 = 0;
-      if (c1 > c0) atomicAdd(g.spared, static_cast<int>(min(static_cast<long long>(c1 - c0) * (g.live[i] - 1), 1ll << 20)));
+      if (c1 > c0) {
+        atomicAdd(g.spared, static_cast<int>(min(static_cast<long long>(c1 - c0) * (g.live[i] - 1), 1ll << 20)));
+        atomicSub(g.pages, (c1 - c0) * g.live[i]);
+        atomicAdd(g.cost, static_cast<int>(Span(g.from[i + 1] - g.from[i], c1 - c0, s.tile).per_head * p.G));
+      }
     }
     g.c0[i] = c0;
     g.c1[i] = c1;
   }
   meet();
-  if (*g.spared < s.least_spared) {
+  const bool few = *g.spared < s.least_spared;
+  if (few)
     for (int i = tid; i < s.N; i += THREADS) g.c0[i] = g.c1[i] = 0;
-    meet();
+  if (tid < 32) {
+    const int own = few ? s.sms : own_sms(static_cast<unsigned>(*g.pages) * p.G, *g.rows * p.G, *g.cost, p.d, s.sms);
+    if (tid == 0) *g.own = own;
   }
+  meet();
 }
 // What plan_groups reports, where nobody needs the plan.
 template <int THREADS>

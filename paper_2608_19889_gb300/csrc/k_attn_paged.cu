@@ -79,26 +79,6 @@ template <> AXON_DEV uint32_t pack_prob<f16>(float a, float b, float& ra, float&
   return *reinterpret_cast<uint32_t*>(&h);
 }
 
-// Pages of a row: `sink` pages from the front, then those from page `first` on, without the `gap` pages from
-// `gap_at` on, which the row's group has in common.
-struct RowPages {
-  int pos, lo, sink, first, n, gap_at, gap;
-};
-AXON_DEV RowPages row_pages(const PagedAttnArgs& p, int pos, int2 common = make_int2(INT_MAX, INT_MAX)) {
-  RowPages r;
-  r.pos = pos;
-  r.gap_at = common.x;
-  r.gap = common.y - common.x;
-  if (pos < 0) {
-    r.lo = r.sink = r.first = r.n = r.gap = 0;
-    return r;
-  }
-  r.lo = (p.window > 0 && pos >= p.window) ? pos - p.window + 1 : 0;
-  r.first = r.lo >> 4;
-  r.sink = min((min(p.sinks, pos + 1) + 15) >> 4, r.first);
-  r.n = r.sink + (pos >> 4) + 1 - r.first - r.gap;
-  return r;
-}
 // Position of row b's query; -1: the row sees nothing.
 AXON_DEV int row_pos(const PagedAttnArgs& p, int b) {
   const int pos = p.ctx[b];
@@ -107,92 +87,23 @@ AXON_DEV int row_pos(const PagedAttnArgs& p, int b) {
   return -1;
 }
 
+// The share of CTA `cta` of `ctas`.
 // LO: q has a second 16-bit term, and o one too where o_lo is given. SH: without the pages that a row's group has in
 // common; a row that has some leaves its state for the join.
 template <int HD, typename T16, int NT, bool LO, bool SH>
-AXON_DEV void paged_decode(const PagedAttnArgs& p, const SharedGroups& sg) {
+AXON_DEV void paged_items(const PagedAttnArgs& p, const SharedGroups& sg, float* const state, const unsigned* const before,
+                          const int* const rpos, const int2* const shared, int* const s_last, unsigned ctas, unsigned cta) {
   using C = DCfg<HD, NT>;
   constexpr int KI = HD / 32;  // 16-byte pieces per key row and lane
   constexpr int VI = HD / 64;  // 16-byte pieces per value row and lane
   constexpr int MT = HD / 16;  // 16-dim tiles of O^T
-  extern __shared__ __align__(16) float sm[];
-  float* const state = sm;                                        // [DW][STATE]
-  unsigned* const before = reinterpret_cast<unsigned*>(sm + DW * C::STATE);  // [B + 1] pages of the rows before
-  int* const rpos = reinterpret_cast<int*>(before + p.B + 1);                // [B] the rows' positions
-  __shared__ int s_scan[DW], s_last[DW];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, c = lane & 3;
   const int HPG = p.H / p.G;
-  if (!SH || sg.alone) grid_dep_launch();
-  grid_dep_wait();
-  if (SH && !sg.alone) grid_dep_launch();  // the prefix pass, which waits for nothing of this kernel until its end
-  // SH: [B] the pages that the row has in common with others, from the first and to the last; then the plan they come from
-  int2* const shared = reinterpret_cast<int2*>(before + 2 * p.B + 2);
-  if constexpr (SH) {
-    const GroupPlan gp(reinterpret_cast<int*>(shared + p.B), sg.N);
-    if (sg.alone) {
-      if (blockIdx.x == 0) check_groups<DW * 32>(p, sg);
-    } else {
-      plan_groups<DW * 32, 0>(p, sg, gp, false);
-    }
-    for (int b = tid; b < p.B; b += DW * 32) {
-      const int n = sg.alone ? -1 : group_of(gp, sg.N, b);
-      shared[b] = n >= 0 && gp.c1[n] > gp.c0[n] ? make_int2(gp.c0[n], gp.c1[n]) : make_int2(INT_MAX, INT_MAX);
-    }
-    __syncthreads();
-  }
   auto common = [&](int b) { return SH ? shared[b] : make_int2(INT_MAX, INT_MAX); };
-
-  // ---- pages before each row
-  if (p.B <= 32) {
-    if (warp == 0) {
-      const int pos = lane < p.B ? row_pos(p, lane) : -1;
-      const int n = row_pages(p, pos, SH && pos >= 0 ? common(lane) : make_int2(INT_MAX, INT_MAX)).n;
-      int inc = n;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int t = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += t;
-      }
-      if (lane < p.B) {
-        before[lane] = inc - n;
-        rpos[lane] = pos;
-      }
-      if (lane == 31) before[p.B] = inc;
-    }
-  } else {
-    int base = 0;
-    for (int b0 = 0; b0 < p.B; b0 += DW * 32) {
-      const int b = b0 + tid;
-      const int pos = b < p.B ? row_pos(p, b) : -1;
-      const int n = row_pages(p, pos, SH && pos >= 0 ? common(b) : make_int2(INT_MAX, INT_MAX)).n;
-      int inc = n;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int t = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += t;
-      }
-      if (lane == 31) s_scan[warp] = inc;
-      __syncthreads();
-      int add = 0, all = 0;
-#pragma unroll
-      for (int w = 0; w < DW; ++w) {
-        add += w < warp ? s_scan[w] : 0;
-        all += s_scan[w];
-      }
-      if (b < p.B) {
-        before[b] = base + add + inc - n;
-        rpos[b] = pos;
-      }
-      base += all;
-      __syncthreads();
-    }
-    if (tid == 0) before[p.B] = base;
-  }
-  __syncthreads();
   const unsigned total = before[p.B] * p.G;  // below 2^31: the launcher saw to it
 
   // ---- rows that see nothing
-  for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
+  for (int b = cta; b < p.B; b += ctas) {
     if (before[b + 1] != before[b]) continue;
     if (SH && row_pages(p, rpos[b], common(b)).gap > 0) {
       // everything that the row sees is in common
@@ -215,13 +126,20 @@ AXON_DEV void paged_decode(const PagedAttnArgs& p, const SharedGroups& sg) {
 
   // ---- workers: more warps share an item the longer the items are
   const unsigned avg = total / (p.B * p.G);
-  const int gs = avg >= 16 ? 4 : avg >= 4 ? 2 : 1;
+  int gs = avg >= 16 ? 4 : avg >= 4 ? 2 : 1;
+  // more items than warps: each takes whole ones, and has nobody to join with
+  if (SH && !sg.alone) {
+    if (p.B * p.G >= ctas * DW)
+      gs = 1;
+    else if (p.B * p.G >= ctas * (DW / 2))
+      gs = min(gs, 2);
+  }
   const int group = warp / gs, wg = warp - group * gs;
-  const unsigned all_groups = gridDim.x * (DW / gs);
+  const unsigned all_groups = ctas * (DW / gs);
   // two pages per warp at least: less work per worker costs more joins than it saves (16 rows of
   // 256 keys, 8B width: 12.8 us with one page, 10.3 with two)
   const unsigned nw = min(all_groups, max(1u, total / (2 * gs)));
-  const unsigned wid = blockIdx.x + gridDim.x * group;
+  const unsigned wid = cta + ctas * group;
   if (wid >= nw) return;
   // the first `extra` workers take a page more than the others
   const unsigned share = total / nw, extra = total - share * nw;
@@ -587,6 +505,110 @@ AXON_DEV void paged_decode(const PagedAttnArgs& p, const SharedGroups& sg) {
   }
 }
 
+template <int HD, typename T16, int NT, bool LO, bool SH>
+AXON_DEV void paged_decode(const PagedAttnArgs& p, const SharedGroups& sg) {
+  using C = DCfg<HD, NT>;
+  extern __shared__ __align__(16) float sm[];
+  float* const state = sm;                                        // [DW][STATE]
+  unsigned* const before = reinterpret_cast<unsigned*>(sm + DW * C::STATE);  // [B + 1] pages of the rows before
+  int* const rpos = reinterpret_cast<int*>(before + p.B + 1);                // [B] the rows' positions
+  __shared__ int s_scan[DW], s_last[DW], s_cta;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  grid_dep_launch();
+  // (SH: the prefix pass before this kernel lets it start once its inputs are there)
+  if (!SH || sg.alone) grid_dep_wait();
+  // CTAs that the work is cut for, and this one's number among them. SH: whoever comes takes the next number, until none is
+  // left, so that all is done wherever and whenever the CTAs run.
+  unsigned ctas = gridDim.x, cta = blockIdx.x;
+  // SH: [B] the pages that the row has in common with others, from the first and to the last; then the plan they come from
+  int2* const shared = reinterpret_cast<int2*>(before + 2 * p.B + 2);
+  if constexpr (SH) {
+    const GroupPlan gp(reinterpret_cast<int*>(shared + p.B), sg.N);
+    if (sg.alone) {
+      if (blockIdx.x == 0) check_groups<DW * 32>(p, sg);
+    } else {
+      // those that come when the prefix pass ends find that nothing is left
+      volatile int* const next = sg.next;
+      if (tid == 0) s_cta = next[1] > 0 && next[0] >= next[1];
+      __syncthreads();
+      if (s_cta) return;
+      plan_groups<DW * 32, 0>(p, sg, gp, false);
+      ctas = min(gridDim.x, (NT == 1 ? 3 : 2) * *gp.own);
+      if (tid == 0) {
+        next[1] = static_cast<int>(ctas);
+        s_cta = atomicAdd(sg.next, 1);
+      }
+      __syncthreads();
+      cta = s_cta;
+      if (cta >= ctas) return;
+    }
+    for (int b = tid; b < p.B; b += DW * 32) {
+      const int n = sg.alone ? -1 : group_of(gp, sg.N, b);
+      shared[b] = n >= 0 && gp.c1[n] > gp.c0[n] ? make_int2(gp.c0[n], gp.c1[n]) : make_int2(INT_MAX, INT_MAX);
+    }
+    __syncthreads();
+  }
+  auto common = [&](int b) { return SH ? shared[b] : make_int2(INT_MAX, INT_MAX); };
+
+  // ---- pages before each row
+  if (p.B <= 32) {
+    if (warp == 0) {
+      const int pos = lane < p.B ? row_pos(p, lane) : -1;
+      const int n = row_pages(p, pos, SH && pos >= 0 ? common(lane) : make_int2(INT_MAX, INT_MAX)).n;
+      int inc = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int t = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += t;
+      }
+      if (lane < p.B) {
+        before[lane] = inc - n;
+        rpos[lane] = pos;
+      }
+      if (lane == 31) before[p.B] = inc;
+    }
+  } else {
+    int base = 0;
+    for (int b0 = 0; b0 < p.B; b0 += DW * 32) {
+      const int b = b0 + tid;
+      const int pos = b < p.B ? row_pos(p, b) : -1;
+      const int n = row_pages(p, pos, SH && pos >= 0 ? common(b) : make_int2(INT_MAX, INT_MAX)).n;
+      int inc = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int t = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += t;
+      }
+      if (lane == 31) s_scan[warp] = inc;
+      __syncthreads();
+      int add = 0, all = 0;
+#pragma unroll
+      for (int w = 0; w < DW; ++w) {
+        add += w < warp ? s_scan[w] : 0;
+        all += s_scan[w];
+      }
+      if (b < p.B) {
+        before[b] = base + add + inc - n;
+        rpos[b] = pos;
+      }
+      base += all;
+      __syncthreads();
+    }
+    if (tid == 0) before[p.B] = base;
+  }
+  __syncthreads();
+
+  for (;;) {
+    paged_items<HD, T16, NT, LO, SH>(p, sg, state, before, rpos, shared, s_last, ctas, cta);
+    if (!SH || sg.alone) return;
+    __syncthreads();
+    if (tid == 0) s_cta = atomicAdd(sg.next, 1);
+    __syncthreads();
+    cta = s_cta;
+    if (cta >= ctas) return;
+  }
+}
+
 template <int HD, typename T16, int NT, bool LO>
 __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_kernel(const PagedAttnArgs p) {
   paged_decode<HD, T16, NT, LO, false>(p, SharedGroups{});
@@ -594,6 +616,7 @@ __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_decode_ke
 template <int HD, typename T16, int NT>
 __global__ void __launch_bounds__(DW * 32, NT == 1 ? 3 : 2) attn_paged_own_kernel(const PagedAttnArgs p, const SharedGroups sg) {
   paged_decode<HD, T16, NT, false, true>(p, sg);
+  grid_dep_wait();  // this kernel's end means the prefix pass's too, for the join
 }
 
 template <int HD, int NT>
@@ -602,7 +625,7 @@ constexpr size_t smem_bytes(int B) {
 }
 
 // What the rows' own parts need beyond it: a pair of words for the alignment, the rows' common pages, the plan.
-size_t shared_smem(int B, int N) { return 4 * (2 + 2 * static_cast<size_t>(B) + GroupPlan::INTS * static_cast<size_t>(N) + 2); }
+size_t shared_smem(int B, int N) { return 4 * (2 + 2 * static_cast<size_t>(B) + GroupPlan::ints(N)); }
 
 template <int HD, typename T16>
 cudaError_t prepare_hd() {
@@ -659,7 +682,8 @@ size_t paged_attn_part_bytes(int H, int G, int d, int num_sms) {
 // A ticket per cut item, which goes by its first worker (no other cut item begins there), and one per
 // worker's slot. They stand in front of the states and their number goes by the SMs alone,
 // so that no call's states lie where another shape or batch has its tickets.
-size_t paged_attn_ticket_bytes(int num_sms) { return 4 * 3 * static_cast<size_t>(num_sms) * 3 * DW; }
+// One more stands behind them, which counts CTAs where rows share prefixes.
+size_t paged_attn_ticket_bytes(int num_sms) { return 4 * 3 * static_cast<size_t>(num_sms) * 3 * DW + 16; }
 
 cudaError_t prepare_attn_paged_kernels() {
   cudaError_t e = prepare_hd<64, bf16>();

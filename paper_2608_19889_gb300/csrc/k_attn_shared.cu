@@ -42,12 +42,9 @@ struct SCfg {
   static constexpr int TILE = CH * CHUNK;           // Q, K or V tile
   static constexpr int STAGES = HD == 128 ? 4 : 8;  // K and V tiles in flight
   static constexpr int BARS = 2 * STAGES + 18;
-  static constexpr int PLAN = 4 * ((GroupPlan::INTS + 1) * MAX_N + 4);
+  static constexpr int PLAN = 4 * (GroupPlan::ints(MAX_N) + MAX_N + 1);
   static constexpr int SMEM = 2 * TILE + STAGES * TILE + 8 * BARS + 16 + PLAN + 1024;
 };
-
-// What a step costs on the line: 3500 cycles with two tiles (the tensor pipe's 3072), 2800 with one (64 KB from HBM).
-constexpr unsigned COST_TWO = 5, COST_ONE = 4;
 
 // How the line is dealt: `workers` CTAs, the first `extra` of them one more than `share`; a CTA takes the steps that begin
 // in its range, which holds one at least.
@@ -67,21 +64,6 @@ AXON_DEV Deal deal(unsigned total, unsigned ctas, unsigned least_steps) {
   d.extra = total - d.share * d.workers;
   return d;
 }
-
-// A group on the line.
-struct Span {
-  int rows, pages, pairs;
-  unsigned steps, last_cost;  // of an item; the cost of a step of the last pair, the others' is COST_TWO
-  unsigned per_head;          // cost of a kv head's items
-  AXON_DEV Span(int rows_, int pages_, int PW) : rows(rows_), pages(pages_) {
-    pairs = (rows + 2 * PW - 1) / (2 * PW);
-    steps = static_cast<unsigned>(pages + 7) >> 3;
-    last_cost = rows - (pairs - 1) * 2 * PW > PW ? COST_TWO : COST_ONE;
-    per_head = steps * ((pairs - 1) * COST_TWO + last_cost);
-  }
-  AXON_DEV unsigned cost(int pair) const { return pair == pairs - 1 ? last_cost : COST_TWO; }
-  AXON_DEV unsigned item(int g, int pair) const { return g * per_head + pair * steps * COST_TWO; }
-};
 
 // A CTA's share of an item.
 struct Part {
@@ -130,7 +112,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   const uint32_t tmem_slot = bars + 8 * C::BARS;
   int* const plan = reinterpret_cast<int*>(smem_raw + (tmem_slot + 16 - raw));
   const GroupPlan gp(plan, sg.N);
-  unsigned* const before = reinterpret_cast<unsigned*>(plan + GroupPlan::INTS * sg.N + 2);  // [N + 1] cost of the groups before
+  unsigned* const before = reinterpret_cast<unsigned*>(plan + GroupPlan::ints(sg.N));  // [N + 1] cost of the groups before
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int HPG = p.H / p.G, PC = 2 * PW;
 
@@ -166,10 +148,13 @@ __global__ void __launch_bounds__(THREADS, 1)
   const uint32_t tmem = *reinterpret_cast<const uint32_t*>(smem_raw + (tmem_slot - raw));
   // what the parts' owners need to know is there once `ready` lets them pass
   auto ready = [&]() { asm volatile("barrier.cta.sync 1, 384;" ::: "memory"); };
+  auto make_ready = [&]() { asm volatile("barrier.cta.sync 2, 128;\n\tbarrier.cta.arrive 1, 384;" ::: "memory"); };
   Deal d{};
   unsigned u0 = 0, u1 = 0;
+  // CTAs that the line is dealt to; the others leave their SMs to the rows' own parts
+  auto ctas = [&]() { return static_cast<unsigned>(min(static_cast<int>(gridDim.x), max(1, sg.sms - *gp.own))); };
   auto take_share = [&]() {
-    d = deal(before[sg.N], gridDim.x, sg.least_steps);
+    d = deal(before[sg.N], ctas(), sg.least_steps);
     u1 = blockIdx.x < d.workers && d.total ? d.begin(blockIdx.x + 1) : 0;
     u0 = u1 ? d.begin(blockIdx.x) : 0;
   };
@@ -216,8 +201,9 @@ __global__ void __launch_bounds__(THREADS, 1)
   if (warp >= 8) {
     // Before `ready`, since the softmax warps wait for these registers; and once for all that these warps do, since what
     // follows a place where the branches meet may be given registers that only the softmax warps have.
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-    grid_dep_launch();
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+    grid_dep_wait();
+    grid_dep_launch();  // the rows' own parts, which wait for nothing of this kernel until their end
     plan_groups<128, 256>(p, sg, gp, blockIdx.x == 0);
     if (warp == 8) {
       unsigned sum = 0;
@@ -236,7 +222,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
       if (lane == 0) before[sg.N] = sum;
     }
-    ready();
+    make_ready();
     take_share();
     if (!(warp & 1)) {
       // ---------------------------------------------------------- producers
@@ -252,7 +238,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         auto pool_row = [&](int s) {
           const int i = s * 8 + lane;
           if (lane >= 8 || i >= t.pages) return pool_rows;
-          const int blk = p.block_table[static_cast<long long>(t.lead) * p.blocks_per_seq + t.page0 + i];
+          const int blk = __ldcg(p.block_table + static_cast<long long>(t.lead) * p.blocks_per_seq + t.page0 + i);
           if (blk < 0 || blk >= p.num_blocks) {
             set_err(p.err, DEVERR_BLOCK);
             return pool_rows;
@@ -285,7 +271,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
       if (kv && blockIdx.x == 0) {
         // what the join has to know of the rows
-        if (lane == 0) sg.plan[0] = make_int4(static_cast<int>(d.total), static_cast<int>(gridDim.x), sg.least_steps, 0);
+        if (lane == 0) sg.plan[0] = make_int4(static_cast<int>(d.total), static_cast<int>(ctas()), sg.least_steps, 0);
         for (int b = lane; b < p.B; b += 32) {
           const int n = live_pos(p, b) >= 0 ? group_of(gp, sg.N, b) : -1;
           sg.plan[1 + b] = n >= 0 && gp.c1[n] > gp.c0[n]
@@ -472,7 +458,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     __syncwarp();
   } else {
     // --------------------------------------------------------------- softmax
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
     const int w = warp >> 2;
     const int i = threadIdx.x & 127;  // row of the tile
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
@@ -618,7 +604,6 @@ __global__ void __launch_bounds__(THREADS, 1)
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
-  grid_dep_wait();  // this kernel's end means the rows' own parts' too, for the join
 }
 
 constexpr int JT = 128;  // threads of the join
@@ -634,6 +619,7 @@ __global__ void __launch_bounds__(JT) attn_join_kernel(const PagedAttnArgs p, co
   const int b = blockIdx.x, h = blockIdx.y, tid = threadIdx.x;
   grid_dep_wait();
   const int4 gp = __ldcg(sg.plan + 1 + b), all = __ldcg(sg.plan);
+  if (!(b | h | tid)) sg.next[0] = sg.next[1] = 0;
   if (!gp.x) return;
   const Deal d = deal(static_cast<unsigned>(all.x), static_cast<unsigned>(all.y), static_cast<unsigned>(all.z));
   const Span sp(gp.w, gp.x, PW);
@@ -748,9 +734,13 @@ cudaError_t launch_join_hd(const LaunchCtx& lc, const PagedAttnArgs& a, const Sh
 template <int HD, typename T16>
 cudaError_t launch_hd(const LaunchCtx& lc, const PagedAttnArgs& a, const SharedGroups& s, const AttnMaps& maps) {
   if (s.alone) return launch_attn_paged_own(lc, a, s);
-  cudaError_t e = launch_attn_paged_own(lc, a, s);
-  if (e == cudaSuccess) e = launch_prefix_hd<HD, T16>(lc, a, s, maps);
-  return e == cudaSuccess ? launch_join_hd<HD, T16>(lc, a, s) : e;
+  // The prefix pass leaves its SMs with all their memory as shared memory, where 28 KB of L1 hold the loads in flight: a pass of
+  // the rows' own parts took 1.6 times as long on them (104 and 170 us). So these two ask for what they need, three CTAs'.
+  LaunchCtx small = lc;
+  small.carveout = 45;
+  cudaError_t e = launch_prefix_hd<HD, T16>(lc, a, s, maps);
+  if (e == cudaSuccess) e = launch_attn_paged_own(small, a, s);
+  return e == cudaSuccess ? launch_join_hd<HD, T16>(small, a, s) : e;
 }
 
 constexpr size_t ALIGN = 256;
@@ -786,10 +776,10 @@ void shared_attn_carve(SharedGroups* s, void* work, int B, int H, int d, int num
 
 // Blocks read again come from L2, at some 10 TB/s, and the prefix pass and the join take some 13 us: less than 128 MB of
 // them is faster read again. GPU time of rows with 16 to 64 tokens of their own, 32 / 8 heads of 128, shared / each for
-// itself: 4 rows on 4096 tokens (50 MB spared) 19 / 17 us, 8 groups of 4 on 1024 (100 MB) 36 / 25, 16 rows on 4096 (251 MB)
-// 23 / 35, 8 groups of 4 on 4096 (403 MB) 54 / 83. AXON_SHARED_MIN_BYTES sets another limit, for measurements and for
+// itself: 4 rows on 4096 tokens (50 MB spared) 21 / 18 us, 8 groups of 4 on 1024 (100 MB) 31 / 25, 16 rows on 4096 (251 MB)
+// 26 / 35, 8 groups of 4 on 4096 (403 MB) 41 / 83. AXON_SHARED_MIN_BYTES sets another limit, for measurements and for
 // tests of small cases.
-void shared_attn_rules(SharedGroups* s, const PagedAttnArgs& a) {
+void shared_attn_rules(SharedGroups* s, const PagedAttnArgs& a, int num_sms) {
   const long long block = 64ll * a.d * a.G;  // bytes of a block's keys and values
   const long long row = paged_attn_most_pages(1, 1, a.blocks_per_seq, a.window, a.sinks);
   s->least = 8;
@@ -798,6 +788,9 @@ void shared_attn_rules(SharedGroups* s, const PagedAttnArgs& a) {
   s->least_spared = static_cast<int>(std::min((bytes + block - 1) / block, 1ll << 20));
   s->least_steps = 2;
   s->alone = row * (a.B - 1) < s->least_spared;
+  s->sms = num_sms;
+  s->tile = attn_tile_positions(a.H, a.G);
+  s->next = a.ticket + paged_attn_ticket_bytes(num_sms) / 4 - 4;
 }
 
 cudaError_t launch_attn_shared(const LaunchCtx& lc, const PagedAttnArgs& a, const SharedGroups& s, const AttnMaps& maps) {

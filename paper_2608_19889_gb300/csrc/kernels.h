@@ -253,6 +253,8 @@ struct SharedGroups {
   int least_spared;  // reads of a block (of one kv head) below which nobody does; at most 2^20
   int least_steps;   // of 8 blocks, for a CTA of the prefix pass
   bool alone;        // no row can share anything worth it: the rows' own parts are all there is
+  int sms, tile;     // SMs; rows of a tile of the prefix pass
+  int* next;         // [2] numbers the CTAs of the rows' own parts; how many there are; zero between calls
   int4* plan;          // [1 + PAGED_ATTN_MAX_B], written by the prefix pass for the join
   float2* state_stats; // [B][H] maximum and sum of the rows' own parts
   float* state;        // [B][H][d] their outputs, not divided
@@ -262,9 +264,9 @@ struct SharedGroups {
 size_t shared_attn_bytes(int B, int H, int d, int num_sms);
 void shared_attn_carve(SharedGroups* s, void* work, int B, int H, int d, int num_sms);
 // When sharing is worth it.
-void shared_attn_rules(SharedGroups* s, const PagedAttnArgs& a);
+void shared_attn_rules(SharedGroups* s, const PagedAttnArgs& a, int num_sms);
 cudaError_t prepare_attn_shared_kernels();
-// Three launches: prefix pass, the rows' own parts, the join; or one (alone).
+// Three launches: prefix pass, the rows' own parts beside it, the join; or one (alone).
 cudaError_t launch_attn_shared(const LaunchCtx& lc, const PagedAttnArgs& a, const SharedGroups& s, const AttnMaps& maps);
 cudaError_t launch_attn_paged_own(const LaunchCtx& lc, const PagedAttnArgs& a, const SharedGroups& s);
 

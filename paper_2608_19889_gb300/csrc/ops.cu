@@ -261,7 +261,7 @@ int axon_attn_shared(const axon_kv_cache* cache, int32_t layer, const void* d_q,
   s.offsets = d_group_offsets;
   s.prefix = d_prefix_lens;
   s.N = num_groups;
-  shared_attn_rules(&s, a);
+  shared_attn_rules(&s, a, lc.num_sms);
   shared_attn_carve(&s, static_cast<char*>(d_workspace) + own, B, num_heads, a.d, lc.num_sms);
   return status(with_limits([&] { return launch_attn_shared(lc, a, s, maps); }));
 }

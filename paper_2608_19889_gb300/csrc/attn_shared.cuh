@@ -54,7 +54,7 @@ AXON_DEV RowPages row_pages(const PagedAttnArgs& p, int pos, int2 common = make_
 constexpr unsigned COST_TWO = 5, COST_ONE = 4, COST_LAST = 3;
 
 // What the rows' own parts take on an SM, in 1/64 of it: a page (of 128 dims; twelve warps share the SM, and each has 1.5 us
-// for a page), and a row's kv head (8 us of a warp: table, first keys, the warps' and parts' states joined); and what they
+// for a page), and a row's kv head (15 us of a warp: table, first keys, the warps' and parts' states joined); and what they
 // take to begin, once the CTAs of the prefix pass that have nothing to do are gone.
 constexpr unsigned OWN_PAGE = 20, OWN_ROW = 200, OWN_BEGIN = 10;
 
@@ -89,7 +89,8 @@ AXON_DEV int own_sms(unsigned pages, unsigned rows, unsigned cost, int d, int sm
   return 1023 - static_cast<int>(__reduce_min_sync(0xffffffffu, best) & 1023);
 }
 
-// Position of row b's query; -1: the row sees nothing.
+// Position of row b's query; -1: the row sees nothing. (From L2, like all that the plan comes from: the rows' own parts start
+// before the kernel in front of them has ended, and an SM's L1 may hold what was there before.)
 AXON_DEV int live_pos(const PagedAttnArgs& p, int b) {
   const int pos = __ldcg(p.ctx + b);
   return pos < p.blocks_per_seq * 16ll ? max(pos, -1) : -1;
@@ -103,7 +104,6 @@ AXON_DEV int group_of(const GroupPlan& g, int N, int b) {
   }
   return lo >= 0 && b < g.from[lo + 1] ? lo : -1;
 }
-// (The prefix pass starts before the kernel in front of it has ended: what it reads comes from L2.)
 // Called by the THREADS threads of the CTA from thread FIRST on, which meet at barrier 2; `report`: sets the error bits.
 // Small calls wait for memory once.
 template <int THREADS, int FIRST>

@@ -79,9 +79,11 @@ template <> AXON_DEV uint32_t pack_prob<f16>(float a, float b, float& ra, float&
   return *reinterpret_cast<uint32_t*>(&h);
 }
 
+// What a kernel may read that starts before the one in front of it has ended, from L2: an SM's L1 may hold what was there before.
+template <bool SH, typename T> AXON_DEV T read(const T* at) { return SH ? __ldcg(at) : *at; }
 // Position of row b's query; -1: the row sees nothing.
-AXON_DEV int row_pos(const PagedAttnArgs& p, int b) {
-  const int pos = p.ctx[b];
+template <bool SH> AXON_DEV int row_pos(const PagedAttnArgs& p, int b) {
+  const int pos = read<SH>(p.ctx + b);
   if (pos < p.blocks_per_seq * 16ll) return max(pos, -1);
   set_err(p.err, DEVERR_POS);
   return -1;
@@ -183,7 +185,7 @@ AXON_DEV void paged_items(const PagedAttnArgs& p, const SharedGroups& sg, float*
       const int k = k0 + lane;
       if (k >= pages) return -1;
       const int j = logical(k);
-      const int blk = p.block_table ? p.block_table[static_cast<long long>(b) * p.blocks_per_seq + j]
+      const int blk = p.block_table ? read<SH>(p.block_table + static_cast<long long>(b) * p.blocks_per_seq + j)
                                     : b * p.blocks_per_seq + j;
       if (blk >= 0 && blk < p.num_blocks) return blk;
       set_err(p.err, DEVERR_BLOCK);
@@ -201,7 +203,7 @@ AXON_DEV void paged_items(const PagedAttnArgs& p, const SharedGroups& sg, float*
         uint4 v = make_uint4(0, 0, 0, 0), w = v;
         if (n * 8 + r < HPG) {
           const long long at = b * p.q_row + (g * HPG + n * 8 + r) * p.q_head + (4 * i + c) * 8;
-          v = ld16(static_cast<const T16*>(p.q) + at);
+          v = read<SH>(reinterpret_cast<const uint4*>(static_cast<const T16*>(p.q) + at));
           if (LO) w = ld16(static_cast<const T16*>(p.q_lo) + at);
         }
         q[n][i][0] = v.x; q[n][i][1] = v.y; q[n][i][2] = v.z; q[n][i][3] = v.w;
@@ -553,7 +555,7 @@ AXON_DEV void paged_decode(const PagedAttnArgs& p, const SharedGroups& sg) {
   // ---- pages before each row
   if (p.B <= 32) {
     if (warp == 0) {
-      const int pos = lane < p.B ? row_pos(p, lane) : -1;
+      const int pos = lane < p.B ? row_pos<SH>(p, lane) : -1;
       const int n = row_pages(p, pos, SH && pos >= 0 ? common(lane) : make_int2(INT_MAX, INT_MAX)).n;
       int inc = n;
 #pragma unroll
@@ -571,7 +573,7 @@ AXON_DEV void paged_decode(const PagedAttnArgs& p, const SharedGroups& sg) {
     int base = 0;
     for (int b0 = 0; b0 < p.B; b0 += DW * 32) {
       const int b = b0 + tid;
-      const int pos = b < p.B ? row_pos(p, b) : -1;
+      const int pos = b < p.B ? row_pos<SH>(p, b) : -1;
       const int n = row_pages(p, pos, SH && pos >= 0 ? common(b) : make_int2(INT_MAX, INT_MAX)).n;
       int inc = n;
 #pragma unroll

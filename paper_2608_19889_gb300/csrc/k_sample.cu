@@ -206,6 +206,8 @@ struct Row {
   float share = 1.f;       // top-p, below 1: asked for
   u64 least = 0;     // min-p: the smallest weight that may stay
   u64 target = 0;    // what the last crossing's running sum had to reach
+  u64 own = 0;       // known: this CTA's weights that are kept (first those up to the crossing bin)
+  bool known = false;
   // what is kept: logits above vcut, and equal ones up to number icut
   float vcut = -INFINITY;
   int icut = 0x7fffffff;
@@ -307,6 +309,7 @@ struct Row {
     const int which = pass & 1, t = threadIdx.x;
     ++pass;
     u64 a[2] = {0, 0};
+    const uint2 ol = reinterpret_cast<const uint2*>(&sh.hist[which][0][0])[t], oh = reinterpret_cast<const uint2*>(&sh.hist[which][1][0])[t];
     for (int r0 = 0; r0 < CL; r0 += 4) {
       uint2 lo[4], hi[4];
 #pragma unroll
@@ -338,7 +341,7 @@ struct Row {
           n += static_cast<unsigned>(fminf(static_cast<float>(a[i]) * exp2f((2 * t + i) * (static_cast<float>(1 << BIN_SHIFT) / STEPS) - 44.f), 1e6f));
       n = __reduce_add_sync(0xffffffffu, n);
       if ((t & 31) == 0 && n) atomicAdd(&sh.estimate, n);
-      __syncthreads();
+      own = cta_sum((2 * t < b ? (static_cast<u64>(oh.x) << 32) + ol.x : 0) + (2 * t + 1 < b ? (static_cast<u64>(oh.y) << 32) + ol.y : 0));
     }
     return any;
   }
@@ -417,14 +420,23 @@ struct Row {
   template <bool TIES, typename T>
   AXON_DEV int locate(float v, T t, u64& its, u64& all) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const u64 mine = amount<TIES>(warp * seg, min(end, warp * seg + seg), v);
-    if (lane == 0) sh.warp[warp] = mine;
-    __syncthreads();
-    u64 x = lane < SW ? sh.warp[lane] : 0, before;
-    const u64 here = warp_sum64(x);
+    u64 x = 0, here = own, before;  // x: the warps' amounts
+    auto count = [&]() {
+      const u64 mine = amount<TIES>(warp * seg, min(end, warp * seg + seg), v);
+      __syncthreads();
+      if (lane == 0) sh.warp[warp] = mine;
+      __syncthreads();
+      x = lane < SW ? sh.warp[lane] : 0;
+    };
+    const bool later = !TIES && known;  // most CTAs never have to
+    if (!later) {
+      count();
+      here = warp_sum64(x);
+    }
     exchange(here, before, all);
     const u64 target = t(all);
     if (target < before || target - before >= here) return -1;  // another CTA's
+    if (later) count();
     u64 rest = target - before;
     u64 inc = warp_scan64(x);
     int at = __ffs(__ballot_sync(0xffffffffu, inc > rest)) - 1;  // the warp's part that it falls into
@@ -579,6 +591,16 @@ struct Row {
     __syncthreads();
     return sh.found[0];
   }
+  // own: with those of this CTA's list (the crossing bin's) that are kept
+  AXON_DEV void add_listed() {
+    u64 sum = 0;
+    for (int i = threadIdx.x; i < static_cast<int>(sh.mine_n); i += ST) {
+      const float l = of_key(sh.mine[i].x);
+      if (kept(l, static_cast<int>(sh.mine[i].y) - first)) sum += weight(c, l, sh.powers);
+    }
+    own += cta_sum(sum);
+    known = true;
+  }
   // v summed over the CTA
   AXON_DEV u64 cta_sum(u64 v) {
     const int lane = threadIdx.x & 31;
@@ -615,7 +637,10 @@ struct Row {
       }
       cg::this_cluster().sync();  // the counts are read before the next list begins
     }
-    if ((!MASS && amount <= SOME) || (MASS && static_cast<float>(amount) * exp2f(b * (static_cast<float>(1 << BIN_SHIFT) / STEPS) - 44.f) <= SOME) || b == NB - 1) {
+    // The logits of the bin in lists, where they have room.
+    const float about = MASS ? static_cast<float>(amount) * exp2f(b * (static_cast<float>(1 << BIN_SHIFT) / STEPS) - 44.f) : static_cast<float>(amount);
+    bool listed = false;
+    if (about <= CL * (LIST * 3 / 4) || b == NB - 1) {
       const int nc = gather(b, b, SOME);
       if (nc <= SOME) {
         u64 before, all;
@@ -623,8 +648,10 @@ struct Row {
         exchange(at, before, all);
         const float v = of_key(static_cast<unsigned>(all >> 32));
         cut_at(v, min(static_cast<int>(all & 0x7fffffffu), v == vcut ? icut : 0x7fffffff));
+        if (MASS) add_listed();
         return false;
       }
+      listed = nc < 0x7fffffff;
     }
     // keys of the bin (the next pass's histogram was cleared with the crossing; the others may still read the last one)
     if (tid < 32) {
@@ -639,10 +666,16 @@ struct Row {
     while (lo < hi && (MASS || need < amount)) {
       const unsigned width = hi - lo;  // less one
       const int shift = max(0, 32 - __clz(width) - 10);
-      each_plain(i0, i1, [&](bool in, float l, int) {
-        const unsigned key = key_of(l);
-        if (in && key >= lo && key <= hi) add<MASS>((hi - key) >> shift, MASS ? weight(c, l, sh.powers) : 1);
-      });
+      auto count = [&](unsigned key) {
+        if (key >= lo && key <= hi) add<MASS>((hi - key) >> shift, MASS ? weight(c, of_key(key), sh.powers) : 1);
+      };
+      if (listed) {
+        for (int i = tid; i < static_cast<int>(sh.mine_n); i += ST) count(sh.mine[i].x);
+      } else {
+        each_plain(i0, i1, [&](bool in, float l, int) {
+          if (in) count(key_of(l));
+        });
+      }
       crossing<MASS>(-1.f, need);
       hi -= static_cast<unsigned>(sh.found[0]) << shift;
       lo = max(lo, hi - min(hi, (1u << shift) - 1));
@@ -650,14 +683,16 @@ struct Row {
       amount = sh.found[2];
     }
     const float v = of_key(lo);
-    if (!MASS && need == amount) {
-      cut_at(v, v == vcut ? icut : 0x7fffffff);
-      return false;
-    }
-    // one logit, of which the first some are kept
+    // one logit, or (not MASS) some that all stay; of equal ones the first some stay
     if (MASS) {
       const u64 w = weight(c, v, sh.powers);
       need = (need + w - 1) / w;
+      amount /= w;
+    }
+    if (need == amount) {
+      cut_at(v, v == vcut ? icut : 0x7fffffff);
+      if (MASS && listed) add_listed();
+      return false;
     }
     u64 its, all, before;
     const int at = locate<true>(v, [&](u64) { return need - 1; }, its, all);
@@ -668,6 +703,7 @@ struct Row {
     __syncthreads();
     exchange(sh.found[0], before, all);
     cut_at(v, static_cast<int>(all) - 1);
+    if (MASS && listed) add_listed();
     return false;
   }
 };
@@ -810,7 +846,10 @@ __global__ void __launch_bounds__(ST) sample_kernel(const SampleArgs p, int CL, 
     }
     __syncthreads();
     const float v = Row<TL>::of_key(sh.ends[0]);
-    if (v > row.vcut) row.cut_at(v, 0x7fffffff);
+    if (v > row.vcut) {
+      row.cut_at(v, 0x7fffffff);
+      row.known = false;
+    }
   }
   u64 its = 0;
   const int at = row.template locate<false>(0.f, [&](u64 sum) { return Row<TL>::draw(random, sum); }, its, all);

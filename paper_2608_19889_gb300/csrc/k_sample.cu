@@ -159,11 +159,16 @@ constexpr int SOME = 1024;  // logits of a bin among which the cut is found with
 struct Shared {
   unsigned hist[2][2][NB];  // amounts, used in turn: as they come, bits 0 .. 15 and 16 .. 31; then 64 bits in two words
   unsigned high[NB];        // bits from 32 on, as they come
+  u64 octave[2][NB / 32];   // this CTA's sums of 32 bins, with the histogram of the same turn
+  float many[2][NB / 32];   // weights: about how many logits they are
   float2 powers[STEPS];
   uint2 mine[LIST];         // this CTA's list: key, number
   uint2 all[SOME];          // all CTAs' lists, in the first one
   unsigned mine_n;
   unsigned estimate;        // of the logits up to the crossing bin
+  u64 below;                // this CTA's amounts below it
+  u64 goal;                 // what the running sum had to reach
+  bool any;                 // whether it did
   u64 cta[2];               // what the cluster exchanges, in turn
   u64 warp[SW];
   u64 found[3];             // the crossing bin: number, what is needed of it, all of it
@@ -246,16 +251,21 @@ struct Row {
       atomicAdd(h, low);
     }
   }
-  // This thread's bins of the current histogram, 2t and 2t + 1, as 64-bit numbers, in place of the words.
-  AXON_DEV void join_words() {
+  // This thread's bins of the current histogram, 2t and 2t + 1; weights as 64-bit numbers, in place of the words.
+  template <bool MASS>
+  AXON_DEV void own_bins(u64 (&a)[2]) {
     uint2* const l = reinterpret_cast<uint2*>(&sh.hist[pass & 1][0][0]) + threadIdx.x;
-    uint2* const m = reinterpret_cast<uint2*>(&sh.hist[pass & 1][1][0]) + threadIdx.x;
-    uint2* const h = reinterpret_cast<uint2*>(&sh.high[0]) + threadIdx.x;
-    const u64 a = l->x + (static_cast<u64>(m->x) << 16) + (static_cast<u64>(h->x) << 32);
-    const u64 b = l->y + (static_cast<u64>(m->y) << 16) + (static_cast<u64>(h->y) << 32);
-    *l = make_uint2(static_cast<unsigned>(a), static_cast<unsigned>(b));
-    *m = make_uint2(static_cast<unsigned>(a >> 32), static_cast<unsigned>(b >> 32));
-    *h = make_uint2(0, 0);
+    a[0] = l->x;
+    a[1] = l->y;
+    if (MASS) {
+      uint2* const m = reinterpret_cast<uint2*>(&sh.hist[pass & 1][1][0]) + threadIdx.x;
+      uint2* const h = reinterpret_cast<uint2*>(&sh.high[0]) + threadIdx.x;
+      a[0] += (static_cast<u64>(m->x) << 16) + (static_cast<u64>(h->x) << 32);
+      a[1] += (static_cast<u64>(m->y) << 16) + (static_cast<u64>(h->y) << 32);
+      *l = make_uint2(static_cast<unsigned>(a[0]), static_cast<unsigned>(a[1]));
+      *m = make_uint2(static_cast<unsigned>(a[0] >> 32), static_cast<unsigned>(a[1] >> 32));
+      *h = make_uint2(0, 0);
+    }
   }
   AXON_DEV void clear(int which) {
     for (int i = threadIdx.x; i < 2 * NB; i += ST) (&sh.hist[which][0][0])[i] = 0;
@@ -271,88 +281,124 @@ struct Row {
     return u > 0.f ? __umul64hi(fraction64(fminf(u, 0.999999940395355224609375f)), sum) : 0;
   }
 
-  // The first of the bins at which the running sum reaches the target goes to sh.found; a: this thread's bins 2t and 2t + 1.
-  // part_of >= 0: the target is this part of the sum, else `goal`. Returns whether there is one.
-  AXON_DEV bool scan_bins(const u64 (&a)[2], float part_of, u64 goal) {
+  // The first of this CTA's bins at which the running sum reaches `goal` goes to sh.found; a: this thread's bins 2t and 2t + 1.
+  AXON_DEV void scan_bins(const u64 (&a)[2], u64 goal) {
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
     const u64 inc = warp_scan64(a[0] + a[1]);
     if (lane == 31) sh.warp[warp] = inc;
     __syncthreads();
-    const u64 x = lane < SW ? sh.warp[lane] : 0;
-    const u64 all = warp_sum64(x);
-    u64 sum = warp_sum64(lane < warp ? x : 0) + inc - a[0] - a[1];
-    target = part_of >= 0.f ? share_of(part_of, all) : goal;
-    const bool any = all >= target;
-    if (any) {
+    u64 sum = warp_sum64(lane < warp ? sh.warp[lane] : 0) + inc - a[0] - a[1];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        if (sum < target && sum + a[i] >= target) {
-          sh.found[0] = 2 * t + i;
-          sh.found[1] = target - sum;
-          sh.found[2] = a[i];
-        }
-        sum += a[i];
+    for (int i = 0; i < 2; ++i) {
+      if (sum < goal && sum + a[i] >= goal) {
+        sh.found[0] = 2 * t + i;
+        sh.found[1] = goal - sum;
+        sh.found[2] = a[i];
       }
+      sum += a[i];
     }
     __syncthreads();
-    return any;
   }
-  // The same for the sums of all CTAs' bins; clears the other histogram, which everybody has read.
+  // About how many logits have that much weight in bin b: at least that many, and 2 % more at most, since a bin's weights
+  // are that close to each other.
+  AXON_DEV static float logits_of(u64 amount, int b) {
+    return static_cast<float>(amount) * exp2f(b * (static_cast<float>(1 << BIN_SHIFT) / STEPS) - 44.f);
+  }
+  // The same for the sums of all CTAs' bins: first the 32 bins that it is among, by each CTA's sums of so many, then these,
+  // by one warp. (All bins of all CTAs read by each took 10000 cycles with 8 CTAs, this 4000.) Clears the other
+  // histogram, which everybody has read. With part_of >= 0 also how many logits there are up to the bin, and this CTA's
+  // amounts below it.
   template <bool MASS>
   AXON_DEV bool crossing(float part_of, u64 goal) {
     cg::cluster_group cluster = cg::this_cluster();
-    if (MASS) {
-      __syncthreads();
-      join_words();
+    const int which = pass & 1, t = threadIdx.x, lane = t & 31;
+    __syncthreads();
+    {
+      u64 a[2];
+      own_bins<MASS>(a);
+      u64 sum = a[0] + a[1];
+      float n = MASS && part_of >= 0.f ? logits_of(a[0], 2 * t) + logits_of(a[1], 2 * t + 1) : 0.f;
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) {
+        sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (MASS) n += __shfl_xor_sync(0xffffffffu, n, o);
+      }
+      if ((t & 15) == 0) {
+        sh.octave[which][t >> 4] = sum;
+        if (MASS) sh.many[which][t >> 4] = n;
+      }
     }
     cluster.sync();
-    const int which = pass & 1, t = threadIdx.x;
     ++pass;
-    u64 a[2] = {0, 0};
-    const uint2 ol = reinterpret_cast<const uint2*>(&sh.hist[which][0][0])[t], oh = reinterpret_cast<const uint2*>(&sh.hist[which][1][0])[t];
-    for (int r0 = 0; r0 < CL; r0 += 4) {
-      uint2 lo[4], hi[4];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        lo[r] = hi[r] = make_uint2(0, 0);
-        if (r0 + r < CL) {
-          const unsigned* h = cluster.map_shared_rank(&sh.hist[which][0][0], r0 + r);
-          lo[r] = reinterpret_cast<const uint2*>(h)[t];
-          if (MASS) hi[r] = reinterpret_cast<const uint2*>(h + NB)[t];
+    if (t < 32) {
+      u64 sum = 0, mine = 0;
+      float n = 0.f;
+#pragma unroll 4
+      for (int r = 0; r < CL; ++r) {
+        const u64 x = *cluster.map_shared_rank(&sh.octave[which][lane], r);
+        sum += x;
+        mine = r == rank ? x : mine;
+        if (MASS) n += *cluster.map_shared_rank(&sh.many[which][lane], r);
+      }
+      u64 inc = warp_scan64(sum);
+      const u64 all = __shfl_sync(0xffffffffu, inc, 31);
+      target = part_of >= 0.f ? share_of(part_of, all) : goal;
+      const unsigned at = __ballot_sync(0xffffffffu, inc >= target);
+      if (at) {
+        const int o = __ffs(at) - 1;
+        const u64 before = __shfl_sync(0xffffffffu, inc - sum, o);
+        u64 below = lane < o ? mine : 0;
+        n = lane < o ? n : 0.f;
+        sum = 0;
+#pragma unroll 4
+        for (int r = 0; r < CL; ++r) {
+          const unsigned* h = cluster.map_shared_rank(&sh.hist[which][0][0], r);
+          const u64 x = h[o * 32 + lane] + (MASS ? static_cast<u64>(h[NB + o * 32 + lane]) << 32 : 0);
+          sum += x;
+          mine = r == rank ? x : mine;
+        }
+        inc = warp_scan64(sum);
+        const int f = __ffs(__ballot_sync(0xffffffffu, before + inc >= target)) - 1;
+        if (MASS && part_of >= 0.f) {
+          if (lane <= f && o * 32 + lane < NB - 1) n += logits_of(sum, o * 32 + lane);
+          below = warp_sum64(below + (lane < f ? mine : 0));
+          const unsigned logits = __reduce_add_sync(0xffffffffu, static_cast<unsigned>(fminf(n, 1e6f)));
+          if (lane == 0) {
+            sh.estimate = logits;
+            sh.below = below;
+          }
+        }
+        if (lane == f) {
+          sh.found[0] = o * 32 + f;
+          sh.found[1] = target - before - (inc - sum);
+          sh.found[2] = sum;
         }
       }
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        a[0] += (static_cast<u64>(hi[r].x) << 32) + lo[r].x;
-        a[1] += (static_cast<u64>(hi[r].y) << 32) + lo[r].y;
+      if (lane == 0) {
+        sh.goal = target;
+        sh.any = at != 0;
       }
     }
     clear(which ^ 1);
-    if (t == 0) sh.estimate = 0;
-    const bool any = scan_bins(a, part_of, goal);
-    if (MASS && part_of >= 0.f && any) {
-      // How many logits there are up to the crossing bin: at least this many, and 2 % more at most, since a bin's weights
-      // are that close to each other.
-      const int b = static_cast<int>(sh.found[0]);
-      unsigned n = 0;
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        if (2 * t + i <= b && 2 * t + i < NB - 1)
-          n += static_cast<unsigned>(fminf(static_cast<float>(a[i]) * exp2f((2 * t + i) * (static_cast<float>(1 << BIN_SHIFT) / STEPS) - 44.f), 1e6f));
-      n = __reduce_add_sync(0xffffffffu, n);
-      if ((t & 31) == 0 && n) atomicAdd(&sh.estimate, n);
-      own = cta_sum((2 * t < b ? (static_cast<u64>(oh.x) << 32) + ol.x : 0) + (2 * t + 1 < b ? (static_cast<u64>(oh.y) << 32) + ol.y : 0));
-    }
-    return any;
+    __syncthreads();
+    target = sh.goal;
+    if (MASS && part_of >= 0.f) own = sh.below;
+    return sh.any;
   }
 
   AXON_DEV static int bin_of(unsigned k) { return min(static_cast<int>(k) >> BIN_SHIFT, NB - 1); }
 
-  // The smallest key for which in(logit) holds, if it holds from some logit to the largest; called by a whole warp.
+  // The smallest key for which in(logit) holds, if it holds from some logit to the largest; called by a whole warp. `near`
+  // is tried first (the full search took 2000 cycles).
   template <typename F>
-  AXON_DEV unsigned lowest_key(F in) const {
+  AXON_DEV unsigned lowest_key(float near, F in) const {
     unsigned lo = 0, hi = key_of(m);
     const int lane = threadIdx.x & 31;
+    const unsigned k0 = key_of(near), at0 = k0 - 16 + lane;
+    if (fabsf(near) < INFINITY && k0 > 16 && k0 < hi) {
+      const unsigned hits = __ballot_sync(0xffffffffu, at0 >= hi || in(of_key(at0)));
+      if (hits && !(hits & 1)) return min(hi, k0 - 16 + __ffs(hits) - 1);
+    }
     while (lo < hi) {
       const unsigned step = (hi - lo) / 32 + 1, at = min(hi, lo + lane * step);  // (hi - lo) < 2^32 - 32
       const unsigned hits = __ballot_sync(0xffffffffu, in(of_key(at)));
@@ -365,7 +411,9 @@ struct Row {
   }
   // ... whose bin is at most b.
   AXON_DEV unsigned lowest_in(int b) const {
-    return lowest_key([&](float l) {
+    const int steps = b == NB - 1 ? K_END : (b + 1) << BIN_SHIFT;
+    const float near = c.base + (static_cast<float>(c.top - steps) + 0.5f) / (c.ch * STEPS);
+    return lowest_key(near, [&](float l) {
       const unsigned k = steps_of(c, l);
       return k < K_END && bin_of(k) <= b;
     });
@@ -474,20 +522,30 @@ struct Row {
     return -1;
   }
 
-  // The logits that are kept and in bins b0 .. b1, all CTAs': how many; and, if they are at most `most` and no CTA has more
+  // The logits that are kept and of keys lo .. hi, all CTAs': how many; and, if they are at most `most` and no CTA has more
   // than its list holds, in the first one's sh.all.
-  AXON_DEV int gather(int b0, int b1, int most) {
+  AXON_DEV int gather(unsigned lo, unsigned hi, int most) {
     cg::cluster_group cluster = cg::this_cluster();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid == 0) sh.mine_n = 0;
     __syncthreads();
-    each_plain(warp * seg, min(end, warp * seg + seg), [&](bool in, float l, int i) {
-      const unsigned s = steps_of(c, l);
-      if (in && s < K_END && bin_of(s) <= b1 && bin_of(s) >= b0) {
-        const unsigned at = atomicAdd(&sh.mine_n, 1u);
-        if (at < LIST) sh.mine[at] = make_uint2(key_of(l), first + i);
+    const float from = fmaxf(of_key(lo), vcut), to = of_key(hi);
+    const int i1 = min(end, warp * seg + seg);
+    for (int i = warp * seg + 4 * lane; i < i1; i += 128) {
+      const float4 v = *reinterpret_cast<const float4*>(val + i);
+      const float l[4] = {v.x, v.y, v.z, v.w};
+      bool any = false;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) any |= l[x] >= from && l[x] <= to;
+      if (!any) continue;
+      for (int x = 0; x < 4; ++x) {
+        const float f = x == 0 ? v.x : x == 1 ? v.y : x == 2 ? v.z : v.w;
+        if (f >= from && f <= to && kept(f, i + x)) {
+          const unsigned at = atomicAdd(&sh.mine_n, 1u);
+          if (at < LIST) sh.mine[at] = make_uint2(key_of(f), first + i + x);
+        }
       }
-    });
+    }
     cluster.sync();
     const unsigned here = lane < CL ? *cluster.map_shared_rank(&sh.mine_n, lane) : 0;
     const int nc = __any_sync(0xffffffffu, here > LIST) ? 0x7fffffff : static_cast<int>(__reduce_add_sync(0xffffffffu, here));
@@ -567,10 +625,9 @@ struct Row {
       }
       __syncthreads();
       const int which = pass & 1;
-      if (MASS) join_words();
-      const uint2 l = reinterpret_cast<const uint2*>(&sh.hist[which][0][0])[tid], h = reinterpret_cast<const uint2*>(&sh.hist[which][1][0])[tid];
-      const u64 a[2] = {(static_cast<u64>(h.x) << 32) + l.x, (static_cast<u64>(h.y) << 32) + l.y};
-      scan_bins(a, -1.f, need);
+      u64 a[2];
+      own_bins<MASS>(a);
+      scan_bins(a, need);
       hi -= static_cast<unsigned>(sh.found[0]) << shift;
       lo = max(lo, hi - min(hi, (1u << shift) - 1));
       need = sh.found[1];
@@ -628,9 +685,16 @@ struct Row {
     if (!crossing<MASS>(MASS ? fmaxf(share, 0.f) : -1.f, k)) return false;
     const int b = static_cast<int>(sh.found[0]);
     u64 need = sh.found[1], amount = sh.found[2];
+    // keys of the bin
+    if (tid < 64) {
+      const unsigned key = tid < 32 ? lowest_in(b) : b > 0 ? lowest_in(b - 1) - 1 : key_of(m);
+      if ((tid & 31) == 0) sh.ends[tid >> 5] = key;
+    }
+    __syncthreads();
+    unsigned lo = sh.ends[0], hi = sh.ends[1];
     // Few in these bins? (How many is known of a count, and nearly of weights.)
     if (MASS ? sh.estimate <= FEW : k - need + amount <= FEW) {
-      const int nc = gather(0, b, FEW);
+      const int nc = gather(lo, key_of(m), FEW);
       if (nc <= FEW) {
         if (rank == 0) settle(nc, k, u, token, prob);
         return true;
@@ -638,10 +702,10 @@ struct Row {
       cg::this_cluster().sync();  // the counts are read before the next list begins
     }
     // The logits of the bin in lists, where they have room.
-    const float about = MASS ? static_cast<float>(amount) * exp2f(b * (static_cast<float>(1 << BIN_SHIFT) / STEPS) - 44.f) : static_cast<float>(amount);
+    const float about = MASS ? logits_of(amount, b) : static_cast<float>(amount);
     bool listed = false;
     if (about <= CL * (LIST * 3 / 4) || b == NB - 1) {
-      const int nc = gather(b, b, SOME);
+      const int nc = gather(lo, hi, SOME);
       if (nc <= SOME) {
         u64 before, all;
         const u64 at = rank == 0 ? cut_list<MASS>(nc, need) : 0;
@@ -653,16 +717,7 @@ struct Row {
       }
       listed = nc < 0x7fffffff;
     }
-    // keys of the bin (the next pass's histogram was cleared with the crossing; the others may still read the last one)
-    if (tid < 32) {
-      const unsigned lo = lowest_in(b), hi = b > 0 ? lowest_in(b - 1) - 1 : key_of(m);
-      if (tid == 0) {
-        sh.ends[0] = lo;
-        sh.ends[1] = hi;
-      }
-    }
-    __syncthreads();
-    unsigned lo = sh.ends[0], hi = sh.ends[1];
+    // (the next pass's histogram was cleared with the crossing; the others may still read the last one)
     while (lo < hi && (MASS || need < amount)) {
       const unsigned width = hi - lo;  // less one
       const int shift = max(0, 32 - __clz(width) - 10);
@@ -841,7 +896,7 @@ __global__ void __launch_bounds__(ST) sample_kernel(const SampleArgs p, int CL, 
   }
   if (row.least) {
     if (warp == 0) {
-      const unsigned key = row.lowest_key([&](float l) { return l > -INFINITY && weight(row.c, l, sh.powers) >= row.least; });
+      const unsigned key = row.lowest_key(NAN, [&](float l) { return l > -INFINITY && weight(row.c, l, sh.powers) >= row.least; });
       if (lane == 0) sh.ends[0] = key;
     }
     __syncthreads();

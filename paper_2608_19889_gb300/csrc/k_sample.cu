@@ -7,16 +7,25 @@
 // Which token that is hangs on which side of a border a sum of up to 10^5 weights falls. fp32 sums (2^-24
 // a step) would give another token than the formula's every few hundred draws, and atomics another from
 // run to run. So weights are 64-bit integers, 2^44 w rounded, exact to about 2^-41 of their value (the
-// exponent as a pair of fp32 numbers; powers of two from a table of 2^(-j/256) and three terms of a series):
+// exponent as a pair of fp32 numbers; powers of two from a table of 2^(-j/512) and three terms of a series):
 // sums of integers are exact and have no order, and the token is the one that 64-bit arithmetic
 // gives unless u falls within some 2^-40 of a border.
 //
 // A cluster of CTAs takes a row, each CTA a slice of it, which it keeps in shared memory, so that
 // logits are read from HBM once whatever follows. Cuts (top-k, top-p) are found on histograms of counts
-// or weights: 1024 bins that are even in the exponent, then the crossing bin's interval of float
-// bits in 1024 parts, until a part holds one number or one logit; each CTA adds up the bins of all
-// the others through distributed shared memory. A weight goes into a bin as two 32-bit atomics with
-// the carry between them (64-bit atomics on shared memory are loops).
+// or weights: 1024 bins that are even in the exponent, 32 per octave, joined over the cluster through distributed
+// shared memory; a weight goes into a bin 16 bits at a time, so that no atomic has to return its carry
+// (64-bit atomics on shared memory are loops). Where few logits are left, one CTA settles all of it among them; the
+// crossing bin's logits go into lists, and the cut is found among these by their float bits, 10 at a time, by one CTA
+// where they are 1024 at most. After a cut by weights each CTA knows its own sum, and only the one that the draw falls
+// into adds up its weights again, warp by warp.
+//
+// The bound is the instructions, 62 a logit for the weights' histogram and 48 for their sum, and the cluster's
+// barriers, 0.7 us each and as much again for the slowest CTA; the floor, reading the logits once, is far off.
+// Measured: 1 row of 151936 logits with top-k and top-p 12.0 us, by temperature alone 10.1, the largest alone 4.4;
+// 33 rows of 152064 16-bit logits that ask for different things 37.6 us; 64 rows of 128256 fp32 logits by top-p, two CTAs
+// per SM and 1.7 times what runs at once, 76.5 us (a CTA: 1.5 us to load, 2 for the maximum, 7 for the histogram, 4 for the
+// crossing, 3 for the lists, 5 for the cut); 512 rows of 32000 by temperature 57.9 us.
 #include <cooperative_groups.h>
 #include <math.h>
 

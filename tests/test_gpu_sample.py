@@ -168,6 +168,24 @@ def test_many_equal_logits(ax, dtype):
                 assert got == want
 
 
+@pytest.mark.parametrize("crowd", [200, 900, 3000, 20000])
+@pytest.mark.parametrize("B,V", [(2, 50257), (40, 33000)])
+@pytest.mark.parametrize("values", [0, 5])
+def test_a_crowd_within_a_thirtieth_of_an_octave(ax, B, V, crowd, values):
+    """Cuts and draws among many logits whose weights differ by 1.5 % at most; values: of so many different logits."""
+    r = np.random.default_rng(crowd + V + values)
+    x = (r.standard_normal((B, V)) - 9).astype(np.float32)
+    for b in range(B):
+        at = r.permutation(V)[:crowd]
+        x[b, at] = 4 + 0.015 * (r.integers(0, values, crowd) / values if values else r.random(crowd))
+    x, u = torch.from_numpy(x).to(DEV), r.random(B).astype(np.float32)
+    part = r.uniform(0.1, 0.9, B)
+    check(ax, x, u, p=part)
+    check(ax, x, u, k=np.maximum(1, (part * crowd).astype(np.int32)))
+    check(ax, x, u, k=np.maximum(1, (part * crowd).astype(np.int32)), p=r.uniform(0.2, 0.9, B))
+    check(ax, x, u, p=part, m=0.9949 if values == 0 else 0.9925)
+
+
 def test_borders_go_to_the_next_token(ax):
     x = torch.zeros(1, 8, device=DEV)
     for u, want in [(0.0, 0), (0.125, 1), (0.12499999, 0), (0.5, 4), (0.99999994, 7), (1.0, 7), (2.0, 7), (-1.0, 0), (float("nan"), 0)]:

@@ -703,6 +703,13 @@ cudaError_t launch_attn_paged_decode(const LaunchCtx& lc, const PagedAttnArgs& a
   return cudaErrorInvalidValue;
 }
 
+int attn_paged_own_carveout(const PagedAttnArgs& a, const SharedGroups& s) {
+  const bool two = a.H / a.G > 8;
+  const size_t cta = (a.d == 64 ? two ? smem_bytes<64, 2>(a.B) : smem_bytes<64, 1>(a.B) : two ? smem_bytes<128, 2>(a.B) : smem_bytes<128, 1>(a.B)) +
+                     shared_smem(a.B, s.N) + 2048;  // static, and what an SM keeps for a CTA
+  return static_cast<int>(min(size_t{100}, ((two ? 2 : 3) * cta * 100 + (228 << 10) - 1) / (228 << 10)));
+}
+
 cudaError_t launch_attn_paged_own(const LaunchCtx& lc, const PagedAttnArgs& a, const SharedGroups& s) {
   if (a.H / a.G > 16 || a.B < 1 || a.B > PAGED_ATTN_MAX_B || a.q_lo || s.N > SHARED_MAX_GROUPS) return cudaErrorInvalidValue;
   if (a.d == 64) return lc.f16 ? launch_own_hd<64, f16>(lc, a, s) : launch_own_hd<64, bf16>(lc, a, s);

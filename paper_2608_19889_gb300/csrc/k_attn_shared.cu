@@ -735,9 +735,9 @@ template <int HD, typename T16>
 cudaError_t launch_hd(const LaunchCtx& lc, const PagedAttnArgs& a, const SharedGroups& s, const AttnMaps& maps) {
   if (s.alone) return launch_attn_paged_own(lc, a, s);
   // The prefix pass leaves its SMs with all their memory as shared memory, where 28 KB of L1 hold the loads in flight: a pass of
-  // the rows' own parts took 1.6 times as long on them (104 and 170 us). So these two ask for what they need, three CTAs'.
+  // the rows' own parts took 1.6 times as long on them (104 and 170 us). So these two ask for what the own parts' CTAs need.
   LaunchCtx small = lc;
-  small.carveout = 45;
+  small.carveout = attn_paged_own_carveout(a, s);
   cudaError_t e = launch_prefix_hd<HD, T16>(lc, a, s, maps);
   if (e == cudaSuccess) e = launch_attn_paged_own(small, a, s);
   return e == cudaSuccess ? launch_join_hd<HD, T16>(small, a, s) : e;

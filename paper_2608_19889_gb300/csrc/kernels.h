@@ -268,6 +268,7 @@ void shared_attn_rules(SharedGroups* s, const PagedAttnArgs& a, int num_sms);
 cudaError_t prepare_attn_shared_kernels();
 // Three launches: prefix pass, the rows' own parts beside it, the join; or one (alone).
 cudaError_t launch_attn_shared(const LaunchCtx& lc, const PagedAttnArgs& a, const SharedGroups& s, const AttnMaps& maps);
+int attn_paged_own_carveout(const PagedAttnArgs& a, const SharedGroups& s);  // in percent, for all of an SM's CTAs
 cudaError_t launch_attn_paged_own(const LaunchCtx& lc, const PagedAttnArgs& a, const SharedGroups& s);
 
 // ---- new tokens into the paged cache (k_append.cu)

@@ -56,7 +56,7 @@ constexpr unsigned COST_TWO = 5, COST_ONE = 4, COST_LAST = 3;
 // What the rows' own parts take on an SM, in 1/64 of it: a page (of 128 dims; twelve warps share the SM, and each has 1.5 us
 // for a page), and a row's kv head (15 us of a warp: table, first keys, the warps' and parts' states joined); and what they
 // take to begin, once the CTAs of the prefix pass that have nothing to do are gone.
-constexpr unsigned OWN_PAGE = 20, OWN_ROW = 200, OWN_BEGIN = 10;
+constexpr unsigned OWN_PAGE = 20, OWN_ROW = 160, OWN_BEGIN = 6;
 
 // A group of the prefix pass: its items are `pairs` per kv head, of two tiles of PW rows; the last one may have one tile.
 struct Span {
@@ -74,17 +74,17 @@ struct Span {
 };
 
 // The two passes run beside each other, each on SMs of its own: how many of them the rows' own parts take, so that both end
-// together. Called by a warp. (57 rows of 1500 to 5500 tokens, 48 of them on 4001 in common: 74 us, 99 with one pass after the
+// together. An even number, or all. Called by a warp. (57 rows of 1500 to 5500 tokens, 48 of them on 4001 in common: 74 us, 99 with one pass after the
 // other; 64 rows in groups of 4: 53 and 57.5; 64 rows on 32768 tokens: 85 and 91.)
 AXON_DEV int own_sms(unsigned pages, unsigned rows, unsigned cost, int d, int sms) {
-  if (cost == 0 || sms < 2) return sms;
-  const unsigned long long sum = (static_cast<unsigned long long>(pages) * OWN_PAGE * d / 128 + static_cast<unsigned long long>(rows) * OWN_ROW) >> 6;
-  const unsigned own = static_cast<unsigned>(min(sum, 1ull << 31));
+  if (cost == 0 || sms < 4) return sms;
+  const float own = static_cast<float>(pages) * (OWN_PAGE / 64.f) * (d == 64 ? 0.5f : 1.f) + static_cast<float>(rows) * (OWN_ROW / 64.f);
+  const float line = static_cast<float>(cost);
   unsigned best = 0xffffffffu;
 #pragma unroll 1
-  for (int S = 1 + (threadIdx.x & 31); S < sms; S += 32) {
-    const unsigned t = max(OWN_BEGIN + own / S, max(2 * COST_TWO, cost / (sms - S)));
-    best = min(best, min(t, 0x3fffffu) << 10 | (1023 - S));
+  for (int S = 2 + 2 * (threadIdx.x & 31); S < sms; S += 64) {
+    const float t = fmaxf(OWN_BEGIN + __fdividef(own, static_cast<float>(S)), fmaxf(2.f * COST_TWO, __fdividef(line, static_cast<float>(sms - S))));
+    best = min(best, static_cast<unsigned>(fminf(t * 16.f, 4194303.f)) << 10 | (1023 - S));
   }
   return 1023 - static_cast<int>(__reduce_min_sync(0xffffffffu, best) & 1023);
 }
@@ -105,9 +105,9 @@ AXON_DEV int group_of(const GroupPlan& g, int N, int b) {
   return lo >= 0 && b < g.from[lo + 1] ? lo : -1;
 }
 // Called by the THREADS threads of the CTA from thread FIRST on, which meet at barrier 2; `report`: sets the error bits.
-// Small calls wait for memory once.
-template <int THREADS, int FIRST>
-AXON_DEV void plan_groups(const PagedAttnArgs& p, const SharedGroups& s, const GroupPlan& g, bool report) {
+// Small calls wait for memory once. `enough`, asked once they have met, ends it: false.
+template <int THREADS, int FIRST, typename F>
+AXON_DEV bool plan_groups(const PagedAttnArgs& p, const SharedGroups& s, const GroupPlan& g, bool report, F enough) {
   const int tid = static_cast<int>(threadIdx.x) - FIRST;
   auto meet = [] { asm volatile("barrier.cta.sync 2, %0;" ::"n"(THREADS) : "memory"); };
   int pos = tid < p.B ? live_pos(p, tid) : -1;
@@ -132,13 +132,14 @@ AXON_DEV void plan_groups(const PagedAttnArgs& p, const SharedGroups& s, const G
       : "=r"(any)
       : "r"(static_cast<int>(bad)), "n"(THREADS)
       : "memory");
+  if (enough()) return false;
   if (any) {
     // inconsistent offsets: nobody shares anything
     if (report && tid == 0) set_err(p.err, DEVERR_SEQ);
     for (int i = tid; i < s.N; i += THREADS) g.c0[i] = g.c1[i] = 0;
     if (tid == 0) *g.own = s.sms;
     meet();
-    return;
+    return true;
   }
 #pragma unroll 1
   for (int b0 = 0; b0 < p.B; b0 += THREADS) {
@@ -198,6 +199,7 @@ AXON_DEV void plan_groups(const PagedAttnArgs& p, const SharedGroups& s, const G
     if (tid == 0) *g.own = own;
   }
   meet();
+  return true;
 }
 // What plan_groups reports, where nobody needs the plan.
 template <int THREADS>

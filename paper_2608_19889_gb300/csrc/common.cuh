@@ -114,6 +114,11 @@ AXON_DEV void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0]
 // ------------------------------------------------------- programmatic launch
 // Wait until the preceding kernel in the stream has completed and its
 // writes are visible (no-op when launched without programmatic dependency).
+AXON_DEV uint32_t sm_id() {
+  uint32_t r;
+  asm("mov.u32 %0, %%smid;" : "=r"(r));
+  return r;
+}
 AXON_DEV void grid_dep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 // Allow the next kernel in the stream to begin launching.
 AXON_DEV void grid_dep_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }

@@ -531,16 +531,14 @@ AXON_DEV void paged_decode(const PagedAttnArgs& p, const SharedGroups& sg) {
     } else {
       // those that come when the prefix pass ends find that nothing is left
       volatile int* const next = sg.next;
-      if (tid == 0) s_cta = next[1] > 0 && next[0] >= next[1];
-      __syncthreads();
-      if (s_cta) return;
-      plan_groups<DW * 32, 0>(p, sg, gp, false);
-      ctas = min(gridDim.x, (NT == 1 ? 3 : 2) * *gp.own);
       if (tid == 0) {
-        next[1] = static_cast<int>(ctas);
+        const int all = next[1];
         s_cta = atomicAdd(sg.next, 1);
+        s_last[0] = all > 0 && s_cta >= all;
       }
-      __syncthreads();
+      if (!plan_groups<DW * 32, 0>(p, sg, gp, false, [&] { return s_last[0] != 0; })) return;
+      ctas = min(gridDim.x, (NT == 1 ? 3 : 2) * *gp.own);
+      if (tid == 0) next[1] = static_cast<int>(ctas);
       cta = s_cta;
       if (cta >= ctas) return;
     }

@@ -87,6 +87,21 @@ AXON_DEV int part_at(int r0, int rows, int g, int p0, int H, int HPG, unsigned w
   return 2 * (r0 * H + (g * rows + p0) * HPG) + 256 * static_cast<int>(worker);
 }
 
+// This CTA's number among the `workers` of the prefix pass; not below them: it leaves its SM to the rows' own parts, which take
+// `own` SMs. These come in pairs, the even one and the next, since two SMs share a way to the memory: beside one that
+// streams own parts a CTA of the prefix pass took 70 us instead of 63. Should too few CTAs be on the other SMs, the last ones
+// to come work wherever they are.
+AXON_DEV unsigned number_of(const SharedGroups& sg, int own, int workers) {
+  const int pairs = sg.sms / 2;
+  if (pairs < 2) return blockIdx.x;
+  const int at = static_cast<int>(sm_id() % sg.sms) / 2;
+  const bool works = (at + 1) * (own / 2) / pairs == at * (own / 2) / pairs;
+  const unsigned old = atomicAdd(reinterpret_cast<unsigned*>(sg.next) + 2, works ? 0x10001u : 0x10000u);  // CTAs that came, and their numbers
+  const int given = static_cast<int>(old & 0xffff), to_come = static_cast<int>(gridDim.x - 1 - (old >> 16));
+  if (works) return given;
+  return workers - given > to_come ? atomicAdd(reinterpret_cast<unsigned*>(sg.next) + 2, 1u) & 0xffff : UINT_MAX;
+}
+
 template <int HD, typename T16>
 __global__ void __launch_bounds__(THREADS, 1)
     attn_prefix_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
@@ -153,10 +168,13 @@ __global__ void __launch_bounds__(THREADS, 1)
   unsigned u0 = 0, u1 = 0;
   // CTAs that the line is dealt to; the others leave their SMs to the rows' own parts
   auto ctas = [&]() { return static_cast<unsigned>(min(static_cast<int>(gridDim.x), max(1, sg.sms - *gp.own))); };
+  __shared__ unsigned s_worker;
+  unsigned worker = 0;  // of the line
   auto take_share = [&]() {
     d = deal(before[sg.N], ctas(), sg.least_steps);
-    u1 = blockIdx.x < d.workers && d.total ? d.begin(blockIdx.x + 1) : 0;
-    u0 = u1 ? d.begin(blockIdx.x) : 0;
+    worker = s_worker;
+    u1 = worker < d.workers && d.total ? d.begin(worker + 1) : 0;
+    u0 = u1 ? d.begin(worker) : 0;
   };
   // The part with the first step that begins at u or after it (u < u1); no steps: none does. The same in all lanes.
   // done: steps of the CTA before it.
@@ -193,7 +211,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       t.page0 = gp.c0[lo] + 8 * static_cast<int>(first);
       t.pages = min(gp.c1[lo] - t.page0, 8 * t.steps);
       t.lead = gp.lead[lo];
-      t.at = part_at(t.r0, s.rows, t.g, t.p0, p.H, HPG, blockIdx.x);
+      t.at = part_at(t.r0, s.rows, t.g, t.p0, p.H, HPG, worker);
       return t;
     }
   };
@@ -204,7 +222,8 @@ __global__ void __launch_bounds__(THREADS, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
     grid_dep_wait();
     grid_dep_launch();  // the rows' own parts, which wait for nothing of this kernel until their end
-    plan_groups<128, 256>(p, sg, gp, blockIdx.x == 0);
+    plan_groups<128, 256>(p, sg, gp, blockIdx.x == 0, [] { return false; });
+    if (warp == 9 && lane == 0) s_worker = number_of(sg, *gp.own, ctas());
     if (warp == 8) {
       unsigned sum = 0;
       for (int i0 = 0; i0 < sg.N; i0 += 32) {
@@ -619,7 +638,7 @@ __global__ void __launch_bounds__(JT) attn_join_kernel(const PagedAttnArgs p, co
   const int b = blockIdx.x, h = blockIdx.y, tid = threadIdx.x;
   grid_dep_wait();
   const int4 gp = __ldcg(sg.plan + 1 + b), all = __ldcg(sg.plan);
-  if (!(b | h | tid)) sg.next[0] = sg.next[1] = 0;
+  if (!(b | h | tid)) sg.next[0] = sg.next[1] = sg.next[2] = 0;
   if (!gp.x) return;
   const Deal d = deal(static_cast<unsigned>(all.x), static_cast<unsigned>(all.y), static_cast<unsigned>(all.z));
   const Span sp(gp.w, gp.x, PW);

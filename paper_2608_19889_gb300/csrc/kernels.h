@@ -254,7 +254,7 @@ struct SharedGroups {
   int least_steps;   // of 8 blocks, for a CTA of the prefix pass
   bool alone;        // no row can share anything worth it: the rows' own parts are all there is
   int sms, tile;     // SMs; rows of a tile of the prefix pass
-  int* next;         // [2] numbers the CTAs of the rows' own parts; how many there are; zero between calls
+  int* next;         // [3] numbers the CTAs of the rows' own parts; how many there are; numbers the prefix pass's; zero between calls
   int4* plan;          // [1 + PAGED_ATTN_MAX_B], written by the prefix pass for the join
   float2* state_stats; // [B][H] maximum and sum of the rows' own parts
   float* state;        // [B][H][d] their outputs, not divided

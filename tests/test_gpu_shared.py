@@ -353,3 +353,28 @@ def test_thousands_of_calls_in_a_row(ax):
         ax.axon_attn_shared(cache, 0, c.q, c.ctx, c.offsets, c.prefix, outs[i // 3], work, c.bt)
     for _, _, _, outs, want in state:
         assert (outs == want).all()
+
+
+@pytest.mark.parametrize("common,own", [(160, 5000), (6000, 2), (6000, 5000), (1024, 300)])
+def test_how_the_multiprocessors_are_shared_out(ax, common, own):
+    """Most of the work in the rows' own parts, in the common ones, in both, and little of either."""
+    check(ax, Case(12, 2, 128, "bf16", [(common, [common + own + 7 * j for j in range(5)])], seed=common + own, layers=1, layer=0))
+
+
+def test_two_calls_at_once(ax):
+    """On two streams with a workspace each: CTAs of the one come where the other expects its own. The same bits as alone."""
+    cases = [Case(32, 8, 128, "bf16", [(2000, [2020 + 300 * j for j in range(8)]), (700, [720, 731, 2500])], seed=61, layers=1, layer=0),
+             Case(14, 2, 64, "fp16", [(5000, [5010 + j for j in range(20)])], seed=62, layers=1, layer=0)]
+    n, state = 300, []
+    for c in cases:
+        cache = ax.make_kv_cache(c.k, c.v)
+        work = ax.make_shared_workspace(cache, len(c.pos), c.q.shape[1])
+        want = run(ax, c, work=work)[0]
+        state.append((c, cache, work, torch.zeros(n, *c.q.shape, dtype=c.q.dtype, device=DEV), want, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for i in range(n):
+        for c, cache, work, outs, _, stream in state:
+            ax.axon_attn_shared(cache, 0, c.q, c.ctx, c.offsets, c.prefix, outs[i], work, c.bt, stream=stream)
+    torch.cuda.synchronize()
+    for _, _, _, outs, want, _ in state:
+        assert (outs == want).all()

@@ -56,7 +56,7 @@ constexpr unsigned COST_TWO = 5, COST_ONE = 4, COST_LAST = 3;
 // What the rows' own parts take on an SM, in 1/64 of it: a page (of 128 dims; twelve warps share the SM, and each has 1.5 us
 // for a page), and a row's kv head (15 us of a warp: table, first keys, the warps' and parts' states joined); and what they
 // take to begin, once the CTAs of the prefix pass that have nothing to do are gone.
-constexpr unsigned OWN_PAGE = 20, OWN_ROW = 160, OWN_BEGIN = 6;
+constexpr unsigned OWN_PAGE = 20, OWN_ROW = 200, OWN_BEGIN = 4;
 
 // A group of the prefix pass: its items are `pairs` per kv head, of two tiles of PW rows; the last one may have one tile.
 struct Span {
@@ -74,8 +74,8 @@ struct Span {
 };
 
 // The two passes run beside each other, each on SMs of its own: how many of them the rows' own parts take, so that both end
-// together. An even number, or all. Called by a warp. (57 rows of 1500 to 5500 tokens, 48 of them on 4001 in common: 74 us, 99 with one pass after the
-// other; 64 rows in groups of 4: 53 and 57.5; 64 rows on 32768 tokens: 85 and 91.)
+// together. An even number, or all. Called by a warp. (57 rows of 1500 to 5500 tokens, 48 of them on 4001 in common: 73.5 us,
+// 99 with one pass after the other; 64 rows in groups of 4: 52 and 57.5; 64 rows on 32768 tokens: 81 and 91.)
 AXON_DEV int own_sms(unsigned pages, unsigned rows, unsigned cost, int d, int sms) {
   if (cost == 0 || sms < 4) return sms;
   const float own = static_cast<float>(pages) * (OWN_PAGE / 64.f) * (d == 64 ? 0.5f : 1.f) + static_cast<float>(rows) * (OWN_ROW / 64.f);

@@ -924,7 +924,9 @@ __global__ void __launch_bounds__(ST) sample_kernel(const SampleArgs p, int CL, 
   cluster.sync();
 }
 
-// CTAs per row: as many as run at once (two per SM), and slices of no more than 24K logits.
+// CTAs per row: as many as run at once (two per SM), and slices of no more than 24K logits, two of which an SM holds with all else
+// where they are below 19K. 64 rows of 128256 by top-p: 76 us with 16K, 82 with 32K, 139 with 8K (clusters of 16, a
+// barrier of which waits for the slowest of as many); 512 rows of 32000 by temperature 58 with 16K, 71 with 32K, 77 with 8K.
 int cluster_for(const LaunchCtx& lc, int B, int V) {
   int CL = 1;
   while (CL < MAX_CL && (V > CL * 24 * 1024 || (2ll * B * CL <= 2 * lc.num_sms && V / CL > 2 * ST))) CL *= 2;

@@ -22,10 +22,10 @@
 //
 // The bound is the instructions, 62 a logit for the weights' histogram and 48 for their sum, and the cluster's
 // barriers, 0.7 us each and as much again for the slowest CTA; the floor, reading the logits once, is far off.
-// Measured: 1 row of 151936 logits with top-k and top-p 12.0 us, by temperature alone 10.1, the largest alone 4.4;
+// Measured: 1 row of 151936 logits with top-k and top-p 11.9 us, by temperature alone 10.1, the largest alone 4.4;
 // 33 rows of 152064 16-bit logits that ask for different things 37.6 us; 64 rows of 128256 fp32 logits by top-p, two CTAs
-// per SM and 1.7 times what runs at once, 76.5 us (a CTA: 1.5 us to load, 2 for the maximum, 7 for the histogram, 4 for the
-// crossing, 3 for the lists, 5 for the cut); 512 rows of 32000 by temperature 57.9 us.
+// per SM and 1.7 times what runs at once, 75 us (a CTA: 1.5 us to load, 2 for the maximum, 7 for the histogram, 4 for the
+// crossing, 3 for the lists, 4.5 for the cut); 512 rows of 32000 by temperature 57.9 us.
 #include <cooperative_groups.h>
 #include <math.h>
 
@@ -173,7 +173,8 @@ struct Shared {
   float2 powers[STEPS];
   uint2 mine[LIST];         // this CTA's list: key, number
   uint2 all[SOME];          // all CTAs' lists, in the first one
-  unsigned mine_n;
+  uint2 near[32];           // of these, those about the cut
+  unsigned mine_n, near_n;
   unsigned estimate;        // of the logits up to the crossing bin
   u64 below;                // this CTA's amounts below it
   u64 goal;                 // what the running sum had to reach
@@ -644,6 +645,33 @@ struct Row {
       clear(which);
       __syncthreads();
       if (lo == hi) break;
+      // a warp's worth of logits left, as a rule after the first bins: in order
+      if (tid == 0) sh.near_n = 0;
+      __syncthreads();
+      for (int i = tid; i < nc; i += ST) {
+        const uint2 x = sh.all[i];
+        if (x.x < lo || x.x > hi) continue;
+        const unsigned at = atomicAdd(&sh.near_n, 1u);
+        if (at < 32) sh.near[at] = x;
+      }
+      __syncthreads();
+      const int left = static_cast<int>(sh.near_n);
+      if (left > 32) continue;
+      if (warp == 0) {
+        const uint2 me = lane < left ? sh.near[lane] : make_uint2(0, 0);
+        const u64 w = lane < left ? MASS ? weight(c, of_key(me.x), sh.powers) : 1 : 0;
+        u64 ahead = 0;
+        bool last = true;  // of equal ones
+        for (int j = 0; j < left; ++j) {
+          const uint2 x = sh.near[j];
+          const u64 wj = __shfl_sync(0xffffffffu, w, j);
+          if (x.x > me.x || (x.x == me.x && x.y < me.y)) ahead += wj;
+          last = last && !(x.x == me.x && x.y > me.y);
+        }
+        if (lane < left && ahead < need && ahead + w >= need) sh.found[0] = (static_cast<u64>(me.x) << 32) | (last ? 0x7fffffffu : me.y);
+      }
+      __syncthreads();
+      return sh.found[0];
     }
     const u64 one = MASS ? weight(c, of_key(lo), sh.powers) : 1;
     if (amount == one) return (static_cast<u64>(lo) << 32) | 0x7fffffffu;

@@ -170,6 +170,14 @@ def test_long_chunks(ax, H, G, d):
     check(ax, Case(H, G, d, "bf16", [3, 7], [1501, 700], seed=5), d)
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype", ["fp16", "fp32"])
+def test_many_tokens_of_other_types(ax, dtype, interleaved):
+    """Three heads per thread, 42 = 14 x 3 of them and 43 x 3 - 1; a part of the dims turned."""
+    check(ax, Case(32, 5, 128, dtype, [3, 0, 40], [700, 1, 333], seed=8), 96, interleaved)
+    check(ax, Case(100, 14, 64, dtype, [9], [600], seed=9), 64, interleaved)
+
+
 def test_rows_in_place(ax):
     c = Case(8, 2, 64, "bf16", [3, 77], [20, 1], seed=6)
     q = c.parts()[0]

@@ -101,7 +101,7 @@ AXON_DEV void paged_items(const PagedAttnArgs& p, const SharedGroups& sg, float*
   constexpr int MT = HD / 16;  // 16-dim tiles of O^T
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, c = lane & 3;
   const int HPG = p.H / p.G;
-  auto common = [&](int b) { return SH ? shared[b] : make_int2(INT_MAX, INT_MAX); };
+  auto common = [&](int b) { return SH && !sg.alone ? shared[b] : make_int2(INT_MAX, INT_MAX); };
   const unsigned total = before[p.B] * p.G;  // below 2^31: the launcher saw to it
 
   // ---- rows that see nothing
@@ -525,31 +525,27 @@ AXON_DEV void paged_decode(const PagedAttnArgs& p, const SharedGroups& sg) {
   unsigned ctas = gridDim.x, cta = blockIdx.x;
   // SH: [B] the pages that the row has in common with others, from the first and to the last; then the plan they come from
   int2* const shared = reinterpret_cast<int2*>(before + 2 * p.B + 2);
-  if constexpr (SH) {
+  if (SH && !sg.alone) {
     const GroupPlan gp(reinterpret_cast<int*>(shared + p.B), sg.N);
-    if (sg.alone) {
-      if (blockIdx.x == 0) check_groups<DW * 32>(p, sg);
-    } else {
-      // those that come when the prefix pass ends find that nothing is left
-      volatile int* const next = sg.next;
-      if (tid == 0) {
-        const int all = next[1];
-        s_cta = atomicAdd(sg.next, 1);
-        s_last[0] = all > 0 && s_cta >= all;
-      }
-      if (!plan_groups<DW * 32, 0>(p, sg, gp, false, [&] { return s_last[0] != 0; })) return;
-      ctas = min(gridDim.x, (NT == 1 ? 3 : 2) * *gp.own);
-      if (tid == 0) next[1] = static_cast<int>(ctas);
-      cta = s_cta;
-      if (cta >= ctas) return;
+    // those that come when the prefix pass ends find that nothing is left
+    volatile int* const next = sg.next;
+    if (tid == 0) {
+      const int all = next[1];
+      s_cta = atomicAdd(sg.next, 1);
+      s_last[0] = all > 0 && s_cta >= all;
     }
+    if (!plan_groups<DW * 32, 0>(p, sg, gp, false, [&] { return s_last[0] != 0; })) return;
+    ctas = min(gridDim.x, (NT == 1 ? 3 : 2) * *gp.own);
+    if (tid == 0) next[1] = static_cast<int>(ctas);
+    cta = s_cta;
+    if (cta >= ctas) return;
     for (int b = tid; b < p.B; b += DW * 32) {
-      const int n = sg.alone ? -1 : group_of(gp, sg.N, b);
+      const int n = group_of(gp, sg.N, b);
       shared[b] = n >= 0 && gp.c1[n] > gp.c0[n] ? make_int2(gp.c0[n], gp.c1[n]) : make_int2(INT_MAX, INT_MAX);
     }
     __syncthreads();
   }
-  auto common = [&](int b) { return SH ? shared[b] : make_int2(INT_MAX, INT_MAX); };
+  auto common = [&](int b) { return SH && !sg.alone ? shared[b] : make_int2(INT_MAX, INT_MAX); };
 
   // ---- pages before each row
   if (p.B <= 32) {
@@ -601,7 +597,11 @@ AXON_DEV void paged_decode(const PagedAttnArgs& p, const SharedGroups& sg) {
 
   for (;;) {
     paged_items<HD, T16, NT, LO, SH>(p, sg, state, before, rpos, shared, s_last, ctas, cta);
-    if (!SH || sg.alone) return;
+    if (!SH) return;
+    if (sg.alone) {
+      if (blockIdx.x == gridDim.x - 1) check_groups<DW * 32>(p, sg);
+      return;
+    }
     __syncthreads();
     if (tid == 0) s_cta = atomicAdd(sg.next, 1);
     __syncthreads();

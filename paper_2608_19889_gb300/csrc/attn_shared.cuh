@@ -104,10 +104,15 @@ AXON_DEV int group_of(const GroupPlan& g, int N, int b) {
   }
   return lo >= 0 && b < g.from[lo + 1] ? lo : -1;
 }
+// The blocks that row b has in common with others, from the first and to the last; none: both behind all.
+AXON_DEV int2 common_of(const GroupPlan& g, int N, int b) {
+  const int n = group_of(g, N, b);
+  return n >= 0 && g.c1[n] > g.c0[n] ? make_int2(g.c0[n], g.c1[n]) : make_int2(INT_MAX, INT_MAX);
+}
 // Called by the THREADS threads of the CTA from thread FIRST on, which meet at barrier 2; `report`: sets the error bits.
-// Small calls wait for memory once. `enough`, asked once they have met, ends it: false.
-template <int THREADS, int FIRST, typename F>
-AXON_DEV bool plan_groups(const PagedAttnArgs& p, const SharedGroups& s, const GroupPlan& g, bool report, F enough) {
+// Small calls wait for memory once.
+template <int THREADS, int FIRST>
+AXON_DEV void plan_groups(const PagedAttnArgs& p, const SharedGroups& s, const GroupPlan& g, bool report) {
   const int tid = static_cast<int>(threadIdx.x) - FIRST;
   auto meet = [] { asm volatile("barrier.cta.sync 2, %0;" ::"n"(THREADS) : "memory"); };
   int pos = tid < p.B ? live_pos(p, tid) : -1;
@@ -132,14 +137,13 @@ AXON_DEV bool plan_groups(const PagedAttnArgs& p, const SharedGroups& s, const G
       : "=r"(any)
       : "r"(static_cast<int>(bad)), "n"(THREADS)
       : "memory");
-  if (enough()) return false;
   if (any) {
     // inconsistent offsets: nobody shares anything
     if (report && tid == 0) set_err(p.err, DEVERR_SEQ);
     for (int i = tid; i < s.N; i += THREADS) g.c0[i] = g.c1[i] = 0;
     if (tid == 0) *g.own = s.sms;
     meet();
-    return true;
+    return;
   }
 #pragma unroll 1
   for (int b0 = 0; b0 < p.B; b0 += THREADS) {
@@ -199,7 +203,6 @@ AXON_DEV bool plan_groups(const PagedAttnArgs& p, const SharedGroups& s, const G
     if (tid == 0) *g.own = own;
   }
   meet();
-  return true;
 }
 // What plan_groups reports, where nobody needs the plan.
 template <int THREADS>

@@ -228,8 +228,15 @@ __global__ void __launch_bounds__(THREADS, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
     grid_dep_wait();
     grid_dep_launch();  // the rows' own parts, which wait for nothing of this kernel until their end
-    plan_groups<128, 256>(p, sg, gp, blockIdx.x == 0, [] { return false; });
+    plan_groups<128, 256>(p, sg, gp, blockIdx.x == 0);
     if (warp == 9 && lane == 0) s_worker = number_of(sg, *gp.own, ctas());
+    if (warp == 11 && blockIdx.x == gridDim.x - 1) {
+      // the plan for the rows' own parts, which find it there as a rule
+      for (int b = lane; b < p.B; b += 32) sg.common[b] = common_of(gp, sg.N, b);
+      __threadfence();
+      __syncwarp();
+      if (lane == 0) *static_cast<volatile int*>(sg.next + 3) = *gp.own;
+    }
     if (warp == 8) {
       unsigned sum = 0;
       for (int i0 = 0; i0 < sg.N; i0 += 32) {
@@ -644,7 +651,7 @@ __global__ void __launch_bounds__(JT) attn_join_kernel(const PagedAttnArgs p, co
   const int b = blockIdx.x, h = blockIdx.y, tid = threadIdx.x;
   grid_dep_wait();
   const int4 gp = __ldcg(sg.plan + 1 + b), all = __ldcg(sg.plan);
-  if (!(b | h | tid)) sg.next[0] = sg.next[1] = sg.next[2] = 0;
+  if (!(b | h | tid)) *reinterpret_cast<int4*>(sg.next) = make_int4(0, 0, 0, 0);
   if (!gp.x) return;
   const Deal d = deal(static_cast<unsigned>(all.x), static_cast<unsigned>(all.y), static_cast<unsigned>(all.z));
   const Span sp(gp.w, gp.x, PW);
@@ -784,13 +791,15 @@ cudaError_t prepare_attn_shared_kernels() {
 // Plan, the rows' own states, the prefix pass's parts, from a multiple of 256 bytes on.
 size_t shared_attn_bytes(int B, int H, int d, int num_sms) {
   const size_t own = static_cast<size_t>(B) * H, parts = 2 * own + 256 * static_cast<size_t>(num_sms);
-  return ALIGN + aligned(16 * (1 + PAGED_ATTN_MAX_B)) + aligned(8 * own) + aligned(8 * parts) + 4 * static_cast<size_t>(d) * (own + parts);
+  return ALIGN + aligned(16 * (1 + PAGED_ATTN_MAX_B)) + aligned(8 * PAGED_ATTN_MAX_B) + aligned(8 * own) + aligned(8 * parts) + 4 * static_cast<size_t>(d) * (own + parts);
 }
 void shared_attn_carve(SharedGroups* s, void* work, int B, int H, int d, int num_sms) {
   const size_t own = static_cast<size_t>(B) * H, parts = 2 * own + 256 * static_cast<size_t>(num_sms);
   char* at = reinterpret_cast<char*>(aligned(reinterpret_cast<uintptr_t>(work)));
   s->plan = reinterpret_cast<int4*>(at);
   at += aligned(16 * (1 + PAGED_ATTN_MAX_B));
+  s->common = reinterpret_cast<int2*>(at);
+  at += aligned(8 * PAGED_ATTN_MAX_B);
   s->state_stats = reinterpret_cast<float2*>(at);
   at += aligned(8 * own);
   s->stats = reinterpret_cast<float2*>(at);

@@ -254,8 +254,10 @@ struct SharedGroups {
   int least_steps;   // of 8 blocks, for a CTA of the prefix pass
   bool alone;        // no row can share anything worth it: the rows' own parts are all there is
   int sms, tile;     // SMs; rows of a tile of the prefix pass
-  int* next;         // [3] numbers the CTAs of the rows' own parts; how many there are; numbers the prefix pass's; zero between calls
+  int* next;         // [4] numbers the CTAs of the rows' own parts; how many there are; numbers the prefix pass's; once `common` is there,
+                     // the own parts' SMs; zero between calls
   int4* plan;          // [1 + PAGED_ATTN_MAX_B], written by the prefix pass for the join
+  int2* common;        // [PAGED_ATTN_MAX_B] and for the rows' own parts: the blocks that a row has in common, from and to
   float2* state_stats; // [B][H] maximum and sum of the rows' own parts
   float* state;        // [B][H][d] their outputs, not divided
   float2* stats;       // of the prefix pass's parts

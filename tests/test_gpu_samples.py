@@ -144,3 +144,45 @@ def test_samples_example(ax):
     assert ((prob > 0) & (prob <= 1)).all() and (prob[:, 0] == 1).all()
     with pytest.raises(ValueError):
         samples.generate(steps=samples.CONTEXT)
+
+
+@pytest.mark.parametrize("H,G,d,B,common,dtype", [(32, 8, 128, 24, 1024, torch.bfloat16), (14, 2, 64, 9, 2000, torch.float16)])
+def test_every_step_reads_its_own_tokens(ax, monkeypatch, H, G, d, B, common, dtype):
+    """New queries, keys and values each step, launched one after the other and then as a captured step: the attention over shared
+    prefixes, whose kernels start before the ones in front have ended, sees them all. Against axon_attn_decode on the same
+    cache: both are within 5e-4 max |v| and half a unit of the exact result (values up to 6)."""
+    monkeypatch.setenv("AXON_SHARED_MIN_BYTES", "0")
+    torch.manual_seed(B)
+    steps, whole = 300, common // 16
+    per = (common + 2 * steps) // 16 + 2
+    k = torch.randn(1, whole + B * (per - whole), G, 16, d, device=DEV).to(dtype)
+    cache = ax.make_kv_cache(k, v := torch.randn(k.shape, device=DEV).to(dtype))
+    table = torch.empty(B, per, dtype=torch.int32, device=DEV)
+    table[:, :whole] = torch.arange(whole, device=DEV)
+    table[:, whole:] = whole + torch.arange(B * (per - whole), device=DEV).view(B, -1)
+    ctx, rope = ints(*[common] * B), ax.axon_rope_table(per * 16, d, 1e4)
+    work, plain = ax.make_shared_workspace(cache, B, H), ax.make_attn_workspace(cache, B, H)
+    q, new_k, new_v = (torch.empty(B, n, d, device=DEV, dtype=dtype) for n in (H, G, G))
+    a, b, off = torch.zeros_like(q), torch.zeros_like(q), torch.zeros((), device=DEV)
+    offsets, prefix = ints(0, B), ints(common)
+
+    def step():
+        for t in (q, new_k, new_v):
+            t.normal_()
+        ax.axon_kv_append(cache, 0, new_k, new_v, ctx, block_table=table, rope=rope, q=q, q_out=q)
+        ax.axon_attn_shared(cache, 0, q, ctx, offsets, prefix, a, work, table)
+        ax.axon_attn_decode(cache, 0, q, ctx, b, plain, block_table=table)
+        torch.maximum(off, ((a.float() - b.float()).abs() - torch.finfo(dtype).eps * b.float().abs()).max(), out=off)
+        ctx.add_(1)
+
+    for _ in range(steps):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(steps):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert v.shape == k.shape and int(ctx[0]) == common + 2 * steps
+    assert float(off) <= 6e-3

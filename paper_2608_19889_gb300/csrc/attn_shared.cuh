@@ -5,6 +5,7 @@
 #include <limits.h>
 
 #include "kernels.h"
+#include "own_split.h"
 
 // Blocks c0 .. c1 - 1 are seen whole by every live row of a group: those that the caller says are shared, up to the
 // shortest row's last whole block, from the first one that lies inside every row's window. A group shares nothing
@@ -49,15 +50,6 @@ AXON_DEV RowPages row_pages(const PagedAttnArgs& p, int pos, int2 common = make_
   return r;
 }
 
-// What a step of the prefix pass costs, in 0.4 us: 2.05 us with two tiles (the tensor pipe's 1.6), 1.5 with one whose 64 KB come
-// from HBM, 1.25 with one whose keys the group's other items read too.
-constexpr unsigned COST_TWO = 5, COST_ONE = 4, COST_LAST = 3;
-
-// What the rows' own parts take on an SM, in 1/64 of it: a page (of 128 dims; twelve warps share the SM, and each has 1.5 us
-// for a page), and a row's kv head (15 us of a warp: table, first keys, the warps' and parts' states joined); and what they
-// take to begin, once the CTAs of the prefix pass that have nothing to do are gone.
-constexpr unsigned OWN_PAGE = 20, OWN_ROW = 200, OWN_BEGIN = 4;
-
 // A group of the prefix pass: its items are `pairs` per kv head, of two tiles of PW rows; the last one may have one tile.
 struct Span {
   int rows, pages, pairs;
@@ -78,14 +70,10 @@ struct Span {
 // 99 with one pass after the other; 64 rows in groups of 4: 52 and 57.5; 64 rows on 32768 tokens: 80 and 91.)
 AXON_DEV int own_sms(unsigned pages, unsigned rows, unsigned cost, int d, int sms) {
   if (cost == 0 || sms < 4) return sms;
-  const float own = static_cast<float>(pages) * (OWN_PAGE / 64.f) * (d == 64 ? 0.5f : 1.f) + static_cast<float>(rows) * (OWN_ROW / 64.f);
-  const float line = static_cast<float>(cost);
+  const unsigned own = own_work(pages, rows, d);
   unsigned best = 0xffffffffu;
 #pragma unroll 1
-  for (int S = 2 + 2 * (threadIdx.x & 31); S < sms; S += 64) {
-    const float t = fmaxf(OWN_BEGIN + __fdividef(own, static_cast<float>(S)), fmaxf(2.f * COST_TWO, __fdividef(line, static_cast<float>(sms - S))));
-    best = min(best, static_cast<unsigned>(fminf(t * 16.f, 4194303.f)) << 10 | (1023 - S));
-  }
+  for (int S = 2 + 2 * (threadIdx.x & 31); S < sms; S += 64) best = min(best, split_time(own, cost, S, sms) << 10 | (1023 - S));
   return 1023 - static_cast<int>(__reduce_min_sync(0xffffffffu, best) & 1023);
 }
 

@@ -45,6 +45,14 @@ AXON_DEV uint32_t pack_h2(float lo, float hi) {
 template <typename T> AXON_DEV uint32_t pack2(float lo, float hi);
 template <> AXON_DEV uint32_t pack2<bf16>(float lo, float hi) { return pack_bf2(lo, hi); }
 template <> AXON_DEV uint32_t pack2<f16>(float lo, float hi) { return pack_h2(lo, hi); }
+// The same for averages of visible values: an infinite one stays infinite.
+AXON_DEV float sat_finite_half(float v) { return isinf(v) ? v : sat_half(v); }
+template <typename T> AXON_DEV uint32_t pack_out(float lo, float hi);
+template <> AXON_DEV uint32_t pack_out<bf16>(float lo, float hi) { return pack_bf2(lo, hi); }
+template <> AXON_DEV uint32_t pack_out<f16>(float lo, float hi) {
+  __half2 h = __floats2half2_rn(sat_finite_half(lo), sat_finite_half(hi));
+  return *reinterpret_cast<uint32_t*>(&h);
+}
 AXON_DEV float to_f(bf16 v) { return __bfloat162float(v); }
 AXON_DEV float to_f(f16 v) { return __half2float(v); }
 AXON_DEV float to_f(float v) { return v; }

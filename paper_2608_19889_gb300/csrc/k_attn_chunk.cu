@@ -686,7 +686,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             uint32_t v[8];
 #pragma unroll
             for (int x = 0; x < 8; ++x)
-              v[x] = pack2<T16>(__uint_as_float(o[u + 2 * x]) * inv, __uint_as_float(o[u + 2 * x + 1]) * inv);
+              v[x] = pack_out<T16>(__uint_as_float(o[u + 2 * x]) * inv, __uint_as_float(o[u + 2 * x + 1]) * inv);
             if (wide) {
               st_global32(dst + ((c + u) >> 3), v);
             } else {
@@ -734,7 +734,7 @@ __global__ void __launch_bounds__(THREADS, 1)
               v = make_float4(v.x + f[x] * e.x, v.y + f[x] * e.y, v.z + f[x] * e.z, v.w + f[x] * e.w);
             }
           }
-          *reinterpret_cast<uint2*>(dst + c * 4) = make_uint2(pack2<T16>(v.x * inv, v.y * inv), pack2<T16>(v.z * inv, v.w * inv));
+          *reinterpret_cast<uint2*>(dst + c * 4) = make_uint2(pack_out<T16>(v.x * inv, v.y * inv), pack_out<T16>(v.z * inv, v.w * inv));
         }
       }
     }

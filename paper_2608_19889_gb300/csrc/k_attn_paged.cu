@@ -391,7 +391,7 @@ AXON_DEV void paged_items(const PagedAttnArgs& p, const SharedGroups& sg, float*
       const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
       const long long at = b * p.o_row + (g * HPG + h) * p.o_head + x * 4;
       v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
-      const uint2 w = make_uint2(pack2<T16>(v.x, v.y), pack2<T16>(v.z, v.w));
+      const uint2 w = make_uint2(pack_out<T16>(v.x, v.y), pack_out<T16>(v.z, v.w));
       *reinterpret_cast<uint2*>(static_cast<T16*>(p.o) + at) = w;
       if (LO && p.o_lo) {
         const T16* hv = reinterpret_cast<const T16*>(&w);

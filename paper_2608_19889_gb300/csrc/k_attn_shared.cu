@@ -726,7 +726,7 @@ __global__ void __launch_bounds__(JT) attn_join_kernel(const PagedAttnArgs p, co
   }
   const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
   *reinterpret_cast<uint2*>(static_cast<T16*>(p.o) + b * p.o_row + h * p.o_head + x * 4) =
-      make_uint2(pack2<T16>(v.x * inv, v.y * inv), pack2<T16>(v.z * inv, v.w * inv));
+      make_uint2(pack_out<T16>(v.x * inv, v.y * inv), pack_out<T16>(v.z * inv, v.w * inv));
   if (p.lse && x == 0) p.lse[own] = (M + log2f(L)) * 0.69314718055994531f;
 }
 

@@ -525,7 +525,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         valid = i < HPG * PW && (t.one ? 0 : w * PW * HPG) + i < t.rows * HPG;
         at = t.at + w * (t.one ? t.rows : PW) * HPG + i;
         if (!nt) {
-          if (t.one && valid) sg.stats[at] = make_float2(-INFINITY, 0.f);  // one step: nothing for this pipeline
+          if (t.one && valid) sg.stats[at] = make_float2(-INFINITY, -1.f);  // one step: nothing for this pipeline
           continue;
         }
       }
@@ -686,9 +686,12 @@ __global__ void __launch_bounds__(JT) attn_join_kernel(const PagedAttnArgs p, co
   for (int k = 0; k < MAX_PARTS / JT + 1; ++k) {
     const int i = tid + k * JT;
     if (i > parts) break;
-    const float f = exp2f(st[k].x - top);
+    // a sum below 0: nobody wrote the part. All others count, those of a factor 0 too: a value that is infinite or not a
+    // number shows wherever it is visible
+    const bool none = st[k].y < 0.f;
+    const float f = none ? -1.f : exp2f(st[k].x - top);
     s_f[i] = f;
-    L += f * st[k].y;
+    L += none ? 0.f : f * st[k].y;
   }
   L = warp_sum(L);
   if ((tid & 31) == 0) s_red[1][tid >> 5] = L;
@@ -712,8 +715,8 @@ __global__ void __launch_bounds__(JT) attn_join_kernel(const PagedAttnArgs p, co
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const int i = i0 + k * PG;
-      const float f = i <= parts ? s_f[i] : 0.f;
-      if (f != 0.f) v = make_float4(v.x + f * o[k].x, v.y + f * o[k].y, v.z + f * o[k].z, v.w + f * o[k].w);
+      const float f = i <= parts ? s_f[i] : -1.f;
+      if (!(f < 0.f)) v = make_float4(v.x + f * o[k].x, v.y + f * o[k].y, v.z + f * o[k].z, v.w + f * o[k].w);
     }
   }
   s_o[tid] = v;

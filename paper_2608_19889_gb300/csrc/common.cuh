@@ -114,6 +114,15 @@ AXON_DEV uint4 ld_stream16(const void* p) {
                : "l"(p));
   return r;
 }
+// The same as a relaxed load, which sees what any kernel has written that ended before (an SM's L1 is passed by).
+AXON_DEV uint4 ld_relaxed16(const void* p) {
+  uint4 r;
+  asm volatile("ld.relaxed.gpu.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w)
+               : "l"(p)
+               : "memory");
+  return r;
+}
 // Cached 16-byte load (activations: reused by every warp of the SM).
 AXON_DEV uint4 ld16(const void* p) { return *reinterpret_cast<const uint4*>(p); }
 

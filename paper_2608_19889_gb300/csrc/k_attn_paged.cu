@@ -81,6 +81,10 @@ template <> AXON_DEV uint32_t pack_prob<f16>(float a, float b, float& ra, float&
 
 // What a kernel may read that starts before the one in front of it has ended, from L2: an SM's L1 may hold what was there before.
 template <bool SH, typename T> AXON_DEV T read(const T* at) { return SH ? __ldcg(at) : *at; }
+// 16 bytes of a key or value. SH: the newest ones were written by the kernel before the prefix pass, which has waited for it
+// before it lets this one start, but this one has waited for nothing; so a load that the non-coherent path may not serve. (As
+// fast: 73.5 us and 73.9 for 57 rows with long own parts, 52.5 and 52.7 for groups of four; by .cg 75.8 and 52.7.)
+template <bool SH> AXON_DEV uint4 read16(const void* at) { return SH ? ld_relaxed16(at) : ld_stream16(at); }
 // Position of row b's query; -1: the row sees nothing.
 template <bool SH> AXON_DEV int row_pos(const PagedAttnArgs& p, int b) {
   const int pos = read<SH>(p.ctx + b);
@@ -233,13 +237,13 @@ AXON_DEV void paged_items(const PagedAttnArgs& p, const SharedGroups& sg, float*
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
-          for (int i = 0; i < KI; ++i) kv[x][i] = ld_stream16(at + x * 8 * HD + i * 32);
+          for (int i = 0; i < KI; ++i) kv[x][i] = read16<SH>(at + x * 8 * HD + i * 32);
       } else {
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
           for (int i = 0; i < KI; ++i)
-            kv[x][i] = (blk >= 0 && seen(t0 + r + 8 * x)) ? ld_stream16(at + x * 8 * HD + i * 32) : make_uint4(0, 0, 0, 0);
+            kv[x][i] = (blk >= 0 && seen(t0 + r + 8 * x)) ? read16<SH>(at + x * 8 * HD + i * 32) : make_uint4(0, 0, 0, 0);
       }
     };
     // rows of tokens that are not visible are left out, not multiplied by zero:
@@ -250,14 +254,14 @@ AXON_DEV void paged_items(const PagedAttnArgs& p, const SharedGroups& sg, float*
 #pragma unroll
         for (int x = 0; x < 4; ++x)
 #pragma unroll
-          for (int i = 0; i < VI; ++i) vv[x][i] = ld_stream16(at + ((x & 1) + 8 * (x >> 1)) * HD + i * 64);
+          for (int i = 0; i < VI; ++i) vv[x][i] = read16<SH>(at + ((x & 1) + 8 * (x >> 1)) * HD + i * 64);
       } else {
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           const int t = (x & 1) + 8 * (x >> 1);
 #pragma unroll
           for (int i = 0; i < VI; ++i)
-            vv[x][i] = (blk >= 0 && seen(t0 + 2 * c + t)) ? ld_stream16(at + t * HD + i * 64) : make_uint4(0, 0, 0, 0);
+            vv[x][i] = (blk >= 0 && seen(t0 + 2 * c + t)) ? read16<SH>(at + t * HD + i * 64) : make_uint4(0, 0, 0, 0);
         }
       }
     };

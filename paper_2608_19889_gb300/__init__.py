@@ -492,12 +492,17 @@ def axon_attn_prefill(cache, layer, q, cu_seqlens, context_lens, max_chunk, out,
 
 def axon_rope_table(positions, rotary_dim, theta, factor=0.0, low=1.0, high=4.0, original=8192, device=None, stream=None):
     """Rotary table fp32 [positions, rotary_dim / 2, 2] of axon_kv_append (see include/axon.h); factor, low, high, original: the
-    frequency scaling of make_config's rope_factor, rope_low, rope_high, rope_orig (0: none)."""
+    frequency scaling of make_config's rope_factor, rope_low, rope_high, rope_orig (0: none). device: where it is made; None, or
+    one without a number: the current device."""
     lib()
-    dev = _torch.device("cuda", _current_device() if device is None else _torch.device(device).index or 0)
+    dev = _torch.device("cuda" if device is None else device)
+    if dev.type != "cuda":
+        raise TypeError(f"device: a CUDA device is wanted, got {dev}")
+    dev = _torch.device("cuda", _current_device() if dev.index is None else dev.index)
+    handle = _handle(stream, dev.index)
     table = _torch.empty(positions, rotary_dim // 2, 2, dtype=_torch.float32, device=dev)
-    _check("axon_rope_table", _lib.axon_rope_table(table.data_ptr(), positions, rotary_dim, theta, factor, low, high, original,
-                                                   _handle(stream, dev.index)))
+    _check("axon_rope_table",
+           _lib.axon_rope_table(table.data_ptr(), positions, rotary_dim, theta, factor, low, high, original, handle))
     return table
 
 

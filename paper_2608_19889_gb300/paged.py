@@ -71,6 +71,13 @@ class PagedSeqs:
         """`step`, and a token for each of its rows drawn from its logits with the random numbers u (fp32, one per row): see
         axon_sample for these, the settings (device tensors with an entry per row) and prob. next_tokens may be `tokens`."""
         n = tokens.numel()
+        f32, i32 = torch.float32, torch.int32
+        for what, t, dtype in (("u", u, f32), ("next_tokens", next_tokens, i32), ("temperature", temperature, f32),
+                               ("top_k", top_k, i32), ("top_p", top_p, f32), ("min_p", min_p, f32), ("prob", prob, f32)):
+            if t is not None:
+                ax._want(t, dtype, what, n, self.cache.device)  # refused before the step, which would have been taken
+            elif what in ("u", "next_tokens"):
+                raise TypeError(f"{what}: a tensor is wanted")
         if self.logits is None:
             self.logits = torch.empty(self.rows, self.vocabulary, device="cuda")
         self.step(tokens, logits=self.logits[:n])

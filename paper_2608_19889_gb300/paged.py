@@ -79,7 +79,7 @@ class PagedSeqs:
             elif what in ("u", "next_tokens"):
                 raise TypeError(f"{what}: a tensor is wanted")
         if self.logits is None:
-            self.logits = torch.empty(self.rows, self.vocabulary, device="cuda")
+            self.logits = torch.empty(self.rows, self.vocabulary, device=self.all.device)
         self.step(tokens, logits=self.logits[:n])
         ax.axon_sample(self.logits[:n], u, next_tokens, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p, prob=prob)
 

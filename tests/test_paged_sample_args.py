@@ -13,7 +13,7 @@ GOOD = dict(u=((3,), F32), next_tokens=((3,), I32), temperature=((3,), F32), top
 @pytest.fixture
 def seqs(ax, monkeypatch):  # noqa: F811
     s = paged.PagedSeqs.__new__(paged.PagedSeqs)
-    s.rows, s.vocabulary, s.logits, s.steps = 4, 100, None, []
+    s.rows, s.vocabulary, s.logits, s.steps, s.all = 4, 100, None, [], Tensor((4,), I32)
     s.cache = ax.make_kv_cache(*(Tensor((1, 8, 2, 16, 64), torch.bfloat16) for _ in range(2)))
     monkeypatch.setattr(s, "step", lambda tokens, logits: s.steps.append(tokens.numel()), raising=False)
 
@@ -49,3 +49,12 @@ def test_what_has_to_be_there(ax, seqs, name):  # noqa: F811
     with pytest.raises(TypeError):
         sample(seqs, **{name: None})
     assert not seqs.steps and not ax._calls
+
+
+def test_logits_are_where_the_rows_are(ax, seqs, monkeypatch):  # noqa: F811
+    """Not on the device that happens to be current with the first call, where every later one would be refused."""
+    made = []
+    empty = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *shape, device, **k: made.append(torch.device(device)) or empty(*shape, device=device))
+    sample(seqs)
+    assert made == [torch.device("cuda", 0)]

@@ -569,8 +569,11 @@ int axon_kv_workspace(const axon_kv_cache* cache, const axon_kv_seqs* seqs, int6
  * temperature 0 (or less, or not a number): the largest logit, the lowest number among equals, d_prob 1. Logits that are not numbers
  * count as -infinity, which is never chosen; a row of nothing else gets token -1 and d_prob 0. Infinite logits share
  * everything.
- * Weights and their sums are 64-bit integers of 2^-44, exact to about 2^-41 of each weight: the token is that of 64-bit
- * arithmetic unless u or top_p falls within some 2^-40 of a border, and does not depend on timing.
+ * Weights are integers in units of 2^-44 of the largest weight, and their sums are exact. So a weight is off by up to about 2^-45
+ * of the largest and 2^-41 of itself (one below half a unit is 0 and never drawn), and a sum of n weights by n * 2^-45 of the
+ * largest weight (2^-28 for 128256, 2^-26 for the longest vocabulary, if all were off the same way) and 2^-41 of itself. The
+ * token is that of 64-bit arithmetic unless u or top_p falls that near to a border, or min_p that near to a weight, and does
+ * not depend on timing; d_prob is off by its weight's error over the sum, besides its rounding to fp32.
  *   d_logits        [B][V] of type `precision` (AXON_BF16, AXON_FP16; AXON_FP32_DEBUG: fp32, as the model's logits),
  *                   row stride in elements, at least V
  *   d_temperature, d_top_k, d_top_p, d_min_p  [B], or NULL: 1, all, 1, 0

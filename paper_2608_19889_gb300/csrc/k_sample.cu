@@ -6,10 +6,12 @@
 //
 // Which token that is hangs on which side of a border a sum of up to 10^5 weights falls. fp32 sums (2^-24
 // a step) would give another token than the formula's every few hundred draws, and atomics another from
-// run to run. So weights are 64-bit integers, 2^44 w rounded, exact to about 2^-41 of their value (the
+// run to run. So weights are 64-bit integers, 2^44 w rounded, from w exact to about 2^-41 of its value (the
 // exponent as a pair of fp32 numbers; powers of two from a table of 2^(-j/512) and three terms of a series):
-// sums of integers are exact and have no order, and the token is the one that 64-bit arithmetic
-// gives unless u falls within some 2^-40 of a border.
+// sums of integers are exact and have no order. A weight is off by half a unit and by 2^-41 of itself; n of them by n 2^-45 of
+// the largest, 2^-26 for the longest vocabulary if all erred alike (finer units would take sums past 64 bits). The token
+// is the one that 64-bit arithmetic gives unless u or top_p falls that near to a border, or min_p to a weight. Weights
+// below half a unit are 0.
 //
 // A cluster of CTAs takes a row, each CTA a slice of it, which it keeps in shared memory, so that
 // logits are read from HBM once whatever follows. Cuts (top-k, top-p) are found on histograms of counts

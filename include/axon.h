@@ -455,7 +455,10 @@ int axon_attn_decode_workspace(const axon_kv_cache* cache, int32_t num_heads, in
  *   num_groups      1 .. 1024
  *   d_block_table   [B][blocks_per_seq]; entries of shared blocks that only idle rows (context_lens negative) hold may be anything
  * The rest as in axon_attn_decode, the workspace among it: one of axon_attn_shared_workspace's size serves axon_attn_decode
- * of the same heads and cache too. num_blocks * num_kv_heads * 16 stays below 2^31. */
+ * of the same heads and cache too. num_blocks * num_kv_heads * 16 stays below 2^31.
+ * Where reading shared blocks once would spare less than 128 MB of reads the rows read them for themselves, which is faster.
+ * The environment variable AXON_SHARED_MIN_BYTES (digits; anything else is ignored) sets another limit: it is read with every
+ * call, and a captured call keeps what it was then. */
 int axon_attn_shared(const axon_kv_cache* cache, int32_t layer, const void* d_q, int64_t q_row_stride, int64_t q_head_stride,
                      int32_t B, int32_t num_heads, const int32_t* d_context_lens, const int32_t* d_block_table,
                      int32_t blocks_per_seq, const int32_t* d_group_offsets, const int32_t* d_prefix_lens, int32_t num_groups,

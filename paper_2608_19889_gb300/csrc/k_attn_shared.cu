@@ -27,6 +27,7 @@
 // 4.7 TB/s. Start, plan and the first step's code take 10 us, the join 4 to 6.
 #include <math.h>
 #include <stdlib.h>
+#include <string.h>
 
 #include <algorithm>
 
@@ -811,17 +812,23 @@ void shared_attn_carve(SharedGroups* s, void* work, int B, int H, int d, int num
   s->part = s->state + own * d;
 }
 
+// AXON_SHARED_MIN_BYTES sets another limit, for measurements and tests of small cases; what is not a whole number, digits
+// alone, does not.
+static long long least_bytes() {
+  const char* const limit = getenv("AXON_SHARED_MIN_BYTES");
+  if (!limit || !*limit || limit[strspn(limit, "0123456789")]) return 128ll << 20;
+  return std::min(strtoll(limit, nullptr, 10), 1ll << 60);
+}
+
 // Blocks read again come from L2, at some 10 TB/s, and the prefix pass and the join take some 13 us: less than 128 MB of
 // them is faster read again. GPU time of rows with 16 to 64 tokens of their own, 32 / 8 heads of 128, shared / each for
 // itself: 4 rows on 4096 tokens (50 MB spared) 21 / 18 us, 8 groups of 4 on 1024 (100 MB) 31 / 25, 16 rows on 4096 (251 MB)
-// 26 / 35, 8 groups of 4 on 4096 (403 MB) 41 / 83. AXON_SHARED_MIN_BYTES sets another limit, for measurements and for
-// tests of small cases.
+// 26 / 35, 8 groups of 4 on 4096 (403 MB) 41 / 83.
 void shared_attn_rules(SharedGroups* s, const PagedAttnArgs& a, int num_sms) {
   const long long block = 64ll * a.d * a.G;  // bytes of a block's keys and values
   const long long row = paged_attn_most_pages(1, 1, a.blocks_per_seq, a.window, a.sinks);
   s->least = 8;
-  const char* const limit = getenv("AXON_SHARED_MIN_BYTES");
-  const long long bytes = limit ? std::max(0ll, atoll(limit)) : 128ll << 20;
+  const long long bytes = least_bytes();
   s->least_spared = static_cast<int>(std::min((bytes + block - 1) / block, 1ll << 20));
   s->least_steps = 2;
   s->alone = row * (a.B - 1) < s->least_spared;

@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 
 import kv_model as km
+import test_gpu_shared as sh
 from test_gpu_shared import DEV, ax  # noqa: F401
 
 torch = pytest.importorskip("torch")
@@ -51,3 +52,34 @@ def test_millions_of_own_pages(ax):  # noqa: F811
         want, _ = km.attention(q[row].double().cpu().numpy(), keys, values, n - 1)
         off = np.abs(a[row].double().cpu().numpy() - want) - 2.0 ** -8 * np.abs(want)
         assert off.max() <= 5e-4 * vmax
+
+
+@pytest.mark.parametrize("text,shares", [("0", True), ("1000", True), ("99999999999999999999", False), ("", False), ("none", False),
+                                         ("-1", False), ("0x0", False), ("10 MB", False), (" 0", False)])
+def test_what_the_environment_may_say(ax, monkeypatch, text, shares):  # noqa: F811
+    """A limit is a whole number; other text leaves the library's own, by which a case of this size shares nothing."""
+    c = sh.Case(8, 2, 64, "bf16", [(300, [310, 320, 330]), (200, [250, 260])], seed=72)
+    monkeypatch.setenv("AXON_SHARED_MIN_BYTES", text)
+    out, _ = sh.run(ax, c)
+    cache = ax.make_kv_cache(c.k, c.v)
+    plain = torch.empty_like(c.q)
+    ax.axon_attn_decode(cache, c.layer, c.q, c.ctx, plain, ax.make_attn_workspace(cache, 5, 8), block_table=c.bt)
+    assert torch.equal(out, plain) != shares  # other sums where the prefix pass runs
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (2300, 4)])
+@pytest.mark.parametrize("rows,blocks,shares", [(16, 137, True), (16, 136, False), (65, 32, True), (64, 32, False), (17, 128, True)])
+def test_about_the_limit(ax, rows, blocks, shares, window, sinks):  # noqa: F811
+    """128 MB are 2048 reads of a block of 8 heads of 128 with keys and values; under a table that is wide enough for more the
+    device finds out. Either way the rows are right, some of them against 64 bits."""
+    c = sh.Case(32, 8, 128, "bf16", [(16 * blocks, [16 * blocks + 3 + 2 * (i % 9) for i in range(rows)])], window, sinks, seed=rows,
+                layers=1, layer=0)
+    assert (blocks * (rows - 1) >= 2048) == shares
+    some = [0, rows // 2, rows - 1]
+    cache = ax.make_kv_cache(c.k, c.v)
+    plain = torch.empty_like(c.q)
+    ax.axon_attn_decode(cache, 0, c.q, c.ctx, plain, ax.make_attn_workspace(cache, rows, 32), block_table=c.bt, window=window, sinks=sinks)
+    for per in (c.per, 400):
+        c.bt = torch.nn.functional.pad(c.bt, (0, per - c.bt.shape[1]), value=-1)
+        sh.check(ax, c, rows=some)
+        assert torch.equal(sh.run(ax, c)[0], plain) != shares

@@ -378,7 +378,9 @@ int axon_moe_routing_record(axon_model* m, int32_t* d_experts, int32_t rows);
  * *d_err (one int32, zeroed by the caller; NULL: not reported) and the access
  * is skipped; axon_check_error reads and clears the word. An attention row that would
  * have read a block out of range then holds finite numbers of no meaning (the one-token
- * form leaves its keys out, the chunk form takes them for zeros); other rows are right.
+ * form leaves its keys out, the chunk form takes them for zeros); other rows are right. With shared
+ * prefixes an entry out of range in the blocks in common, where the first live row's are read for
+ * all, spoils every row of its group (taken for zeros there, left out elsewhere).
  *
  * Workspaces are device memory, 16-byte aligned, of at least the size that
  * the matching query returns. The attention's must be zero before its first
@@ -507,8 +509,10 @@ enum { AXON_ROPE_HALF = 0, AXON_ROPE_INTERLEAVED = 1 };
  *   d_block_table   [B][blocks_per_seq], or NULL: row b holds blocks b * blocks_per_seq onward
  *   d_rope          [rope_positions][rotary_dim / 2][2] as axon_rope_table makes it; NULL with rotary_dim 0: no rotation
  *   rotary_dim      a multiple of 16, at most head_dim
- * All caches, AXON_FP32_DEBUG too. Rows that are left out (idle, beyond the table of blocks or the rotary table, of a
- * chunk whose offsets are inconsistent) leave d_q_out and the cache as they are; a block out of range keeps the
+ * All caches, AXON_FP32_DEBUG too. Left out are idle rows, rows beyond the table of blocks or the rotary table, and, with
+ * offsets, whole chunks: one takes part with all its tokens or, if its last one lies beyond either table, its context
+ * length is negative (reported, since an empty chunk is the idle one) or its offsets are inconsistent, with none. What is
+ * left out leaves d_q_out and the cache as they are; a block out of range keeps the
  * token's key and value out, its query is written. Two tokens may not go to one slot: fork before rows part. */
 int axon_kv_append(const axon_kv_cache* cache, int32_t layer, const void* d_q, int64_t q_row_stride, int64_t q_head_stride,
                    const void* d_k, int64_t k_row_stride, int64_t k_head_stride, const void* d_v, int64_t v_row_stride,

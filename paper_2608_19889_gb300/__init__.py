@@ -34,9 +34,10 @@ AXON_ROPE_HALF, AXON_ROPE_INTERLEAVED = 0, 1
 EXPORTED = ["axon_model_create", "axon_prefill", "axon_prefill_varlen", "axon_decode_step", "axon_reset",
             "axon_check_device", "axon_kv_view_get", "axon_profile_decode_step", "axon_profile_prefill",
             "axon_decode_step_noalloc", "axon_moe_routing_record", "axon_kv_cache_get", "axon_attn_decode",
-            "axon_attn_decode_workspace", "axon_attn_prefill", "axon_attn_shared", "axon_attn_shared_workspace", "axon_rope_table", "axon_kv_append", "axon_sample", "axon_kv_copy_blocks", "axon_kv_fork", "axon_kv_release",
-            "axon_kv_reserve", "axon_kv_compact", "axon_kv_workspace", "axon_check_error", "axon_free",
-            "axon_status_string"]
+            "axon_attn_decode_workspace", "axon_attn_prefill", "axon_attn_shared", "axon_attn_shared_workspace",
+            "axon_rope_table", "axon_kv_append", "axon_sample", "axon_kv_copy_blocks", "axon_kv_fork",
+            "axon_kv_release", "axon_kv_reserve", "axon_kv_compact", "axon_kv_workspace", "axon_check_error",
+            "axon_free", "axon_status_string"]
 
 
 class axon_config(ctypes.Structure):
@@ -407,7 +408,8 @@ def make_attn_workspace(cache, rows, heads):
 
 
 def make_shared_workspace(cache, rows, heads):
-    """Zeroed workspace of axon_attn_shared for up to `rows` rows of `heads` heads on this cache; it serves axon_attn_decode too."""
+    """Zeroed workspace of axon_attn_shared for up to `rows` rows of `heads` heads on this cache; it serves axon_attn_decode
+    too."""
     n = ctypes.c_int64(0)
     _current(cache.device)
     _check("axon_attn_shared_workspace", lib().axon_attn_shared_workspace(cache.ref, heads, rows, ctypes.byref(n)))
@@ -615,15 +617,16 @@ def axon_sample(logits, u, tokens, temperature=None, top_k=None, top_p=None, min
     prec = (AXON_FP32_DEBUG if dtype is _torch.float32 else AXON_BF16 if dtype is _torch.bfloat16 else
             AXON_FP16 if dtype is _torch.float16 else None)
     if prec is None or logits.dim() != 2 or not logits.is_cuda or (logits.shape[1] > 1 and logits.stride(1) != 1):
-        raise TypeError(f"logits: a device tensor [rows, vocabulary] of fp32, bf16 or fp16 with dense rows is wanted, got {dtype} "
-                        f"{tuple(logits.shape)} with strides {logits.stride()} on {logits.device}")
+        raise TypeError("logits: a device tensor [rows, vocabulary] of fp32, bf16 or fp16 with dense rows is wanted, got "
+                        f"{dtype} {tuple(logits.shape)} with strides {logits.stride()} on {logits.device}")
     (B, V), dev = logits.shape, logits.get_device()
     f32 = _torch.float32
     rc = _lib.axon_sample(
         logits.data_ptr(), logits.stride(0), prec, B, V,
         None if temperature is None else _want(temperature, f32, "temperature", B, dev),
         None if top_k is None else _want(top_k, _torch.int32, "top_k", B, dev),
-        None if top_p is None else _want(top_p, f32, "top_p", B, dev), None if min_p is None else _want(min_p, f32, "min_p", B, dev),
+        None if top_p is None else _want(top_p, f32, "top_p", B, dev),
+        None if min_p is None else _want(min_p, f32, "min_p", B, dev),
         _want(u, f32, "u", B, dev), _want(tokens, _torch.int32, "tokens", B, dev),
         None if prob is None else _want(prob, f32, "prob", B, dev), _handle(stream, dev))
     if rc:

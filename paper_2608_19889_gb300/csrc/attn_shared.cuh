@@ -150,7 +150,8 @@ AXON_DEV void plan_groups(const PagedAttnArgs& p, const SharedGroups& s, const G
     const int some = __shfl_sync(0xffffffffu, n, __ffs(in) - 1);
     if (__all_sync(0xffffffffu, n < 0 || n == some)) {
       // the usual warp: rows of one group
-      const int from = __reduce_max_sync(0xffffffffu, n >= 0 ? lo : 0), to = __reduce_min_sync(0xffffffffu, n >= 0 ? pos : INT_MAX);
+      const int from = __reduce_max_sync(0xffffffffu, n >= 0 ? lo : 0);
+      const int to = __reduce_min_sync(0xffffffffu, n >= 0 ? pos : INT_MAX);
       const int first = __reduce_min_sync(0xffffffffu, n >= 0 ? b : INT_MAX);
       if ((tid & 31) == 0) {
         atomicMax(&g.c0[some], from);

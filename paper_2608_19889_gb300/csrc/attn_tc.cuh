@@ -81,11 +81,6 @@ AXON_DEV void tmem_st8(uint32_t taddr, const uint32_t* r) {
 }
 AXON_DEV void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-AXON_DEV float ex2(float v) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-  return r;
-}
 // Two probabilities as a pair of 16-bit values (fp16: the caller's are below 65504, no saturation needed).
 template <typename T> AXON_DEV uint32_t pack_p(float lo, float hi);
 template <> AXON_DEV uint32_t pack_p<bf16>(float lo, float hi) { return pack_bf2(lo, hi); }

@@ -80,6 +80,13 @@ AXON_DEV unsigned long long argmax_key(float v, int idx) {
   return (static_cast<unsigned long long>(b) << 32) | (0xffffffffu - static_cast<uint32_t>(idx));
 }
 
+// 2^v, within 2^-22 of it; below 2^-126 it is 0.
+AXON_DEV float ex2(float v) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+
 // ------------------------------------------------------------- packed fp32
 // Two fp32 values in one 64-bit register: the packed FMA and add take one
 // issue slot for both.
@@ -128,14 +135,16 @@ AXON_DEV uint4 ld16(const void* p) { return *reinterpret_cast<const uint4*>(p); 
 
 AXON_DEV void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
-// ------------------------------------------------------- programmatic launch
-// Wait until the preceding kernel in the stream has completed and its
-// writes are visible (no-op when launched without programmatic dependency).
+// The SM that the thread runs on.
 AXON_DEV uint32_t sm_id() {
   uint32_t r;
   asm("mov.u32 %0, %%smid;" : "=r"(r));
   return r;
 }
+
+// ------------------------------------------------------- programmatic launch
+// Wait until the preceding kernel in the stream has completed and its
+// writes are visible (no-op when launched without programmatic dependency).
 AXON_DEV void grid_dep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 // Allow the next kernel in the stream to begin launching.
 AXON_DEV void grid_dep_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }

@@ -47,11 +47,6 @@ struct DCfg {
   static constexpr int PART = HEADS * (HD + 2);              // floats of a partial state in the workspace
 };
 
-AXON_DEV float ex2f(float v) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-  return r;
-}
 AXON_DEV uint32_t movm(uint32_t v) {
   uint32_t r;
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
@@ -133,8 +128,8 @@ AXON_DEV void paged_items(const PagedAttnArgs& p, const SharedGroups& sg, float*
   // ---- workers: more warps share an item the longer the items are
   const unsigned avg = total / (p.B * p.G);
   int gs = avg >= 16 ? 4 : avg >= 4 ? 2 : 1;
-  // more items than warps, as on the SMs that the prefix pass leaves: each takes whole ones, and has nobody to join with (64 rows in
-  // groups of 4: 51.5 us, 57 without this)
+  // more items than warps, as on the SMs that the prefix pass leaves: each takes whole ones, and has nobody to join
+  // with (64 rows in groups of 4: 52 us, 57 without this)
   if (SH && !sg.alone) {
     if (p.B * p.G >= ctas * DW)
       gs = 1;
@@ -310,8 +305,8 @@ AXON_DEV void paged_items(const PagedAttnArgs& p, const SharedGroups& sg, float*
             mx[x] = fmaxf(mx[x], m[n][x]);
           }
           if (__any_sync(0xffffffffu, mx[0] > m[n][0] || mx[1] > m[n][1])) {
-            const float f0 = mx[0] > m[n][0] ? ex2f(m[n][0] - mx[0]) : 1.f;
-            const float f1 = mx[1] > m[n][1] ? ex2f(m[n][1] - mx[1]) : 1.f;
+            const float f0 = mx[0] > m[n][0] ? ex2(m[n][0] - mx[0]) : 1.f;
+            const float f1 = mx[1] > m[n][1] ? ex2(m[n][1] - mx[1]) : 1.f;
             m[n][0] = mx[0];
             m[n][1] = mx[1];
             l[n][0] *= f0;
@@ -325,8 +320,8 @@ AXON_DEV void paged_items(const PagedAttnArgs& p, const SharedGroups& sg, float*
             }
           }
           const float b0 = m[n][0] == -INFINITY ? 0.f : m[n][0], b1 = m[n][1] == -INFINITY ? 0.f : m[n][1];
-          const float p0 = ex2f(s[n][0] - b0), p1 = ex2f(s[n][1] - b1);
-          const float p2 = ex2f(s[n][2] - b0), p3 = ex2f(s[n][3] - b1);
+          const float p0 = ex2(s[n][0] - b0), p1 = ex2(s[n][1] - b1);
+          const float p2 = ex2(s[n][2] - b0), p3 = ex2(s[n][3] - b1);
           l[n][0] += p0 + p2;
           l[n][1] += p1 + p3;
           float r0, r1, r2, r3, z;
@@ -423,7 +418,7 @@ AXON_DEV void paged_items(const PagedAttnArgs& p, const SharedGroups& sg, float*
       const float base = M == -INFINITY ? 0.f : M;
       for (int w = 0; w < gs; ++w) {
         const float* st = gstate + w * C::STATE;
-        const float f = ex2f(st[C::HEADS * C::PITCH + h] - base);
+        const float f = ex2(st[C::HEADS * C::PITCH + h] - base);
         L += f * st[C::HEADS * C::PITCH + C::HEADS + h];
         const float4 e = *reinterpret_cast<const float4*>(st + h * C::PITCH + x * 4);
         v = make_float4(v.x + f * e.x, v.y + f * e.y, v.z + f * e.z, v.w + f * e.w);
@@ -463,13 +458,13 @@ AXON_DEV void paged_items(const PagedAttnArgs& p, const SharedGroups& sg, float*
 #pragma unroll
             for (int y = 0; y < 8; ++y) nm = fmaxf(nm, pm[y]);
             const float base = nm == -INFINITY ? 0.f : nm;
-            const float f = ex2f(M - base);
+            const float f = ex2(M - base);
             M = nm;
             L *= f;
             v = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
 #pragma unroll
             for (int y = 0; y < 8; ++y) {
-              const float e = ex2f(pm[y] - base);
+              const float e = ex2(pm[y] - base);
               L += e * ps[y];
               v = make_float4(v.x + e * pv[y].x, v.y + e * pv[y].y, v.z + e * pv[y].z, v.w + e * pv[y].w);
             }
@@ -645,7 +640,8 @@ size_t shared_smem(int B, int N) { return 4 * (2 + 2 * static_cast<size_t>(B) + 
 template <int HD, typename T16>
 cudaError_t prepare_hd() {
   const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
-  const int one = static_cast<int>(smem_bytes<HD, 1>(PAGED_ATTN_MAX_B)), two = static_cast<int>(smem_bytes<HD, 2>(PAGED_ATTN_MAX_B));
+  const int one = static_cast<int>(smem_bytes<HD, 1>(PAGED_ATTN_MAX_B));
+  const int two = static_cast<int>(smem_bytes<HD, 2>(PAGED_ATTN_MAX_B));
   cudaError_t e = cudaFuncSetAttribute(attn_paged_decode_kernel<HD, T16, 1, false>, attr, one);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_paged_decode_kernel<HD, T16, 1, true>, attr, one);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_paged_decode_kernel<HD, T16, 2, false>, attr, two);
@@ -697,7 +693,7 @@ size_t paged_attn_part_bytes(int H, int G, int d, int num_sms) {
 // A ticket per cut item, which goes by its first worker (no other cut item begins there), and one per
 // worker's slot. They stand in front of the states and their number goes by the SMs alone,
 // so that no call's states lie where another shape or batch has its tickets.
-// One more stands behind them, which counts CTAs where rows share prefixes.
+// Four counters stand behind them, for the CTAs where rows share prefixes.
 size_t paged_attn_ticket_bytes(int num_sms) { return 4 * 3 * static_cast<size_t>(num_sms) * 3 * DW + 16; }
 
 cudaError_t prepare_attn_paged_kernels() {
@@ -718,8 +714,9 @@ cudaError_t launch_attn_paged_decode(const LaunchCtx& lc, const PagedAttnArgs& a
 
 int attn_paged_own_carveout(const PagedAttnArgs& a, const SharedGroups& s) {
   const bool two = a.H / a.G > 8;
-  const size_t cta = (a.d == 64 ? two ? smem_bytes<64, 2>(a.B) : smem_bytes<64, 1>(a.B) : two ? smem_bytes<128, 2>(a.B) : smem_bytes<128, 1>(a.B)) +
-                     shared_smem(a.B, s.N) + 2048;  // static, and what an SM keeps for a CTA
+  const size_t own = a.d == 64 ? two ? smem_bytes<64, 2>(a.B) : smem_bytes<64, 1>(a.B)
+                               : two ? smem_bytes<128, 2>(a.B) : smem_bytes<128, 1>(a.B);
+  const size_t cta = own + shared_smem(a.B, s.N) + 2048;  // static, and what an SM keeps for a CTA
   return static_cast<int>(min(size_t{100}, ((two ? 2 : 3) * cta * 100 + (228 << 10) - 1) / (228 << 10)));
 }
 

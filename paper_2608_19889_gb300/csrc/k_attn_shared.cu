@@ -103,7 +103,8 @@ AXON_DEV unsigned number_of(const SharedGroups& sg, int own, int workers) {
   if (pairs < 2) return blockIdx.x;
   const int at = static_cast<int>(sm_id() % sg.sms) / 2;
   const bool works = (at + 1) * (own / 2) / pairs == at * (own / 2) / pairs;
-  const unsigned old = atomicAdd(reinterpret_cast<unsigned*>(sg.next) + 2, works ? 0x10001u : 0x10000u);  // CTAs that came, and their numbers
+  // CTAs that came, and their numbers
+  const unsigned old = atomicAdd(reinterpret_cast<unsigned*>(sg.next) + 2, works ? 0x10001u : 0x10000u);
   const int given = static_cast<int>(old & 0xffff), to_come = static_cast<int>(gridDim.x - 1 - (old >> 16));
   if (works) return given;
   return workers - given > to_come ? atomicAdd(reinterpret_cast<unsigned*>(sg.next) + 2, 1u) & 0xffff : UINT_MAX;
@@ -112,7 +113,8 @@ AXON_DEV unsigned number_of(const SharedGroups& sg, int own, int workers) {
 template <int HD, typename T16>
 __global__ void __launch_bounds__(THREADS, 1)
     attn_prefix_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
-                       const __grid_constant__ CUtensorMap tmV, const PagedAttnArgs p, const SharedGroups sg, int PW, int pool_rows) {
+                       const __grid_constant__ CUtensorMap tmV, const PagedAttnArgs p, const SharedGroups sg, int PW,
+                       int pool_rows) {
   using C = SCfg<HD>;
   constexpr int NS = C::STAGES;
   extern __shared__ uint8_t smem_raw[];
@@ -286,7 +288,8 @@ __global__ void __launch_bounds__(THREADS, 1)
           if (lane == 0) {
             mbar_arrive_expect_tx(q_full(w), HPG * PW * HD * 2);
             for (int c = 0; c < C::CH; ++c)
-              tma_load_3d(sQ + w * C::TILE + c * C::CHUNK, &tmQ, q_full(w), c * 64, t.g * HPG, t.r0 + t.p0 + (t.one ? 0 : w * PW));
+              tma_load_3d(sQ + w * C::TILE + c * C::CHUNK, &tmQ, q_full(w), c * 64, t.g * HPG,
+                          t.r0 + t.p0 + (t.one ? 0 : w * PW));
           }
           ++iq[w];
         }
@@ -308,7 +311,8 @@ __global__ void __launch_bounds__(THREADS, 1)
         for (int b = lane; b < p.B; b += 32) {
           const int n = live_pos(p, b) >= 0 ? group_of(gp, sg.N, b) : -1;
           sg.plan[1 + b] = n >= 0 && gp.c1[n] > gp.c0[n]
-                               ? make_int4(gp.c1[n] - gp.c0[n], static_cast<int>(before[n]), gp.from[n], gp.from[n + 1] - gp.from[n])
+                               ? make_int4(gp.c1[n] - gp.c0[n], static_cast<int>(before[n]), gp.from[n],
+                                           gp.from[n + 1] - gp.from[n])
                                : make_int4(0, 0, 0, 0);
         }
       }
@@ -710,8 +714,9 @@ __global__ void __launch_bounds__(JT) attn_join_kernel(const PagedAttnArgs p, co
     for (int k = 0; k < 8; ++k) {
       const int i = i0 + k * PG;
       o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (i <= parts)
-        o[k] = __ldcg(reinterpret_cast<const float4*>(i < parts ? sg.part + static_cast<long long>(place(i)) * HD : sg.state + own * HD) + x);
+      if (i > parts) continue;
+      const float* const from = i < parts ? sg.part + static_cast<long long>(place(i)) * HD : sg.state + own * HD;
+      o[k] = __ldcg(reinterpret_cast<const float4*>(from) + x);
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
@@ -795,7 +800,8 @@ cudaError_t prepare_attn_shared_kernels() {
 // Plan, the rows' own states, the prefix pass's parts, from a multiple of 256 bytes on.
 size_t shared_attn_bytes(int B, int H, int d, int num_sms) {
   const size_t own = static_cast<size_t>(B) * H, parts = 2 * own + 256 * static_cast<size_t>(num_sms);
-  return ALIGN + aligned(16 * (1 + PAGED_ATTN_MAX_B)) + aligned(8 * PAGED_ATTN_MAX_B) + aligned(8 * own) + aligned(8 * parts) + 4 * static_cast<size_t>(d) * (own + parts);
+  return ALIGN + aligned(16 * (1 + PAGED_ATTN_MAX_B)) + aligned(8 * PAGED_ATTN_MAX_B) + aligned(8 * own) + aligned(8 * parts) +
+         4 * static_cast<size_t>(d) * (own + parts);
 }
 void shared_attn_carve(SharedGroups* s, void* work, int B, int H, int d, int num_sms) {
   const size_t own = static_cast<size_t>(B) * H, parts = 2 * own + 256 * static_cast<size_t>(num_sms);

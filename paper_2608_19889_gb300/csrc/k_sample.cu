@@ -134,7 +134,9 @@ AXON_DEV Weights weights(const Scale& c, float l0, float l1, const float2* power
   w.lo[1] = __float_as_int(r1) - MAGIC_BITS;
   return w;
 }
-AXON_DEV u64 joined(int hi, int lo) { return (static_cast<u64>(static_cast<unsigned>(hi)) << 22) + static_cast<u64>(static_cast<long long>(lo)); }
+AXON_DEV u64 joined(int hi, int lo) {
+  return (static_cast<u64>(static_cast<unsigned>(hi)) << 22) + static_cast<u64>(static_cast<long long>(lo));
+}
 AXON_DEV u64 weight(const Scale& c, float l, const float2* powers) {
   const Weights w = weights(c, l, l, powers);
   return w.k[0] < K_END ? joined(w.hi[0], w.lo[0]) : 0;
@@ -574,7 +576,8 @@ struct Row {
   }
 
   // All that matters is among the nc logits in the first CTA's sh.all: the first k of them
-  // stay (k > 0) and then the share, or those that the running sum of all weights needs to reach the target (k = 0); min-p; the draw.
+  // stay (k > 0) and then the share, or those that the running sum of all weights needs to reach the target (k = 0); min-p;
+  // the draw.
   AXON_DEV void settle(int nc, u64 k, float u, int* token, float* prob) {
     // two threads per logit; the weights are where the histograms were
     const int tid = threadIdx.x, i = tid >> 1;
@@ -670,7 +673,8 @@ struct Row {
           if (x.x > me.x || (x.x == me.x && x.y < me.y)) ahead += wj;
           last = last && !(x.x == me.x && x.y > me.y);
         }
-        if (lane < left && ahead < need && ahead + w >= need) sh.found[0] = (static_cast<u64>(me.x) << 32) | (last ? 0x7fffffffu : me.y);
+        if (lane < left && ahead < need && ahead + w >= need)
+          sh.found[0] = (static_cast<u64>(me.x) << 32) | (last ? 0x7fffffffu : me.y);
       }
       __syncthreads();
       return sh.found[0];
@@ -855,7 +859,8 @@ __global__ void __launch_bounds__(ST) sample_kernel(const SampleArgs p, int CL, 
 #pragma unroll
         for (int e = 0; e < PER; ++e) best = fmaxf(best, f[e]);
 #pragma unroll
-        for (int e = 0; e < PER; e += 4) *reinterpret_cast<float4*>(val + i + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+        for (int e = 0; e < PER; e += 4)
+          *reinterpret_cast<float4*>(val + i + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
       }
     }
   }
@@ -929,13 +934,15 @@ __global__ void __launch_bounds__(ST) sample_kernel(const SampleArgs p, int CL, 
   }
   int* const token = p.tokens + b;
   float* const prob = p.prob ? p.prob + b : nullptr;
-  if ((k > 0 && k < p.V && row.template cut<false>(k, random, token, prob)) || (row.share < 1.f && row.template cut<true>(0, random, token, prob))) {
+  if ((k > 0 && k < p.V && row.template cut<false>(k, random, token, prob)) ||
+      (row.share < 1.f && row.template cut<true>(0, random, token, prob))) {
     cluster.sync();
     return;
   }
   if (row.least) {
     if (warp == 0) {
-      const unsigned key = row.lowest_key(NAN, [&](float l) { return l > -INFINITY && weight(row.c, l, sh.powers) >= row.least; });
+      const unsigned key = row.lowest_key(
+          NAN, [&](float l) { return l > -INFINITY && weight(row.c, l, sh.powers) >= row.least; });
       if (lane == 0) sh.ends[0] = key;
     }
     __syncthreads();

@@ -250,12 +250,12 @@ struct SharedGroups {
   const int* prefix;   // [N] tokens whose whole blocks are the same
   int N;
   int least;         // blocks in common below which a group shares nothing
-  int least_spared;  // reads of a block (of one kv head) below which nobody does; at most 2^20
+  int least_spared;  // reads of a block, of all kv heads, below which nobody does; at most 2^20
   int least_steps;   // of 8 blocks, for a CTA of the prefix pass
   bool alone;        // no row can share anything worth it: the rows' own parts are all there is
   int sms, tile;     // SMs; rows of a tile of the prefix pass
-  int* next;         // [4] numbers the CTAs of the rows' own parts; how many there are; numbers the prefix pass's; once `common` is there,
-                     // the own parts' SMs; zero between calls
+  int* next;         // [4] numbers the CTAs of the rows' own parts; how many there are; numbers the prefix pass's; once
+                     // `common` is there, the own parts' SMs; zero between calls
   int4* plan;          // [1 + PAGED_ATTN_MAX_B], written by the prefix pass for the join
   int2* common;        // [PAGED_ATTN_MAX_B] and for the rows' own parts: the blocks that a row has in common, from and to
   float2* state_stats; // [B][H] maximum and sum of the rows' own parts

@@ -1,6 +1,6 @@
 // C entry points of the operators on a paged key/value cache: attention that
-// reads it, new tokens, and its blocks' management; and of tokens from logits. They check what the host can see, take
-// the caller's buffers and launch; nothing is allocated and nothing is kept.
+// reads it, new tokens, and its blocks' management; and of tokens from logits. They check what the
+// host can see, take the caller's buffers and launch; nothing is allocated and nothing is kept.
 #include <limits.h>
 #include <math.h>
 #include <stdint.h>
@@ -338,7 +338,8 @@ int axon_kv_append(const axon_kv_cache* cache, int32_t layer, const void* d_q, i
   if (B < 1 || T < 1 || num_heads < 0 || !d_context_lens || (!d_cu_seqlens && T != B)) return AXON_ERR_INVALID_ARG;
   if (blocks_per_seq < 1 || blocks_per_seq > MAX_BLOCKS_PER_SEQ) return AXON_ERR_INVALID_ARG;
   if (!d_block_table && static_cast<long long>(B) * blocks_per_seq > cache->num_blocks) return AXON_ERR_INVALID_ARG;
-  if (rotary_dim < 0 || rotary_dim > d || (rotary_dim > 0) != (d_rope != nullptr) || unaligned(d_rope)) return AXON_ERR_INVALID_ARG;
+  if (rotary_dim < 0 || rotary_dim > d || (rotary_dim > 0) != (d_rope != nullptr) || unaligned(d_rope))
+    return AXON_ERR_INVALID_ARG;
   if (rotary_dim > 0 && (rope_positions < 1 || (rope_layout != AXON_ROPE_HALF && rope_layout != AXON_ROPE_INTERLEAVED)))
     return AXON_ERR_INVALID_ARG;
   if ((num_heads > 0) != (d_q != nullptr) || (d_q != nullptr) != (d_q_out != nullptr) || unaligned(d_q) || unaligned(d_q_out))

@@ -83,3 +83,13 @@ def test_about_the_limit(ax, rows, blocks, shares, window, sinks):  # noqa: F811
         c.bt = torch.nn.functional.pad(c.bt, (0, per - c.bt.shape[1]), value=-1)
         sh.check(ax, c, rows=some)
         assert torch.equal(sh.run(ax, c)[0], plain) != shares
+
+
+@pytest.mark.parametrize("rows", [2, 3])
+def test_most_rows_and_groups_of_the_widest_heads(ax, monkeypatch, rows):  # noqa: F811
+    """2048 rows in as many groups as they make, 16 query heads per kv head of 128 dims: the most shared memory that a call takes."""
+    monkeypatch.setenv("AXON_SHARED_MIN_BYTES", "0")
+    groups = [(160, [165 + i for i in range(rows)])] * (2048 // rows)
+    c = sh.Case(16, 1, 128, "fp16", groups + [(0, [40])] * (2048 % rows), seed=73, layers=1, layer=0)
+    assert len(c.pos) == 2048 and c.prefix.numel() <= 1024
+    sh.check(ax, c, rows=[0, 1, 1000, 2046, 2047])

@@ -66,8 +66,8 @@ struct Span {
 };
 
 // The two passes run beside each other, each on SMs of its own: how many of them the rows' own parts take, so that both end
-// together. An even number, or all. Called by a warp. (57 rows of 1500 to 5500 tokens, 48 of them on 4001 in common: 72.5 us,
-// 99 with one pass after the other; 64 rows in groups of 4: 52 and 57.5; 64 rows on 32768 tokens: 80 and 91.)
+// together. An even number, or all. Called by a warp. (57 rows of 1500 to 5500 tokens, 48 of them on 4001 in common: 73.5 us,
+// 99 with one pass after the other; 64 rows in groups of 4: 53 and 57.5; 64 rows on 32768 tokens: 83 and 91.)
 AXON_DEV int own_sms(unsigned pages, unsigned rows, unsigned cost, int d, int sms) {
   if (cost == 0 || sms < 4) return sms;
   const unsigned own = own_work(pages, rows, d);

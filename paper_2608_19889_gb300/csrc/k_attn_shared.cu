@@ -22,9 +22,9 @@
 //
 // The bound is the tensor pipe where the rows fill two tiles (three products of 128 x 128 x 128 per tile and step, 1536 cycles, a
 // third of them the second terms'), and HBM where they fill one. Measured: 64 rows of 40 / 8 heads of 128 on 32768 tokens,
-// 157 tokens each of their own, 81 us in all: the pass 57 on 128 SMs, 0.75 PFLOP/s without the second terms, a step of two tiles
-// 2.05 us (3900 cycles); the own parts beside it. 64 rows of 32 / 8 heads in groups of 4 on 512 to 4096 tokens 52 us, the pass 32 of them, at
-// 4.7 TB/s. Start, plan and the first step's code take 10 us, the join 4 to 6.
+// 157 tokens each of their own, 83 us in all: the pass 57 on 128 SMs, 0.75 PFLOP/s without the second terms, a step of two tiles
+// 2.05 us (3900 cycles); the own parts beside it. 64 rows of 32 / 8 heads in groups of 4 on 512 to 4096 tokens 53 us, the
+// pass 32 of them, at 4.7 TB/s. Start, plan and the first step's code take 10 us, the join 4 to 6.
 #include <math.h>
 #include <stdlib.h>
 #include <string.h>

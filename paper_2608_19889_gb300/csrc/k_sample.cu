@@ -24,10 +24,10 @@
 //
 // The bound is the instructions, 62 a logit for the weights' histogram and 48 for their sum, and the cluster's
 // barriers, 0.7 us each and as much again for the slowest CTA; the floor, reading the logits once, is far off.
-// Measured: 1 row of 151936 logits with top-k and top-p 11.9 us, by temperature alone 10.1, the largest alone 4.4;
-// 33 rows of 152064 16-bit logits that ask for different things 37.6 us; 64 rows of 128256 fp32 logits by top-p, two CTAs
-// per SM and 1.7 times what runs at once, 75 us (a CTA: 1.5 us to load, 2 for the maximum, 7 for the histogram, 4 for the
-// crossing, 3 for the lists, 4.5 for the cut); 512 rows of 32000 by temperature 57.9 us.
+// Measured: 1 row of 151936 logits with top-k and top-p 12.2 us, by temperature alone 10.1, the largest alone 4.4;
+// 33 rows of 152064 16-bit logits that ask for different things 38.5 us; 64 rows of 128256 fp32 logits by top-p, two CTAs
+// per SM and 1.7 times what runs at once, 76 us (a CTA: 1.5 us to load, 2 for the maximum, 7 for the histogram, 4 for the
+// crossing, 3 for the lists, 4.5 for the cut); 512 rows of 32000 by temperature 58.5 us.
 #include <cooperative_groups.h>
 #include <math.h>
 
